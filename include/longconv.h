@@ -64,7 +64,7 @@ typedef enum { LONGCONV_F32 = 0, LONGCONV_F16 = 1, LONGCONV_BF16 = 2 } longconv_
 typedef enum {
     LONGCONV_OK = 0,
     LONGCONV_ERR_NULL = 1,       /* a required pointer is NULL */
-    LONGCONV_ERR_SHAPE = 2,      /* B or H < 1, N not a power of two or out of range */
+    LONGCONV_ERR_SHAPE = 2,      /* B or H < 1, N not a power of two or out of range; other arguments out of range */
     LONGCONV_ERR_DTYPE = 3,      /* dtype not one of longconv_dtype_t */
     LONGCONV_ERR_ALIGN = 4,      /* a pointer is not 16-byte aligned */
     LONGCONV_ERR_WORKSPACE = 5,  /* workspace NULL or smaller than longconv_workspace_bytes() */
@@ -249,6 +249,77 @@ int longconv_kreg_fwd(const float* k, const float* drop_mask, float* kbar, int64
  * dk must not alias any input. */
 int longconv_kreg_bwd(const float* k, const float* drop_mask, const float* dkbar, float* dk,
                       int64_t H, int64_t N, int p, float lambda, void* stream);
+
+/* ---- operators around the convolution --------------------------------------------------------------------------------------
+ * Conventions as above (device pointers, dense tensors, 16-byte aligned bases, caller-owned buffers, work on `stream` alone, checks
+ * before any launch), except that lengths are any numbers of at least one; empty tensors are LONGCONV_ERR_SHAPE.  Arithmetic is
+ * fp32 whatever the I/O dtype, each result is rounded to it once, and sums are taken in a fixed order (bitwise repeatable). */
+
+/* Dropout whose mask is never stored.  Philox4x32 with seven rounds (Salmon, Moraes, Dror, Shaw, SC 2011) of the counter (i / 8, call)
+ * under the key `seed` gives four words for entries 8 (i / 8) .. + 7 of a tensor in memory order; entry i has 16 bits of them, half
+ * i mod 8 (the low half of a word first), and is kept iff these are >= T = round(65536 p), so p counts in steps of 2^-16:
+ *     y[i] = residual[i] + m[i] x[i],      m[i] = kept ? 65536 / (65536 - T) : 0
+ * A dropped x counts for nothing, NaN and infinities included.  Entries 0 .. tie - 1, tie .. 2 tie - 1, ... share one value, that of
+ * entry i / tie (tie = N: one value for a head's whole row of [B,H,N]; 1: each entry its own); tie divides n.  `call` numbers the
+ * masks under one seed: two masks that must not repeat each other (layers, steps, forward passes) need two numbers, and the backward
+ * pass takes the number of its forward pass.  `step` may point to one int64 on the device, which is added to `call` when the kernel
+ * runs: a captured graph that increments it draws new masks at every replay.  residual may be NULL; y may be x or residual itself,
+ * dx may be dy (no other overlap).  0 <= p <= 1, 1 <= n <= 2^34. */
+int longconv_dropout_fwd(const void* x, const void* residual, void* y, int64_t n, int64_t tie, int io, float p, uint64_t seed,
+                         uint64_t call, const int64_t* step, void* stream);
+int longconv_dropout_bwd(const void* dy, void* dx, int64_t n, int64_t tie, int io, float p, uint64_t seed, uint64_t call,
+                         const int64_t* step, void* stream);
+
+/* The kernel regularisers with such a mask in the place of drop_mask (Algorithm 1 line 1): m over the entries of K [H,N], dropped with
+ * probability q.  Otherwise as longconv_kreg_fwd and longconv_kreg_bwd. */
+int longconv_kreg_fwd_seeded(const float* k, float* kbar, int64_t H, int64_t N, int p, float lambda, float q, uint64_t seed,
+                             uint64_t call, const int64_t* step, void* stream);
+int longconv_kreg_bwd_seeded(const float* k, const float* dkbar, float* dk, int64_t H, int64_t N, int p, float lambda, float q,
+                             uint64_t seed, uint64_t call, const int64_t* step, void* stream);
+
+typedef enum {
+    LONGCONV_CHANNELS_LAST = 0,  /* [B,N,H], the layout of dense layers */
+    LONGCONV_CHANNELS_FIRST = 1  /* [B,H,N], the convolution's */
+} longconv_layout_t;
+
+/* Embedding: rows of a table E [V,H] for tokens ids [B,N], scaled and dropped out,
+ *     y[b,t,:] = m . scale . E[ids[b,t],:]
+ * in either layout; m as longconv_dropout_fwd draws it for y (p = 0: none).  ids: int32 or int64 (id_bytes 4 or 8).  A token outside
+ * 0 .. V-1 names no row (padding is -1, say): zeros, and no gradient.  E is float32 or has the I/O dtype (`table`).
+ * 1 <= V <= 2^24, 1 <= H <= 65535, B N <= 2^26, B N H <= 2^34, and for LONGCONV_CHANNELS_FIRST fewer than 2^24 tiles of 64 x 64. */
+int longconv_embed_fwd(const void* ids, int id_bytes, const void* E, int table, void* y, int64_t B, int64_t N, int64_t V, int64_t H,
+                       int io, int layout, float scale, float p, uint64_t seed, uint64_t call, const int64_t* step, void* stream);
+
+/* Its gradient, every row of dE [V,H] float32 written (zeros where no token names it):
+ *     dE[v,:] = scale . sum over ids[b,t] = v of m . dy[b,t,:]
+ * The tokens' places are sorted in the workspace, and each token's gradients added up in the order of their places.
+ * longconv_embed_workspace_bytes (0 on bad arguments) does not fall as B grows. */
+size_t longconv_embed_workspace_bytes(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout);
+int longconv_embed_bwd(const void* dy, const void* ids, int id_bytes, float* dE, int64_t B, int64_t N, int64_t V, int64_t H, int io,
+                       int layout, float scale, float p, uint64_t seed, uint64_t call, const int64_t* step, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+typedef enum {
+    LONGCONV_ACT_NONE = 0,
+    LONGCONV_ACT_SILU = 1,       /* z / (1 + exp(-z)) */
+    LONGCONV_ACT_GELU = 2,       /* z (1 + erf(z / sqrt 2)) / 2 */
+    LONGCONV_ACT_RELU = 3        /* max(z, 0); slope 0 at 0 */
+} longconv_act_t;
+
+/* Group norm with an activation, channels last: x, y [B,S,C] (S positions: N of a sequence, N1 N2 of an image), G groups of C / G
+ * neighbouring channels each, statistics over a group's channels and all positions of one b:
+ *     y = act(gamma[c] (x - mean[b,g]) rstd[b,g] + beta[c]),      rstd = 1 / sqrt(variance + eps)
+ * gamma, beta [C] float32, each may be NULL (ones, zeros).  mean, rstd [B,G] float32 are written and are what the backward pass
+ * reads.  eps >= 0 and finite.  1 <= G, G divides C, C <= 65535, B C <= 2^25, B S C <= 2^34. */
+size_t longconv_gnorm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t G, int io, int backward);
+int longconv_gnorm_fwd(const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, int64_t B, int64_t S,
+                       int64_t C, int64_t G, float eps, int act, int io, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward: dx in the I/O dtype, dgamma and dbeta [C] float32 (each may be NULL).  longconv_gnorm_workspace_bytes (0 on bad arguments,
+ * backward = 1; it serves the forward pass too) does not fall as B grows. */
+int longconv_gnorm_bwd(const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd,
+                       void* dx, float* dgamma, float* dbeta, int64_t B, int64_t S, int64_t C, int64_t G, int act, int io,
+                       void* workspace, size_t workspace_bytes, void* stream);
 
 /* Debug and test switches (process-wide; not needed in normal use).  Each selects among
  * kernels that compute the same result: "engine" (0 by dtype, 1 fp32 vector-ALU engine,

@@ -17,7 +17,10 @@ Functions mirror the C ABI of ``include/longconv.h``:
     longconv_set_option, longconv_fwd_noalloc, longconv_kreg_fwd, longconv_kreg_bwd,
     longconv_fwd_gated, longconv_bwd_gated, longconv2d_workspace_bytes, longconv2d_fwd, longconv2d_bwd,
     longconv_lbfly_workspace_bytes, longconv_lbfly_spectrum, longconv_lbfly_spectrum_bwd, longconv_lbfly_fwd,
-    longconv_lbfly_bwd, longconv_blocksize_fwd
+    longconv_lbfly_bwd, longconv_blocksize_fwd,
+    longconv_dropout_fwd, longconv_dropout_bwd, longconv_kreg_fwd_seeded, longconv_kreg_bwd_seeded,
+    longconv_embed_workspace_bytes, longconv_embed_fwd, longconv_embed_bwd,
+    longconv_gnorm_workspace_bytes, longconv_gnorm_fwd, longconv_gnorm_bwd
 """
 from __future__ import annotations
 
@@ -43,7 +46,10 @@ EXPORTS = ("longconv_init", "longconv_kspec_bytes", "longconv_workspace_bytes",
            "longconv_fwd_gated", "longconv_bwd_gated",
            "longconv2d_workspace_bytes", "longconv2d_fwd", "longconv2d_bwd",
            "longconv_lbfly_workspace_bytes", "longconv_lbfly_spectrum", "longconv_lbfly_spectrum_bwd",
-           "longconv_lbfly_fwd", "longconv_lbfly_bwd", "longconv_blocksize_fwd")
+           "longconv_lbfly_fwd", "longconv_lbfly_bwd", "longconv_blocksize_fwd",
+           "longconv_dropout_fwd", "longconv_dropout_bwd", "longconv_kreg_fwd_seeded", "longconv_kreg_bwd_seeded",
+           "longconv_embed_workspace_bytes", "longconv_embed_fwd", "longconv_embed_bwd",
+           "longconv_gnorm_workspace_bytes", "longconv_gnorm_fwd", "longconv_gnorm_bwd")
 
 
 class LongconvError(RuntimeError):
@@ -103,6 +109,22 @@ def lib():
         L.longconv_lbfly_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, vp, sz, vp]
         L.longconv_blocksize_fwd.restype = ci
         L.longconv_blocksize_fwd.argtypes = [vp, vp, vp, i64, i64, i64, ci, ci, vp]
+        f32, u64 = ctypes.c_float, ctypes.c_uint64
+        random = [f32, u64, u64, vp]                      # share dropped, seed, number of the call, step
+        for name, args in {
+                "longconv_dropout_fwd": [vp, vp, vp, i64, i64, ci, *random, vp],
+                "longconv_dropout_bwd": [vp, vp, i64, i64, ci, *random, vp],
+                "longconv_kreg_fwd_seeded": [vp, vp, i64, i64, ci, f32, *random, vp],
+                "longconv_kreg_bwd_seeded": [vp, vp, vp, i64, i64, ci, f32, *random, vp],
+                "longconv_embed_fwd": [vp, ci, vp, ci, vp, i64, i64, i64, i64, ci, ci, f32, *random, vp],
+                "longconv_embed_bwd": [vp, vp, ci, vp, i64, i64, i64, i64, ci, ci, f32, *random, vp, sz, vp],
+                "longconv_gnorm_fwd": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, f32, ci, ci, vp, sz, vp],
+                "longconv_gnorm_bwd": [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, sz, vp]}.items():
+            getattr(L, name).restype, getattr(L, name).argtypes = ci, args
+        L.longconv_embed_workspace_bytes.restype = sz
+        L.longconv_embed_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, ci]
+        L.longconv_gnorm_workspace_bytes.restype = sz
+        L.longconv_gnorm_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, ci]
         L.longconv_set_option.restype = ci
         L.longconv_set_option.argtypes = [ctypes.c_char_p, ci]
         _lib = L
@@ -413,3 +435,156 @@ def longconv_bwd(dy, u, k, D, du, dk, dD, workspace, kspec=None, stream=None) ->
     _need(dk, "dk", torch.float32, (H, N)); _need(dD, "dD", torch.float32, (H,))
     _check(lib().longconv_bwd(_ptr(dy), _ptr(u), _ptr(k), _ptr(D), _ptr(kspec), _ptr(du), _ptr(dk), _ptr(dD),
                               B, H, N, io, _ptr(workspace), workspace.numel(), _stream(stream)), "longconv_bwd")
+
+
+# ---- operators around the convolution ----------------------------------------------------------------------------------------
+
+CHANNELS_LAST, CHANNELS_FIRST = 0, 1                      # [B, N, H] of dense layers, [B, H, N] of the convolution
+_ACT = {"none": 0, "silu": 1, "gelu": 2, "relu": 3}
+_IDS = {torch.int32: 4, torch.int64: 8}
+
+
+def _random(p, seed, call, step):
+    """The arguments of a mask.  seed and call are taken modulo 2**64; step: one int64 on the device, or None."""
+    _need(step, "step", torch.int64, (1,))
+    return float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(call) & 0xFFFFFFFFFFFFFFFF, _ptr(step)
+
+
+def longconv_dropout_fwd(x, y, p: float, seed: int, call: int, residual=None, tie: int = 1, step=None, stream=None) -> None:
+    """y <- residual + m x, m = 0 with probability p and 1 / (1 - p) otherwise, drawn for entry i // tie from (seed, call [+ step])
+    and never stored.  Tensors of any shape, in memory order; y may be x or residual.  tie = N: one value for each row of [B, H, N]."""
+    if _done((_bound or _fast()).dropout_fwd(x, y, p, seed, call, residual, tie, step, stream), "longconv_dropout_fwd"):
+        return
+    io = dtype_code(x)
+    for t, name in ((x, "x"), (y, "y"), (residual, "residual")):
+        _need(t, name, _TORCH_DTYPE[io], x.shape)
+    _check(lib().longconv_dropout_fwd(_ptr(x), _ptr(residual), _ptr(y), x.numel(), int(tie), io,
+                                      *_random(p, seed, call, step), _stream(stream)), "longconv_dropout_fwd")
+
+
+def longconv_dropout_bwd(dy, dx, p: float, seed: int, call: int, tie: int = 1, step=None, stream=None) -> None:
+    """dx <- m dy with the mask of the forward call of the same p, seed, call, tie and step (the residual's gradient is dy)."""
+    if _done((_bound or _fast()).dropout_bwd(dy, dx, p, seed, call, tie, step, stream), "longconv_dropout_bwd"):
+        return
+    io = dtype_code(dy)
+    _need(dy, "dy", _TORCH_DTYPE[io], dy.shape); _need(dx, "dx", _TORCH_DTYPE[io], dy.shape)
+    _check(lib().longconv_dropout_bwd(_ptr(dy), _ptr(dx), dy.numel(), int(tie), io, *_random(p, seed, call, step),
+                                      _stream(stream)), "longconv_dropout_bwd")
+
+
+def longconv_kreg_fwd_seeded(k, kbar, p: int, lam: float, q: float, seed: int, call: int, step=None, stream=None) -> None:
+    """kbar <- Squash(Smooth(m k)): longconv_kreg_fwd with a mask that drops with probability q and is never stored."""
+    if _done((_bound or _fast()).kreg_fwd_seeded(k, kbar, p, lam, q, seed, call, step, stream), "longconv_kreg_fwd_seeded"):
+        return
+    H, N = k.shape
+    _need(k, "k", torch.float32, (H, N)); _need(kbar, "kbar", torch.float32, (H, N))
+    _check(lib().longconv_kreg_fwd_seeded(_ptr(k), _ptr(kbar), H, N, int(p), float(lam), *_random(q, seed, call, step),
+                                          _stream(stream)), "longconv_kreg_fwd_seeded")
+
+
+def longconv_kreg_bwd_seeded(k, dkbar, dk, p: int, lam: float, q: float, seed: int, call: int, step=None, stream=None) -> None:
+    """dk <- longconv_kreg_bwd with the mask of longconv_kreg_fwd_seeded."""
+    if _done((_bound or _fast()).kreg_bwd_seeded(k, dkbar, dk, p, lam, q, seed, call, step, stream), "longconv_kreg_bwd_seeded"):
+        return
+    H, N = k.shape
+    for t, name in ((k, "k"), (dkbar, "dkbar"), (dk, "dk")):
+        _need(t, name, torch.float32, (H, N))
+    _check(lib().longconv_kreg_bwd_seeded(_ptr(k), _ptr(dkbar), _ptr(dk), H, N, int(p), float(lam),
+                                          *_random(q, seed, call, step), _stream(stream)), "longconv_kreg_bwd_seeded")
+
+
+def longconv_embed_workspace_bytes(B: int, N: int, V: int, H: int, io: int, layout: int = CHANNELS_LAST) -> int:
+    return int(lib().longconv_embed_workspace_bytes(B, N, V, H, io, layout))
+
+
+def new_workspace_embed(B, N, V, H, io, layout=CHANNELS_LAST, device="cuda"):
+    n = longconv_embed_workspace_bytes(B, N, V, H, io, layout)
+    if n == 0:
+        raise LongconvError("bad shape or dtype")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _embed_args(ids, rows, H, layout, name):
+    """B, N and the I/O type of tokens [B, N] and the rows made of them, or their gradient."""
+    B, N = ids.shape
+    if ids.dtype not in _IDS:
+        raise LongconvError(f"ids: expected torch.int32 or torch.int64, got {ids.dtype}")
+    io = dtype_code(rows)
+    _need(ids, "ids", ids.dtype, (B, N))
+    _need(rows, name, _TORCH_DTYPE[io], (B, H, N) if layout == CHANNELS_FIRST else (B, N, H))
+    return B, N, io
+
+
+def longconv_embed_fwd(ids, E, y, scale: float, layout: int = CHANNELS_LAST, p: float = 0.0, seed: int = 0, call: int = 0,
+                       step=None, stream=None) -> None:
+    """y [B, N, H] (or [B, H, N] for CHANNELS_FIRST) <- m . scale . E[ids]; ids outside 0 .. V-1 give zeros.  E [V, H] in fp32 or
+    in y's dtype; m as longconv_dropout_fwd would draw it for y."""
+    if _done((_bound or _fast()).embed_fwd(ids, E, y, scale, layout, p, seed, call, step, stream), "longconv_embed_fwd"):
+        return
+    V, H = E.shape
+    B, N, io = _embed_args(ids, y, H, layout, "y")
+    _need(E, "E", torch.float32 if E.dtype == torch.float32 else _TORCH_DTYPE[io], (V, H))
+    _check(lib().longconv_embed_fwd(_ptr(ids), _IDS[ids.dtype], _ptr(E), dtype_code(E), _ptr(y), B, N, V, H, io, int(layout),
+                                    float(scale), *_random(p, seed, call, step), _stream(stream)), "longconv_embed_fwd")
+
+
+def longconv_embed_bwd(dy, ids, dE, scale: float, layout: int, workspace, p: float = 0.0, seed: int = 0, call: int = 0,
+                       step=None, stream=None) -> None:
+    """dE [V, H] fp32 <- the gradient of longconv_embed_fwd's table, every row written."""
+    if _done((_bound or _fast()).embed_bwd(dy, ids, dE, scale, layout, workspace, p, seed, call, step, stream), "longconv_embed_bwd"):
+        return
+    V, H = dE.shape
+    B, N, io = _embed_args(ids, dy, H, layout, "dy")
+    _need(dE, "dE", torch.float32, (V, H))
+    _check(lib().longconv_embed_bwd(_ptr(dy), _ptr(ids), _IDS[ids.dtype], _ptr(dE), B, N, V, H, io, int(layout), float(scale),
+                                    *_random(p, seed, call, step), _ptr(workspace), workspace.numel(), _stream(stream)),
+           "longconv_embed_bwd")
+
+
+def longconv_gnorm_workspace_bytes(B: int, S: int, C: int, G: int, io: int, backward) -> int:
+    return int(lib().longconv_gnorm_workspace_bytes(B, S, C, G, io, int(bool(backward))))
+
+
+def new_workspace_gnorm(B, S, C, G, io, backward, device="cuda"):
+    n = longconv_gnorm_workspace_bytes(B, S, C, G, io, backward)
+    if n == 0:
+        raise LongconvError("bad shape or dtype")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _gnorm_args(x, mean, rstd, gamma, beta, others):
+    B, S, C = x.shape
+    G = mean.shape[1]
+    io = dtype_code(x)
+    for t, name in ((x, "x"), *others):
+        _need(t, name, _TORCH_DTYPE[io], (B, S, C))
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _need(t, name, torch.float32, (B, G))
+    for t, name in ((gamma, "gamma"), (beta, "beta")):
+        _need(t, name, torch.float32, (C,))
+    return B, S, C, G, io
+
+
+def longconv_gnorm_fwd(x, gamma, beta, y, mean, rstd, eps: float, act: str, workspace, stream=None) -> None:
+    """y [B, S, C] <- act(gamma (x - mean) rstd + beta), statistics over S and the C / G channels of a group, G = mean.shape[1];
+    mean, rstd [B, G] are written for the backward pass.  gamma, beta may be None; act: "none", "silu", "gelu", "relu"."""
+    code = _ACT[act]
+    if _done((_bound or _fast()).gnorm_fwd(x, gamma, beta, y, mean, rstd, eps, code, workspace, stream), "longconv_gnorm_fwd"):
+        return
+    B, S, C, G, io = _gnorm_args(x, mean, rstd, gamma, beta, ((y, "y"),))
+    _check(lib().longconv_gnorm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd), B, S, C, G, float(eps), code, io,
+                                    _ptr(workspace), workspace.numel(), _stream(stream)), "longconv_gnorm_fwd")
+
+
+def longconv_gnorm_bwd(dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, act: str, workspace, stream=None) -> None:
+    """dx, dgamma, dbeta <- gradients of longconv_gnorm_fwd (any of the three may be None)."""
+    code = _ACT[act]
+    if _done((_bound or _fast()).gnorm_bwd(dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, code, workspace, stream),
+             "longconv_gnorm_bwd"):
+        return
+    B, S, C, G, io = _gnorm_args(x, mean, rstd, gamma, beta, ((dy, "dy"), (dx, "dx")))
+    for t, name in ((dgamma, "dgamma"), (dbeta, "dbeta")):
+        _need(t, name, torch.float32, (C,))
+    _check(lib().longconv_gnorm_bwd(_ptr(dy), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma),
+                                    _ptr(dbeta), B, S, C, G, code, io, _ptr(workspace), workspace.numel(), _stream(stream)),
+           "longconv_gnorm_bwd")

@@ -4,14 +4,14 @@
 // multipass.hip (outer passes), engine_valu.hip (fp32 I/O), engine_mfma.hip (first-generation in-place kernel, kept as a
 // cross-check behind a switch and for 256-point inner transforms), kreg.hip (kernel regularisers), gate.hip (the gate's streaming
 // pass) and conv2d.hip (row padding of the 2-D convolution), lbfly.hip (learned Butterfly extension), bsize.hip (block-size
-// study); nothing here computes on the host.
+// study); dropout.hip, embed.hip and gnorm.hip hold the operators around the convolution.  Nothing here computes on the host.
 #include <atomic>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
 
-#include "engines.hpp"
+#include "operators.hpp"
 
 namespace lc {
 
@@ -864,6 +864,160 @@ int longconv_kreg_bwd(const float* k, const float* drop_mask, const float* dkbar
     return LONGCONV_OK;
 }
 
+// ---- operators around the convolution ----------------------------------------------------------------------------------
+
+static bool bad_dtype(int io) { return io != LONGCONV_F32 && io != LONGCONV_F16 && io != LONGCONV_BF16; }
+static bool bad_share(float p) { return !(p >= 0.f && p <= 1.f); }
+constexpr int64_t MAX_ELEMENTS = int64_t(1) << 34;      // of one tensor: what one launch covers
+
+static int run_dropout(const void* x, const void* residual, void* y, int64_t n, int64_t tie, int io, float p, uint64_t seed, uint64_t call,
+                       const int64_t* step, void* stream)
+{
+    if (bad_dtype(io)) return LONGCONV_ERR_DTYPE;
+    if (n < 1 || n > MAX_ELEMENTS || tie < 1 || tie > n || n % tie || bad_share(p)) return LONGCONV_ERR_SHAPE;
+    if (!x || !y) return LONGCONV_ERR_NULL;
+    if (misaligned(x) || misaligned(residual) || misaligned(y) || (reinterpret_cast<uintptr_t>(step) & 7u)) return LONGCONV_ERR_ALIGN;
+    return note(dropout(x, residual, y, n, tie, io, make_drop(p, seed, call, step), (hipStream_t)stream), "dropout") == hipSuccess
+               ? LONGCONV_OK
+               : LONGCONV_ERR_HIP;
+}
+
+int longconv_dropout_fwd(const void* x, const void* residual, void* y, int64_t n, int64_t tie, int io, float p, uint64_t seed, uint64_t call,
+                         const int64_t* step, void* stream)
+{
+    return run_dropout(x, residual, y, n, tie, io, p, seed, call, step, stream);
+}
+
+int longconv_dropout_bwd(const void* dy, void* dx, int64_t n, int64_t tie, int io, float p, uint64_t seed, uint64_t call, const int64_t* step,
+                         void* stream)
+{
+    return run_dropout(dy, nullptr, dx, n, tie, io, p, seed, call, step, stream);
+}
+
+int longconv_kreg_fwd_seeded(const float* k, float* kbar, int64_t H, int64_t N, int p, float lambda, float q, uint64_t seed, uint64_t call,
+                             const int64_t* step, void* stream)
+{
+    int s = kreg_check(k, kbar, kbar, H, N, p, lambda);
+    if (s != LONGCONV_OK) return s;
+    if (bad_share(q)) return LONGCONV_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(step) & 7u) return LONGCONV_ERR_ALIGN;
+    return note(kreg_fwd_seeded(k, kbar, H, N, p, lambda, make_drop(q, seed, call, step), (hipStream_t)stream), "kreg fwd") == hipSuccess
+               ? LONGCONV_OK
+               : LONGCONV_ERR_HIP;
+}
+
+int longconv_kreg_bwd_seeded(const float* k, const float* dkbar, float* dk, int64_t H, int64_t N, int p, float lambda, float q, uint64_t seed,
+                             uint64_t call, const int64_t* step, void* stream)
+{
+    int s = kreg_check(k, dkbar, dk, H, N, p, lambda);
+    if (s != LONGCONV_OK) return s;
+    if (bad_share(q)) return LONGCONV_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(step) & 7u) return LONGCONV_ERR_ALIGN;
+    return note(kreg_bwd_seeded(k, dkbar, dk, H, N, p, lambda, make_drop(q, seed, call, step), (hipStream_t)stream), "kreg bwd") == hipSuccess
+               ? LONGCONV_OK
+               : LONGCONV_ERR_HIP;
+}
+
+static int check_embed(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
+{
+    if (bad_dtype(io)) return LONGCONV_ERR_DTYPE;
+    if (B < 1 || N < 1 || V < 1 || H < 1 || V > (int64_t(1) << 24) || H > 65535) return LONGCONV_ERR_SHAPE;
+    if (B > (int64_t(1) << 26) || N > (int64_t(1) << 26) / B || B * N > MAX_ELEMENTS / H) return LONGCONV_ERR_SHAPE;
+    if (layout != LONGCONV_CHANNELS_LAST && layout != LONGCONV_CHANNELS_FIRST) return LONGCONV_ERR_SHAPE;
+    if (layout == LONGCONV_CHANNELS_FIRST && B * ((N + 63) / 64) * ((H + 63) / 64) >= (int64_t(1) << 24)) return LONGCONV_ERR_SHAPE;
+    return LONGCONV_OK;
+}
+
+size_t longconv_embed_workspace_bytes(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
+{
+    return check_embed(B, N, V, H, io, layout) == LONGCONV_OK ? embed_workspace_bytes(B, N, V, H, io, layout) : 0;
+}
+
+static int check_embed_call(const void* ids, int id_bytes, int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout, float p,
+                            const int64_t* step)
+{
+    int s = check_embed(B, N, V, H, io, layout);
+    if (s != LONGCONV_OK) return s;
+    if (id_bytes != 4 && id_bytes != 8) return LONGCONV_ERR_DTYPE;
+    if (bad_share(p)) return LONGCONV_ERR_SHAPE;
+    if (!ids) return LONGCONV_ERR_NULL;
+    return misaligned(ids) || (reinterpret_cast<uintptr_t>(step) & 7u) ? LONGCONV_ERR_ALIGN : LONGCONV_OK;
+}
+
+int longconv_embed_fwd(const void* ids, int id_bytes, const void* E, int table, void* y, int64_t B, int64_t N, int64_t V, int64_t H, int io,
+                       int layout, float scale, float p, uint64_t seed, uint64_t call, const int64_t* step, void* stream)
+{
+    int s = check_embed_call(ids, id_bytes, B, N, V, H, io, layout, p, step);
+    if (s != LONGCONV_OK) return s;
+    if (table != LONGCONV_F32 && table != io) return LONGCONV_ERR_DTYPE;
+    if (!E || !y) return LONGCONV_ERR_NULL;
+    if (misaligned(E) || misaligned(y)) return LONGCONV_ERR_ALIGN;
+    const EmbedArgs a{ids, id_bytes, B, N, V, H, io, layout, scale, make_drop(p, seed, call, step)};
+    return note(embed_fwd(a, E, table, y, (hipStream_t)stream), "embed fwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+int longconv_embed_bwd(const void* dy, const void* ids, int id_bytes, float* dE, int64_t B, int64_t N, int64_t V, int64_t H, int io,
+                       int layout, float scale, float p, uint64_t seed, uint64_t call, const int64_t* step, void* workspace,
+                       size_t workspace_bytes, void* stream)
+{
+    int s = check_embed_call(ids, id_bytes, B, N, V, H, io, layout, p, step);
+    if (s != LONGCONV_OK) return s;
+    if (!dy || !dE) return LONGCONV_ERR_NULL;
+    if (misaligned(dy) || misaligned(dE) || misaligned(workspace)) return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < embed_workspace_bytes(B, N, V, H, io, layout)) return LONGCONV_ERR_WORKSPACE;
+    const EmbedArgs a{ids, id_bytes, B, N, V, H, io, layout, scale, make_drop(p, seed, call, step)};
+    return note(embed_bwd(a, dy, dE, workspace, (hipStream_t)stream), "embed bwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+static int check_gnorm(int64_t B, int64_t S, int64_t C, int64_t G, int io)
+{
+    if (bad_dtype(io)) return LONGCONV_ERR_DTYPE;
+    if (B < 1 || S < 1 || C < 1 || C > 65535 || G < 1 || G > C || C % G) return LONGCONV_ERR_SHAPE;
+    if (B > (int64_t(1) << 25) / C || S > MAX_ELEMENTS / (B * C)) return LONGCONV_ERR_SHAPE;
+    return LONGCONV_OK;
+}
+
+size_t longconv_gnorm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t G, int io, int backward)
+{
+    return check_gnorm(B, S, C, G, io) == LONGCONV_OK ? gnorm_workspace_bytes(B, S, C, G, io, backward) : 0;
+}
+
+static bool bad_act(int act) { return act < LONGCONV_ACT_NONE || act > LONGCONV_ACT_RELU; }
+
+int longconv_gnorm_fwd(const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, int64_t B, int64_t S, int64_t C,
+                       int64_t G, float eps, int act, int io, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int s = check_gnorm(B, S, C, G, io);
+    if (s != LONGCONV_OK) return s;
+    if (bad_act(act) || !(eps >= 0.f && eps < 3.0e38f)) return LONGCONV_ERR_SHAPE;
+    if (!x || !y || !mean || !rstd) return LONGCONV_ERR_NULL;
+    if (misaligned(x) || misaligned(gamma) || misaligned(beta) || misaligned(y) || misaligned(mean) || misaligned(rstd) || misaligned(workspace))
+        return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < gnorm_workspace_bytes(B, S, C, G, io, 0)) return LONGCONV_ERR_WORKSPACE;
+    const GnormArgs a{gamma, beta, B, S, C, G, io, act};
+    return note(gnorm_fwd(a, x, y, mean, rstd, eps, workspace, (hipStream_t)stream), "gnorm fwd") == hipSuccess ? LONGCONV_OK
+                                                                                                                 : LONGCONV_ERR_HIP;
+}
+
+int longconv_gnorm_bwd(const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, void* dx,
+                       float* dgamma, float* dbeta, int64_t B, int64_t S, int64_t C, int64_t G, int act, int io, void* workspace,
+                       size_t workspace_bytes, void* stream)
+{
+    int s = check_gnorm(B, S, C, G, io);
+    if (s != LONGCONV_OK) return s;
+    if (bad_act(act)) return LONGCONV_ERR_SHAPE;
+    if (!dy || !x || !mean || !rstd) return LONGCONV_ERR_NULL;
+    if (misaligned(dy) || misaligned(x) || misaligned(gamma) || misaligned(beta) || misaligned(mean) || misaligned(rstd) || misaligned(dx) ||
+        misaligned(dgamma) || misaligned(dbeta) || misaligned(workspace))
+        return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < gnorm_workspace_bytes(B, S, C, G, io, 1)) return LONGCONV_ERR_WORKSPACE;
+    if (!dx && !dgamma && !dbeta) return LONGCONV_OK;
+    const GnormArgs a{gamma, beta, B, S, C, G, io, act};
+    return note(gnorm_bwd(a, dy, x, mean, rstd, dx, dgamma, dbeta, workspace, (hipStream_t)stream), "gnorm bwd") == hipSuccess
+               ? LONGCONV_OK
+               : LONGCONV_ERR_HIP;
+}
+
 int longconv_set_option(const char* name, int value)
 {
     if (!name) return LONGCONV_ERR_NULL;
@@ -882,7 +1036,7 @@ const char* longconv_status_string(int status)
     switch (status) {
         case LONGCONV_OK: return "ok";
         case LONGCONV_ERR_NULL: return "a required pointer is NULL";
-        case LONGCONV_ERR_SHAPE: return "bad shape: need B,H >= 1 and N a power of two in [256, 131072]";
+        case LONGCONV_ERR_SHAPE: return "bad shape or argument (convolutions: B,H >= 1 and N a power of two in [256, 131072])";
         case LONGCONV_ERR_DTYPE: return "unsupported dtype";
         case LONGCONV_ERR_ALIGN: return "pointer not 16-byte aligned";
         case LONGCONV_ERR_WORKSPACE: return "workspace missing or too small";

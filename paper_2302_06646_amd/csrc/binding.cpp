@@ -31,6 +31,14 @@ struct Api {
     decltype(&longconv_lbfly_spectrum_bwd) lbfly_spectrum_bwd;
     decltype(&longconv_lbfly_fwd) lbfly_fwd;
     decltype(&longconv_lbfly_bwd) lbfly_bwd;
+    decltype(&longconv_dropout_fwd) dropout_fwd;
+    decltype(&longconv_dropout_bwd) dropout_bwd;
+    decltype(&longconv_kreg_fwd_seeded) kreg_fwd_seeded;
+    decltype(&longconv_kreg_bwd_seeded) kreg_bwd_seeded;
+    decltype(&longconv_embed_fwd) embed_fwd;
+    decltype(&longconv_embed_bwd) embed_bwd;
+    decltype(&longconv_gnorm_fwd) gnorm_fwd;
+    decltype(&longconv_gnorm_bwd) gnorm_bwd;
 } g_api = {};
 
 // a plain device tensor: torch.Tensor or Parameter, strided, its own storage, no functional transform around it
@@ -78,6 +86,14 @@ struct Args {
         if (!ok) return 0;
         const long v = PyLong_CheckExact(a[i]) ? PyLong_AsLong(a[i]) : -1;
         if (v < 0 || v > 0x7fffffffL) { PyErr_Clear(); ok = false; }
+        return v;
+    }
+    uint64_t number64(int i)
+    {
+        if (!ok) return 0;
+        if (!PyLong_CheckExact(a[i])) { ok = false; return 0; }
+        const unsigned long long v = PyLong_AsUnsignedLongLong(a[i]);
+        if (PyErr_Occurred()) { PyErr_Clear(); ok = false; return 0; }
         return v;
     }
     double real(int i)
@@ -339,6 +355,191 @@ PyObject* lbfly_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)  // dy, u, shat
     });
 }
 
+// share dropped, seed, number of the call (arguments i ..) and the device's step (argument j)
+struct Random {
+    float p;
+    uint64_t seed, call;
+    const int64_t* step;
+    Random(Args& A, int i, int j)
+        : p((float)A.real(i)), seed(A.number64(i + 1)), call(A.number64(i + 2)), step((const int64_t*)A.ptr(j, at::kLong, {1}))
+    {
+    }
+};
+
+// a tensor of any shape whose I/O type and number of elements the call takes
+const at::Tensor* whole(Args& A, int i, int* io)
+{
+    const at::Tensor* t = plain(A.a[i]);
+    if (!t || (*io = io_code(t->scalar_type())) < 0) { A.ok = false; return nullptr; }
+    return t;
+}
+
+PyObject* dropout_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)       // x, y, p, seed, call, residual, tie, step, stream
+{
+    return guarded(a, n, 9, g_api.dropout_fwd, [&](Args& A, auto& call) {
+        int io;
+        const at::Tensor* t = whole(A, 0, &io);
+        if (!t) return;
+        const void *x = A.ptr(0, t->scalar_type(), t->sizes(), false), *r = A.ptr(5, t->scalar_type(), t->sizes());
+        void* y = A.ptr(1, t->scalar_type(), t->sizes());
+        const Random m(A, 2, 7);
+        const int64_t tie = A.number(6);
+        void* st = A.stream(8);
+        call([&] { return g_api.dropout_fwd(x, r, y, t->numel(), tie, io, m.p, m.seed, m.call, m.step, st); });
+    });
+}
+
+PyObject* dropout_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)       // dy, dx, p, seed, call, tie, step, stream
+{
+    return guarded(a, n, 8, g_api.dropout_bwd, [&](Args& A, auto& call) {
+        int io;
+        const at::Tensor* t = whole(A, 0, &io);
+        if (!t) return;
+        const void* dy = A.ptr(0, t->scalar_type(), t->sizes(), false);
+        void* dx = A.ptr(1, t->scalar_type(), t->sizes());
+        const Random m(A, 2, 6);
+        const int64_t tie = A.number(5);
+        void* st = A.stream(7);
+        call([&] { return g_api.dropout_bwd(dy, dx, t->numel(), tie, io, m.p, m.seed, m.call, m.step, st); });
+    });
+}
+
+PyObject* kreg_fwd_seeded(PyObject*, PyObject* const* a, Py_ssize_t n)   // k, kbar, p, lam, q, seed, call, step, stream
+{
+    return guarded(a, n, 9, g_api.kreg_fwd_seeded, [&](Args& A, auto& call) {
+        const at::Tensor* t = A.first(0, 2);
+        if (!t) return;
+        const int64_t H = t->size(0), N = t->size(1);
+        const auto k = (const float*)A.ptr(0, F, {H, N});
+        const auto kbar = (float*)A.ptr(1, F, {H, N});
+        const int p = (int)A.number(2);
+        const float lam = (float)A.real(3);
+        const Random m(A, 4, 7);
+        void* st = A.stream(8);
+        call([&] { return g_api.kreg_fwd_seeded(k, kbar, H, N, p, lam, m.p, m.seed, m.call, m.step, st); });
+    });
+}
+
+PyObject* kreg_bwd_seeded(PyObject*, PyObject* const* a, Py_ssize_t n)   // k, dkbar, dk, p, lam, q, seed, call, step, stream
+{
+    return guarded(a, n, 10, g_api.kreg_bwd_seeded, [&](Args& A, auto& call) {
+        const at::Tensor* t = A.first(0, 2);
+        if (!t) return;
+        const int64_t H = t->size(0), N = t->size(1);
+        const auto k = (const float*)A.ptr(0, F, {H, N}), dkbar = (const float*)A.ptr(1, F, {H, N});
+        const auto dk = (float*)A.ptr(2, F, {H, N});
+        const int p = (int)A.number(3);
+        const float lam = (float)A.real(4);
+        const Random m(A, 5, 8);
+        void* st = A.stream(9);
+        call([&] { return g_api.kreg_bwd_seeded(k, dkbar, dk, H, N, p, lam, m.p, m.seed, m.call, m.step, st); });
+    });
+}
+
+// tokens [B,N] in argument i, a table or its gradient [V,H] in argument j
+struct Tokens {
+    int64_t B = 0, N = 0, V = 0, H = 0;
+    const void* ids = nullptr;
+    int bytes = 0, layout = 0;
+    Tokens(Args& A, int i, int j, int at_layout)
+    {
+        const at::Tensor *t = A.first(i, 2), *e = A.first(j, 2);
+        if (!t || !e) return;
+        bytes = t->scalar_type() == at::kLong ? 8 : t->scalar_type() == at::kInt ? 4 : 0;
+        layout = (int)A.number(at_layout);
+        if (!bytes || layout > 1) { A.ok = false; return; }
+        B = t->size(0);
+        N = t->size(1);
+        V = e->size(0);
+        H = e->size(1);
+        ids = A.ptr(i, t->scalar_type(), {B, N});
+    }
+    void* rows(Args& A, int i, c10::ScalarType dt) const
+    {
+        return layout == LONGCONV_CHANNELS_FIRST ? A.ptr(i, dt, {B, H, N}) : A.ptr(i, dt, {B, N, H});
+    }
+};
+
+PyObject* embed_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)         // ids, E, y, scale, layout, p, seed, call, step, stream
+{
+    return guarded(a, n, 10, g_api.embed_fwd, [&](Args& A, auto& call) {
+        const Tokens t(A, 0, 1, 4);
+        int io = -1;
+        const at::Tensor* y = A.ok ? whole(A, 2, &io) : nullptr;
+        const at::Tensor* e = plain(a[1]);
+        if (!y || !e) return;
+        const int table = io_code(e->scalar_type());
+        if (table < 0) { A.ok = false; return; }
+        const void* E = A.ptr(1, e->scalar_type(), {t.V, t.H});
+        void* to = t.rows(A, 2, y->scalar_type());
+        const float scale = (float)A.real(3);
+        const Random m(A, 5, 8);
+        void* st = A.stream(9);
+        if (table != LONGCONV_F32 && table != io) { A.ok = false; return; }
+        call([&] {
+            return g_api.embed_fwd(t.ids, t.bytes, E, table, to, t.B, t.N, t.V, t.H, io, t.layout, scale, m.p, m.seed, m.call, m.step, st);
+        });
+    });
+}
+
+PyObject* embed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)   // dy, ids, dE, scale, layout, workspace, p, seed, call, step, stream
+{
+    return guarded(a, n, 11, g_api.embed_bwd, [&](Args& A, auto& call) {
+        const Tokens t(A, 1, 2, 4);
+        int io = -1;
+        const at::Tensor* g = A.ok ? whole(A, 0, &io) : nullptr;
+        if (!g) return;
+        size_t wb;
+        const void* dy = t.rows(A, 0, g->scalar_type());
+        const auto dE = (float*)A.ptr(2, F, {t.V, t.H});
+        const float scale = (float)A.real(3);
+        void* ws = A.raw(5, &wb, false);
+        const Random m(A, 6, 9);
+        void* st = A.stream(10);
+        call([&] {
+            return g_api.embed_bwd(dy, t.ids, t.bytes, dE, t.B, t.N, t.V, t.H, io, t.layout, scale, m.p, m.seed, m.call, m.step, ws, wb, st);
+        });
+    });
+}
+
+PyObject* gnorm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)   // x, gamma, beta, y, mean, rstd, eps, act, workspace, stream
+{
+    return guarded(a, n, 10, g_api.gnorm_fwd, [&](Args& A, auto& call) {
+        const Rows r(A, 0, 3);
+        const at::Tensor* mn = A.first(4, 2);
+        if (!A.ok || !mn) return;
+        const int64_t G = mn->size(1);
+        size_t wb;
+        const void* x = A.ptr(0, r.dt, {r.B, r.H, r.N});
+        const auto ga = (const float*)A.ptr(1, F, {r.N}), be = (const float*)A.ptr(2, F, {r.N});
+        void* y = A.ptr(3, r.dt, {r.B, r.H, r.N});
+        const auto mean = (float*)A.ptr(4, F, {r.B, G}), rstd = (float*)A.ptr(5, F, {r.B, G});
+        const float eps = (float)A.real(6);
+        const int act = (int)A.number(7);
+        void *ws = A.raw(8, &wb, false), *st = A.stream(9);
+        call([&] { return g_api.gnorm_fwd(x, ga, be, y, mean, rstd, r.B, r.H, r.N, G, eps, act, r.io, ws, wb, st); });
+    });
+}
+
+PyObject* gnorm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)   // dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, act, workspace, stream
+{
+    return guarded(a, n, 12, g_api.gnorm_bwd, [&](Args& A, auto& call) {
+        const Rows r(A, 1, 3);
+        const at::Tensor* mn = A.first(4, 2);
+        if (!A.ok || !mn) return;
+        const int64_t G = mn->size(1);
+        size_t wb;
+        const void *dy = A.ptr(0, r.dt, {r.B, r.H, r.N}), *x = A.ptr(1, r.dt, {r.B, r.H, r.N});
+        const auto ga = (const float*)A.ptr(2, F, {r.N}), be = (const float*)A.ptr(3, F, {r.N});
+        const auto mean = (const float*)A.ptr(4, F, {r.B, G}), rstd = (const float*)A.ptr(5, F, {r.B, G});
+        void* dx = A.ptr(6, r.dt, {r.B, r.H, r.N});
+        const auto dga = (float*)A.ptr(7, F, {r.N}), dbe = (float*)A.ptr(8, F, {r.N});
+        const int act = (int)A.number(9);
+        void *ws = A.raw(10, &wb, false), *st = A.stream(11);
+        call([&] { return g_api.gnorm_bwd(dy, x, ga, be, mean, rstd, dx, dga, dbe, r.B, r.H, r.N, G, act, r.io, ws, wb, st); });
+    });
+}
+
 // bind({name: address}): the entry points of the library that the binding has loaded
 PyObject* bind(PyObject*, PyObject* arg)
 {
@@ -366,6 +567,14 @@ PyObject* bind(PyObject*, PyObject* arg)
     set(g_api.lbfly_spectrum_bwd, "longconv_lbfly_spectrum_bwd");
     set(g_api.lbfly_fwd, "longconv_lbfly_fwd");
     set(g_api.lbfly_bwd, "longconv_lbfly_bwd");
+    set(g_api.dropout_fwd, "longconv_dropout_fwd");
+    set(g_api.dropout_bwd, "longconv_dropout_bwd");
+    set(g_api.kreg_fwd_seeded, "longconv_kreg_fwd_seeded");
+    set(g_api.kreg_bwd_seeded, "longconv_kreg_bwd_seeded");
+    set(g_api.embed_fwd, "longconv_embed_fwd");
+    set(g_api.embed_bwd, "longconv_embed_bwd");
+    set(g_api.gnorm_fwd, "longconv_gnorm_fwd");
+    set(g_api.gnorm_bwd, "longconv_gnorm_bwd");
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "an entry point is missing");
         return nullptr;
@@ -377,7 +586,8 @@ PyObject* bind(PyObject*, PyObject* arg)
 PyMethodDef methods[] = {
     {"bind", bind, METH_O, nullptr}, FAST(kspec_compute), FAST(fwd), FAST(bwd), FAST(fwd_gated), FAST(bwd_gated), FAST(fwd2d),
     FAST(bwd2d), FAST(kreg_fwd), FAST(kreg_bwd), FAST(lbfly_spectrum), FAST(lbfly_spectrum_bwd), FAST(lbfly_fwd),
-    FAST(lbfly_bwd), {nullptr, nullptr, 0, nullptr}};
+    FAST(lbfly_bwd), FAST(dropout_fwd), FAST(dropout_bwd), FAST(kreg_fwd_seeded), FAST(kreg_bwd_seeded), FAST(embed_fwd),
+    FAST(embed_bwd), FAST(gnorm_fwd), FAST(gnorm_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,485 @@
+// Embedding: y = m . scale . E[id] with m a dropout mask (vec8.hpp), in the layout of dense layers [B,N,H] or in the convolution's
+// [B,H,N], and the gradient dE[v] = scale . sum over the places with id = v of m . dy.
+//
+// The gradient adds up in a fixed order: the tokens' places are sorted by token (stable, so by place within a token), a thread
+// takes eight columns of a chunk of consecutive sorted places and sums runs of one token in fp32; a run that crosses chunks leaves
+// a partial sum in each, which are added in the chunks' order.  Every row of dy is read once.
+#include <type_traits>
+
+#include "vec8.hpp"
+
+namespace lc {
+namespace {
+
+constexpr int RADIX = 512, SORT_T = 256, TILE_MIN = 2048, TILES_MAX = 256;      // digits of at most nine bits; tiles of a sorting pass
+constexpr int CHUNK = 32;                                                       // sorted places of a thread
+
+// a token's row, or V for one that names none
+template <class ID>
+__device__ __forceinline__ uint32_t row_of(const ID* ids, int64_t i, uint32_t V)
+{
+    const ID v = ids[i];
+    return v >= 0 && (uint64_t)v < V ? (uint32_t)v : V;
+}
+
+// ---- forward ---------------------------------------------------------------------------------------------------------
+
+// [B,N,H]: a thread writes eight consecutive elements, of one row or of the end of one and the beginning of the next ones.
+template <class IO, class W, class ID, class I>
+__global__ void __launch_bounds__(256)
+embed_rows_kernel(const ID* __restrict__ ids, const typename W::T* __restrict__ E, typename IO::T* __restrict__ y, I n, uint32_t H, uint32_t V,
+                  float scale, Drop d)
+{
+    const I e = ((I)blockIdx.x * 256 + threadIdx.x) * VE;
+    if (e >= n) return;
+    const int here = n - e < (I)VE ? (int)(n - e) : VE;
+    const I row = e / H;
+    const uint32_t c = (uint32_t)(e - row * H);
+    float v[VE];
+    if (c + VE <= H) {
+        const uint32_t r = row_of(ids, (int64_t)row, V);
+        if (r < V) load8<W>(E + (size_t)r * H + c, VE, v);
+        else
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[i] = 0.f;
+    } else {
+        I rw = row;
+        uint32_t cc = c;
+        for (int i = 0; i < here; ++i) {
+            const uint32_t r = row_of(ids, (int64_t)rw, V);
+            const float t = r < V ? W::ld(E, (size_t)r * H + cc) : 0.f;
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+                if (j == i) v[j] = t;
+            if (++cc == H) { cc = 0; ++rw; }
+        }
+    }
+    const uint32_t m = d.threshold ? kept8(e >> 3, d, call_of(d)) : 0xffu;
+    const float f = scale * d.scale;
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? v[i] * f : 0.f;
+    store8<IO>(y + e, here, v);
+}
+
+constexpr int TT = 64, TH = 64;      // tokens and channels of a tile
+
+// [B,H,N]: a workgroup takes a tile of 64 tokens and 64 channels through LDS
+template <class IO, class W, class ID>
+__global__ void __launch_bounds__(256)
+embed_columns_kernel(const ID* __restrict__ ids, const typename W::T* __restrict__ E, typename IO::T* __restrict__ y, uint32_t N, uint32_t H,
+                     uint32_t V, uint32_t tiles_t, uint32_t tiles_h, float scale, Drop d)
+{
+    __shared__ float tile[TH][TT + 1];
+    const uint32_t tt = blockIdx.x % tiles_t, th = blockIdx.x / tiles_t % tiles_h, b = blockIdx.x / tiles_t / tiles_h;
+    const uint32_t t0 = tt * TT, h0 = th * TH, tid = threadIdx.x, s = tid % 8;
+#pragma unroll
+    for (uint32_t k = 0; k < TT / 32; ++k) {
+        const uint32_t t = tid / 8 + 32 * k, h = h0 + VE * s;
+        const uint32_t r = t0 + t < N ? row_of(ids, (int64_t)b * N + t0 + t, V) : V;
+        float v[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = 0.f;
+        if (r < V && h < H) load8<W>(E + (size_t)r * H + h, (int)(H - h), v);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) tile[VE * s + i][t] = v[i];
+    }
+    __syncthreads();
+    const uint64_t call = call_of(d);
+    const float f = scale * d.scale;
+#pragma unroll
+    for (uint32_t k = 0; k < TH / 32; ++k) {
+        const uint32_t h = h0 + tid / 8 + 32 * k, t = t0 + VE * s;
+        if (h >= H || t >= N) continue;
+        const size_t e = ((size_t)b * H + h) * N + t;
+        const uint32_t m = d.threshold ? kept8_at(e, d, call) : 0xffu;
+        float v[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? tile[h - h0][VE * s + i] * f : 0.f;
+        store8<IO>(y + e, (int)(N - t), v);
+    }
+}
+
+// ---- gradient --------------------------------------------------------------------------------------------------------
+
+__global__ void __launch_bounds__(256) embed_zero_kernel(float* __restrict__ p, int64_t n)
+{
+    const int64_t stride = (int64_t)gridDim.x * 256 * 4;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += stride) {
+        if (i + 4 <= n) *reinterpret_cast<float4*>(p + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+        else
+            for (int64_t j = i; j < n; ++j) p[j] = 0.f;
+    }
+}
+
+// [B,H,N] -> rows of `stride` channels, dropped entries zero (the factor of the kept ones comes in with `scale`, so nothing is rounded)
+template <class IO>
+__global__ void __launch_bounds__(256)
+embed_transpose_kernel(const typename IO::T* __restrict__ dy, typename IO::T* __restrict__ out, uint32_t N, uint32_t H, uint32_t stride,
+                       uint32_t tiles_t, uint32_t tiles_h, Drop d)
+{
+    __shared__ float tile[TT][TH + 1];
+    const uint32_t tt = blockIdx.x % tiles_t, th = blockIdx.x / tiles_t % tiles_h, b = blockIdx.x / tiles_t / tiles_h;
+    const uint32_t t0 = tt * TT, h0 = th * TH, tid = threadIdx.x, s = tid % 8;
+    const uint64_t call = call_of(d);
+#pragma unroll
+    for (uint32_t k = 0; k < TH / 32; ++k) {
+        const uint32_t hh = tid / 8 + 32 * k, h = h0 + hh, t = t0 + VE * s;
+        float v[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = 0.f;
+        if (h < H && t < N) {
+            const size_t e = ((size_t)b * H + h) * N + t;
+            load8<IO>(dy + e, (int)(N - t), v);
+            const uint32_t m = d.threshold ? kept8_at(e, d, call) : 0xffu;
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? v[i] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < VE; ++i) tile[VE * s + i][hh] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t k = 0; k < TT / 32; ++k) {
+        const uint32_t t = tid / 8 + 32 * k, h = h0 + VE * s;
+        if (t0 + t >= N || h >= stride) continue;      // (stride is a multiple of eight)
+        float v[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = tile[t][VE * s + i];
+        store8<IO>(out + ((size_t)b * N + t0 + t) * stride + h, VE, v);
+    }
+}
+
+// One pass of the stable sort by token: `shift` and `bits` name the digit.  ID: the pass reads the tokens themselves, whose places are
+// their numbers; without (void) it reads the pairs that the pass before left.
+template <class ID>
+struct Tokens {
+    const ID* ids;
+    const uint32_t *key, *pos;
+    uint32_t V;
+    __device__ __forceinline__ uint32_t k(int64_t i) const
+    {
+        if constexpr (std::is_void<ID>::value) return key[i];
+        else return row_of(ids, i, V);
+    }
+    __device__ __forceinline__ uint32_t p(int64_t i) const
+    {
+        if constexpr (std::is_void<ID>::value) return pos[i];
+        else return (uint32_t)i;
+    }
+};
+
+// hist[tile][digit] = how many tokens of the tile have the digit
+template <class ID>
+__global__ void __launch_bounds__(SORT_T)
+sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, int64_t M, int64_t tile, int shift, int bits)
+{
+    __shared__ uint32_t n[RADIX];
+    for (int i = threadIdx.x; i < RADIX; i += SORT_T) n[i] = 0;
+    __syncthreads();
+    const int64_t from = blockIdx.x * tile, to = from + tile < M ? from + tile : M;
+    const uint32_t mask = (1u << bits) - 1u;
+    for (int64_t i = from + threadIdx.x; i < to; i += SORT_T) atomicAdd(&n[in.k(i) >> shift & mask], 1u);
+    __syncthreads();
+    for (int i = threadIdx.x; i < RADIX; i += SORT_T) hist[(size_t)blockIdx.x * RADIX + i] = n[i];
+}
+
+// Puts a tile's tokens where they belong: behind all of smaller digits, those of the same digit in earlier tiles, in earlier waves'
+// shares of the tile, in earlier rows of 64, and in earlier lanes.
+template <class ID>
+__global__ void __launch_bounds__(SORT_T)
+sort_place_kernel(Tokens<ID> in, const uint32_t* __restrict__ hist, uint32_t* __restrict__ key, uint32_t* __restrict__ pos, int64_t M,
+                  int64_t tile, int shift, int bits)
+{
+    constexpr int WAVES = SORT_T / 64, D = RADIX / SORT_T;
+    __shared__ uint32_t at[WAVES][RADIX];      // next place of a wave's tokens with a digit
+    __shared__ uint32_t sums[SORT_T];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t mask = (1u << bits) - 1u;
+    const int64_t share = tile / WAVES, from = blockIdx.x * tile + wave * share;
+    for (int i = tid; i < WAVES * RADIX; i += SORT_T) (&at[0][0])[i] = 0;
+    __syncthreads();
+    for (int64_t i = from + lane; i < from + share && i < M; i += 64) atomicAdd(&at[wave][in.k(i) >> shift & mask], 1u);
+    // digits D tid .. D tid + D - 1: all their tokens, and those of earlier tiles
+    uint32_t all[D] = {}, before[D] = {};
+    for (uint32_t t = 0; t < gridDim.x; ++t)
+#pragma unroll
+        for (int j = 0; j < D; ++j) {
+            const uint32_t c = hist[(size_t)t * RADIX + D * tid + j];
+            all[j] += c;
+            if (t < blockIdx.x) before[j] += c;
+        }
+    uint32_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < D; ++j) mine += all[j];
+    sums[tid] = mine;
+    __syncthreads();
+    for (int s = 1; s < SORT_T; s <<= 1) {
+        const uint32_t v = tid >= s ? sums[tid - s] : 0;
+        __syncthreads();
+        sums[tid] += v;
+        __syncthreads();
+    }
+    uint32_t start = sums[tid] - mine;
+#pragma unroll
+    for (int j = 0; j < D; ++j) {
+        uint32_t next = start + before[j];
+        for (int w = 0; w < WAVES; ++w) {
+            const uint32_t c = at[w][D * tid + j];
+            at[w][D * tid + j] = next;
+            next += c;
+        }
+        start += all[j];
+    }
+    __syncthreads();
+    for (int64_t r = from; r < from + share && r < M; r += 64) {      // (the same rows for every lane of a wave)
+        const int64_t i = r + lane;
+        const bool there = i < M;
+        const uint32_t k = there ? in.k(i) : 0, digit = k >> shift & mask;
+        uint64_t same = __ballot(there);
+        for (int b = 0; b < bits; ++b) {
+            const bool one = digit >> b & 1u;
+            const uint64_t ones = __ballot(one);
+            same &= one ? ones : ~ones;
+        }
+        const int leader = there ? __ffsll((unsigned long long)same) - 1 : lane;
+        uint32_t first = 0;
+        if (there && lane == leader) first = atomicAdd(&at[wave][digit], (uint32_t)__popcll(same));
+        first = (uint32_t)__shfl((int)first, leader);
+        if (there) {
+            const uint32_t to = first + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+            key[to] = k;
+            pos[to] = in.p(i);
+        }
+    }
+}
+
+// Sums of runs.  Partial sums lie at part[2 chunk + w]: w = 0 of a run that came in from the chunk before, 1 of one that began here
+// and goes on.
+template <class IO, bool DROP>
+__global__ void __launch_bounds__(256)
+embed_sum_kernel(const typename IO::T* __restrict__ dy, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
+                 float* __restrict__ dE, float* __restrict__ part, int64_t M, uint32_t H, uint32_t stride, uint32_t P, uint32_t V,
+                 uint32_t chunks, float scale, Drop d)
+{
+    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t chunk = (uint32_t)(id / P), c = (uint32_t)(id - (uint64_t)chunk * P) * VE;
+    if (chunk >= chunks) return;
+    const int64_t from = (int64_t)chunk * CHUNK, to = from + CHUNK < M ? from + CHUNK : M;
+    const int wide = (int)(H - c);
+    const uint64_t call = DROP ? call_of(d) : 0;
+    const float f = scale * d.scale;
+    uint32_t cur = key[from];
+    bool came_in = from > 0 && key[from - 1] == cur;
+    float acc[VE] = {};
+    const auto keep = [&](int w) {
+        float* q = part + ((size_t)chunk * 2 + w) * (P * VE) + c;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) q[i] = acc[i];
+    };
+    const auto finish = [&] {
+        if (cur >= V) return;
+        if (came_in) { keep(0); return; }
+        float v[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = acc[i] * f;
+        store8<IoF32>(dE + (size_t)cur * H + c, wide, v);
+    };
+    for (int64_t i = from; i < to; ++i) {
+        const uint32_t k = key[i];
+        const size_t p = pos[i];
+        if (k >= V) { if (cur < V) { finish(); cur = k; came_in = false; } break; }      // the sentinel sorts last
+        float v[VE];
+        load8<IO>(dy + p * stride + c, wide, v);
+        if (DROP) {
+            const uint32_t m = kept8_at(p * H + c, d, call);
+#pragma unroll
+            for (int j = 0; j < VE; ++j) v[j] = m >> j & 1u ? v[j] : 0.f;
+        }
+        if (k != cur) {
+            finish();
+            cur = k;
+            came_in = false;
+#pragma unroll
+            for (int j = 0; j < VE; ++j) acc[j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < VE; ++j) acc[j] += v[j];
+    }
+    if (cur >= V) return;
+    if (to < M && key[to] == cur) keep(came_in ? 0 : 1);
+    else finish();
+}
+
+// A run that begins in this chunk and goes on: its partial sums, in the chunks' order.
+__global__ void __launch_bounds__(256)
+embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ part, float* __restrict__ dE, int64_t M, uint32_t H, uint32_t P,
+                  uint32_t V, float f)
+{
+    const uint32_t chunk = blockIdx.x;
+    const int64_t from = (int64_t)chunk * CHUNK, to = from + CHUNK;
+    if (to >= M) return;
+    const uint32_t k = key[to - 1];
+    if (k >= V || key[to] != k) return;
+    if (from > 0 && key[from] == k && key[from - 1] == k) return;      // began earlier
+    int64_t lo = to + 1, hi = M;                                       // the run's end: the first place from `to` on with another token
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (key[mid] == k) lo = mid + 1;
+        else hi = mid;
+    }
+    const uint32_t last = (uint32_t)((lo - 1) / CHUNK);
+    for (uint32_t c = threadIdx.x; c < H; c += 256) {
+        float s = part[((size_t)chunk * 2 + 1) * (P * VE) + c];
+        for (uint32_t q = chunk + 1; q <= last; ++q) s += part[(size_t)q * 2 * (P * VE) + c];
+        dE[(size_t)k * H + c] = s * f;
+    }
+}
+
+size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
+
+struct Layout {      // of the workspace
+    size_t hist, key[2], pos[2], part, rows, total;
+    int64_t M, tile, tiles, chunks;
+    uint32_t P;
+    int passes, bits;
+};
+
+Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
+{
+    Layout l;
+    l.M = B * N;
+    // a pass reads the counts of every tile in every tile: no more than 256 of them, however many tokens there are
+    l.tile = TILE_MIN * ((l.M + (int64_t)TILE_MIN * TILES_MAX - 1) / ((int64_t)TILE_MIN * TILES_MAX));
+    l.tiles = (l.M + l.tile - 1) / l.tile;
+    l.chunks = (l.M + CHUNK - 1) / CHUNK;
+    l.P = (uint32_t)((H + VE - 1) / VE);
+    int need = 0;
+    while (V >> need) ++need;                       // bits of V, the number of no token
+    l.passes = (need + 8) / 9;
+    l.bits = (need + l.passes - 1) / l.passes;
+    size_t off = 0;
+    const auto take = [&](size_t bytes) { const size_t at = off; off += up256(bytes); return at; };
+    l.hist = take((size_t)(l.M < (int64_t)TILE_MIN * TILES_MAX ? (l.M + TILE_MIN - 1) / TILE_MIN : TILES_MAX) * RADIX * sizeof(uint32_t));
+    for (int i = 0; i < 2; ++i) {
+        l.key[i] = take((size_t)l.M * sizeof(uint32_t));
+        l.pos[i] = take((size_t)l.M * sizeof(uint32_t));
+    }
+    l.part = take((size_t)l.chunks * 2 * l.P * VE * sizeof(float));
+    l.rows = take(layout == LONGCONV_CHANNELS_FIRST ? (size_t)l.M * l.P * VE * (io == LONGCONV_F32 ? 4 : 2) : 0);
+    l.total = off;
+    return l;
+}
+
+template <class ID>
+hipError_t sort_pass(const Tokens<ID>& in, char* ws, const Layout& l, int pass, int to, hipStream_t st)
+{
+    uint32_t* hist = (uint32_t*)(ws + l.hist);
+    const dim3 g((unsigned)l.tiles);
+    hipLaunchKernelGGL((sort_count_kernel<ID>), g, dim3(SORT_T), 0, st, in, hist, l.M, l.tile, pass * l.bits, l.bits);
+    hipLaunchKernelGGL((sort_place_kernel<ID>), g, dim3(SORT_T), 0, st, in, (const uint32_t*)hist, (uint32_t*)(ws + l.key[to]),
+                       (uint32_t*)(ws + l.pos[to]), l.M, l.tile, pass * l.bits, l.bits);
+    return hipGetLastError();
+}
+
+template <class ID>
+hipError_t sort_tokens(const ID* ids, int64_t V, char* ws, const Layout& l, hipStream_t st)      // -> key[0], pos[0] or [1], by passes
+{
+    hipError_t e = sort_pass<ID>(Tokens<ID>{ids, nullptr, nullptr, (uint32_t)V}, ws, l, 0, 0, st);
+    for (int pass = 1; pass < l.passes && e == hipSuccess; ++pass) {
+        const int from = (pass - 1) & 1;
+        const Tokens<void> in{nullptr, (const uint32_t*)(ws + l.key[from]), (const uint32_t*)(ws + l.pos[from]), (uint32_t)V};
+        e = sort_pass<void>(in, ws, l, pass, pass & 1, st);
+    }
+    return e;
+}
+
+template <class IO, class W, class ID>
+hipError_t forward(const EmbedArgs& a, const void* E, void* y, hipStream_t st)
+{
+    using T = typename IO::T;
+    dim3 g;
+    const ID* ids = (const ID*)a.ids;
+    const typename W::T* table = (const typename W::T*)E;
+    if (a.layout == LONGCONV_CHANNELS_FIRST) {
+        const uint64_t tt = (a.N + TT - 1) / TT, th = (a.H + TH - 1) / TH;
+        const hipError_t e = launch_grid(a.B * tt * th, 256, &g);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((embed_columns_kernel<IO, W, ID>), g, dim3(256), 0, st, ids, table, (T*)y, (uint32_t)a.N, (uint32_t)a.H,
+                           (uint32_t)a.V, (uint32_t)tt, (uint32_t)th, a.scale, a.drop);
+        return hipGetLastError();
+    }
+    const int64_t n = a.B * a.N * a.H;
+    const hipError_t e = launch_grid((uint64_t)((n + 256 * VE - 1) / (256 * VE)), 256, &g);
+    if (e != hipSuccess) return e;
+    if (n < (int64_t(1) << 31))
+        hipLaunchKernelGGL((embed_rows_kernel<IO, W, ID, uint32_t>), g, dim3(256), 0, st, ids, table, (T*)y, (uint32_t)n, (uint32_t)a.H,
+                           (uint32_t)a.V, a.scale, a.drop);
+    else
+        hipLaunchKernelGGL((embed_rows_kernel<IO, W, ID, uint64_t>), g, dim3(256), 0, st, ids, table, (T*)y, (uint64_t)n, (uint32_t)a.H,
+                           (uint32_t)a.V, a.scale, a.drop);
+    return hipGetLastError();
+}
+
+template <class IO>
+hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hipStream_t st)
+{
+    using T = typename IO::T;
+    const Layout l = lay_out(a.B, a.N, a.V, a.H, a.io, a.layout);
+    dim3 g;
+    hipLaunchKernelGGL(embed_zero_kernel, dim3(2048), dim3(256), 0, st, dE, a.V * a.H);
+    hipError_t e = a.id_bytes == 8 ? sort_tokens((const int64_t*)a.ids, a.V, ws, l, st) : sort_tokens((const int32_t*)a.ids, a.V, ws, l, st);
+    if (e != hipSuccess) return e;
+    const T* rows = (const T*)dy;
+    uint32_t stride = (uint32_t)a.H;
+    if (a.layout == LONGCONV_CHANNELS_FIRST) {
+        const uint64_t tt = (a.N + TT - 1) / TT, th = (a.H + TH - 1) / TH;
+        if ((e = launch_grid(a.B * tt * th, 256, &g)) != hipSuccess) return e;
+        stride = l.P * VE;
+        hipLaunchKernelGGL(embed_transpose_kernel<IO>, g, dim3(256), 0, st, rows, (T*)(ws + l.rows), (uint32_t)a.N, (uint32_t)a.H, stride,
+                           (uint32_t)tt, (uint32_t)th, a.drop);
+        rows = (const T*)(ws + l.rows);
+    }
+    const int last = (l.passes - 1) & 1;
+    const uint32_t *key = (const uint32_t*)(ws + l.key[last]), *pos = (const uint32_t*)(ws + l.pos[last]);
+    float* part = (float*)(ws + l.part);
+    if ((e = launch_grid(((uint64_t)l.chunks * l.P + 255) / 256, 256, &g)) != hipSuccess) return e;
+    if (a.drop.threshold && a.layout == LONGCONV_CHANNELS_LAST)
+        hipLaunchKernelGGL((embed_sum_kernel<IO, true>), g, dim3(256), 0, st, rows, key, pos, dE, part, l.M, (uint32_t)a.H, stride, l.P,
+                           (uint32_t)a.V, (uint32_t)l.chunks, a.scale, a.drop);
+    else
+        hipLaunchKernelGGL((embed_sum_kernel<IO, false>), g, dim3(256), 0, st, rows, key, pos, dE, part, l.M, (uint32_t)a.H, stride, l.P,
+                           (uint32_t)a.V, (uint32_t)l.chunks, a.scale, a.drop);
+    if (l.chunks > 1)
+        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)l.chunks), dim3(256), 0, st, key, (const float*)part, dE, l.M, (uint32_t)a.H,
+                           l.P, (uint32_t)a.V, a.scale * a.drop.scale);
+    return hipGetLastError();
+}
+
+template <class IO, class W>
+hipError_t forward_ids(const EmbedArgs& a, const void* E, void* y, hipStream_t st)
+{
+    return a.id_bytes == 8 ? forward<IO, W, int64_t>(a, E, y, st) : forward<IO, W, int32_t>(a, E, y, st);
+}
+
+}  // namespace
+
+hipError_t embed_fwd(const EmbedArgs& a, const void* E, int table, void* y, hipStream_t st)
+{
+    if (a.io == LONGCONV_F32) return forward_ids<IoF32, IoF32>(a, E, y, st);
+    if (a.io == LONGCONV_F16)
+        return table == LONGCONV_F32 ? forward_ids<IoF16, IoF32>(a, E, y, st) : forward_ids<IoF16, IoF16>(a, E, y, st);
+    return table == LONGCONV_F32 ? forward_ids<IoBF16, IoF32>(a, E, y, st) : forward_ids<IoBF16, IoBF16>(a, E, y, st);
+}
+
+size_t embed_workspace_bytes(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
+{
+    return lay_out(B, N, V, H, io, layout).total;
+}
+
+hipError_t embed_bwd(const EmbedArgs& a, const void* dy, float* dE, void* ws, hipStream_t st)
+{
+    if (a.io == LONGCONV_F32) return backward<IoF32>(a, dy, dE, (char*)ws, st);
+    return a.io == LONGCONV_F16 ? backward<IoF16>(a, dy, dE, (char*)ws, st) : backward<IoBF16>(a, dy, dE, (char*)ws, st);
+}
+
+}  // namespace lc

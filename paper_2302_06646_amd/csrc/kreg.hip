@@ -6,12 +6,15 @@
 //   Kbar = sign(K2) max(|K2| - lambda, 0)        Squash
 //   dK = M * Smooth^T( dKbar * [|K2| > lambda] ) (Smooth with this boundary rule is its own transpose)
 //
+// Instead of a mask the caller may pass a seed: M is then what the counter-based generator (vec8.hpp) gives for the entries of K in
+// memory order.  The window of a workgroup spans at most 49 of its blocks of eight entries: one lane each makes them, into LDS.
+//
 // Plain streaming kernels, bound by one round trip to memory and the launch: a workgroup is one wave (no barriers) with 256
 // consecutive entries of one head, and asks for everything it needs before it uses any of it, four entries of each tensor per lane
 // and their halo; the masked kernel goes through LDS (2p entries per side for the backward chain, which needs K2 on a halo of p).
 // H = 768, N = 1024, p = 1, against a workgroup of 256 threads with an entry each: forward 5.3 -> 4.4 us, backward, which asked for
 // the gradient behind the gate and for the mask a second time, 6.9 -> 5.1; with two entries per lane the two take 1.5 us more.
-#include "engines.hpp"
+#include "vec8.hpp"
 
 namespace lc {
 namespace {
@@ -19,10 +22,10 @@ namespace {
 constexpr int KT = 64, KV = 4, KE = KT * KV;      // lanes, entries of a lane (64 apart), entries of a workgroup
 constexpr int KREG_P_MAX = 32;                    // widest half window
 
-template <bool BWD>
+template <bool BWD, bool SEEDED>
 __global__ void __launch_bounds__(KT)
 kreg_kernel(const float* __restrict__ k, const float* __restrict__ mask, const float* __restrict__ dkbar,
-            float* __restrict__ out, int64_t N, int p, float lam)
+            float* __restrict__ out, int64_t N, int p, float lam, Drop drop)
 {
     constexpr int KH = (BWD ? 4 : 2) * KREG_P_MAX / KT;      // entries of a lane in the halos, at the widest window
     __shared__ float s1[KE + 4 * KREG_P_MAX];      // K1 on [n0 - halo, n0 + KE + halo)
@@ -39,7 +42,7 @@ kreg_kernel(const float* __restrict__ k, const float* __restrict__ mask, const f
 #pragma unroll
     for (int j = 0; j < KV; ++j) {
         kv[j] = get(kr, n0 + t + KT * j);
-        mv[j] = mr ? get(mr, n0 + t + KT * j) : 1.f;
+        if (!SEEDED) mv[j] = mr ? get(mr, n0 + t + KT * j) : 1.f;
         if (BWD) gv[j] = get(dkbar + h * N, n0 + t + KT * j);
     }
 #pragma unroll
@@ -47,14 +50,31 @@ kreg_kernel(const float* __restrict__ k, const float* __restrict__ mask, const f
         const int e = t + KT * j;
         const int64_t n = e < 2 * halo ? n0 + halo_at(e, halo) : -1;
         kh[j] = get(kr, n);
-        mh[j] = mr ? get(mr, n) : 1.f;
+        if (!SEEDED) mh[j] = mr ? get(mr, n) : 1.f;
     }
     if (BWD && t < 2 * p) gh = get(dkbar + h * N, n0 + halo_at(t, p));
+    if constexpr (SEEDED) {
+        __shared__ uint32_t kept[KT];
+        static_assert((KE + 4 * KREG_P_MAX + 2 * VE - 2) / VE < KT, "a lane for every block of the widest window");
+        const int64_t e0 = h * N + n0, first = (e0 - halo) >> 3;      // the window's first block (before the tensor: entries that count as zero)
+        if (first + t <= (e0 + KE + halo - 1) >> 3) kept[t] = kept8((uint64_t)(first + t), drop, call_of(drop));
+        __syncthreads();
+        const auto factor = [&](int i) {
+            const int64_t e = e0 + i;
+            return kept[(e >> 3) - first] >> (e & 7) & 1u ? drop.scale : 0.f;
+        };
 #pragma unroll
-    for (int j = 0; j < KV; ++j) s1[halo + t + KT * j] = kv[j] * mv[j];
+        for (int j = 0; j < KV; ++j) mv[j] = factor(t + KT * j);
+#pragma unroll
+        for (int j = 0; j < KH; ++j) mh[j] = t + KT * j < 2 * halo ? factor(halo_at(t + KT * j, halo)) : 0.f;
+    }
+    // (an entry that the generator drops counts for nothing, whatever it holds)
+    const auto times = [](float v, float m) { return SEEDED && m == 0.f ? 0.f : v * m; };
+#pragma unroll
+    for (int j = 0; j < KV; ++j) s1[halo + t + KT * j] = times(kv[j], mv[j]);
 #pragma unroll
     for (int j = 0; j < KH; ++j)
-        if (t + KT * j < 2 * halo) s1[halo + halo_at(t + KT * j, halo)] = kh[j] * mh[j];
+        if (t + KT * j < 2 * halo) s1[halo + halo_at(t + KT * j, halo)] = times(kh[j], mh[j]);
     __syncthreads();
     // sums of s[i .. i + 2p] at the lane's entries, i = at + t + 64 j, side by side (one after the other they wait for LDS alone)
     const auto windows = [&](const float* s, int at, float (&a)[KV]) {
@@ -91,28 +111,42 @@ kreg_kernel(const float* __restrict__ k, const float* __restrict__ mask, const f
 #pragma unroll
     for (int j = 0; j < KV; ++j) {
         const int64_t n = n0 + t + KT * j;
-        if (n < N) out[h * N + n] = mr ? a[j] * inv * mv[j] : a[j] * inv;
+        if (n < N) out[h * N + n] = SEEDED || mr ? times(a[j] * inv, mv[j]) : a[j] * inv;
     }
 }
 
 }  // namespace
 
-hipError_t kreg_fwd(const float* k, const float* mask, float* kbar, int64_t H, int64_t N, int p, float lam,
-                    hipStream_t st)
+template <bool BWD, bool SEEDED>
+static hipError_t run(const float* k, const float* mask, const float* dkbar, float* out, int64_t H, int64_t N, int p, float lam,
+                      const Drop& drop, hipStream_t st)
 {
     if (p < 0 || p > KREG_P_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)((N + KE - 1) / KE), (unsigned)H);
-    hipLaunchKernelGGL(kreg_kernel<false>, grid, dim3(KT), 0, st, k, mask, (const float*)nullptr, kbar, N, p, lam);
+    hipLaunchKernelGGL((kreg_kernel<BWD, SEEDED>), grid, dim3(KT), 0, st, k, mask, dkbar, out, N, p, lam, drop);
     return hipGetLastError();
 }
 
-hipError_t kreg_bwd(const float* k, const float* mask, const float* dkbar, float* dk, int64_t H, int64_t N, int p,
-                    float lam, hipStream_t st)
+hipError_t kreg_fwd(const float* k, const float* mask, float* kbar, int64_t H, int64_t N, int p, float lam, hipStream_t st)
 {
-    if (p < 0 || p > KREG_P_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((N + KE - 1) / KE), (unsigned)H);
-    hipLaunchKernelGGL(kreg_kernel<true>, grid, dim3(KT), 0, st, k, mask, dkbar, dk, N, p, lam);
-    return hipGetLastError();
+    return run<false, false>(k, mask, nullptr, kbar, H, N, p, lam, Drop{}, st);
+}
+
+hipError_t kreg_bwd(const float* k, const float* mask, const float* dkbar, float* dk, int64_t H, int64_t N, int p, float lam,
+                    hipStream_t st)
+{
+    return run<true, false>(k, mask, dkbar, dk, H, N, p, lam, Drop{}, st);
+}
+
+hipError_t kreg_fwd_seeded(const float* k, float* kbar, int64_t H, int64_t N, int p, float lam, const Drop& drop, hipStream_t st)
+{
+    return run<false, true>(k, nullptr, nullptr, kbar, H, N, p, lam, drop, st);
+}
+
+hipError_t kreg_bwd_seeded(const float* k, const float* dkbar, float* dk, int64_t H, int64_t N, int p, float lam, const Drop& drop,
+                           hipStream_t st)
+{
+    return run<true, true>(k, nullptr, dkbar, dk, H, N, p, lam, drop, st);
 }
 
 }  // namespace lc

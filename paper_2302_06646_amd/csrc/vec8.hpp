@@ -1,0 +1,162 @@
+// Shared by the streaming operators around the convolution (dropout.hip, embed.hip, gnorm.hip, kreg.hip): eight elements of a
+// tensor at a time as floats, at any element's address, and the counter-based generator behind every dropout mask.
+#pragma once
+#include "mfma_util.hpp"
+#include "operators.hpp"
+
+namespace lc {
+
+// Sixteen bytes at the address of any element: gfx950 loads and stores them in one instruction whatever the alignment.
+template <class IO>
+struct __attribute__((packed)) Any16 {
+    uint32_t w[4];
+};
+constexpr int VE = 8;      // elements of a piece
+
+template <class IO>
+__device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b)
+{
+    if constexpr (mu::IsBf<IO>::v) {
+        a = __uint_as_float(w << 16);
+        b = __uint_as_float(w & 0xffff0000u);
+    } else {
+        union { uint32_t u; mu::h2 h; } x;
+        x.u = w;
+        a = (float)x.h[0];
+        b = (float)x.h[1];
+    }
+}
+
+// a piece as it lies in memory: 4 words of two 16-bit elements, or 8 words of one float
+template <class IO>
+struct Raw8 {
+    static constexpr int W = sizeof(typename IO::T) == 4 ? 8 : 4;
+    uint32_t w[W];
+    __device__ __forceinline__ void load(const typename IO::T* p)
+    {
+        const Any16<IO>* q = reinterpret_cast<const Any16<IO>*>(p);
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) {
+            const Any16<IO> v = q[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[4 * i + j] = v.w[j];
+        }
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void get(float (&v)[VE]) const
+    {
+        if constexpr (W == 8) {
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) unpack2<IO>(w[i], v[2 * i], v[2 * i + 1]);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[VE])      // rounds to the nearest, the one rounding of a result
+    {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (W == 8) w[i] = __float_as_uint(v[i]);
+            else w[i] = mu::IsBf<IO>::v ? mu::pack_bf2(v[2 * i], v[2 * i + 1]) : mu::pack_h2(v[2 * i], v[2 * i + 1]);
+        }
+    }
+    __device__ __forceinline__ void store(typename IO::T* p) const
+    {
+        Any16<IO>* q = reinterpret_cast<Any16<IO>*>(p);
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) {
+            Any16<IO> v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v.w[j] = w[4 * i + j];
+            q[i] = v;
+        }
+    }
+};
+
+// eight elements, or the first `n` of them (the others read as zero)
+template <class IO>
+__device__ __forceinline__ void load8(const typename IO::T* p, int n, float (&v)[VE])
+{
+    if (n >= VE) {
+        Raw8<IO> r;
+        r.load(p);
+        r.get(v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = i < n ? IO::ld(p, i) : 0.f;
+}
+template <class IO>
+__device__ __forceinline__ void store8(typename IO::T* p, int n, const float (&v)[VE])
+{
+    if (n >= VE) {
+        Raw8<IO> r;
+        r.set(v);
+        r.store(p);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < VE; ++i)
+        if (i < n) IO::st(p, i, v[i]);
+}
+
+// ---------------------------------------------------------------------------------
+// Dropout masks.  Philox4x32 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): a bijection of a
+// 128-bit counter under a 64-bit key, so every piece of a mask is a function of its place alone and nothing is ever stored.  Seven
+// rounds, the fewest that the authors report to pass BigCrush.  Sixteen bits decide an entry (p is therefore a multiple of 2^-16), so
+// one counter serves the eight entries of a piece: entry e has half e mod 8 of counter (e / 8, call), low half of a word first.
+// ---------------------------------------------------------------------------------
+__device__ __forceinline__ uint64_t call_of(const Drop& d) { return d.step ? d.call + (uint64_t)*d.step : d.call; }
+
+__device__ __forceinline__ uint4 philox(uint64_t block, uint64_t call, uint64_t seed)
+{
+    uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)call, c3 = (uint32_t)(call >> 32);
+    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+#pragma unroll
+    for (int r = 0; r < 7; ++r) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+
+// bit j: entry 8 block + j is kept
+__device__ __forceinline__ uint32_t kept8(uint64_t block, const Drop& d, uint64_t call)
+{
+    const uint4 r = philox(block, call, d.seed);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m |= (w[i] & 0xffffu) >= d.threshold ? 1u << (2 * i) : 0u;
+        m |= (w[i] >> 16) >= d.threshold ? 2u << (2 * i) : 0u;
+    }
+    return m;
+}
+// bit j: entry e + j is kept
+__device__ __forceinline__ uint32_t kept8_at(uint64_t e, const Drop& d, uint64_t call)
+{
+    const uint32_t at = (uint32_t)e & 7u;
+    uint32_t m = kept8(e >> 3, d, call);
+    if (at) m = (m | kept8((e >> 3) + 1, d, call) << 8) >> at;
+    return m & 0xffu;
+}
+
+inline hipError_t launch_grid(uint64_t blocks, uint32_t threads, dim3* g)      // 1-D grid; a launch holds fewer than 2^32 threads
+{
+    if (blocks == 0 || blocks * threads > 0xffffffffull) return hipErrorInvalidValue;
+    *g = dim3((unsigned)blocks);
+    return hipSuccess;
+}
+
+}  // namespace lc
