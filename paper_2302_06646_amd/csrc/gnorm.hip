@@ -16,11 +16,34 @@ constexpr int GT = 256;              // threads
 constexpr int SLAB = 64;             // pieces of eight channels of a workgroup, at most
 constexpr int GROUPS_WANTED = 2048;  // workgroups of a pass over the tensor
 
+// The normal distribution function, and e = exp(-z^2 / 2) beside it.  erfc(x) exp(x^2) is t Q(t), t = 1 / (1 + 0.4 x), for x >= 0, Q the
+// polynomial of degree eight of the least largest relative error (fitted by weighted least squares): 1.3e-7, and 2.2e-7 absolute in
+// fp32.  Below zero the result is not a difference, so its relative error is that of e, 8e-7 down to z = -4.
+__device__ __forceinline__ float normal_cdf(float z, float& e)
+{
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.28284271247461901f, fabsf(z), 1.f));
+    float q = 0.0502542145550251f;
+    q = __builtin_fmaf(q, t, -0.18287357687950134f);
+    q = __builtin_fmaf(q, t, 0.16904595494270325f);
+    q = __builtin_fmaf(q, t, -0.0055788299068808556f);
+    q = __builtin_fmaf(q, t, 0.14142005145549774f);
+    q = __builtin_fmaf(q, t, 0.16854438185691833f);
+    q = __builtin_fmaf(q, t, 0.20784245431423187f);
+    q = __builtin_fmaf(q, t, 0.22566960752010345f);
+    q = __builtin_fmaf(q, t, 0.22567586600780487f);
+    e = exp2f(z * z * -0.72134752044448170f);
+    const float h = 0.5f * q * t * e;
+    return z < 0.f ? h : 1.f - h;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_of(float z)
 {
     if constexpr (ACT == LONGCONV_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
-    if constexpr (ACT == LONGCONV_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == LONGCONV_ACT_GELU) {
+        float e;
+        return z * normal_cdf(z, e);
+    }
     if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
     return z;
 }
@@ -31,8 +54,11 @@ __device__ __forceinline__ float slope_of(float z)
         const float q = __builtin_amdgcn_rcpf(1.f + __expf(-z));
         return q * (1.f + z * (1.f - q));
     }
-    if constexpr (ACT == LONGCONV_ACT_GELU)
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+    if constexpr (ACT == LONGCONV_ACT_GELU) {
+        float e;
+        const float c = normal_cdf(z, e);
+        return __builtin_fmaf(z * 0.39894228040143268f, e, c);
+    }
     if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? 1.f : 0.f;
     return 1.f;
 }
