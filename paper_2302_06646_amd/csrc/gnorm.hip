@@ -12,9 +12,10 @@
 namespace lc {
 namespace {
 
-constexpr int GT = 256;              // threads
+constexpr int GT = 512;              // threads
 constexpr int SLAB = 64;             // pieces of eight channels of a workgroup, at most
-constexpr int GROUPS_WANTED = 2048;  // workgroups of a pass over the tensor
+constexpr int GROUPS_WANTED = 1024;  // workgroups of a pass over the tensor
+constexpr int AHEAD = 4;             // pieces that a thread asks for before it uses the first
 
 // The normal distribution function, and e = exp(-z^2 / 2) beside it.  erfc(x) exp(x^2) is t Q(t), t = 1 / (1 + 0.4 x), for x >= 0, Q the
 // polynomial of degree eight of the least largest relative error (fitted by weighted least squares): 1.3e-7, and 2.2e-7 absolute in
@@ -31,7 +32,7 @@ __device__ __forceinline__ float normal_cdf(float z, float& e)
     q = __builtin_fmaf(q, t, 0.20784245431423187f);
     q = __builtin_fmaf(q, t, 0.22566960752010345f);
     q = __builtin_fmaf(q, t, 0.22567586600780487f);
-    e = exp2f(z * z * -0.72134752044448170f);
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
     const float h = 0.5f * q * t * e;
     return z < 0.f ? h : 1.f - h;
 }
@@ -39,7 +40,7 @@ __device__ __forceinline__ float normal_cdf(float z, float& e)
 template <int ACT>
 __device__ __forceinline__ float act_of(float z)
 {
-    if constexpr (ACT == LONGCONV_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    if constexpr (ACT == LONGCONV_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
     if constexpr (ACT == LONGCONV_ACT_GELU) {
         float e;
         return z * normal_cdf(z, e);
@@ -51,7 +52,7 @@ template <int ACT>
 __device__ __forceinline__ float slope_of(float z)
 {
     if constexpr (ACT == LONGCONV_ACT_SILU) {
-        const float q = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        const float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
         return q * (1.f + z * (1.f - q));
     }
     if constexpr (ACT == LONGCONV_ACT_GELU) {
@@ -67,7 +68,7 @@ __device__ __forceinline__ float slope_of(float z)
 __device__ __forceinline__ void merge(float& n, float& mean, float& m2, float n2, float mean2, float m22)
 {
     if (n2 == 0.f) return;
-    const float all = n + n2, d = mean2 - mean, f = n2 / all;
+    const float all = n + n2, d = mean2 - mean, f = n2 * __builtin_amdgcn_rcpf(all);
     mean = __builtin_fmaf(d, f, mean);
     m2 += m22 + d * d * n * f;
     n = all;
@@ -134,16 +135,24 @@ gnorm_stats_kernel(const typename IO::T* __restrict__ x, float* __restrict__ par
     const Place p = place(w, S, C);
     float mean[VE] = {}, m2[VE] = {}, n = 0.f;
     if (p.on)
-        for (int64_t i = p.from + p.r; i < p.to; i += w.rows) {
-            float v[VE];
-            load8<IO>(x + ((int64_t)p.b * S + i) * C + p.c, p.wide, v);
-            n += 1.f;
-            const float f = __builtin_amdgcn_rcpf(n);
+        for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD * w.rows) {
+            Raw8<IO> raw[AHEAD];
 #pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                const float d = v[j] - mean[j];
-                mean[j] = __builtin_fmaf(d, f, mean[j]);
-                m2[j] = __builtin_fmaf(d, v[j] - mean[j], m2[j]);
+            for (int u = 0; u < AHEAD; ++u)
+                load_raw<IO>(x + ((int64_t)p.b * S + i + u * w.rows) * C + p.c, i + u * w.rows < p.to ? p.wide : 0, raw[u]);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (i + u * w.rows >= p.to) break;
+                float v[VE];
+                raw[u].get(v);
+                n += 1.f;
+                const float f = __builtin_amdgcn_rcpf(n);
+#pragma unroll
+                for (int j = 0; j < VE; ++j) {
+                    const float d = v[j] - mean[j];
+                    mean[j] = __builtin_fmaf(d, f, mean[j]);
+                    m2[j] = __builtin_fmaf(d, v[j] - mean[j], m2[j]);
+                }
             }
         }
     const int t = threadIdx.x;
@@ -227,14 +236,21 @@ gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restr
     if (!p.on) return;
     Channels k;
     k.load(p, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
-    for (int64_t i = p.from + p.r; i < p.to; i += w.rows) {
-        const size_t e = ((size_t)p.b * S + i) * C + p.c;
-        float v[VE];
-        load8<IO>(x + e, p.wide, v);
+    for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD * w.rows) {
+        const size_t e = ((size_t)p.b * S + i) * C + p.c, more = (size_t)w.rows * C;
+        Raw8<IO> raw[AHEAD];
 #pragma unroll
-        for (int j = 0; j < VE; ++j)
-            v[j] = act_of<ACT>(__builtin_fmaf((v[j] - k.mean[j]) * k.rstd[j], k.gamma[j], k.beta[j]));
-        store8<IO>(y + e, p.wide, v);
+        for (int u = 0; u < AHEAD; ++u) load_raw<IO>(x + e + u * more, i + u * w.rows < p.to ? p.wide : 0, raw[u]);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (i + u * w.rows >= p.to) break;
+            float v[VE];
+            raw[u].get(v);
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+                v[j] = act_of<ACT>(__builtin_fmaf((v[j] - k.mean[j]) * k.rstd[j], k.gamma[j], k.beta[j]));
+            store8<IO>(y + e + u * more, p.wide, v);
+        }
     }
 }
 
@@ -251,17 +267,28 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
     if (p.on) {
         Channels k;
         k.load(p, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
-        for (int64_t i = p.from + p.r; i < p.to; i += w.rows) {
-            const size_t e = ((size_t)p.b * S + i) * C + p.c;
-            float v[VE], g[VE];
-            load8<IO>(x + e, p.wide, v);
-            load8<IO>(dy + e, p.wide, g);
+        for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD / 2 * w.rows) {
+            const size_t e = ((size_t)p.b * S + i) * C + p.c, more = (size_t)w.rows * C;
+            Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
 #pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                const float h = (v[j] - k.mean[j]) * k.rstd[j];
-                const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
-                a[j] += dz;
-                b[j] = __builtin_fmaf(dz, h, b[j]);
+            for (int u = 0; u < AHEAD / 2; ++u) {
+                const int n = i + u * w.rows < p.to ? p.wide : 0;
+                load_raw<IO>(x + e + u * more, n, rx[u]);
+                load_raw<IO>(dy + e + u * more, n, rg[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD / 2; ++u) {
+                if (i + u * w.rows >= p.to) break;
+                float v[VE], g[VE];
+                rx[u].get(v);
+                rg[u].get(g);
+#pragma unroll
+                for (int j = 0; j < VE; ++j) {
+                    const float h = (v[j] - k.mean[j]) * k.rstd[j];
+                    const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
+                    a[j] += dz;
+                    b[j] = __builtin_fmaf(dz, h, b[j]);
+                }
             }
         }
     }
@@ -294,17 +321,23 @@ __device__ __forceinline__ float wave_sum(float v)
     return v;
 }
 
-// waves 0 .. B G - 1: s1 and s2 of a group; the next C: dgamma and dbeta of a channel
-__global__ void __launch_bounds__(64)
+constexpr int RT = 1024, RC = 16;      // threads of a workgroup that sums channels, and channels of it
+
+// workgroups 0 .. ceil(C / 16) - 1: dgamma and dbeta of sixteen channels, the rows of partial results spread over the threads; behind
+// them sixteen groups each, s1 and s2 by a wave for every group
+__global__ void __launch_bounds__(RT)
 gnorm_gather_kernel(const float* __restrict__ part, const float* __restrict__ gamma, float* __restrict__ s1, float* __restrict__ s2,
                     float* __restrict__ dgamma, float* __restrict__ dbeta, int64_t B, int64_t C, uint32_t G, uint32_t parts)
 {
-    const uint32_t D = (uint32_t)(C / G);
+    __shared__ float sa[RT], sh[RT];
+    const uint32_t D = (uint32_t)(C / G), blocks = (uint32_t)((C + RC - 1) / RC);
     float a = 0.f, h = 0.f;
-    if (blockIdx.x < B * G) {
-        const uint32_t b = blockIdx.x / G, g = blockIdx.x % G;
-        for (uint64_t i = threadIdx.x; i < (uint64_t)parts * D; i += 64) {
-            const uint32_t q = (uint32_t)(i / D), c = g * D + (uint32_t)(i - (uint64_t)q * D);
+    if (blockIdx.x >= blocks) {
+        const uint32_t id = (blockIdx.x - blocks) * (RT / 64) + threadIdx.x / 64;
+        if (id >= (uint32_t)B * G) return;
+        const uint32_t b = id / G, g = id % G;
+        for (uint32_t i = threadIdx.x % 64; i < parts * D; i += 64) {
+            const uint32_t q = i / D, c = g * D + (i - q * D);
             const float* row = part + ((size_t)b * parts + q) * 2 * C;
             const float ga = gamma ? gamma[c] : 1.f;
             a = __builtin_fmaf(ga, row[c], a);
@@ -312,22 +345,32 @@ gnorm_gather_kernel(const float* __restrict__ part, const float* __restrict__ ga
         }
         a = wave_sum(a);
         h = wave_sum(h);
-        if (threadIdx.x == 0) {
-            s1[blockIdx.x] = a;
-            s2[blockIdx.x] = h;
+        if (threadIdx.x % 64 == 0) {
+            s1[id] = a;
+            s2[id] = h;
         }
         return;
     }
-    const uint32_t c = blockIdx.x - (uint32_t)(B * G);
-    for (uint64_t i = threadIdx.x; i < (uint64_t)B * parts; i += 64) {
-        a += part[i * 2 * C + c];
-        h += part[i * 2 * C + C + c];
+    const uint32_t c = blockIdx.x * RC + threadIdx.x % RC, rows = (uint32_t)B * parts;
+    if (c < C) {
+#pragma unroll 8
+        for (uint32_t i = threadIdx.x / RC; i < rows; i += RT / RC) {
+            a += part[(size_t)i * 2 * C + c];
+            h += part[(size_t)i * 2 * C + C + c];
+        }
     }
-    a = wave_sum(a);
-    h = wave_sum(h);
-    if (threadIdx.x == 0) {
-        if (dbeta) dbeta[c] = a;
-        if (dgamma) dgamma[c] = h;
+    sa[threadIdx.x] = a;
+    sh[threadIdx.x] = h;
+    for (int s = RT / 2; s >= RC; s >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < s) {
+            sa[threadIdx.x] += sa[threadIdx.x + s];
+            sh[threadIdx.x] += sh[threadIdx.x + s];
+        }
+    }
+    if (threadIdx.x < RC && c < C) {
+        if (dbeta) dbeta[c] = sa[threadIdx.x];
+        if (dgamma) dgamma[c] = sh[threadIdx.x];
     }
 }
 
@@ -349,18 +392,29 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
         c1[j] = s1[g] * inv;
         c2[j] = s2[g] * inv;
     }
-    for (int64_t i = p.from + p.r; i < p.to; i += w.rows) {
-        const size_t e = ((size_t)p.b * S + i) * C + p.c;
-        float v[VE], g[VE];
-        load8<IO>(x + e, p.wide, v);
-        load8<IO>(dy + e, p.wide, g);
+    for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD / 2 * w.rows) {
+        const size_t e = ((size_t)p.b * S + i) * C + p.c, more = (size_t)w.rows * C;
+        Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
 #pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            const float h = (v[j] - k.mean[j]) * k.rstd[j];
-            const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
-            v[j] = k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - h * c2[j]);
+        for (int u = 0; u < AHEAD / 2; ++u) {
+            const int n = i + u * w.rows < p.to ? p.wide : 0;
+            load_raw<IO>(x + e + u * more, n, rx[u]);
+            load_raw<IO>(dy + e + u * more, n, rg[u]);
         }
-        store8<IO>(dx + e, p.wide, v);
+#pragma unroll
+        for (int u = 0; u < AHEAD / 2; ++u) {
+            if (i + u * w.rows >= p.to) break;
+            float v[VE], g[VE];
+            rx[u].get(v);
+            rg[u].get(g);
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                const float h = (v[j] - k.mean[j]) * k.rstd[j];
+                const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
+                v[j] = k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - h * c2[j]);
+            }
+            store8<IO>(dx + e + u * more, p.wide, v);
+        }
     }
 }
 
@@ -391,14 +445,14 @@ hipError_t backward(const GnormArgs& a, const void* dy, const void* x, const flo
     const Walk w = walk(a.B, a.S, a.C);
     dim3 g, gg;
     hipError_t e = launch_grid((uint64_t)a.B * w.parts * w.slabs, GT, &g);
-    if (e == hipSuccess) e = launch_grid((uint64_t)a.B * a.G + (uint64_t)a.C, 64, &gg);
+    if (e == hipSuccess) e = launch_grid((uint64_t)(a.C + RC - 1) / RC + ((uint64_t)a.B * a.G + RT / 64 - 1) / (RT / 64), RT, &gg);
     if (e != hipSuccess) return e;
     float* part = (float*)ws;
     float* s1 = (float*)((char*)ws + up256(part_rows(a.B, a.S, a.C) * 2 * a.C * sizeof(float)));
     float* s2 = s1 + a.B * a.G;
     hipLaunchKernelGGL((gnorm_sums_kernel<IO, ACT>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta, part, a.S,
                        a.C, (uint32_t)a.G, w);
-    hipLaunchKernelGGL(gnorm_gather_kernel, gg, dim3(64), 0, st, (const float*)part, a.gamma, s1, s2, dgamma, dbeta, a.B, a.C, (uint32_t)a.G,
+    hipLaunchKernelGGL(gnorm_gather_kernel, gg, dim3(RT), 0, st, (const float*)part, a.gamma, s1, s2, dgamma, dbeta, a.B, a.C, (uint32_t)a.G,
                        w.parts);
     if (dx)
         hipLaunchKernelGGL((gnorm_dx_kernel<IO, ACT>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta,

@@ -78,6 +78,19 @@ struct Raw8 {
     }
 };
 
+// a piece, or its first `n` elements (the others read as zero); n < 1: none
+template <class IO>
+__device__ __forceinline__ void load_raw(const typename IO::T* p, int n, Raw8<IO>& r)
+{
+    if (n >= VE) { r.load(p); return; }
+    r.zero();
+#pragma unroll
+    for (int i = 0; i < VE; ++i)
+        if (i < n) {
+            if constexpr (Raw8<IO>::W == 8) r.w[i] = __float_as_uint(p[i]);
+            else r.w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (i % 2 * 16);
+        }
+}
 // eight elements, or the first `n` of them (the others read as zero)
 template <class IO>
 __device__ __forceinline__ void load8(const typename IO::T* p, int n, float (&v)[VE])
