@@ -46,7 +46,7 @@ dropout_kernel(const typename IO::T* x, const typename IO::T* r, typename IO::T*
     // (a dropped entry counts for nothing, whatever it holds)
 #pragma unroll
     for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? __builtin_fmaf(v[i], d.scale, s[i]) : s[i];
-    store8<IO>(y + e, here, v);
+    store8<IO, true>(y + e, here, v);
 }
 
 template <class IO>

@@ -58,7 +58,7 @@ embed_rows_kernel(const ID* __restrict__ ids, const typename W::T* __restrict__ 
     const float f = scale * d.scale;
 #pragma unroll
     for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? v[i] * f : 0.f;
-    store8<IO>(y + e, here, v);
+    store8<IO, true>(y + e, here, v);
 }
 
 constexpr int TT = 64, TH = 64;      // tokens and channels of a tile
@@ -95,7 +95,7 @@ embed_columns_kernel(const ID* __restrict__ ids, const typename W::T* __restrict
         float v[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? tile[h - h0][VE * s + i] * f : 0.f;
-        store8<IO>(y + e, (int)(N - t), v);
+        store8<IO, true>(y + e, (int)(N - t), v);
     }
 }
 

@@ -210,18 +210,40 @@ gnorm_group_kernel(const float* __restrict__ part, float* __restrict__ mean, flo
     }
 }
 
+// eight parameters of the channels from c on (those beyond a tensor's last as `or_else`); p may be null
+__device__ __forceinline__ void load_params(const float* p, int c, int wide, float or_else, float (&v)[VE])
+{
+#pragma unroll
+    for (int j = 0; j < VE; ++j) v[j] = or_else;
+    if (!p || wide < 1) return;
+    load8<IoF32>(p + c, wide, v);
+}
+
 struct Channels {      // of a thread's piece
     float mean[VE], rstd[VE], gamma[VE], beta[VE];
     __device__ __forceinline__ void load(const Place& p, const float* mn, const float* rs, const float* ga, const float* be, uint32_t G, uint32_t D)
     {
+        load_params(ga, p.c, p.wide, 1.f, gamma);
+        load_params(be, p.c, p.wide, 0.f, beta);
+        each_group(p, G, D, [&](int j, size_t g) {
+            mean[j] = mn[g];
+            rstd[j] = rs[g];
+        });
+    }
+    // f(j, number of the group of channel j): one division for the eight
+    template <class F>
+    static __device__ __forceinline__ void each_group(const Place& p, uint32_t G, uint32_t D, F&& f)
+    {
+        uint32_t g = (uint32_t)p.c / D, at = (uint32_t)p.c - g * D;
+        if (at + VE <= D) {
+#pragma unroll
+            for (int j = 0; j < VE; ++j) f(j, (size_t)p.b * G + g);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-            const bool on = j < p.wide;
-            const uint32_t c = (uint32_t)(p.c + j), g = on ? c / D : 0;
-            mean[j] = on ? mn[(size_t)p.b * G + g] : 0.f;
-            rstd[j] = on ? rs[(size_t)p.b * G + g] : 0.f;
-            gamma[j] = on && ga ? ga[c] : 1.f;
-            beta[j] = on && be ? be[c] : 0.f;
+            f(j, (size_t)p.b * G + (g < G ? g : G - 1));
+            if (++at == D) { at = 0; ++g; }
         }
     }
 };
@@ -249,7 +271,7 @@ gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restr
 #pragma unroll
             for (int j = 0; j < VE; ++j)
                 v[j] = act_of<ACT>(__builtin_fmaf((v[j] - k.mean[j]) * k.rstd[j], k.gamma[j], k.beta[j]));
-            store8<IO>(y + e + u * more, p.wide, v);
+            store8<IO, true>(y + e + u * more, p.wide, v);
         }
     }
 }
@@ -386,12 +408,10 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
     Channels k;
     k.load(p, mean, rstd, gamma, beta, G, D);
     float c1[VE], c2[VE];
-#pragma unroll
-    for (int j = 0; j < VE; ++j) {
-        const size_t g = (size_t)p.b * G + (j < p.wide ? (uint32_t)(p.c + j) / D : 0);
+    Channels::each_group(p, G, D, [&](int j, size_t g) {
         c1[j] = s1[g] * inv;
         c2[j] = s2[g] * inv;
-    }
+    });
     for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD / 2 * w.rows) {
         const size_t e = ((size_t)p.b * S + i) * C + p.c, more = (size_t)w.rows * C;
         Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
@@ -413,7 +433,7 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
                 const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
                 v[j] = k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - h * c2[j]);
             }
-            store8<IO>(dx + e + u * more, p.wide, v);
+            store8<IO, true>(dx + e + u * more, p.wide, v);
         }
     }
 }

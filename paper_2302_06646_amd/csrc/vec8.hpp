@@ -1,16 +1,16 @@
 // Shared by the streaming operators around the convolution (dropout.hip, embed.hip, gnorm.hip, kreg.hip): eight elements of a
 // tensor at a time as floats, at any element's address, and the counter-based generator behind every dropout mask.
 #pragma once
+#include <type_traits>
+
 #include "mfma_util.hpp"
 #include "operators.hpp"
 
 namespace lc {
 
 // Sixteen bytes at the address of any element: gfx950 loads and stores them in one instruction whatever the alignment.
-template <class IO>
-struct __attribute__((packed)) Any16 {
-    uint32_t w[4];
-};
+typedef uint32_t At2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t At4 __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int VE = 8;      // elements of a piece
 
 template <class IO>
@@ -31,15 +31,16 @@ __device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b)
 template <class IO>
 struct Raw8 {
     static constexpr int W = sizeof(typename IO::T) == 4 ? 8 : 4;
+    typedef typename std::conditional<W == 8, At4, At2>::type V;
     uint32_t w[W];
     __device__ __forceinline__ void load(const typename IO::T* p)
     {
-        const Any16<IO>* q = reinterpret_cast<const Any16<IO>*>(p);
+        const V* q = reinterpret_cast<const V*>(p);
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
-            const Any16<IO> v = q[i];
+            const V v = q[i];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[4 * i + j] = v.w[j];
+            for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
         }
     }
     __device__ __forceinline__ void zero()
@@ -65,15 +66,16 @@ struct Raw8 {
             else w[i] = mu::IsBf<IO>::v ? mu::pack_bf2(v[2 * i], v[2 * i + 1]) : mu::pack_h2(v[2 * i], v[2 * i + 1]);
         }
     }
+    // ONCE: with the hint that the line is not read again soon (put_once)
+    template <bool ONCE = false>
     __device__ __forceinline__ void store(typename IO::T* p) const
     {
-        Any16<IO>* q = reinterpret_cast<Any16<IO>*>(p);
+        V* q = reinterpret_cast<V*>(p);
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
-            Any16<IO> v;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v.w[j] = w[4 * i + j];
-            q[i] = v;
+            const V v = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+            if constexpr (ONCE) __builtin_nontemporal_store(v, q + i);
+            else q[i] = v;
         }
     }
 };
@@ -104,13 +106,13 @@ __device__ __forceinline__ void load8(const typename IO::T* p, int n, float (&v)
 #pragma unroll
     for (int i = 0; i < VE; ++i) v[i] = i < n ? IO::ld(p, i) : 0.f;
 }
-template <class IO>
+template <class IO, bool ONCE = false>
 __device__ __forceinline__ void store8(typename IO::T* p, int n, const float (&v)[VE])
 {
     if (n >= VE) {
         Raw8<IO> r;
         r.set(v);
-        r.store(p);
+        r.template store<ONCE>(p);
         return;
     }
 #pragma unroll
