@@ -868,7 +868,6 @@ int longconv_kreg_bwd(const float* k, const float* drop_mask, const float* dkbar
 
 static bool bad_dtype(int io) { return io != LONGCONV_F32 && io != LONGCONV_F16 && io != LONGCONV_BF16; }
 static bool bad_share(float p) { return !(p >= 0.f && p <= 1.f); }
-constexpr int64_t MAX_ELEMENTS = int64_t(1) << 34;      // of one tensor: what one launch covers
 
 static int run_dropout(const void* x, const void* residual, void* y, int64_t n, int64_t tie, int io, float p, uint64_t seed, uint64_t call,
                        const int64_t* step, void* stream)

@@ -90,7 +90,8 @@ Walk walk(int64_t B, int64_t S, int64_t C)
     int64_t parts = GROUPS_WANTED / (B * w.slabs);
     const int64_t most = (S + 4 * w.rows - 1) / (4 * w.rows);      // four positions of a thread at least
     if (parts > most) parts = most;
-    if (parts < 1) parts = 1;
+    const int64_t least = (S * C >> 28) + 1;                       // of less than 2^28 elements each: byte offsets fit 31 bits
+    if (parts < least) parts = least;
     w.per = (S + parts - 1) / parts;
     w.parts = (uint32_t)((S + w.per - 1) / w.per);
     return w;
@@ -100,49 +101,160 @@ size_t part_rows(int64_t B, int64_t S, int64_t C)
 {
     const Walk w = walk(1, S, C);
     const int64_t most = (S + 4 * w.rows - 1) / (4 * w.rows), wanted = GROUPS_WANTED / w.slabs;
-    const int64_t all = B * most;
-    return (size_t)(all < wanted ? all : B > wanted ? B : wanted);
+    const int64_t some = B > wanted ? B : wanted, least = B + (MAX_ELEMENTS >> 28);      // (parts of 2^28 elements: so many more than B at most)
+    const int64_t rows = B * most < some ? B * most : some;
+    return (size_t)(rows > least ? rows : least);
 }
 
-struct Place {
-    uint32_t b, part, slab, s, r;
-    int64_t from, to;
-    int c, wide;          // first channel of the thread's piece, channels it has there (0: none)
+// the sum over a wave, in every lane: rows of sixteen lanes by permutations within the vector registers, then the four rows
+__device__ __forceinline__ float wave_sum(float v)
+{
+    const auto moved = [](float x, auto control) {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(control)::value, 0xf, 0xf, false));
+    };
+    v += moved(v, std::integral_constant<int, 0xB1>());       // neighbours within a pair
+    v += moved(v, std::integral_constant<int, 0x4E>());       // pairs within four
+    v += moved(v, std::integral_constant<int, 0x141>());      // fours within eight, mirrored
+    v += moved(v, std::integral_constant<int, 0x140>());      // eights within sixteen, mirrored
+    const auto row = [&](int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); };
+    return (row(0) + row(16)) + (row(32) + row(48));
+}
+
+// A thread's eight channels.  The last piece of a row ends with the row: it begins `skip` channels early, which belong to the piece
+// before, so that every load is whole and inside the tensor.  (Rows of fewer than eight channels, NARROW: one piece, loaded by elements.)
+struct Piece {
+    int c, skip, wide;           // first channel; channels of another thread; channels loaded
     bool on;
+    uint32_t off, step, end;     // bytes from a part's first element to the thread's first piece; to its next one; to the last there may be
+    template <class IO>
+    __device__ __forceinline__ void from_row(uint32_t row, uint32_t rows, uint32_t positions, int64_t C)
+    {
+        const uint32_t size = sizeof(typename IO::T), bytes = (uint32_t)C * size;
+        off = row * bytes + (uint32_t)c * size;
+        step = rows * bytes;
+        end = (positions - 1u) * bytes + (uint32_t)c * size;
+    }
+    __device__ __forceinline__ bool has(uint32_t o) const { return o <= end; }
+    // where a piece is, or the last one of the part where it lies behind that
+    template <class T>
+    __device__ __forceinline__ T* at(T* base, uint32_t o) const
+    {
+        const uint32_t in = o < end ? o : end;
+        typedef typename std::conditional<std::is_const<T>::value, const char, char>::type Byte;
+        return reinterpret_cast<T*>(reinterpret_cast<Byte*>(base) + in);
+    }
+    __device__ __forceinline__ void set(int slot, bool there, int64_t C)
+    {
+        on = there && slot * VE < C;
+        const int from = on ? slot * VE : 0, last = (int)C - VE;
+        c = last < 0 ? 0 : from < last ? from : last;
+        skip = from - c;
+        wide = C < VE ? (int)C : VE;
+    }
+    __device__ __forceinline__ bool mine(int j) const { return on && j >= skip && j < wide; }
 };
+template <class IO, bool NARROW>
+__device__ __forceinline__ void fetch(const typename IO::T* p, const Piece& q, Raw8<IO>& r)
+{
+    if constexpr (NARROW) load_raw<IO>(p, q.wide, r);
+    else r.load(p);
+}
+template <class IO>
+__device__ __forceinline__ void put(typename IO::T* p, const Piece& q, const float (&v)[VE])
+{
+    if (q.skip == 0 && q.wide == VE) {
+        store8<IO, true>(p, VE, v);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < VE; ++j)
+        if (q.mine(j)) IO::st(p, j, v[j]);
+}
+// a thread's numbers for its channels, those of others zero, at q[0 .. 7] in the order of the slots of its piece
+__device__ __forceinline__ void to_slots(float* q, const Piece& p, const float (&v)[VE])
+{
+    if (p.skip == 0 && p.on && p.wide == VE) {
+        reinterpret_cast<float4*>(q)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(q)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < VE; ++j) q[(j - p.skip) & (VE - 1)] = p.mine(j) ? v[j] : 0.f;
+}
+// eight parameters; p may be null
+__device__ __forceinline__ void load_params(const float* p, const Piece& q, float or_else, float (&v)[VE])
+{
+#pragma unroll
+    for (int j = 0; j < VE; ++j) v[j] = or_else;
+    if (p) load8<IoF32>(p + q.c, q.wide, v);
+}
+// f(j, group of channel j), one division for the eight; channels beyond the last: the last group
+template <class F>
+__device__ __forceinline__ void each_group(int c, uint32_t G, uint32_t D, F&& f)
+{
+    uint32_t g = (uint32_t)c / D, at = (uint32_t)c - g * D;
+    if (at + VE <= D) {
+#pragma unroll
+        for (int j = 0; j < VE; ++j) f(j, g);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+        f(j, g < G ? g : G - 1);
+        if (++at == D) { at = 0; ++g; }
+    }
+}
+
+struct Channels {      // of a thread's piece
+    float mean[VE], rstd[VE], gamma[VE], beta[VE];
+    __device__ __forceinline__ void load(const Piece& p, size_t b, const float* mn, const float* rs, const float* ga, const float* be, uint32_t G,
+                                         uint32_t D)
+    {
+        load_params(ga, p, 1.f, gamma);
+        load_params(be, p, 0.f, beta);
+        each_group(p.c, G, D, [&](int j, uint32_t g) {
+            mean[j] = mn[b * G + g];
+            rstd[j] = rs[b * G + g];
+        });
+    }
+};
+
+struct Place : Piece {
+    uint32_t b, part, slab, r;
+    int64_t from;      // the part's first position
+    size_t base;       // and its first element
+};
+template <class IO>
 __device__ __forceinline__ Place place(const Walk& w, int64_t S, int64_t C)
 {
     Place p;
     p.slab = blockIdx.x % w.slabs;
     p.part = blockIdx.x / w.slabs % w.parts;
     p.b = blockIdx.x / w.slabs / w.parts;
-    p.s = threadIdx.x % w.slices;
     p.r = threadIdx.x / w.slices;
     p.from = p.part * w.per;
-    p.to = p.from + w.per < S ? p.from + w.per : S;
-    p.c = (int)(p.slab * w.slices + p.s) * VE;
-    p.on = p.r < w.rows && p.c < C;
-    p.wide = p.on ? (int)(C - p.c < VE ? C - p.c : VE) : 0;
+    p.base = ((size_t)p.b * S + p.from) * C;
+    p.set((int)(p.slab * w.slices + threadIdx.x % w.slices), p.r < w.rows, C);
+    p.template from_row<IO>(p.r, w.rows, (uint32_t)(S - p.from < w.per ? S - p.from : w.per), C);
     return p;
 }
 
 // mean and sum of squared differences of every channel over the part's positions -> part[(b, part)][2][C]
-template <class IO>
+template <class IO, bool NARROW>
 __global__ void __launch_bounds__(GT)
 gnorm_stats_kernel(const typename IO::T* __restrict__ x, float* __restrict__ part, int64_t S, int64_t C, Walk w)
 {
     __shared__ float sm[GT * VE], s2[GT * VE], sn[GT];
-    const Place p = place(w, S, C);
+    const Place p = place<IO>(w, S, C);
     float mean[VE] = {}, m2[VE] = {}, n = 0.f;
     if (p.on)
-        for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD * w.rows) {
+        for (uint32_t o = p.off; p.has(o); o += AHEAD * p.step) {
             Raw8<IO> raw[AHEAD];
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                load_raw<IO>(x + ((int64_t)p.b * S + i + u * w.rows) * C + p.c, i + u * w.rows < p.to ? p.wide : 0, raw[u]);
+            for (int u = 0; u < AHEAD; ++u) fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, raw[u]);
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                if (i + u * w.rows >= p.to) break;
+                if (!p.has(o + u * p.step)) break;
                 float v[VE];
                 raw[u].get(v);
                 n += 1.f;
@@ -156,11 +268,8 @@ gnorm_stats_kernel(const typename IO::T* __restrict__ x, float* __restrict__ par
             }
         }
     const int t = threadIdx.x;
-#pragma unroll
-    for (int j = 0; j < VE; ++j) {
-        sm[t * VE + j] = mean[j];
-        s2[t * VE + j] = m2[j];
-    }
+    to_slots(sm + t * VE, p, mean);
+    to_slots(s2 + t * VE, p, m2);
     sn[t] = n;
     __syncthreads();
     const int wide = (int)w.slices * VE;
@@ -210,97 +319,56 @@ gnorm_group_kernel(const float* __restrict__ part, float* __restrict__ mean, flo
     }
 }
 
-// eight parameters of the channels from c on (those beyond a tensor's last as `or_else`); p may be null
-__device__ __forceinline__ void load_params(const float* p, int c, int wide, float or_else, float (&v)[VE])
-{
-#pragma unroll
-    for (int j = 0; j < VE; ++j) v[j] = or_else;
-    if (!p || wide < 1) return;
-    load8<IoF32>(p + c, wide, v);
-}
-
-struct Channels {      // of a thread's piece
-    float mean[VE], rstd[VE], gamma[VE], beta[VE];
-    __device__ __forceinline__ void load(const Place& p, const float* mn, const float* rs, const float* ga, const float* be, uint32_t G, uint32_t D)
-    {
-        load_params(ga, p.c, p.wide, 1.f, gamma);
-        load_params(be, p.c, p.wide, 0.f, beta);
-        each_group(p, G, D, [&](int j, size_t g) {
-            mean[j] = mn[g];
-            rstd[j] = rs[g];
-        });
-    }
-    // f(j, number of the group of channel j): one division for the eight
-    template <class F>
-    static __device__ __forceinline__ void each_group(const Place& p, uint32_t G, uint32_t D, F&& f)
-    {
-        uint32_t g = (uint32_t)p.c / D, at = (uint32_t)p.c - g * D;
-        if (at + VE <= D) {
-#pragma unroll
-            for (int j = 0; j < VE; ++j) f(j, (size_t)p.b * G + g);
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            f(j, (size_t)p.b * G + (g < G ? g : G - 1));
-            if (++at == D) { at = 0; ++g; }
-        }
-    }
-};
-
-template <class IO, int ACT>
+template <class IO, int ACT, bool NARROW>
 __global__ void __launch_bounds__(GT)
 gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restrict__ y, const float* __restrict__ mean,
                    const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, int64_t S, int64_t C,
                    uint32_t G, Walk w)
 {
-    const Place p = place(w, S, C);
+    const Place p = place<IO>(w, S, C);
     if (!p.on) return;
     Channels k;
-    k.load(p, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
-    for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD * w.rows) {
-        const size_t e = ((size_t)p.b * S + i) * C + p.c, more = (size_t)w.rows * C;
+    k.load(p, p.b, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
+    for (uint32_t o = p.off; p.has(o); o += AHEAD * p.step) {
         Raw8<IO> raw[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) load_raw<IO>(x + e + u * more, i + u * w.rows < p.to ? p.wide : 0, raw[u]);
+        for (int u = 0; u < AHEAD; ++u) fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, raw[u]);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            if (i + u * w.rows >= p.to) break;
+            if (!p.has(o + u * p.step)) break;
             float v[VE];
             raw[u].get(v);
 #pragma unroll
             for (int j = 0; j < VE; ++j)
                 v[j] = act_of<ACT>(__builtin_fmaf((v[j] - k.mean[j]) * k.rstd[j], k.gamma[j], k.beta[j]));
-            store8<IO, true>(y + e + u * more, p.wide, v);
+            put<IO>(p.at(y + p.base, o + u * p.step), p, v);
         }
     }
 }
 
 // sums of dz and dz xhat of every channel over the part's positions -> part[(b, part)][2][C]
-template <class IO, int ACT>
+template <class IO, int ACT, bool NARROW>
 __global__ void __launch_bounds__(GT)
 gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __restrict__ x, const float* __restrict__ mean,
                   const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, float* __restrict__ part,
                   int64_t S, int64_t C, uint32_t G, Walk w)
 {
     __shared__ float sa[GT * VE], sb[GT * VE];
-    const Place p = place(w, S, C);
+    const Place p = place<IO>(w, S, C);
     float a[VE] = {}, b[VE] = {};
     if (p.on) {
         Channels k;
-        k.load(p, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
-        for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD / 2 * w.rows) {
-            const size_t e = ((size_t)p.b * S + i) * C + p.c, more = (size_t)w.rows * C;
+        k.load(p, p.b, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
+        for (uint32_t o = p.off; p.has(o); o += AHEAD / 2 * p.step) {
             Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
 #pragma unroll
             for (int u = 0; u < AHEAD / 2; ++u) {
-                const int n = i + u * w.rows < p.to ? p.wide : 0;
-                load_raw<IO>(x + e + u * more, n, rx[u]);
-                load_raw<IO>(dy + e + u * more, n, rg[u]);
+                fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, rx[u]);
+                fetch<IO, NARROW>(p.at(dy + p.base, o + u * p.step), p, rg[u]);
             }
 #pragma unroll
             for (int u = 0; u < AHEAD / 2; ++u) {
-                if (i + u * w.rows >= p.to) break;
+                if (!p.has(o + u * p.step)) break;
                 float v[VE], g[VE];
                 rx[u].get(v);
                 rg[u].get(g);
@@ -315,11 +383,8 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
         }
     }
     const int t = threadIdx.x;
-#pragma unroll
-    for (int j = 0; j < VE; ++j) {
-        sa[t * VE + j] = a[j];
-        sb[t * VE + j] = b[j];
-    }
+    to_slots(sa + t * VE, p, a);
+    to_slots(sb + t * VE, p, b);
     __syncthreads();
     const int wide = (int)w.slices * VE;
     for (int i = t; i < wide; i += GT) {
@@ -334,13 +399,6 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
         q[c] = ta;
         q[C + c] = tb;
     }
-}
-
-__device__ __forceinline__ float wave_sum(float v)
-{
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) v += __shfl_xor(v, s);
-    return v;
 }
 
 constexpr int RT = 1024, RC = 16;      // threads of a workgroup that sums channels, and channels of it
@@ -396,34 +454,32 @@ gnorm_gather_kernel(const float* __restrict__ part, const float* __restrict__ ga
     }
 }
 
-template <class IO, int ACT>
+template <class IO, int ACT, bool NARROW>
 __global__ void __launch_bounds__(GT)
 gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __restrict__ x, const float* __restrict__ mean,
                 const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, const float* __restrict__ s1,
                 const float* __restrict__ s2, typename IO::T* __restrict__ dx, int64_t S, int64_t C, uint32_t G, float inv, Walk w)
 {
-    const Place p = place(w, S, C);
+    const Place p = place<IO>(w, S, C);
     if (!p.on) return;
     const uint32_t D = (uint32_t)(C / G);
     Channels k;
-    k.load(p, mean, rstd, gamma, beta, G, D);
+    k.load(p, p.b, mean, rstd, gamma, beta, G, D);
     float c1[VE], c2[VE];
-    Channels::each_group(p, G, D, [&](int j, size_t g) {
-        c1[j] = s1[g] * inv;
-        c2[j] = s2[g] * inv;
+    each_group(p.c, G, D, [&](int j, uint32_t g) {
+        c1[j] = s1[(size_t)p.b * G + g] * inv;
+        c2[j] = s2[(size_t)p.b * G + g] * inv;
     });
-    for (int64_t i = p.from + p.r; i < p.to; i += (int64_t)AHEAD / 2 * w.rows) {
-        const size_t e = ((size_t)p.b * S + i) * C + p.c, more = (size_t)w.rows * C;
+    for (uint32_t o = p.off; p.has(o); o += AHEAD / 2 * p.step) {
         Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
 #pragma unroll
         for (int u = 0; u < AHEAD / 2; ++u) {
-            const int n = i + u * w.rows < p.to ? p.wide : 0;
-            load_raw<IO>(x + e + u * more, n, rx[u]);
-            load_raw<IO>(dy + e + u * more, n, rg[u]);
+            fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, rx[u]);
+            fetch<IO, NARROW>(p.at(dy + p.base, o + u * p.step), p, rg[u]);
         }
 #pragma unroll
         for (int u = 0; u < AHEAD / 2; ++u) {
-            if (i + u * w.rows >= p.to) break;
+            if (!p.has(o + u * p.step)) break;
             float v[VE], g[VE];
             rx[u].get(v);
             rg[u].get(g);
@@ -433,8 +489,248 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
                 const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
                 v[j] = k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - h * c2[j]);
             }
-            store8<IO, true>(dx + e + u * more, p.wide, v);
+            put<IO>(p.at(dx + p.base, o + u * p.step), p, v);
         }
+    }
+}
+
+// ---- groups that fit a workgroup -------------------------------------------------------------------------------------
+// A workgroup holds a slab of whole groups of one b in registers, as it came from memory: one read, one launch.  Its threads are `rows`
+// positions by `slices` pieces; a thread has NP pieces, `rows` positions apart.
+constexpr int HT = 512, HSLAB = 128;      // threads, and pieces of a slab, at most
+
+struct Hold {
+    uint32_t P, slices, slabs, rows, np, blocks;      // blocks: rounded up to eight times a whole number; 0: does not fit
+};
+Hold hold(int64_t B, int64_t S, int64_t C, int64_t G, int bytes, uint32_t most)
+{
+    Hold h{};
+    if (C < VE) return h;
+    h.P = (uint32_t)((C + VE - 1) / VE);
+    const uint32_t D = (uint32_t)(C / G);
+    uint32_t unit = D;                                 // pieces of the smallest slab of whole groups and whole pieces
+    while (unit % VE) unit += D;
+    unit /= VE;
+    if (unit > h.P) unit = h.P;
+    // 64 bytes of a row and more, so that a line is asked for by two workgroups at most
+    uint32_t slices = unit;
+    while (slices < h.P && slices * VE * bytes < 64) slices += unit;
+    if (slices > h.P) slices = h.P;
+    while (slices > unit && (uint64_t)S * slices > (uint64_t)HT * most) slices -= slices == h.P && h.P % unit ? h.P % unit : unit;
+    if (slices > HSLAB || (uint64_t)S * slices > (uint64_t)HT * most) return h;
+    for (h.np = 1; (S + h.np - 1) / h.np * slices > HT; h.np *= 2) {}
+    if (h.np > most) return h;
+    h.slices = slices;
+    h.slabs = (h.P + slices - 1) / slices;
+    h.rows = (uint32_t)((S + h.np - 1) / h.np);
+    h.blocks = (uint32_t)(((uint64_t)B * h.slabs + 7) / 8 * 8);
+    return h;
+}
+
+struct Held : Piece {
+    uint32_t b, s, r, W;       // W: channels of the slab's pieces
+    int first;                 // the slab's first channel
+    size_t base;               // the first element of b
+    bool any;
+    __device__ __forceinline__ uint32_t piece(int u) const { return off + u * step; }
+};
+// every XCD (workgroups go round them) takes neighbouring slabs, which share lines
+template <class IO>
+__device__ __forceinline__ Held held(const Hold& h, uint32_t B, int64_t S, int64_t C)
+{
+    Held p;
+    const uint32_t id = (blockIdx.x & 7u) * (h.blocks / 8) + (blockIdx.x >> 3);
+    p.any = id < B * h.slabs;
+    p.b = id / h.slabs;
+    p.s = threadIdx.x % h.slices;
+    p.r = threadIdx.x / h.slices;
+    p.W = h.slices * VE;
+    p.first = (int)((id - p.b * h.slabs) * p.W);
+    p.base = (size_t)p.b * S * C;
+    p.set(p.first / VE + (int)p.s, p.r < h.rows, C);
+    p.template from_row<IO>(p.r, h.rows, (uint32_t)S, C);
+    return p;
+}
+
+// f(j, group of channel j counted from the slab's first); channels that belong to the slab before: 0, for nothing
+template <class F>
+__device__ __forceinline__ void in_slab(const Held& p, uint32_t G, uint32_t D, F&& f)
+{
+    const uint32_t before = (uint32_t)p.first / D;
+    each_group(p.c, G, D, [&](int j, uint32_t g) { f(j, g > before ? g - before : 0u); });
+}
+
+// v[j]: a number of the thread for its channel j.  cols[k W + c]: its sums over the rows, in K shares (the return value).
+__device__ __forceinline__ uint32_t sum_rows(const float (&v)[VE], float* all, float* cols, const Hold& h, const Held& p)
+{
+    const uint32_t T = blockDim.x;
+    __syncthreads();
+    if (p.r < h.rows) to_slots(all + p.r * p.W + p.s * VE, p, v);
+    __syncthreads();
+    uint32_t K = T / p.W;
+    if (K < 1) K = 1;
+    if (K > h.rows) K = h.rows;
+    for (uint32_t i = threadIdx.x; i < K * p.W; i += T) {
+        const uint32_t k = i / p.W;
+        float t = 0.f;
+#pragma unroll 8
+        for (uint32_t r = k; r < h.rows; r += K) t += all[r * p.W + (i - k * p.W)];
+        cols[i] = t;
+    }
+    __syncthreads();
+    return K;
+}
+// group[g] = last(the sum of weight(c) cols over a group's channels and shares); a wave each
+template <class F, class E>
+__device__ __forceinline__ void sum_groups(const float* cols, float* group, uint32_t K, uint32_t D, uint32_t W, F&& weight, E&& last)
+{
+    for (uint32_t g = threadIdx.x / 64; g * D < W; g += blockDim.x / 64) {
+        float t = 0.f;
+        for (uint32_t i = threadIdx.x % 64; i < K * D; i += 64) {
+            const uint32_t k = i / D, c = g * D + (i - k * D);
+            if (c < W) t = __builtin_fmaf(weight(c), cols[k * W + c], t);      // (a group wider than the last slab's pieces ends with the channels)
+        }
+        t = wave_sum(t);
+        if (threadIdx.x % 64 == 0) group[g] = last(t);
+    }
+    __syncthreads();
+}
+
+template <class IO, int ACT, int NP>
+__global__ void __launch_bounds__(HT)
+gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
+                      typename IO::T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, uint32_t B, int64_t S, int64_t C,
+                      uint32_t G, float n, float eps, Hold h)
+{
+    __shared__ float all[HT * VE], cols[HSLAB * VE], group[HSLAB * VE];
+    const Held p = held<IO>(h, B, S, C);
+    if (!p.any) return;
+    const uint32_t D = (uint32_t)(C / G);
+    Raw8<IO> raw[NP];
+#pragma unroll
+    for (int u = 0; u < NP; ++u) raw[u].load(p.at(x + p.base, p.piece(u)));
+    float ga[VE], be[VE];
+    load_params(gamma, p, 1.f, ga);
+    load_params(beta, p, 0.f, be);
+    const auto one = [](uint32_t) { return 1.f; };
+    float t[VE] = {}, mn[VE], rs[VE];
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        if (!p.has(p.piece(u))) break;
+        float v[VE];
+        raw[u].get(v);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) t[j] += v[j];
+    }
+    uint32_t K = sum_rows(t, all, cols, h, p);
+    sum_groups(cols, group, K, D, p.W, one, [&](float s) { return s / n; });
+    in_slab(p, G, D, [&](int j, uint32_t g) { mn[j] = group[g]; });
+#pragma unroll
+    for (int j = 0; j < VE; ++j) t[j] = 0.f;
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        if (!p.has(p.piece(u))) break;
+        float v[VE];
+        raw[u].get(v);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            const float d = v[j] - mn[j];
+            t[j] = __builtin_fmaf(d, d, t[j]);
+        }
+    }
+    K = sum_rows(t, all, cols, h, p);
+    sum_groups(cols, group, K, D, p.W, one, [&](float s) { return 1.f / sqrtf(s / n + eps); });
+    in_slab(p, G, D, [&](int j, uint32_t g) { rs[j] = group[g]; });
+    if (p.r == 0) {      // the first channel of a group writes its numbers
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            const uint32_t c = (uint32_t)(p.c + j), g = c / D;
+            if (p.mine(j) && g * D == c) {
+                mean[(size_t)p.b * G + g] = mn[j];
+                rstd[(size_t)p.b * G + g] = rs[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        if (!p.has(p.piece(u)) || !p.on) break;
+        float v[VE];
+        raw[u].get(v);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT>(__builtin_fmaf((v[j] - mn[j]) * rs[j], ga[j], be[j]));
+        put<IO>(p.at(y + p.base, p.piece(u)), p, v);
+    }
+}
+
+// part[b][2][C]: sums of dz and dz xhat over the positions
+template <class IO, int ACT, int NP>
+__global__ void __launch_bounds__(HT)
+gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __restrict__ x, const float* __restrict__ mean,
+                      const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, float* __restrict__ part,
+                      typename IO::T* __restrict__ dx, uint32_t B, int64_t S, int64_t C, uint32_t G, float inv, Hold h)
+{
+    __shared__ float all[HT * VE], ca[HSLAB * VE], ch[HSLAB * VE], g1[HSLAB * VE], g2[HSLAB * VE];
+    const Held p = held<IO>(h, B, S, C);
+    if (!p.any) return;
+    const uint32_t D = (uint32_t)(C / G);
+    Raw8<IO> rx[NP], rg[NP];
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        rx[u].load(p.at(x + p.base, p.piece(u)));
+        rg[u].load(p.at(dy + p.base, p.piece(u)));
+    }
+    Channels k;
+    k.load(p, p.b, mean, rstd, gamma, beta, G, D);
+    float a[VE] = {}, b[VE] = {};
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        if (!p.has(p.piece(u))) break;
+        float v[VE], g[VE];
+        rx[u].get(v);
+        rg[u].get(g);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            const float xh = (v[j] - k.mean[j]) * k.rstd[j];
+            const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(xh, k.gamma[j], k.beta[j]));
+            a[j] += dz;
+            b[j] = __builtin_fmaf(dz, xh, b[j]);
+        }
+    }
+    const uint32_t K = sum_rows(a, all, ca, h, p);
+    sum_rows(b, all, ch, h, p);
+    for (uint32_t i = threadIdx.x; i < p.W && p.first + (int)i < C; i += blockDim.x) {
+        float ta = 0.f, tb = 0.f;
+        for (uint32_t q = 0; q < K; ++q) {
+            ta += ca[q * p.W + i];
+            tb += ch[q * p.W + i];
+        }
+        float* q = part + (size_t)p.b * 2 * C + p.first + i;
+        q[0] = ta;
+        q[C] = tb;
+    }
+    if (!dx) return;
+    const auto weight = [&](uint32_t c) { return gamma && p.first + (int)c < C ? gamma[p.first + c] : 1.f; };
+    const auto mean_of = [&](float s) { return s * inv; };
+    sum_groups(ca, g1, K, D, p.W, weight, mean_of);
+    sum_groups(ch, g2, K, D, p.W, weight, mean_of);
+    float c1[VE], c2[VE];
+    in_slab(p, G, D, [&](int j, uint32_t g) {
+        c1[j] = g1[g];
+        c2[j] = g2[g];
+    });
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+        if (!p.has(p.piece(u)) || !p.on) break;
+        float v[VE], g[VE];
+        rx[u].get(v);
+        rg[u].get(g);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            const float xh = (v[j] - k.mean[j]) * k.rstd[j];
+            const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(xh, k.gamma[j], k.beta[j]));
+            v[j] = k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - xh * c2[j]);
+        }
+        put<IO>(p.at(dx + p.base, p.piece(u)), p, v);
     }
 }
 
@@ -444,16 +740,36 @@ template <class IO, int ACT>
 hipError_t forward(const GnormArgs& a, const void* x, void* y, float* mean, float* rstd, float eps, void* ws, hipStream_t st)
 {
     using T = typename IO::T;
-    const Walk w = walk(a.B, a.S, a.C);
     dim3 g, gg;
+    const Hold h = hold(a.B, a.S, a.C, a.G, sizeof(T), 64 / Raw8<IO>::W);
+    if (h.blocks) {
+        const hipError_t e = launch_grid(h.blocks, HT, &g);
+        if (e != hipSuccess) return e;
+        const auto go = [&](auto np) {
+            hipLaunchKernelGGL((gnorm_hold_fwd_kernel<IO, ACT, decltype(np)::value>), g, dim3((h.slices * h.rows + 63) / 64 * 64), 0, st, (const T*)x,
+                               a.gamma, a.beta, (T*)y, mean, rstd, (uint32_t)a.B, a.S, a.C, (uint32_t)a.G, (float)(a.S * (a.C / a.G)), eps, h);
+        };
+        if (h.np == 1) go(std::integral_constant<int, 1>());
+        else if (h.np == 2) go(std::integral_constant<int, 2>());
+        else if (h.np == 4) go(std::integral_constant<int, 4>());
+        else if (h.np == 8) go(std::integral_constant<int, 8>());
+        else if constexpr (Raw8<IO>::W == 4) go(std::integral_constant<int, 16>());
+        return hipGetLastError();
+    }
+    const Walk w = walk(a.B, a.S, a.C);
     hipError_t e = launch_grid((uint64_t)a.B * w.parts * w.slabs, GT, &g);
     if (e == hipSuccess) e = launch_grid((uint64_t)a.B * a.G, 64, &gg);
     if (e != hipSuccess) return e;
     float* part = (float*)ws;
-    hipLaunchKernelGGL(gnorm_stats_kernel<IO>, g, dim3(GT), 0, st, (const T*)x, part, a.S, a.C, w);
+    if (a.C < VE) hipLaunchKernelGGL((gnorm_stats_kernel<IO, true>), g, dim3(GT), 0, st, (const T*)x, part, a.S, a.C, w);
+    else hipLaunchKernelGGL((gnorm_stats_kernel<IO, false>), g, dim3(GT), 0, st, (const T*)x, part, a.S, a.C, w);
     hipLaunchKernelGGL(gnorm_group_kernel, gg, dim3(64), 0, st, (const float*)part, mean, rstd, a.S, a.C, (uint32_t)a.G, w.parts, w.per, eps);
-    hipLaunchKernelGGL((gnorm_apply_kernel<IO, ACT>), g, dim3(GT), 0, st, (const T*)x, (T*)y, (const float*)mean, (const float*)rstd, a.gamma,
-                       a.beta, a.S, a.C, (uint32_t)a.G, w);
+    const auto apply = [&](auto narrow) {
+        hipLaunchKernelGGL((gnorm_apply_kernel<IO, ACT, decltype(narrow)::value>), g, dim3(GT), 0, st, (const T*)x, (T*)y, (const float*)mean,
+                           (const float*)rstd, a.gamma, a.beta, a.S, a.C, (uint32_t)a.G, w);
+    };
+    if (a.C < VE) apply(std::true_type());
+    else apply(std::false_type());
     return hipGetLastError();
 }
 
@@ -462,21 +778,45 @@ hipError_t backward(const GnormArgs& a, const void* dy, const void* x, const flo
                     float* dbeta, void* ws, hipStream_t st)
 {
     using T = typename IO::T;
-    const Walk w = walk(a.B, a.S, a.C);
     dim3 g, gg;
+    const float inv = (float)(1.0 / ((double)a.S * (a.C / a.G)));
+    const Hold h = hold(a.B, a.S, a.C, a.G, sizeof(T), 32 / Raw8<IO>::W);
+    if (h.blocks) {
+        const hipError_t e = launch_grid(h.blocks, HT, &g);
+        if (e != hipSuccess) return e;
+        const auto go = [&](auto np) {
+            hipLaunchKernelGGL((gnorm_hold_bwd_kernel<IO, ACT, decltype(np)::value>), g, dim3((h.slices * h.rows + 63) / 64 * 64), 0, st,
+                               (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta, (float*)ws, (T*)dx, (uint32_t)a.B, a.S, a.C, (uint32_t)a.G,
+                               inv, h);
+        };
+        if (h.np == 1) go(std::integral_constant<int, 1>());
+        else if (h.np == 2) go(std::integral_constant<int, 2>());
+        else if (h.np == 4) go(std::integral_constant<int, 4>());
+        else if constexpr (Raw8<IO>::W == 4) go(std::integral_constant<int, 8>());
+        if (dgamma || dbeta)
+            hipLaunchKernelGGL(gnorm_gather_kernel, dim3((unsigned)((a.C + RC - 1) / RC)), dim3(RT), 0, st, (const float*)ws, a.gamma, (float*)nullptr,
+                               (float*)nullptr, dgamma, dbeta, a.B, a.C, (uint32_t)a.G, 1u);
+        return hipGetLastError();
+    }
+    const Walk w = walk(a.B, a.S, a.C);
     hipError_t e = launch_grid((uint64_t)a.B * w.parts * w.slabs, GT, &g);
     if (e == hipSuccess) e = launch_grid((uint64_t)(a.C + RC - 1) / RC + ((uint64_t)a.B * a.G + RT / 64 - 1) / (RT / 64), RT, &gg);
     if (e != hipSuccess) return e;
     float* part = (float*)ws;
     float* s1 = (float*)((char*)ws + up256(part_rows(a.B, a.S, a.C) * 2 * a.C * sizeof(float)));
     float* s2 = s1 + a.B * a.G;
-    hipLaunchKernelGGL((gnorm_sums_kernel<IO, ACT>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta, part, a.S,
-                       a.C, (uint32_t)a.G, w);
-    hipLaunchKernelGGL(gnorm_gather_kernel, gg, dim3(RT), 0, st, (const float*)part, a.gamma, s1, s2, dgamma, dbeta, a.B, a.C, (uint32_t)a.G,
-                       w.parts);
-    if (dx)
-        hipLaunchKernelGGL((gnorm_dx_kernel<IO, ACT>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta,
-                           (const float*)s1, (const float*)s2, (T*)dx, a.S, a.C, (uint32_t)a.G, (float)(1.0 / ((double)a.S * (a.C / a.G))), w);
+    const auto go = [&](auto narrow) {
+        constexpr bool N = decltype(narrow)::value;
+        hipLaunchKernelGGL((gnorm_sums_kernel<IO, ACT, N>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta, part, a.S,
+                           a.C, (uint32_t)a.G, w);
+        hipLaunchKernelGGL(gnorm_gather_kernel, gg, dim3(RT), 0, st, (const float*)part, a.gamma, s1, s2, dgamma, dbeta, a.B, a.C, (uint32_t)a.G,
+                           w.parts);
+        if (dx)
+            hipLaunchKernelGGL((gnorm_dx_kernel<IO, ACT, N>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta,
+                               (const float*)s1, (const float*)s2, (T*)dx, a.S, a.C, (uint32_t)a.G, inv, w);
+    };
+    if (a.C < VE) go(std::true_type());
+    else go(std::false_type());
     return hipGetLastError();
 }
 

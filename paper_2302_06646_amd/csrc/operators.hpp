@@ -5,6 +5,8 @@
 
 namespace lc {
 
+constexpr int64_t MAX_ELEMENTS = int64_t(1) << 34;      // of one tensor: what one launch covers
+
 // A dropout mask that is never stored (generator: vec8.hpp)
 struct Drop {
     uint32_t threshold;      // an entry is kept if its 16 bits are at least this; 0: all are kept, 65536: none
