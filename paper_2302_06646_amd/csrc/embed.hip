@@ -12,7 +12,10 @@ namespace lc {
 namespace {
 
 constexpr int RADIX = 512, SORT_T = 256, TILE_MIN = 2048, TILES_MAX = 256;      // digits of at most nine bits; tiles of a sorting pass
-constexpr int CHUNK = 32;                                                       // sorted places of a thread
+constexpr int ALONE = 16384, ALONE_T = 1024;                                    // tokens that one workgroup sorts by itself, its threads
+constexpr int CHUNK_MIN = 8;                                                    // sorted places of a thread, at least
+constexpr int AHEAD = 8;                                                        // rows of dy that a thread asks for before it adds the first
+constexpr int JOIN_T = 1024;                                                    // threads of a workgroup that joins a run's partial sums
 
 // a token's row, or V for one that names none
 template <class ID>
@@ -101,13 +104,23 @@ embed_columns_kernel(const ID* __restrict__ ids, const typename W::T* __restrict
 
 // ---- gradient --------------------------------------------------------------------------------------------------------
 
-__global__ void __launch_bounds__(256) embed_zero_kernel(float* __restrict__ p, int64_t n)
+// dE <- 0, by the workgroups of a sorting launch that have nothing to sort: the sort takes its time and hardly any of the memory's
+struct Fill {
+    float* p;
+    int64_t n;
+    unsigned groups(int threads) const      // four pieces of sixteen bytes a thread, and 1024 workgroups at most
+    {
+        const int64_t want = (n + threads * 16 - 1) / (threads * 16);
+        return (unsigned)(want < 1024 ? want : 1024);
+    }
+};
+__device__ __forceinline__ void fill_zero(const Fill& f, int64_t group, int64_t groups)
 {
-    const int64_t stride = (int64_t)gridDim.x * 256 * 4;
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += stride) {
-        if (i + 4 <= n) *reinterpret_cast<float4*>(p + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int64_t stride = groups * blockDim.x * 4;
+    for (int64_t i = (group * blockDim.x + threadIdx.x) * 4; i < f.n; i += stride) {
+        if (i + 4 <= f.n) put_once(reinterpret_cast<float4*>(f.p + i), make_float4(0.f, 0.f, 0.f, 0.f));
         else
-            for (int64_t j = i; j < n; ++j) p[j] = 0.f;
+            for (int64_t j = i; j < f.n; ++j) f.p[j] = 0.f;
     }
 }
 
@@ -171,9 +184,15 @@ struct Tokens {
 // hist[tile][digit] = how many tokens of the tile have the digit
 template <class ID>
 __global__ void __launch_bounds__(SORT_T)
-sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, int64_t M, int64_t tile, int shift, int bits)
+sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, uint32_t* __restrict__ joins, int64_t M, int64_t tile, uint32_t tiles, int shift,
+                  int bits, Fill fill)
 {
     __shared__ uint32_t n[RADIX];
+    if (blockIdx.x >= tiles) {
+        fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *joins = 0;
     for (int i = threadIdx.x; i < RADIX; i += SORT_T) n[i] = 0;
     __syncthreads();
     const int64_t from = blockIdx.x * tile, to = from + tile < M ? from + tile : M;
@@ -181,6 +200,23 @@ sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, int64_t M, int64_t
     for (int64_t i = from + threadIdx.x; i < to; i += SORT_T) atomicAdd(&n[in.k(i) >> shift & mask], 1u);
     __syncthreads();
     for (int i = threadIdx.x; i < RADIX; i += SORT_T) hist[(size_t)blockIdx.x * RADIX + i] = n[i];
+}
+
+// The place of a lane's token among those of its wave's share with the digit: behind those of earlier rows (next[digit], which the
+// first lane with the digit moves on by their number) and of earlier lanes.
+__device__ __forceinline__ uint32_t place_of(uint32_t digit, bool there, int bits, uint32_t* next)
+{
+    const int lane = threadIdx.x & 63;
+    uint64_t same = __ballot(there);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t ones = __ballot(digit >> b & 1u), want = (uint64_t)0 - (digit >> b & 1u);
+        same &= ~(ones ^ want);
+    }
+    const int leader = there ? __ffsll((unsigned long long)same) - 1 : lane;
+    uint32_t first = 0;
+    if (there && lane == leader) first = atomicAdd(&next[digit], (uint32_t)__popcll(same));
+    first = (uint32_t)__shfl((int)first, leader);
+    return first + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
 }
 
 // Puts a tile's tokens where they belong: behind all of smaller digits, those of the same digit in earlier tiles, in earlier waves'
@@ -234,47 +270,115 @@ sort_place_kernel(Tokens<ID> in, const uint32_t* __restrict__ hist, uint32_t* __
     for (int64_t r = from; r < from + share && r < M; r += 64) {      // (the same rows for every lane of a wave)
         const int64_t i = r + lane;
         const bool there = i < M;
-        const uint32_t k = there ? in.k(i) : 0, digit = k >> shift & mask;
-        uint64_t same = __ballot(there);
-        for (int b = 0; b < bits; ++b) {
-            const bool one = digit >> b & 1u;
-            const uint64_t ones = __ballot(one);
-            same &= one ? ones : ~ones;
-        }
-        const int leader = there ? __ffsll((unsigned long long)same) - 1 : lane;
-        uint32_t first = 0;
-        if (there && lane == leader) first = atomicAdd(&at[wave][digit], (uint32_t)__popcll(same));
-        first = (uint32_t)__shfl((int)first, leader);
+        const uint32_t k = there ? in.k(i) : 0, to = place_of(k >> shift & mask, there, bits, at[wave]);
         if (there) {
-            const uint32_t to = first + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
             key[to] = k;
             pos[to] = in.p(i);
         }
     }
 }
 
+// All passes by one workgroup (the first of the launch); each wave keeps its share's tokens in registers, counts them and, once the
+// starts are known, puts them in their places.  16384 tokens and 16 bits: 15 us, behind the zeros that the other workgroups write.
+template <class ID>
+__global__ void __launch_bounds__(ALONE_T)
+sort_alone_kernel(Tokens<ID> in, uint32_t* __restrict__ key0, uint32_t* __restrict__ pos0, uint32_t* __restrict__ key1, uint32_t* __restrict__ pos1,
+                  uint32_t* __restrict__ joins, int M, int passes, int bits, Fill fill)
+{
+    constexpr int WAVES = ALONE_T / 64, ROWS = ALONE / ALONE_T;
+    __shared__ uint32_t at[WAVES][RADIX];
+    __shared__ uint32_t sums[RADIX];
+    if (blockIdx.x > 0) {
+        fill_zero(fill, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (tid == 0) *joins = 0;
+    const uint32_t mask = (1u << bits) - 1u;
+    const int share = (M + ALONE_T - 1) / ALONE_T * 64, from = wave * share + lane;      // rows of 64 of a wave, in order
+    for (int pass = 0; pass < passes; ++pass) {
+        const uint32_t *sk = pass & 1 ? key0 : key1, *sp = pass & 1 ? pos0 : pos1;
+        uint32_t *tk = pass & 1 ? key1 : key0, *tp = pass & 1 ? pos1 : pos0;
+        const int shift = pass * bits;
+        for (int i = tid; i < WAVES * RADIX; i += ALONE_T) (&at[0][0])[i] = 0;
+        uint32_t k[ROWS], p[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const int i = from + 64 * r;
+            const bool there = 64 * r < share && i < M;
+            k[r] = p[r] = 0;
+            if (there) {
+                k[r] = pass ? sk[i] : in.k(i);
+                p[r] = pass ? sp[i] : (uint32_t)i;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            if (64 * r < share && from + 64 * r < M) atomicAdd(&at[wave][k[r] >> shift & mask], 1u);
+        __syncthreads();
+        uint32_t mine = 0;
+        if (tid < RADIX) {
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) mine += at[w][tid];
+            sums[tid] = mine;
+        }
+        __syncthreads();
+        for (int s = 1; s < RADIX; s <<= 1) {
+            const uint32_t v = tid < RADIX && tid >= s ? sums[tid - s] : 0;
+            __syncthreads();
+            if (tid < RADIX) sums[tid] += v;
+            __syncthreads();
+        }
+        if (tid < RADIX) {
+            uint32_t next = sums[tid] - mine;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const uint32_t c = at[w][tid];
+                at[w][tid] = next;
+                next += c;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (64 * r >= share || from - lane + 64 * r >= M) break;      // (the same for every lane of a wave)
+            const bool there = from + 64 * r < M;
+            const uint32_t to = place_of(k[r] >> shift & mask, there, bits, at[wave]);
+            if (there) {
+                tk[to] = k[r];
+                tp[to] = p[r];
+            }
+        }
+        __syncthreads();      // (what a pass has written, the next one reads)
+    }
+}
+
 // Sums of runs.  Partial sums lie at part[2 chunk + w]: w = 0 of a run that came in from the chunk before, 1 of one that began here
-// and goes on.
-template <class IO, bool DROP>
+// and goes on, which is noted down in `joins` (how many, then their chunks; in any order, they have nothing to do with each other).
+// A thread's columns are eight from c on; where the row's end is not a multiple of eight the last thread begins `skip` columns early
+// (NARROW: rows of fewer than eight).  key, pos: readable up to a whole chunk.
+template <class IO, bool DROP, bool NARROW>
 __global__ void __launch_bounds__(256)
 embed_sum_kernel(const typename IO::T* __restrict__ dy, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
-                 float* __restrict__ dE, float* __restrict__ part, int64_t M, uint32_t H, uint32_t stride, uint32_t P, uint32_t V,
-                 uint32_t chunks, float scale, Drop d)
+                 float* __restrict__ dE, float* __restrict__ part, uint32_t* __restrict__ joins, uint32_t M, uint32_t H, uint32_t stride, uint32_t P,
+                 uint32_t V, uint32_t chunk_size, uint32_t chunks, float scale, Drop d)
 {
     const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint32_t chunk = (uint32_t)(id / P), c = (uint32_t)(id - (uint64_t)chunk * P) * VE;
+    const uint32_t chunk = (uint32_t)(id / P), slice = (uint32_t)(id - (uint64_t)chunk * P);
     if (chunk >= chunks) return;
-    const int64_t from = (int64_t)chunk * CHUNK, to = from + CHUNK < M ? from + CHUNK : M;
-    const int wide = (int)(H - c);
+    const uint32_t from = chunk * chunk_size, to = from + chunk_size < M ? from + chunk_size : M;
+    const uint32_t last = H > VE ? H - VE : 0, c = slice * VE < last ? slice * VE : last, skip = slice * VE - c;
+    const int wide = NARROW ? (int)H : VE;
     const uint64_t call = DROP ? call_of(d) : 0;
     const float f = scale * d.scale;
     uint32_t cur = key[from];
     bool came_in = from > 0 && key[from - 1] == cur;
     float acc[VE] = {};
     const auto keep = [&](int w) {
-        float* q = part + ((size_t)chunk * 2 + w) * (P * VE) + c;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) q[i] = acc[i];
+        float4* q = reinterpret_cast<float4*>(part + (((size_t)chunk * 2 + w) * P + slice) * VE);
+        q[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        q[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
     };
     const auto finish = [&] {
         if (cur >= V) return;
@@ -282,64 +386,104 @@ embed_sum_kernel(const typename IO::T* __restrict__ dy, const uint32_t* __restri
         float v[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) v[i] = acc[i] * f;
-        store8<IoF32>(dE + (size_t)cur * H + c, wide, v);
+        float* row = dE + (size_t)cur * H + c;
+        if (skip == 0 && wide == VE) store8<IoF32>(row, VE, v);
+        else
+#pragma unroll
+            for (int i = 0; i < VE; ++i)
+                if (i >= (int)skip && i < wide) row[i] = v[i];
     };
-    for (int64_t i = from; i < to; ++i) {
-        const uint32_t k = key[i];
-        const size_t p = pos[i];
-        if (k >= V) { if (cur < V) { finish(); cur = k; came_in = false; } break; }      // the sentinel sorts last
-        float v[VE];
-        load8<IO>(dy + p * stride + c, wide, v);
-        if (DROP) {
-            const uint32_t m = kept8_at(p * H + c, d, call);
+    for (uint32_t i = from; i < to; i += AHEAD) {
+        uint32_t k[AHEAD], p[AHEAD];
 #pragma unroll
-            for (int j = 0; j < VE; ++j) v[j] = m >> j & 1u ? v[j] : 0.f;
+        for (int u = 0; u < AHEAD; u += 4) {
+            const uint4 a = *reinterpret_cast<const uint4*>(key + i + u), b = *reinterpret_cast<const uint4*>(pos + i + u);
+            k[u] = a.x; k[u + 1] = a.y; k[u + 2] = a.z; k[u + 3] = a.w;
+            p[u] = b.x; p[u + 1] = b.y; p[u + 2] = b.z; p[u + 3] = b.w;
         }
-        if (k != cur) {
-            finish();
-            cur = k;
-            came_in = false;
+        Raw8<IO> raw[AHEAD];
 #pragma unroll
-            for (int j = 0; j < VE; ++j) acc[j] = 0.f;
+        for (int u = 0; u < AHEAD; ++u) {
+            if (i + u >= to) k[u] = V;
+            if (k[u] >= V) p[u] = 0;      // (a row that is there, and goes nowhere)
+            const typename IO::T* row = dy + (size_t)p[u] * stride + c;
+            if constexpr (NARROW) load_raw<IO>(row, wide, raw[u]);
+            else raw[u].load(row);
         }
 #pragma unroll
-        for (int j = 0; j < VE; ++j) acc[j] += v[j];
+        for (int u = 0; u < AHEAD; ++u) {
+            if (k[u] != cur) {
+                finish();
+                cur = k[u];
+                came_in = false;
+#pragma unroll
+                for (int j = 0; j < VE; ++j) acc[j] = 0.f;
+            }
+            float v[VE];
+            raw[u].get(v);
+            const uint32_t m = DROP ? kept8_at((size_t)p[u] * H + c, d, call) : 0xffu;
+#pragma unroll
+            for (int j = 0; j < VE; ++j) acc[j] += !DROP || (m >> j & 1u) ? v[j] : 0.f;
+        }
+        if (k[AHEAD - 1] >= V) break;      // the tokens that name no row sort last
     }
     if (cur >= V) return;
-    if (to < M && key[to] == cur) keep(came_in ? 0 : 1);
-    else finish();
+    if (to < M && key[to] == cur) {
+        keep(came_in ? 0 : 1);
+        if (!came_in && slice == 0) joins[1 + atomicAdd(joins, 1u)] = chunk;
+    } else finish();
 }
 
-// A run that begins in this chunk and goes on: its partial sums, in the chunks' order.
-__global__ void __launch_bounds__(256)
-embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ part, float* __restrict__ dE, int64_t M, uint32_t H, uint32_t P,
-                  uint32_t V, float f)
+// Runs over several chunks: their partial sums, by the waves of a workgroup in turn and the waves' sums in order.  A lane takes four
+// columns.
+__global__ void __launch_bounds__(JOIN_T)
+embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ part, const uint32_t* __restrict__ joins, float* __restrict__ dE,
+                  uint32_t M, uint32_t H, uint32_t P, uint32_t chunk_size, float f)
 {
-    const uint32_t chunk = blockIdx.x;
-    const int64_t from = (int64_t)chunk * CHUNK, to = from + CHUNK;
-    if (to >= M) return;
-    const uint32_t k = key[to - 1];
-    if (k >= V || key[to] != k) return;
-    if (from > 0 && key[from] == k && key[from - 1] == k) return;      // began earlier
-    int64_t lo = to + 1, hi = M;                                       // the run's end: the first place from `to` on with another token
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (key[mid] == k) lo = mid + 1;
-        else hi = mid;
-    }
-    const uint32_t last = (uint32_t)((lo - 1) / CHUNK);
-    for (uint32_t c = threadIdx.x; c < H; c += 256) {
-        float s = part[((size_t)chunk * 2 + 1) * (P * VE) + c];
-        for (uint32_t q = chunk + 1; q <= last; ++q) s += part[(size_t)q * 2 * (P * VE) + c];
-        dE[(size_t)k * H + c] = s * f;
+    constexpr int WAVES = JOIN_T / 64;
+    __shared__ float4 sums[WAVES][64];
+    const uint32_t n = joins[0], blocks = (P * 2 + 63) / 64, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    for (uint32_t item = blockIdx.x; item < n * blocks; item += gridDim.x) {
+        const uint32_t chunk = joins[1 + item / blocks], col = item % blocks * 64 + lane, to = (chunk + 1) * chunk_size, k = key[to];
+        uint32_t lo = to + 1, hi = M;      // the run's end: the first place behind `to` with another token
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) >> 1;
+            if (key[mid] == k) lo = mid + 1;
+            else hi = mid;
+        }
+        const uint32_t last = (lo - 1) / chunk_size;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (col < P * 2) {
+#pragma unroll 4
+            for (uint32_t q = chunk + wave; q <= last; q += WAVES) {
+                const float4 v = *reinterpret_cast<const float4*>(part + ((size_t)q * 2 + (q == chunk)) * (P * VE) + col * 4);
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+        }
+        sums[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && col < P * 2) {
+            for (uint32_t w = 1; w < WAVES && w <= last - chunk; ++w) {
+                const float4 v = sums[w][lane];
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            const float v[4] = {s.x * f, s.y * f, s.z * f, s.w * f};
+            const uint32_t slice = col / 2, from = slice * VE, at = H > VE ? (from < H - VE ? from : H - VE) : 0;
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {      // (column at + i; those before `from` are the slice's before)
+                const uint32_t i = col % 2 * 4 + j;
+                if (at + i >= from && at + i < H) dE[(size_t)k * H + at + i] = v[j];
+            }
+        }
+        __syncthreads();
     }
 }
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Layout {      // of the workspace
-    size_t hist, key[2], pos[2], part, rows, total;
-    int64_t M, tile, tiles, chunks;
+    size_t hist, key[2], pos[2], part, joins, rows, total;
+    int64_t M, tile, tiles, chunk, chunks;
     uint32_t P;
     int passes, bits;
 };
@@ -351,8 +495,11 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
     // a pass reads the counts of every tile in every tile: no more than 256 of them, however many tokens there are
     l.tile = TILE_MIN * ((l.M + (int64_t)TILE_MIN * TILES_MAX - 1) / ((int64_t)TILE_MIN * TILES_MAX));
     l.tiles = (l.M + l.tile - 1) / l.tile;
-    l.chunks = (l.M + CHUNK - 1) / CHUNK;
     l.P = (uint32_t)((H + VE - 1) / VE);
+    // long chunks leave few partial sums, short ones make enough threads: at least 2^17 where there are so many
+    l.chunk = 32;
+    while (l.chunk > CHUNK_MIN && l.M / l.chunk * l.P < (1 << 17)) l.chunk /= 2;
+    l.chunks = (l.M + l.chunk - 1) / l.chunk;
     int need = 0;
     while (V >> need) ++need;                       // bits of V, the number of no token
     l.passes = (need + 8) / 9;
@@ -361,34 +508,44 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
     const auto take = [&](size_t bytes) { const size_t at = off; off += up256(bytes); return at; };
     l.hist = take((size_t)(l.M < (int64_t)TILE_MIN * TILES_MAX ? (l.M + TILE_MIN - 1) / TILE_MIN : TILES_MAX) * RADIX * sizeof(uint32_t));
     for (int i = 0; i < 2; ++i) {
-        l.key[i] = take((size_t)l.M * sizeof(uint32_t));
-        l.pos[i] = take((size_t)l.M * sizeof(uint32_t));
+        l.key[i] = take((size_t)(l.M + 32) * sizeof(uint32_t));
+        l.pos[i] = take((size_t)(l.M + 32) * sizeof(uint32_t));
     }
-    l.part = take((size_t)l.chunks * 2 * l.P * VE * sizeof(float));
+    // (room for the number of chunks that grows with M: those of 32 places, or so many shorter ones that there are 2^17 threads and twice that)
+    const int64_t most = (l.M + CHUNK_MIN - 1) / CHUNK_MIN, some = (l.M + 31) / 32 + ((1 << 18) + l.P - 1) / l.P + 1;
+    l.part = take((size_t)(most < some ? most : some) * 2 * l.P * VE * sizeof(float));
+    l.joins = take((size_t)((most < some ? most : some) + 1) * sizeof(uint32_t));
     l.rows = take(layout == LONGCONV_CHANNELS_FIRST ? (size_t)l.M * l.P * VE * (io == LONGCONV_F32 ? 4 : 2) : 0);
     l.total = off;
     return l;
 }
 
 template <class ID>
-hipError_t sort_pass(const Tokens<ID>& in, char* ws, const Layout& l, int pass, int to, hipStream_t st)
+hipError_t sort_pass(const Tokens<ID>& in, char* ws, const Layout& l, int pass, int to, const Fill& fill, hipStream_t st)
 {
     uint32_t* hist = (uint32_t*)(ws + l.hist);
-    const dim3 g((unsigned)l.tiles);
-    hipLaunchKernelGGL((sort_count_kernel<ID>), g, dim3(SORT_T), 0, st, in, hist, l.M, l.tile, pass * l.bits, l.bits);
-    hipLaunchKernelGGL((sort_place_kernel<ID>), g, dim3(SORT_T), 0, st, in, (const uint32_t*)hist, (uint32_t*)(ws + l.key[to]),
+    hipLaunchKernelGGL((sort_count_kernel<ID>), dim3((unsigned)l.tiles + fill.groups(SORT_T)), dim3(SORT_T), 0, st, in, hist, (uint32_t*)(ws + l.joins), l.M, l.tile,
+                       (uint32_t)l.tiles, pass * l.bits, l.bits, fill);
+    hipLaunchKernelGGL((sort_place_kernel<ID>), dim3((unsigned)l.tiles), dim3(SORT_T), 0, st, in, (const uint32_t*)hist, (uint32_t*)(ws + l.key[to]),
                        (uint32_t*)(ws + l.pos[to]), l.M, l.tile, pass * l.bits, l.bits);
     return hipGetLastError();
 }
 
+// -> key[0], pos[0] or [1], by passes; and the zeros
 template <class ID>
-hipError_t sort_tokens(const ID* ids, int64_t V, char* ws, const Layout& l, hipStream_t st)      // -> key[0], pos[0] or [1], by passes
+hipError_t sort_tokens(const ID* ids, int64_t V, char* ws, const Layout& l, const Fill& fill, hipStream_t st)
 {
-    hipError_t e = sort_pass<ID>(Tokens<ID>{ids, nullptr, nullptr, (uint32_t)V}, ws, l, 0, 0, st);
+    const Tokens<ID> in{ids, nullptr, nullptr, (uint32_t)V};
+    if (l.M <= ALONE) {
+        hipLaunchKernelGGL((sort_alone_kernel<ID>), dim3(1 + fill.groups(ALONE_T)), dim3(ALONE_T), 0, st, in, (uint32_t*)(ws + l.key[0]), (uint32_t*)(ws + l.pos[0]),
+                           (uint32_t*)(ws + l.key[1]), (uint32_t*)(ws + l.pos[1]), (uint32_t*)(ws + l.joins), (int)l.M, l.passes, l.bits, fill);
+        return hipGetLastError();
+    }
+    hipError_t e = sort_pass<ID>(in, ws, l, 0, 0, fill, st);
     for (int pass = 1; pass < l.passes && e == hipSuccess; ++pass) {
         const int from = (pass - 1) & 1;
-        const Tokens<void> in{nullptr, (const uint32_t*)(ws + l.key[from]), (const uint32_t*)(ws + l.pos[from]), (uint32_t)V};
-        e = sort_pass<void>(in, ws, l, pass, pass & 1, st);
+        const Tokens<void> pairs{nullptr, (const uint32_t*)(ws + l.key[from]), (const uint32_t*)(ws + l.pos[from]), (uint32_t)V};
+        e = sort_pass<void>(pairs, ws, l, pass, pass & 1, Fill{nullptr, 0}, st);
     }
     return e;
 }
@@ -426,8 +583,9 @@ hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hip
     using T = typename IO::T;
     const Layout l = lay_out(a.B, a.N, a.V, a.H, a.io, a.layout);
     dim3 g;
-    hipLaunchKernelGGL(embed_zero_kernel, dim3(2048), dim3(256), 0, st, dE, a.V * a.H);
-    hipError_t e = a.id_bytes == 8 ? sort_tokens((const int64_t*)a.ids, a.V, ws, l, st) : sort_tokens((const int32_t*)a.ids, a.V, ws, l, st);
+    const Fill fill{dE, a.V * a.H};
+    hipError_t e = a.id_bytes == 8 ? sort_tokens((const int64_t*)a.ids, a.V, ws, l, fill, st)
+                                   : sort_tokens((const int32_t*)a.ids, a.V, ws, l, fill, st);
     if (e != hipSuccess) return e;
     const T* rows = (const T*)dy;
     uint32_t stride = (uint32_t)a.H;
@@ -442,16 +600,18 @@ hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hip
     const int last = (l.passes - 1) & 1;
     const uint32_t *key = (const uint32_t*)(ws + l.key[last]), *pos = (const uint32_t*)(ws + l.pos[last]);
     float* part = (float*)(ws + l.part);
+    uint32_t* joins = (uint32_t*)(ws + l.joins);
     if ((e = launch_grid(((uint64_t)l.chunks * l.P + 255) / 256, 256, &g)) != hipSuccess) return e;
-    if (a.drop.threshold && a.layout == LONGCONV_CHANNELS_LAST)
-        hipLaunchKernelGGL((embed_sum_kernel<IO, true>), g, dim3(256), 0, st, rows, key, pos, dE, part, l.M, (uint32_t)a.H, stride, l.P,
-                           (uint32_t)a.V, (uint32_t)l.chunks, a.scale, a.drop);
-    else
-        hipLaunchKernelGGL((embed_sum_kernel<IO, false>), g, dim3(256), 0, st, rows, key, pos, dE, part, l.M, (uint32_t)a.H, stride, l.P,
-                           (uint32_t)a.V, (uint32_t)l.chunks, a.scale, a.drop);
+    const auto sum = [&](auto drop, auto narrow) {
+        hipLaunchKernelGGL((embed_sum_kernel<IO, decltype(drop)::value, decltype(narrow)::value>), g, dim3(256), 0, st, rows, key, pos, dE, part, joins,
+                           (uint32_t)l.M, (uint32_t)a.H, stride, l.P, (uint32_t)a.V, (uint32_t)l.chunk, (uint32_t)l.chunks, a.scale, a.drop);
+    };
+    const bool drop = a.drop.threshold && a.layout == LONGCONV_CHANNELS_LAST;
+    if (a.H < VE) drop ? sum(std::true_type(), std::true_type()) : sum(std::false_type(), std::true_type());
+    else drop ? sum(std::true_type(), std::false_type()) : sum(std::false_type(), std::false_type());
     if (l.chunks > 1)
-        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)l.chunks), dim3(256), 0, st, key, (const float*)part, dE, l.M, (uint32_t)a.H,
-                           l.P, (uint32_t)a.V, a.scale * a.drop.scale);
+        hipLaunchKernelGGL(embed_join_kernel, dim3(512), dim3(JOIN_T), 0, st, key, (const float*)part, (const uint32_t*)joins, dE, (uint32_t)l.M,
+                           (uint32_t)a.H, l.P, (uint32_t)l.chunk, a.scale * a.drop.scale);
     return hipGetLastError();
 }
 
