@@ -11,8 +11,9 @@
 namespace lc {
 namespace {
 
-constexpr int RADIX = 512, SORT_T = 256, TILE_MIN = 2048, TILES_MAX = 256;      // digits of at most nine bits; tiles of a sorting pass
-constexpr int ALONE = 16384, ALONE_T = 1024;                                    // tokens that one workgroup sorts by itself, its threads
+constexpr int RADIX = 512, SORT_T = 256, SORT_W = SORT_T / 64;                  // digits of at most nine bits; threads and waves of a tile
+constexpr int TILE_MIN = 1024, TILES_MAX = 64, ROWS = TILE_MIN / SORT_T;        // tiles of a sorting pass; rows of 64 that a wave asks for at once
+constexpr int ALONE = 4096, ALONE_T = 1024;                                     // tokens that one workgroup sorts by itself, its threads
 constexpr int CHUNK_MIN = 8;                                                    // sorted places of a thread, at least
 constexpr int AHEAD = 8;                                                        // rows of dy that a thread asks for before it adds the first
 constexpr int JOIN_T = 1024;                                                    // threads of a workgroup that joins a run's partial sums
@@ -108,6 +109,11 @@ embed_columns_kernel(const ID* __restrict__ ids, const typename W::T* __restrict
 struct Fill {
     float* p;
     int64_t n;
+    Fill share(int i, int of) const      // piece i of so many, whole sixteen bytes each
+    {
+        const int64_t each = (n / 4 + of - 1) / of * 4, from = each * i < n ? each * i : n, to = i + 1 < of && from + each < n ? from + each : n;
+        return {p + from, to - from};
+    }
     unsigned groups(int threads) const      // four pieces of sixteen bytes a thread, and 1024 workgroups at most
     {
         const int64_t want = (n + threads * 16 - 1) / (threads * 16);
@@ -181,27 +187,6 @@ struct Tokens {
     }
 };
 
-// hist[tile][digit] = how many tokens of the tile have the digit
-template <class ID>
-__global__ void __launch_bounds__(SORT_T)
-sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, uint32_t* __restrict__ joins, int64_t M, int64_t tile, uint32_t tiles, int shift,
-                  int bits, Fill fill)
-{
-    __shared__ uint32_t n[RADIX];
-    if (blockIdx.x >= tiles) {
-        fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
-        return;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *joins = 0;
-    for (int i = threadIdx.x; i < RADIX; i += SORT_T) n[i] = 0;
-    __syncthreads();
-    const int64_t from = blockIdx.x * tile, to = from + tile < M ? from + tile : M;
-    const uint32_t mask = (1u << bits) - 1u;
-    for (int64_t i = from + threadIdx.x; i < to; i += SORT_T) atomicAdd(&n[in.k(i) >> shift & mask], 1u);
-    __syncthreads();
-    for (int i = threadIdx.x; i < RADIX; i += SORT_T) hist[(size_t)blockIdx.x * RADIX + i] = n[i];
-}
-
 // The place of a lane's token among those of its wave's share with the digit: behind those of earlier rows (next[digit], which the
 // first lane with the digit moves on by their number) and of earlier lanes.
 __device__ __forceinline__ uint32_t place_of(uint32_t digit, bool there, int bits, uint32_t* next)
@@ -219,135 +204,196 @@ __device__ __forceinline__ uint32_t place_of(uint32_t digit, bool there, int bit
     return first + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
 }
 
+// Sum of the numbers of the threads before, for threads 0 .. 255 of a workgroup (all of it has to call).
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t (&waves)[SORT_W])
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t t = (uint32_t)__shfl_up((int)s, d);
+        if (lane >= d) s += t;
+    }
+    if (tid < SORT_T && lane == 63) waves[tid >> 6] = s;
+    __syncthreads();
+    s -= v;
+#pragma unroll
+    for (int w = 0; w < SORT_W; ++w)
+        if (w < (tid >> 6)) s += waves[w];
+    return s;
+}
+
+// Counts of a tile's tokens by digit: hist[tile][digit], and by waves behind those of all tiles: hist[tiles + 4 tile + wave][digit].
+template <class ID>
+__global__ void __launch_bounds__(SORT_T)
+sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, uint32_t* __restrict__ joins, int64_t M, int64_t tile, uint32_t tiles, int shift,
+                  int bits, Fill fill)
+{
+    __shared__ uint32_t n[SORT_W][RADIX];
+    if (blockIdx.x >= tiles) {
+        fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *joins = 0;
+    const int tid = threadIdx.x, wave = tid >> 6, digits = 1 << bits;
+    const uint32_t mask = (uint32_t)digits - 1u;
+    const int64_t share = tile / SORT_W, from = blockIdx.x * tile + wave * share + (tid & 63);
+    for (int i = tid; i < digits; i += SORT_T)
+#pragma unroll
+        for (int w = 0; w < SORT_W; ++w) n[w][i] = 0;
+    __syncthreads();
+    for (int64_t r = 0; r < share; r += 64 * ROWS) {
+        uint32_t k[ROWS];
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) k[u] = in.k(from + r + 64 * u < M ? from + r + 64 * u : M - 1);
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+            if (from + r + 64 * u < M) atomicAdd(&n[wave][k[u] >> shift & mask], 1u);
+    }
+    __syncthreads();
+    for (int i = tid; i < digits; i += SORT_T) {
+        uint32_t all = 0;
+#pragma unroll
+        for (int w = 0; w < SORT_W; ++w) {
+            hist[((size_t)tiles + blockIdx.x * SORT_W + w) * RADIX + i] = n[w][i];
+            all += n[w][i];
+        }
+        hist[(size_t)blockIdx.x * RADIX + i] = all;
+    }
+}
+
 // Puts a tile's tokens where they belong: behind all of smaller digits, those of the same digit in earlier tiles, in earlier waves'
 // shares of the tile, in earlier rows of 64, and in earlier lanes.
 template <class ID>
 __global__ void __launch_bounds__(SORT_T)
 sort_place_kernel(Tokens<ID> in, const uint32_t* __restrict__ hist, uint32_t* __restrict__ key, uint32_t* __restrict__ pos, int64_t M,
-                  int64_t tile, int shift, int bits)
+                  int64_t tile, uint32_t tiles, int shift, int bits, Fill fill)
 {
-    constexpr int WAVES = SORT_T / 64, D = RADIX / SORT_T;
-    __shared__ uint32_t at[WAVES][RADIX];      // next place of a wave's tokens with a digit
-    __shared__ uint32_t sums[SORT_T];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t mask = (1u << bits) - 1u;
-    const int64_t share = tile / WAVES, from = blockIdx.x * tile + wave * share;
-    for (int i = tid; i < WAVES * RADIX; i += SORT_T) (&at[0][0])[i] = 0;
-    __syncthreads();
-    for (int64_t i = from + lane; i < from + share && i < M; i += 64) atomicAdd(&at[wave][in.k(i) >> shift & mask], 1u);
-    // digits D tid .. D tid + D - 1: all their tokens, and those of earlier tiles
-    uint32_t all[D] = {}, before[D] = {};
-    for (uint32_t t = 0; t < gridDim.x; ++t)
-#pragma unroll
-        for (int j = 0; j < D; ++j) {
-            const uint32_t c = hist[(size_t)t * RADIX + D * tid + j];
-            all[j] += c;
-            if (t < blockIdx.x) before[j] += c;
-        }
-    uint32_t mine = 0;
-#pragma unroll
-    for (int j = 0; j < D; ++j) mine += all[j];
-    sums[tid] = mine;
-    __syncthreads();
-    for (int s = 1; s < SORT_T; s <<= 1) {
-        const uint32_t v = tid >= s ? sums[tid - s] : 0;
-        __syncthreads();
-        sums[tid] += v;
-        __syncthreads();
+    __shared__ uint32_t at[SORT_W][RADIX];      // next place of a wave's tokens with a digit
+    __shared__ uint32_t waves[SORT_W];
+    if (blockIdx.x >= tiles) {
+        fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
+        return;
     }
-    uint32_t start = sums[tid] - mine;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
+    const uint32_t mask = (uint32_t)digits - 1u;
+    const int64_t share = tile / SORT_W, from = blockIdx.x * tile + wave * share;
+    uint32_t k[ROWS], p[ROWS];
+    const auto ask = [&](int64_t r) {
 #pragma unroll
-    for (int j = 0; j < D; ++j) {
-        uint32_t next = start + before[j];
-        for (int w = 0; w < WAVES; ++w) {
-            const uint32_t c = at[w][D * tid + j];
-            at[w][D * tid + j] = next;
-            next += c;
+        for (int u = 0; u < ROWS; ++u) {
+            const int64_t i = from + r + 64 * u + lane < M ? from + r + 64 * u + lane : M - 1;
+            k[u] = in.k(i);
+            p[u] = in.p(i);
         }
-        start += all[j];
+    };
+    ask(0);
+    uint2 all = make_uint2(0, 0), before = make_uint2(0, 0), own[SORT_W];      // digits 2 tid, 2 tid + 1
+    if (2 * tid < digits) {
+        const auto counts = [&](uint32_t row) { return *reinterpret_cast<const uint2*>(hist + (size_t)row * RADIX + 2 * tid); };
+#pragma unroll
+        for (int w = 0; w < SORT_W; ++w) own[w] = counts(tiles + blockIdx.x * SORT_W + w);
+#pragma unroll 16
+        for (uint32_t t = 0; t < tiles; ++t) {
+            const uint2 c = counts(t);
+            all.x += c.x;
+            all.y += c.y;
+            if (t < blockIdx.x) { before.x += c.x; before.y += c.y; }
+        }
+    }
+    const uint32_t start = sum_before(all.x + all.y, waves);
+    if (2 * tid < digits) {
+        uint2 next = make_uint2(start + before.x, start + all.x + before.y);
+#pragma unroll
+        for (int w = 0; w < SORT_W; ++w) {
+            *reinterpret_cast<uint2*>(&at[w][2 * tid]) = next;
+            next.x += own[w].x;
+            next.y += own[w].y;
+        }
     }
     __syncthreads();
-    for (int64_t r = from; r < from + share && r < M; r += 64) {      // (the same rows for every lane of a wave)
-        const int64_t i = r + lane;
-        const bool there = i < M;
-        const uint32_t k = there ? in.k(i) : 0, to = place_of(k >> shift & mask, there, bits, at[wave]);
-        if (there) {
-            key[to] = k;
-            pos[to] = in.p(i);
+    for (int64_t r = 0; r < share && from + r < M; r += 64 * ROWS) {      // (the same for every lane of a wave)
+        if (r) ask(r);
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const bool there = from + r + 64 * u + lane < M;
+            const uint32_t to = place_of(k[u] >> shift & mask, there, bits, at[wave]);
+            if (there) {
+                key[to] = k[u];
+                pos[to] = p[u];
+            }
         }
     }
 }
 
-// All passes by one workgroup (the first of the launch); each wave keeps its share's tokens in registers, counts them and, once the
-// starts are known, puts them in their places.  16384 tokens and 16 bits: 15 us, behind the zeros that the other workgroups write.
+// All passes by one workgroup (the first of the launch), for few tokens: they stay in LDS, and each wave's share in its registers.
 template <class ID>
 __global__ void __launch_bounds__(ALONE_T)
-sort_alone_kernel(Tokens<ID> in, uint32_t* __restrict__ key0, uint32_t* __restrict__ pos0, uint32_t* __restrict__ key1, uint32_t* __restrict__ pos1,
-                  uint32_t* __restrict__ joins, int M, int passes, int bits, Fill fill)
+sort_alone_kernel(Tokens<ID> in, uint32_t* __restrict__ key, uint32_t* __restrict__ pos, uint32_t* __restrict__ joins, int M, int passes, int bits,
+                  Fill fill)
 {
-    constexpr int WAVES = ALONE_T / 64, ROWS = ALONE / ALONE_T;
-    __shared__ uint32_t at[WAVES][RADIX];
-    __shared__ uint32_t sums[RADIX];
+    constexpr int WAVES = ALONE_T / 64, R = ALONE / ALONE_T;
+    __shared__ uint32_t at[WAVES][RADIX], lk[ALONE], lp[ALONE], waves[SORT_W];
     if (blockIdx.x > 0) {
         fill_zero(fill, blockIdx.x - 1, gridDim.x - 1);
         return;
     }
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
     if (tid == 0) *joins = 0;
-    const uint32_t mask = (1u << bits) - 1u;
-    const int share = (M + ALONE_T - 1) / ALONE_T * 64, from = wave * share + lane;      // rows of 64 of a wave, in order
-    for (int pass = 0; pass < passes; ++pass) {
-        const uint32_t *sk = pass & 1 ? key0 : key1, *sp = pass & 1 ? pos0 : pos1;
-        uint32_t *tk = pass & 1 ? key1 : key0, *tp = pass & 1 ? pos1 : pos0;
-        const int shift = pass * bits;
-        for (int i = tid; i < WAVES * RADIX; i += ALONE_T) (&at[0][0])[i] = 0;
-        uint32_t k[ROWS], p[ROWS];
+    const uint32_t mask = (uint32_t)digits - 1u;
+    const int rows = (M + ALONE_T - 1) / ALONE_T, from = wave * rows * 64;      // rows of 64 of a wave, in order
+    uint32_t k[R], p[R];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const int i = from + 64 * r;
-            const bool there = 64 * r < share && i < M;
-            k[r] = p[r] = 0;
-            if (there) {
-                k[r] = pass ? sk[i] : in.k(i);
-                p[r] = pass ? sp[i] : (uint32_t)i;
+    for (int r = 0; r < R; ++r) {
+        const int i = from + 64 * r + lane < M ? from + 64 * r + lane : M - 1;
+        k[r] = in.k(i);
+        p[r] = (uint32_t)i;
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * bits;
+        for (int i = lane; i < digits; i += 64) at[wave][i] = 0;
+        if (pass) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int i = from + 64 * r + lane < M ? from + 64 * r + lane : M - 1;
+                k[r] = lk[i];
+                p[r] = lp[i];
             }
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-            if (64 * r < share && from + 64 * r < M) atomicAdd(&at[wave][k[r] >> shift & mask], 1u);
+        for (int r = 0; r < R; ++r)
+            if (r < rows && from + 64 * r + lane < M) atomicAdd(&at[wave][k[r] >> shift & mask], 1u);
         __syncthreads();
-        uint32_t mine = 0;
-        if (tid < RADIX) {
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) mine += at[w][tid];
-            sums[tid] = mine;
-        }
-        __syncthreads();
-        for (int s = 1; s < RADIX; s <<= 1) {
-            const uint32_t v = tid < RADIX && tid >= s ? sums[tid - s] : 0;
-            __syncthreads();
-            if (tid < RADIX) sums[tid] += v;
-            __syncthreads();
-        }
-        if (tid < RADIX) {
-            uint32_t next = sums[tid] - mine;
+        uint2 mine = make_uint2(0, 0);
+        if (2 * tid < digits)
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
-                const uint32_t c = at[w][tid];
-                at[w][tid] = next;
-                next += c;
+                mine.x += at[w][2 * tid];
+                mine.y += at[w][2 * tid + 1];
+            }
+        const uint32_t start = sum_before(mine.x + mine.y, waves);
+        if (2 * tid < digits) {
+            uint2 next = make_uint2(start, start + mine.x);
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                uint2* a = reinterpret_cast<uint2*>(&at[w][2 * tid]);
+                const uint2 c = *a;
+                *a = next;
+                next.x += c.x;
+                next.y += c.y;
             }
         }
         __syncthreads();
+        const bool out = pass == passes - 1;
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            if (64 * r >= share || from - lane + 64 * r >= M) break;      // (the same for every lane of a wave)
-            const bool there = from + 64 * r < M;
+        for (int r = 0; r < R; ++r) {
+            if (r >= rows || from + 64 * r >= M) break;      // (the same for every lane of a wave)
+            const bool there = from + 64 * r + lane < M;
             const uint32_t to = place_of(k[r] >> shift & mask, there, bits, at[wave]);
             if (there) {
-                tk[to] = k[r];
-                tp[to] = p[r];
+                (out ? key : lk)[to] = k[r];
+                (out ? pos : lp)[to] = p[r];
             }
         }
         __syncthreads();      // (what a pass has written, the next one reads)
@@ -485,14 +531,14 @@ struct Layout {      // of the workspace
     size_t hist, key[2], pos[2], part, joins, rows, total;
     int64_t M, tile, tiles, chunk, chunks;
     uint32_t P;
-    int passes, bits;
+    int passes, bits, sorted;      // which of the two pairs the last pass leaves
 };
 
 Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
 {
     Layout l;
     l.M = B * N;
-    // a pass reads the counts of every tile in every tile: no more than 256 of them, however many tokens there are
+    // a pass reads the counts of every tile in every tile: no more than 64 of them, however many tokens there are
     l.tile = TILE_MIN * ((l.M + (int64_t)TILE_MIN * TILES_MAX - 1) / ((int64_t)TILE_MIN * TILES_MAX));
     l.tiles = (l.M + l.tile - 1) / l.tile;
     l.P = (uint32_t)((H + VE - 1) / VE);
@@ -504,9 +550,10 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
     while (V >> need) ++need;                       // bits of V, the number of no token
     l.passes = (need + 8) / 9;
     l.bits = (need + l.passes - 1) / l.passes;
+    l.sorted = (l.passes - 1) & 1;
     size_t off = 0;
     const auto take = [&](size_t bytes) { const size_t at = off; off += up256(bytes); return at; };
-    l.hist = take((size_t)(l.M < (int64_t)TILE_MIN * TILES_MAX ? (l.M + TILE_MIN - 1) / TILE_MIN : TILES_MAX) * RADIX * sizeof(uint32_t));
+    l.hist = take((size_t)(l.M < (int64_t)TILE_MIN * TILES_MAX ? (l.M + TILE_MIN - 1) / TILE_MIN : TILES_MAX) * (1 + SORT_W) * RADIX * sizeof(uint32_t));
     for (int i = 0; i < 2; ++i) {
         l.key[i] = take((size_t)(l.M + 32) * sizeof(uint32_t));
         l.pos[i] = take((size_t)(l.M + 32) * sizeof(uint32_t));
@@ -524,28 +571,30 @@ template <class ID>
 hipError_t sort_pass(const Tokens<ID>& in, char* ws, const Layout& l, int pass, int to, const Fill& fill, hipStream_t st)
 {
     uint32_t* hist = (uint32_t*)(ws + l.hist);
-    hipLaunchKernelGGL((sort_count_kernel<ID>), dim3((unsigned)l.tiles + fill.groups(SORT_T)), dim3(SORT_T), 0, st, in, hist, (uint32_t*)(ws + l.joins), l.M, l.tile,
-                       (uint32_t)l.tiles, pass * l.bits, l.bits, fill);
-    hipLaunchKernelGGL((sort_place_kernel<ID>), dim3((unsigned)l.tiles), dim3(SORT_T), 0, st, in, (const uint32_t*)hist, (uint32_t*)(ws + l.key[to]),
-                       (uint32_t*)(ws + l.pos[to]), l.M, l.tile, pass * l.bits, l.bits);
+    const unsigned tiles = (unsigned)l.tiles;
+    const Fill a = fill.share(2 * pass, 2 * l.passes), b = fill.share(2 * pass + 1, 2 * l.passes);
+    hipLaunchKernelGGL((sort_count_kernel<ID>), dim3(tiles + a.groups(SORT_T)), dim3(SORT_T), 0, st, in, hist, (uint32_t*)(ws + l.joins), l.M, l.tile,
+                       tiles, pass * l.bits, l.bits, a);
+    hipLaunchKernelGGL((sort_place_kernel<ID>), dim3(tiles + b.groups(SORT_T)), dim3(SORT_T), 0, st, in, (const uint32_t*)hist,
+                       (uint32_t*)(ws + l.key[to]), (uint32_t*)(ws + l.pos[to]), l.M, l.tile, tiles, pass * l.bits, l.bits, b);
     return hipGetLastError();
 }
 
-// -> key[0], pos[0] or [1], by passes; and the zeros
+// -> key[], pos[] of Layout::sorted; and the zeros
 template <class ID>
 hipError_t sort_tokens(const ID* ids, int64_t V, char* ws, const Layout& l, const Fill& fill, hipStream_t st)
 {
     const Tokens<ID> in{ids, nullptr, nullptr, (uint32_t)V};
     if (l.M <= ALONE) {
-        hipLaunchKernelGGL((sort_alone_kernel<ID>), dim3(1 + fill.groups(ALONE_T)), dim3(ALONE_T), 0, st, in, (uint32_t*)(ws + l.key[0]), (uint32_t*)(ws + l.pos[0]),
-                           (uint32_t*)(ws + l.key[1]), (uint32_t*)(ws + l.pos[1]), (uint32_t*)(ws + l.joins), (int)l.M, l.passes, l.bits, fill);
+        hipLaunchKernelGGL((sort_alone_kernel<ID>), dim3(1 + fill.groups(ALONE_T)), dim3(ALONE_T), 0, st, in, (uint32_t*)(ws + l.key[l.sorted]),
+                           (uint32_t*)(ws + l.pos[l.sorted]), (uint32_t*)(ws + l.joins), (int)l.M, l.passes, l.bits, fill);
         return hipGetLastError();
     }
     hipError_t e = sort_pass<ID>(in, ws, l, 0, 0, fill, st);
     for (int pass = 1; pass < l.passes && e == hipSuccess; ++pass) {
         const int from = (pass - 1) & 1;
         const Tokens<void> pairs{nullptr, (const uint32_t*)(ws + l.key[from]), (const uint32_t*)(ws + l.pos[from]), (uint32_t)V};
-        e = sort_pass<void>(pairs, ws, l, pass, pass & 1, Fill{nullptr, 0}, st);
+        e = sort_pass<void>(pairs, ws, l, pass, pass & 1, fill, st);
     }
     return e;
 }
@@ -597,8 +646,7 @@ hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hip
                            (uint32_t)tt, (uint32_t)th, a.drop);
         rows = (const T*)(ws + l.rows);
     }
-    const int last = (l.passes - 1) & 1;
-    const uint32_t *key = (const uint32_t*)(ws + l.key[last]), *pos = (const uint32_t*)(ws + l.pos[last]);
+    const uint32_t *key = (const uint32_t*)(ws + l.key[l.sorted]), *pos = (const uint32_t*)(ws + l.pos[l.sorted]);
     float* part = (float*)(ws + l.part);
     uint32_t* joins = (uint32_t*)(ws + l.joins);
     if ((e = launch_grid(((uint64_t)l.chunks * l.P + 255) / 256, 256, &g)) != hipSuccess) return e;
