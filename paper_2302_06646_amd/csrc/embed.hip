@@ -130,26 +130,41 @@ __device__ __forceinline__ void fill_zero(const Fill& f, int64_t group, int64_t 
     }
 }
 
-// [B,H,N] -> rows of `stride` channels, dropped entries zero (the factor of the kept ones comes in with `scale`, so nothing is rounded)
+// [B,H,N] -> rows of `stride` channels, dropped entries zero (the factor of the kept ones comes in with `scale`, so nothing is rounded),
+// in tiles of 64 x 64: by a kernel, or behind a sort's launches as the zeros are.
+struct Transpose {
+    const void* dy;
+    void* out;
+    uint32_t N, H, stride, tiles_t, tiles_h;
+    Drop d;
+    uint32_t from, tiles;      // this launch's share of the tiles
+    Transpose share(int i, int of) const
+    {
+        Transpose t = *this;
+        const uint32_t each = (tiles + of - 1) / of, at = each * i < tiles ? each * i : tiles;
+        t.from = from + at;
+        t.tiles = tiles - at < each ? tiles - at : each;
+        return t;
+    }
+};
+typedef float TransposeTile[TT][TH + 1];
 template <class IO>
-__global__ void __launch_bounds__(256)
-embed_transpose_kernel(const typename IO::T* __restrict__ dy, typename IO::T* __restrict__ out, uint32_t N, uint32_t H, uint32_t stride,
-                       uint32_t tiles_t, uint32_t tiles_h, Drop d)
+__device__ __forceinline__ void transpose_tile(const Transpose& a, uint32_t number, TransposeTile& tile)
 {
-    __shared__ float tile[TT][TH + 1];
-    const uint32_t tt = blockIdx.x % tiles_t, th = blockIdx.x / tiles_t % tiles_h, b = blockIdx.x / tiles_t / tiles_h;
+    typedef typename IO::T T;
+    const uint32_t id = a.from + number, tt = id % a.tiles_t, th = id / a.tiles_t % a.tiles_h, b = id / a.tiles_t / a.tiles_h;
     const uint32_t t0 = tt * TT, h0 = th * TH, tid = threadIdx.x, s = tid % 8;
-    const uint64_t call = call_of(d);
+    const uint64_t call = call_of(a.d);
 #pragma unroll
     for (uint32_t k = 0; k < TH / 32; ++k) {
         const uint32_t hh = tid / 8 + 32 * k, h = h0 + hh, t = t0 + VE * s;
         float v[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) v[i] = 0.f;
-        if (h < H && t < N) {
-            const size_t e = ((size_t)b * H + h) * N + t;
-            load8<IO>(dy + e, (int)(N - t), v);
-            const uint32_t m = d.threshold ? kept8_at(e, d, call) : 0xffu;
+        if (h < a.H && t < a.N) {
+            const size_t e = ((size_t)b * a.H + h) * a.N + t;
+            load8<IO>((const T*)a.dy + e, (int)(a.N - t), v);
+            const uint32_t m = a.d.threshold ? kept8_at(e, a.d, call) : 0xffu;
 #pragma unroll
             for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? v[i] : 0.f;
         }
@@ -160,12 +175,18 @@ embed_transpose_kernel(const typename IO::T* __restrict__ dy, typename IO::T* __
 #pragma unroll
     for (uint32_t k = 0; k < TT / 32; ++k) {
         const uint32_t t = tid / 8 + 32 * k, h = h0 + VE * s;
-        if (t0 + t >= N || h >= stride) continue;      // (stride is a multiple of eight)
+        if (t0 + t >= a.N || h >= a.stride) continue;      // (stride is a multiple of eight)
         float v[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) v[i] = tile[t][VE * s + i];
-        store8<IO>(out + ((size_t)b * N + t0 + t) * stride + h, VE, v);
+        store8<IO>((T*)a.out + ((size_t)b * a.N + t0 + t) * a.stride + h, VE, v);
     }
+}
+template <class IO>
+__global__ void __launch_bounds__(256) embed_transpose_kernel(Transpose a)
+{
+    __shared__ TransposeTile tile;
+    transpose_tile<IO>(a, blockIdx.x, tile);
 }
 
 // One pass of the stable sort by token: `shift` and `bits` name the digit.  ID: the pass reads the tokens themselves, whose places are
@@ -223,17 +244,40 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t (&waves)[SOR
     return s;
 }
 
+// What the workgroups behind a sorting launch's tiles do meanwhile: zeros, then tiles of the transposition (IO void: there is none).
+struct Beside {
+    Fill fill;
+    uint32_t fills;
+    Transpose t;
+};
+template <class IO>
+union SortRoom {
+    uint32_t at[SORT_W][RADIX];
+    TransposeTile tile;
+};
+template <>
+union SortRoom<void> {
+    uint32_t at[SORT_W][RADIX];
+};
+template <class IO>
+__device__ __forceinline__ void beside_the_sort(const Beside& a, uint32_t group, SortRoom<IO>& room)
+{
+    if (group < a.fills) fill_zero(a.fill, group, a.fills);
+    else if constexpr (!std::is_void<IO>::value) transpose_tile<IO>(a.t, group - a.fills, room.tile);
+}
+
 // Counts of a tile's tokens by digit: hist[tile][digit], and by waves behind those of all tiles: hist[tiles + 4 tile + wave][digit].
-template <class ID>
+template <class ID, class IO>
 __global__ void __launch_bounds__(SORT_T)
 sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, uint32_t* __restrict__ joins, int64_t M, int64_t tile, uint32_t tiles, int shift,
-                  int bits, Fill fill)
+                  int bits, Beside beside)
 {
-    __shared__ uint32_t n[SORT_W][RADIX];
+    __shared__ SortRoom<IO> room;
     if (blockIdx.x >= tiles) {
-        fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
+        beside_the_sort<IO>(beside, blockIdx.x - tiles, room);
         return;
     }
+    uint32_t(&n)[SORT_W][RADIX] = room.at;
     if (blockIdx.x == 0 && threadIdx.x == 0) *joins = 0;
     const int tid = threadIdx.x, wave = tid >> 6, digits = 1 << bits;
     const uint32_t mask = (uint32_t)digits - 1u;
@@ -264,17 +308,18 @@ sort_count_kernel(Tokens<ID> in, uint32_t* __restrict__ hist, uint32_t* __restri
 
 // Puts a tile's tokens where they belong: behind all of smaller digits, those of the same digit in earlier tiles, in earlier waves'
 // shares of the tile, in earlier rows of 64, and in earlier lanes.
-template <class ID>
+template <class ID, class IO>
 __global__ void __launch_bounds__(SORT_T)
 sort_place_kernel(Tokens<ID> in, const uint32_t* __restrict__ hist, uint32_t* __restrict__ key, uint32_t* __restrict__ pos, int64_t M,
-                  int64_t tile, uint32_t tiles, int shift, int bits, Fill fill)
+                  int64_t tile, uint32_t tiles, int shift, int bits, Beside beside)
 {
-    __shared__ uint32_t at[SORT_W][RADIX];      // next place of a wave's tokens with a digit
+    __shared__ SortRoom<IO> room;
     __shared__ uint32_t waves[SORT_W];
     if (blockIdx.x >= tiles) {
-        fill_zero(fill, blockIdx.x - tiles, gridDim.x - tiles);
+        beside_the_sort<IO>(beside, blockIdx.x - tiles, room);
         return;
     }
+    uint32_t(&at)[SORT_W][RADIX] = room.at;      // next place of a wave's tokens with a digit
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << bits;
     const uint32_t mask = (uint32_t)digits - 1u;
     const int64_t share = tile / SORT_W, from = blockIdx.x * tile + wave * share;
@@ -491,11 +536,14 @@ embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ pa
     const uint32_t n = joins[0], blocks = (P * 2 + 63) / 64, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     for (uint32_t item = blockIdx.x; item < n * blocks; item += gridDim.x) {
         const uint32_t chunk = joins[1 + item / blocks], col = item % blocks * 64 + lane, to = (chunk + 1) * chunk_size, k = key[to];
-        uint32_t lo = to + 1, hi = M;      // the run's end: the first place behind `to` with another token
+        // the run's end: the first place behind `to` with another token; the lanes of a wave look at 64 places at once
+        uint32_t lo = to + 1, hi = M;
         while (lo < hi) {
-            const uint32_t mid = (lo + hi) >> 1;
-            if (key[mid] == k) lo = mid + 1;
-            else hi = mid;
+            const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const uint32_t same = (uint32_t)__popcll(__ballot(at < hi && key[at] == k));      // (the first so many lanes)
+            const uint32_t end = lo + same * step;
+            if (same) lo = end - step + 1;
+            if (end < hi) hi = end;
         }
         const uint32_t last = (lo - 1) / chunk_size;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -567,34 +615,43 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
     return l;
 }
 
-template <class ID>
-hipError_t sort_pass(const Tokens<ID>& in, char* ws, const Layout& l, int pass, int to, const Fill& fill, hipStream_t st)
+template <class IO, class ID>
+hipError_t sort_pass(const Tokens<ID>& in, char* ws, const Layout& l, int pass, int to, const Fill& fill, const Transpose* t, hipStream_t st)
 {
     uint32_t* hist = (uint32_t*)(ws + l.hist);
     const unsigned tiles = (unsigned)l.tiles;
-    const Fill a = fill.share(2 * pass, 2 * l.passes), b = fill.share(2 * pass + 1, 2 * l.passes);
-    hipLaunchKernelGGL((sort_count_kernel<ID>), dim3(tiles + a.groups(SORT_T)), dim3(SORT_T), 0, st, in, hist, (uint32_t*)(ws + l.joins), l.M, l.tile,
-                       tiles, pass * l.bits, l.bits, a);
-    hipLaunchKernelGGL((sort_place_kernel<ID>), dim3(tiles + b.groups(SORT_T)), dim3(SORT_T), 0, st, in, (const uint32_t*)hist,
-                       (uint32_t*)(ws + l.key[to]), (uint32_t*)(ws + l.pos[to]), l.M, l.tile, tiles, pass * l.bits, l.bits, b);
+    Beside part[2] = {};
+    dim3 g[2];
+    for (int i = 0; i < 2; ++i) {
+        part[i].fill = fill.share(2 * pass + i, 2 * l.passes);
+        part[i].fills = part[i].fill.groups(SORT_T);
+        if (t) part[i].t = t->share(2 * pass + i, 2 * l.passes);
+        const hipError_t e = launch_grid((uint64_t)tiles + part[i].fills + part[i].t.tiles, SORT_T, &g[i]);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((sort_count_kernel<ID, IO>), g[0], dim3(SORT_T), 0, st, in, hist, (uint32_t*)(ws + l.joins), l.M, l.tile, tiles, pass * l.bits,
+                       l.bits, part[0]);
+    hipLaunchKernelGGL((sort_place_kernel<ID, IO>), g[1], dim3(SORT_T), 0, st, in, (const uint32_t*)hist, (uint32_t*)(ws + l.key[to]),
+                       (uint32_t*)(ws + l.pos[to]), l.M, l.tile, tiles, pass * l.bits, l.bits, part[1]);
     return hipGetLastError();
 }
 
-// -> key[], pos[] of Layout::sorted; and the zeros
-template <class ID>
-hipError_t sort_tokens(const ID* ids, int64_t V, char* ws, const Layout& l, const Fill& fill, hipStream_t st)
+// -> key[], pos[] of Layout::sorted; and the zeros and the transposition (if any)
+template <class IO, class ID>
+hipError_t sort_tokens(const ID* ids, int64_t V, char* ws, const Layout& l, const Fill& fill, const Transpose* t, hipStream_t st)
 {
     const Tokens<ID> in{ids, nullptr, nullptr, (uint32_t)V};
     if (l.M <= ALONE) {
         hipLaunchKernelGGL((sort_alone_kernel<ID>), dim3(1 + fill.groups(ALONE_T)), dim3(ALONE_T), 0, st, in, (uint32_t*)(ws + l.key[l.sorted]),
                            (uint32_t*)(ws + l.pos[l.sorted]), (uint32_t*)(ws + l.joins), (int)l.M, l.passes, l.bits, fill);
+        if constexpr (!std::is_void<IO>::value) hipLaunchKernelGGL(embed_transpose_kernel<IO>, dim3(t->tiles), dim3(256), 0, st, *t);
         return hipGetLastError();
     }
-    hipError_t e = sort_pass<ID>(in, ws, l, 0, 0, fill, st);
+    hipError_t e = sort_pass<IO, ID>(in, ws, l, 0, 0, fill, t, st);
     for (int pass = 1; pass < l.passes && e == hipSuccess; ++pass) {
         const int from = (pass - 1) & 1;
         const Tokens<void> pairs{nullptr, (const uint32_t*)(ws + l.key[from]), (const uint32_t*)(ws + l.pos[from]), (uint32_t)V};
-        e = sort_pass<void>(pairs, ws, l, pass, pass & 1, fill, st);
+        e = sort_pass<IO, void>(pairs, ws, l, pass, pass & 1, fill, t, st);
     }
     return e;
 }
@@ -633,19 +690,21 @@ hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hip
     const Layout l = lay_out(a.B, a.N, a.V, a.H, a.io, a.layout);
     dim3 g;
     const Fill fill{dE, a.V * a.H};
-    hipError_t e = a.id_bytes == 8 ? sort_tokens((const int64_t*)a.ids, a.V, ws, l, fill, st)
-                                   : sort_tokens((const int32_t*)a.ids, a.V, ws, l, fill, st);
-    if (e != hipSuccess) return e;
     const T* rows = (const T*)dy;
     uint32_t stride = (uint32_t)a.H;
+    hipError_t e;
     if (a.layout == LONGCONV_CHANNELS_FIRST) {
-        const uint64_t tt = (a.N + TT - 1) / TT, th = (a.H + TH - 1) / TH;
-        if ((e = launch_grid(a.B * tt * th, 256, &g)) != hipSuccess) return e;
-        stride = l.P * VE;
-        hipLaunchKernelGGL(embed_transpose_kernel<IO>, g, dim3(256), 0, st, rows, (T*)(ws + l.rows), (uint32_t)a.N, (uint32_t)a.H, stride,
-                           (uint32_t)tt, (uint32_t)th, a.drop);
+        const uint32_t tt = (uint32_t)((a.N + TT - 1) / TT), th = (uint32_t)((a.H + TH - 1) / TH);
         rows = (const T*)(ws + l.rows);
+        stride = l.P * VE;
+        const Transpose t{dy, ws + l.rows, (uint32_t)a.N, (uint32_t)a.H, stride, tt, th, a.drop, 0, (uint32_t)a.B * tt * th};
+        e = a.id_bytes == 8 ? sort_tokens<IO>((const int64_t*)a.ids, a.V, ws, l, fill, &t, st)
+                            : sort_tokens<IO>((const int32_t*)a.ids, a.V, ws, l, fill, &t, st);
+    } else {
+        e = a.id_bytes == 8 ? sort_tokens<void>((const int64_t*)a.ids, a.V, ws, l, fill, nullptr, st)
+                            : sort_tokens<void>((const int32_t*)a.ids, a.V, ws, l, fill, nullptr, st);
     }
+    if (e != hipSuccess) return e;
     const uint32_t *key = (const uint32_t*)(ws + l.key[l.sorted]), *pos = (const uint32_t*)(ws + l.pos[l.sorted]);
     float* part = (float*)(ws + l.part);
     uint32_t* joins = (uint32_t*)(ws + l.joins);
