@@ -1,837 +1,15 @@
-// Group norm with an activation, channels last: x [B,S,C], groups of C / G neighbouring channels over all S positions,
-//     xhat = (x - mean) rstd,   z = gamma xhat + beta,   y = act(z)
-// and its backward pass, with dz = dy act'(z) and m = S C / G:
-//     dbeta = sum dz,   dgamma = sum dz xhat (over b and positions),   dx = rstd (gamma dz - (s1 + xhat s2) / m),
-//     s1 = sum gamma dz,   s2 = sum gamma dz xhat over the group.
-//
-// Sums go by channel first: a thread keeps eight channels and walks over positions, so a group may be of any width, and dgamma, dbeta
-// and the group's sums come from the same numbers.  Mean and variance are carried as (mean, sum of squared differences), merged
-// pairwise, so a mean that is large against the deviation costs nothing.  All in fp32, in a fixed order.
-#include "vec8.hpp"
+// Group norm: the C-ABI layer's entry points, and the kernels (gnorm.hpp) of fp32 rows.  Those of fp16 and bf16 rows are compiled beside
+// it, in files of their own.
+#include "gnorm.hpp"
 
 namespace lc {
-namespace {
 
-constexpr int GT = 512;              // threads
-constexpr int SLAB = 64;             // pieces of eight channels of a workgroup, at most
-constexpr int GROUPS_WANTED = 1024;  // workgroups of a pass over the tensor
-constexpr int AHEAD = 4;             // pieces that a thread asks for before it uses the first
-
-// The normal distribution function, and e = exp(-z^2 / 2) beside it.  erfc(x) exp(x^2) is t Q(t), t = 1 / (1 + 0.4 x), for x >= 0, Q the
-// polynomial of degree eight of the least largest relative error (fitted by weighted least squares): 1.3e-7, and 2.2e-7 absolute in
-// fp32.  Below zero the result is not a difference, so its relative error is that of e, 8e-7 down to z = -4.
-__device__ __forceinline__ float normal_cdf(float z, float& e)
-{
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.28284271247461901f, fabsf(z), 1.f));
-    float q = 0.0502542145550251f;
-    q = __builtin_fmaf(q, t, -0.18287357687950134f);
-    q = __builtin_fmaf(q, t, 0.16904595494270325f);
-    q = __builtin_fmaf(q, t, -0.0055788299068808556f);
-    q = __builtin_fmaf(q, t, 0.14142005145549774f);
-    q = __builtin_fmaf(q, t, 0.16854438185691833f);
-    q = __builtin_fmaf(q, t, 0.20784245431423187f);
-    q = __builtin_fmaf(q, t, 0.22566960752010345f);
-    q = __builtin_fmaf(q, t, 0.22567586600780487f);
-    e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
-    const float h = 0.5f * q * t * e;
-    return z < 0.f ? h : 1.f - h;
-}
-
-template <int ACT>
-__device__ __forceinline__ float act_of(float z)
-{
-    if constexpr (ACT == LONGCONV_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
-    if constexpr (ACT == LONGCONV_ACT_GELU) {
-        float e;
-        return z * normal_cdf(z, e);
-    }
-    if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
-    return z;
-}
-template <int ACT>
-__device__ __forceinline__ float slope_of(float z)
-{
-    if constexpr (ACT == LONGCONV_ACT_SILU) {
-        const float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
-        return q * (1.f + z * (1.f - q));
-    }
-    if constexpr (ACT == LONGCONV_ACT_GELU) {
-        float e;
-        const float c = normal_cdf(z, e);
-        return __builtin_fmaf(z * 0.39894228040143268f, e, c);
-    }
-    if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    return 1.f;
-}
-
-// (n, mean, m2) <- both sets together
-__device__ __forceinline__ void merge(float& n, float& mean, float& m2, float n2, float mean2, float m22)
-{
-    if (n2 == 0.f) return;
-    const float all = n + n2, d = mean2 - mean, f = n2 * __builtin_amdgcn_rcpf(all);
-    mean = __builtin_fmaf(d, f, mean);
-    m2 += m22 + d * d * n * f;
-    n = all;
-}
-
-// How a pass walks over a tensor: workgroup (b, part, slab) takes `slices` pieces of eight channels of `per` positions; its threads
-// are `rows` positions by `slices`.
-struct Walk {
-    uint32_t P, slices, slabs, rows, parts;
-    int64_t per;
-};
-Walk walk(int64_t B, int64_t S, int64_t C)
-{
-    Walk w;
-    w.P = (uint32_t)((C + VE - 1) / VE);
-    w.slices = w.P < SLAB ? w.P : SLAB;
-    w.slabs = (w.P + w.slices - 1) / w.slices;
-    w.rows = GT / w.slices;
-    int64_t parts = GROUPS_WANTED / (B * w.slabs);
-    const int64_t most = (S + 4 * w.rows - 1) / (4 * w.rows);      // four positions of a thread at least
-    if (parts > most) parts = most;
-    const int64_t least = (S * C >> 28) + 1;                       // of less than 2^28 elements each: byte offsets fit 31 bits
-    if (parts < least) parts = least;
-    w.per = (S + parts - 1) / parts;
-    w.parts = (uint32_t)((S + w.per - 1) / w.per);
-    return w;
-}
-// most rows (b, part) of partial results there can be: does not fall as B grows
-size_t part_rows(int64_t B, int64_t S, int64_t C)
-{
-    const Walk w = walk(1, S, C);
-    const int64_t most = (S + 4 * w.rows - 1) / (4 * w.rows), wanted = GROUPS_WANTED / w.slabs;
-    const int64_t some = B > wanted ? B : wanted, least = B + (MAX_ELEMENTS >> 28);      // (parts of 2^28 elements: so many more than B at most)
-    const int64_t rows = B * most < some ? B * most : some;
-    return (size_t)(rows > least ? rows : least);
-}
-
-// the sum over a wave, in every lane: rows of sixteen lanes by permutations within the vector registers, then the four rows
-__device__ __forceinline__ float wave_sum(float v)
-{
-    const auto moved = [](float x, auto control) {
-        return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(control)::value, 0xf, 0xf, false));
-    };
-    v += moved(v, std::integral_constant<int, 0xB1>());       // neighbours within a pair
-    v += moved(v, std::integral_constant<int, 0x4E>());       // pairs within four
-    v += moved(v, std::integral_constant<int, 0x141>());      // fours within eight, mirrored
-    v += moved(v, std::integral_constant<int, 0x140>());      // eights within sixteen, mirrored
-    const auto row = [&](int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); };
-    return (row(0) + row(16)) + (row(32) + row(48));
-}
-
-// A thread's eight channels.  The last piece of a row ends with the row: it begins `skip` channels early, which belong to the piece
-// before, so that every load is whole and inside the tensor.  (Rows of fewer than eight channels, NARROW: one piece, loaded by elements.)
-struct Piece {
-    int c, skip, wide;           // first channel; channels of another thread; channels loaded
-    bool on;
-    uint32_t off, step, end;     // bytes from a part's first element to the thread's first piece; to its next one; to the last there may be
-    template <class IO>
-    __device__ __forceinline__ void from_row(uint32_t row, uint32_t rows, uint32_t positions, int64_t C)
-    {
-        const uint32_t size = sizeof(typename IO::T), bytes = (uint32_t)C * size;
-        off = row * bytes + (uint32_t)c * size;
-        step = rows * bytes;
-        end = (positions - 1u) * bytes + (uint32_t)c * size;
-    }
-    __device__ __forceinline__ bool has(uint32_t o) const { return o <= end; }
-    // where a piece is, or the last one of the part where it lies behind that
-    template <class T>
-    __device__ __forceinline__ T* at(T* base, uint32_t o) const
-    {
-        const uint32_t in = o < end ? o : end;
-        typedef typename std::conditional<std::is_const<T>::value, const char, char>::type Byte;
-        return reinterpret_cast<T*>(reinterpret_cast<Byte*>(base) + in);
-    }
-    __device__ __forceinline__ void set(int slot, bool there, int64_t C)
-    {
-        on = there && slot * VE < C;
-        const int from = on ? slot * VE : 0, last = (int)C - VE;
-        c = last < 0 ? 0 : from < last ? from : last;
-        skip = from - c;
-        wide = C < VE ? (int)C : VE;
-    }
-    __device__ __forceinline__ bool mine(int j) const { return on && j >= skip && j < wide; }
-};
-template <class IO, bool NARROW>
-__device__ __forceinline__ void fetch(const typename IO::T* p, const Piece& q, Raw8<IO>& r)
-{
-    if constexpr (NARROW) load_raw<IO>(p, q.wide, r);
-    else r.load(p);
-}
-template <class IO>
-__device__ __forceinline__ void put(typename IO::T* p, const Piece& q, const float (&v)[VE])
-{
-    if (q.skip == 0 && q.wide == VE) {
-        store8<IO, true>(p, VE, v);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < VE; ++j)
-        if (q.mine(j)) IO::st(p, j, v[j]);
-}
-// a thread's numbers for its channels, those of others zero, at q[0 .. 7] in the order of the slots of its piece
-__device__ __forceinline__ void to_slots(float* q, const Piece& p, const float (&v)[VE])
-{
-    if (p.skip == 0 && p.on && p.wide == VE) {
-        reinterpret_cast<float4*>(q)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(q)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < VE; ++j) q[(j - p.skip) & (VE - 1)] = p.mine(j) ? v[j] : 0.f;
-}
-// eight parameters; p may be null
-__device__ __forceinline__ void load_params(const float* p, const Piece& q, float or_else, float (&v)[VE])
-{
-#pragma unroll
-    for (int j = 0; j < VE; ++j) v[j] = or_else;
-    if (p) load8<IoF32>(p + q.c, q.wide, v);
-}
-// f(j, group of channel j), one division for the eight; channels beyond the last: the last group
-template <class F>
-__device__ __forceinline__ void each_group(int c, uint32_t G, uint32_t D, F&& f)
-{
-    uint32_t g = (uint32_t)c / D, at = (uint32_t)c - g * D;
-    if (at + VE <= D) {
-#pragma unroll
-        for (int j = 0; j < VE; ++j) f(j, g);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < VE; ++j) {
-        f(j, g < G ? g : G - 1);
-        if (++at == D) { at = 0; ++g; }
-    }
-}
-
-struct Channels {      // of a thread's piece
-    float mean[VE], rstd[VE], gamma[VE], beta[VE];
-    __device__ __forceinline__ void load(const Piece& p, size_t b, const float* mn, const float* rs, const float* ga, const float* be, uint32_t G,
-                                         uint32_t D)
-    {
-        load_params(ga, p, 1.f, gamma);
-        load_params(be, p, 0.f, beta);
-        each_group(p.c, G, D, [&](int j, uint32_t g) {
-            mean[j] = mn[b * G + g];
-            rstd[j] = rs[b * G + g];
-        });
-    }
-};
-
-struct Place : Piece {
-    uint32_t b, part, slab, r;
-    int64_t from;      // the part's first position
-    size_t base;       // and its first element
-};
-template <class IO>
-__device__ __forceinline__ Place place(const Walk& w, int64_t S, int64_t C)
-{
-    Place p;
-    p.slab = blockIdx.x % w.slabs;
-    p.part = blockIdx.x / w.slabs % w.parts;
-    p.b = blockIdx.x / w.slabs / w.parts;
-    p.r = threadIdx.x / w.slices;
-    p.from = p.part * w.per;
-    p.base = ((size_t)p.b * S + p.from) * C;
-    p.set((int)(p.slab * w.slices + threadIdx.x % w.slices), p.r < w.rows, C);
-    p.template from_row<IO>(p.r, w.rows, (uint32_t)(S - p.from < w.per ? S - p.from : w.per), C);
-    return p;
-}
-
-// mean and sum of squared differences of every channel over the part's positions -> part[(b, part)][2][C]
-template <class IO, bool NARROW>
-__global__ void __launch_bounds__(GT)
-gnorm_stats_kernel(const typename IO::T* __restrict__ x, float* __restrict__ part, int64_t S, int64_t C, Walk w)
-{
-    __shared__ float sm[GT * VE], s2[GT * VE], sn[GT];
-    const Place p = place<IO>(w, S, C);
-    float mean[VE] = {}, m2[VE] = {}, n = 0.f;
-    if (p.on)
-        for (uint32_t o = p.off; p.has(o); o += AHEAD * p.step) {
-            Raw8<IO> raw[AHEAD];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, raw[u]);
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (!p.has(o + u * p.step)) break;
-                float v[VE];
-                raw[u].get(v);
-                n += 1.f;
-                const float f = __builtin_amdgcn_rcpf(n);
-#pragma unroll
-                for (int j = 0; j < VE; ++j) {
-                    const float d = v[j] - mean[j];
-                    mean[j] = __builtin_fmaf(d, f, mean[j]);
-                    m2[j] = __builtin_fmaf(d, v[j] - mean[j], m2[j]);
-                }
-            }
-        }
-    const int t = threadIdx.x;
-    to_slots(sm + t * VE, p, mean);
-    to_slots(s2 + t * VE, p, m2);
-    sn[t] = n;
-    __syncthreads();
-    const int wide = (int)w.slices * VE;
-    for (int i = t; i < wide; i += GT) {
-        const int64_t c = (int64_t)p.slab * wide + i;
-        if (c >= C) break;
-        float an = 0.f, am = 0.f, a2 = 0.f;
-        for (uint32_t r = 0; r < w.rows; ++r) {
-            const int from = (int)(r * w.slices);
-            merge(an, am, a2, sn[from + i / VE], sm[from * VE + i], s2[from * VE + i]);
-        }
-        float* q = part + ((size_t)p.b * w.parts + p.part) * 2 * C;
-        q[c] = am;
-        q[C + c] = a2;
-    }
-}
-
-// a wave for each group: its channels' and parts' results together
-__global__ void __launch_bounds__(64)
-gnorm_group_kernel(const float* __restrict__ part, float* __restrict__ mean, float* __restrict__ rstd, int64_t S, int64_t C, uint32_t G,
-                   uint32_t parts, int64_t per, float eps)
-{
-    const uint32_t b = blockIdx.x / G, g = blockIdx.x % G, D = (uint32_t)(C / G);
-    float n = 0.f, m = 0.f, m2 = 0.f;
-    for (uint64_t i = threadIdx.x; i < (uint64_t)parts * D; i += 64) {
-        const uint32_t q = (uint32_t)(i / D), c = g * D + (uint32_t)(i - (uint64_t)q * D);
-        const float* row = part + ((size_t)b * parts + q) * 2 * C;
-        const int64_t here = S - q * per < per ? S - q * per : per;
-        merge(n, m, m2, (float)here, row[c], row[C + c]);
-    }
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        // the lower lane of a pair first, on both sides: every lane ends with the same numbers
-        float n2 = __shfl_xor(n, s), a2 = __shfl_xor(m, s), b2 = __shfl_xor(m2, s);
-        if (threadIdx.x & s) {
-            float t;
-            t = n; n = n2; n2 = t;
-            t = m; m = a2; a2 = t;
-            t = m2; m2 = b2; b2 = t;
-        }
-        if (n == 0.f) { n = n2; m = a2; m2 = b2; }
-        else merge(n, m, m2, n2, a2, b2);
-    }
-    if (threadIdx.x == 0) {
-        mean[blockIdx.x] = m;
-        rstd[blockIdx.x] = 1.f / sqrtf(m2 / n + eps);
-    }
-}
-
-template <class IO, int ACT, bool NARROW>
-__global__ void __launch_bounds__(GT)
-gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restrict__ y, const float* __restrict__ mean,
-                   const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, int64_t S, int64_t C,
-                   uint32_t G, Walk w)
-{
-    const Place p = place<IO>(w, S, C);
-    if (!p.on) return;
-    Channels k;
-    k.load(p, p.b, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
-    for (uint32_t o = p.off; p.has(o); o += AHEAD * p.step) {
-        Raw8<IO> raw[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, raw[u]);
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            if (!p.has(o + u * p.step)) break;
-            float v[VE];
-            raw[u].get(v);
-#pragma unroll
-            for (int j = 0; j < VE; ++j)
-                v[j] = act_of<ACT>(__builtin_fmaf((v[j] - k.mean[j]) * k.rstd[j], k.gamma[j], k.beta[j]));
-            put<IO>(p.at(y + p.base, o + u * p.step), p, v);
-        }
-    }
-}
-
-// sums of dz and dz xhat of every channel over the part's positions -> part[(b, part)][2][C]
-template <class IO, int ACT, bool NARROW>
-__global__ void __launch_bounds__(GT)
-gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __restrict__ x, const float* __restrict__ mean,
-                  const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, float* __restrict__ part,
-                  int64_t S, int64_t C, uint32_t G, Walk w)
-{
-    __shared__ float sa[GT * VE], sb[GT * VE];
-    const Place p = place<IO>(w, S, C);
-    float a[VE] = {}, b[VE] = {};
-    if (p.on) {
-        Channels k;
-        k.load(p, p.b, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
-        for (uint32_t o = p.off; p.has(o); o += AHEAD / 2 * p.step) {
-            Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
-#pragma unroll
-            for (int u = 0; u < AHEAD / 2; ++u) {
-                fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, rx[u]);
-                fetch<IO, NARROW>(p.at(dy + p.base, o + u * p.step), p, rg[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < AHEAD / 2; ++u) {
-                if (!p.has(o + u * p.step)) break;
-                float v[VE], g[VE];
-                rx[u].get(v);
-                rg[u].get(g);
-#pragma unroll
-                for (int j = 0; j < VE; ++j) {
-                    const float h = (v[j] - k.mean[j]) * k.rstd[j];
-                    const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
-                    a[j] += dz;
-                    b[j] = __builtin_fmaf(dz, h, b[j]);
-                }
-            }
-        }
-    }
-    const int t = threadIdx.x;
-    to_slots(sa + t * VE, p, a);
-    to_slots(sb + t * VE, p, b);
-    __syncthreads();
-    const int wide = (int)w.slices * VE;
-    for (int i = t; i < wide; i += GT) {
-        const int64_t c = (int64_t)p.slab * wide + i;
-        if (c >= C) break;
-        float ta = 0.f, tb = 0.f;
-        for (uint32_t r = 0; r < w.rows; ++r) {
-            ta += sa[r * wide + i];
-            tb += sb[r * wide + i];
-        }
-        float* q = part + ((size_t)p.b * w.parts + p.part) * 2 * C;
-        q[c] = ta;
-        q[C + c] = tb;
-    }
-}
-
-constexpr int RT = 1024, RC = 16;      // threads of a workgroup that sums channels, and channels of it
-
-// workgroups 0 .. ceil(C / 16) - 1: dgamma and dbeta of sixteen channels, the rows of partial results spread over the threads; behind
-// them sixteen groups each, s1 and s2 by a wave for every group
-__global__ void __launch_bounds__(RT)
-gnorm_gather_kernel(const float* __restrict__ part, const float* __restrict__ gamma, float* __restrict__ s1, float* __restrict__ s2,
-                    float* __restrict__ dgamma, float* __restrict__ dbeta, int64_t B, int64_t C, uint32_t G, uint32_t parts)
-{
-    __shared__ float sa[RT], sh[RT];
-    const uint32_t D = (uint32_t)(C / G), blocks = (uint32_t)((C + RC - 1) / RC);
-    float a = 0.f, h = 0.f;
-    if (blockIdx.x >= blocks) {
-        const uint32_t id = (blockIdx.x - blocks) * (RT / 64) + threadIdx.x / 64;
-        if (id >= (uint32_t)B * G) return;
-        const uint32_t b = id / G, g = id % G;
-        for (uint32_t i = threadIdx.x % 64; i < parts * D; i += 64) {
-            const uint32_t q = i / D, c = g * D + (i - q * D);
-            const float* row = part + ((size_t)b * parts + q) * 2 * C;
-            const float ga = gamma ? gamma[c] : 1.f;
-            a = __builtin_fmaf(ga, row[c], a);
-            h = __builtin_fmaf(ga, row[C + c], h);
-        }
-        a = wave_sum(a);
-        h = wave_sum(h);
-        if (threadIdx.x % 64 == 0) {
-            s1[id] = a;
-            s2[id] = h;
-        }
-        return;
-    }
-    const uint32_t c = blockIdx.x * RC + threadIdx.x % RC, rows = (uint32_t)B * parts;
-    if (c < C) {
-#pragma unroll 8
-        for (uint32_t i = threadIdx.x / RC; i < rows; i += RT / RC) {
-            a += part[(size_t)i * 2 * C + c];
-            h += part[(size_t)i * 2 * C + C + c];
-        }
-    }
-    sa[threadIdx.x] = a;
-    sh[threadIdx.x] = h;
-    for (int s = RT / 2; s >= RC; s >>= 1) {
-        __syncthreads();
-        if ((int)threadIdx.x < s) {
-            sa[threadIdx.x] += sa[threadIdx.x + s];
-            sh[threadIdx.x] += sh[threadIdx.x + s];
-        }
-    }
-    if (threadIdx.x < RC && c < C) {
-        if (dbeta) dbeta[c] = sa[threadIdx.x];
-        if (dgamma) dgamma[c] = sh[threadIdx.x];
-    }
-}
-
-template <class IO, int ACT, bool NARROW>
-__global__ void __launch_bounds__(GT)
-gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __restrict__ x, const float* __restrict__ mean,
-                const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, const float* __restrict__ s1,
-                const float* __restrict__ s2, typename IO::T* __restrict__ dx, int64_t S, int64_t C, uint32_t G, float inv, Walk w)
-{
-    const Place p = place<IO>(w, S, C);
-    if (!p.on) return;
-    const uint32_t D = (uint32_t)(C / G);
-    Channels k;
-    k.load(p, p.b, mean, rstd, gamma, beta, G, D);
-    float c1[VE], c2[VE];
-    each_group(p.c, G, D, [&](int j, uint32_t g) {
-        c1[j] = s1[(size_t)p.b * G + g] * inv;
-        c2[j] = s2[(size_t)p.b * G + g] * inv;
-    });
-    for (uint32_t o = p.off; p.has(o); o += AHEAD / 2 * p.step) {
-        Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
-#pragma unroll
-        for (int u = 0; u < AHEAD / 2; ++u) {
-            fetch<IO, NARROW>(p.at(x + p.base, o + u * p.step), p, rx[u]);
-            fetch<IO, NARROW>(p.at(dy + p.base, o + u * p.step), p, rg[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD / 2; ++u) {
-            if (!p.has(o + u * p.step)) break;
-            float v[VE], g[VE];
-            rx[u].get(v);
-            rg[u].get(g);
-#pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                const float h = (v[j] - k.mean[j]) * k.rstd[j];
-                const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
-                v[j] = k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - h * c2[j]);
-            }
-            put<IO>(p.at(dx + p.base, o + u * p.step), p, v);
-        }
-    }
-}
-
-// ---- groups that fit a workgroup -------------------------------------------------------------------------------------
-// A workgroup holds a slab of whole groups of one b in registers, as it came from memory: one read, one launch.  Its threads are `rows`
-// positions by `slices` pieces; a thread has NP pieces, `rows` positions apart.
-constexpr int HT = 512, HSLAB = 128;      // threads, and pieces of a slab, at most
-
-struct Hold {
-    uint32_t P, slices, slabs, rows, np, blocks;      // blocks: rounded up to eight times a whole number; 0: does not fit
-};
-Hold hold(int64_t B, int64_t S, int64_t C, int64_t G, int bytes, uint32_t most)
-{
-    Hold h{};
-    if (C < VE) return h;
-    h.P = (uint32_t)((C + VE - 1) / VE);
-    const uint32_t D = (uint32_t)(C / G);
-    uint32_t unit = D;                                 // pieces of the smallest slab of whole groups and whole pieces
-    while (unit % VE) unit += D;
-    unit /= VE;
-    if (unit > h.P) unit = h.P;
-    // 64 bytes of a row and more, so that a line is asked for by two workgroups at most
-    uint32_t slices = unit;
-    while (slices < h.P && slices * VE * bytes < 64) slices += unit;
-    if (slices > h.P) slices = h.P;
-    while (slices > unit && (uint64_t)S * slices > (uint64_t)HT * most) slices -= slices == h.P && h.P % unit ? h.P % unit : unit;
-    if (slices > HSLAB || (uint64_t)S * slices > (uint64_t)HT * most) return h;
-    for (h.np = 1; (S + h.np - 1) / h.np * slices > HT; h.np *= 2) {}
-    if (h.np > most) return h;
-    h.slices = slices;
-    h.slabs = (h.P + slices - 1) / slices;
-    h.rows = (uint32_t)((S + h.np - 1) / h.np);
-    h.blocks = (uint32_t)(((uint64_t)B * h.slabs + 7) / 8 * 8);
-    return h;
-}
-
-struct Held : Piece {
-    uint32_t b, s, r, W;       // W: channels of the slab's pieces
-    int first;                 // the slab's first channel
-    size_t base;               // the first element of b
-    bool any;
-    __device__ __forceinline__ uint32_t piece(int u) const { return off + u * step; }
-};
-// every XCD (workgroups go round them) takes neighbouring slabs, which share lines
-template <class IO>
-__device__ __forceinline__ Held held(const Hold& h, uint32_t B, int64_t S, int64_t C)
-{
-    Held p;
-    const uint32_t id = (blockIdx.x & 7u) * (h.blocks / 8) + (blockIdx.x >> 3);
-    p.any = id < B * h.slabs;
-    p.b = id / h.slabs;
-    p.s = threadIdx.x % h.slices;
-    p.r = threadIdx.x / h.slices;
-    p.W = h.slices * VE;
-    p.first = (int)((id - p.b * h.slabs) * p.W);
-    p.base = (size_t)p.b * S * C;
-    p.set(p.first / VE + (int)p.s, p.r < h.rows, C);
-    p.template from_row<IO>(p.r, h.rows, (uint32_t)S, C);
-    return p;
-}
-
-// f(j, group of channel j counted from the slab's first); channels that belong to the slab before: 0, for nothing
-template <class F>
-__device__ __forceinline__ void in_slab(const Held& p, uint32_t G, uint32_t D, F&& f)
-{
-    const uint32_t before = (uint32_t)p.first / D;
-    each_group(p.c, G, D, [&](int j, uint32_t g) { f(j, g > before ? g - before : 0u); });
-}
-
-// v[j]: a number of the thread for its channel j.  cols[k W + c]: its sums over the rows, in K shares (the return value).
-__device__ __forceinline__ uint32_t sum_rows(const float (&v)[VE], float* all, float* cols, const Hold& h, const Held& p)
-{
-    const uint32_t T = blockDim.x;
-    __syncthreads();
-    if (p.r < h.rows) to_slots(all + p.r * p.W + p.s * VE, p, v);
-    __syncthreads();
-    uint32_t K = T / p.W;
-    if (K < 1) K = 1;
-    if (K > h.rows) K = h.rows;
-    for (uint32_t i = threadIdx.x; i < K * p.W; i += T) {
-        const uint32_t k = i / p.W;
-        float t = 0.f;
-#pragma unroll 8
-        for (uint32_t r = k; r < h.rows; r += K) t += all[r * p.W + (i - k * p.W)];
-        cols[i] = t;
-    }
-    __syncthreads();
-    return K;
-}
-// group[g] = last(the sum of weight(c) cols over a group's channels and shares); a wave each
-template <class F, class E>
-__device__ __forceinline__ void sum_groups(const float* cols, float* group, uint32_t K, uint32_t D, uint32_t W, F&& weight, E&& last)
-{
-    for (uint32_t g = threadIdx.x / 64; g * D < W; g += blockDim.x / 64) {
-        float t = 0.f;
-        for (uint32_t i = threadIdx.x % 64; i < K * D; i += 64) {
-            const uint32_t k = i / D, c = g * D + (i - k * D);
-            if (c < W) t = __builtin_fmaf(weight(c), cols[k * W + c], t);      // (a group wider than the last slab's pieces ends with the channels)
-        }
-        t = wave_sum(t);
-        if (threadIdx.x % 64 == 0) group[g] = last(t);
-    }
-    __syncthreads();
-}
-
-template <class IO, int ACT, int NP>
-__global__ void __launch_bounds__(HT)
-gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
-                      typename IO::T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, uint32_t B, int64_t S, int64_t C,
-                      uint32_t G, float n, float eps, Hold h)
-{
-    __shared__ float all[HT * VE], cols[HSLAB * VE], group[HSLAB * VE];
-    const Held p = held<IO>(h, B, S, C);
-    if (!p.any) return;
-    const uint32_t D = (uint32_t)(C / G);
-    Raw8<IO> raw[NP];
-#pragma unroll
-    for (int u = 0; u < NP; ++u) raw[u].load(p.at(x + p.base, p.piece(u)));
-    float ga[VE], be[VE];
-    load_params(gamma, p, 1.f, ga);
-    load_params(beta, p, 0.f, be);
-    const auto one = [](uint32_t) { return 1.f; };
-    float t[VE] = {}, mn[VE], rs[VE];
-#pragma unroll
-    for (int u = 0; u < NP; ++u) {
-        if (!p.has(p.piece(u))) break;
-        float v[VE];
-        raw[u].get(v);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) t[j] += v[j];
-    }
-    uint32_t K = sum_rows(t, all, cols, h, p);
-    sum_groups(cols, group, K, D, p.W, one, [&](float s) { return s / n; });
-    in_slab(p, G, D, [&](int j, uint32_t g) { mn[j] = group[g]; });
-#pragma unroll
-    for (int j = 0; j < VE; ++j) t[j] = 0.f;
-#pragma unroll
-    for (int u = 0; u < NP; ++u) {
-        if (!p.has(p.piece(u))) break;
-        float v[VE];
-        raw[u].get(v);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            const float d = v[j] - mn[j];
-            t[j] = __builtin_fmaf(d, d, t[j]);
-        }
-    }
-    K = sum_rows(t, all, cols, h, p);
-    sum_groups(cols, group, K, D, p.W, one, [&](float s) { return 1.f / sqrtf(s / n + eps); });
-    in_slab(p, G, D, [&](int j, uint32_t g) { rs[j] = group[g]; });
-    if (p.r == 0) {      // the first channel of a group writes its numbers
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            const uint32_t c = (uint32_t)(p.c + j), g = c / D;
-            if (p.mine(j) && g * D == c) {
-                mean[(size_t)p.b * G + g] = mn[j];
-                rstd[(size_t)p.b * G + g] = rs[j];
-            }
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < NP; ++u) {
-        if (!p.has(p.piece(u)) || !p.on) break;
-        float v[VE];
-        raw[u].get(v);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT>(__builtin_fmaf((v[j] - mn[j]) * rs[j], ga[j], be[j]));
-        put<IO>(p.at(y + p.base, p.piece(u)), p, v);
-    }
-}
-
-// part[b][2][C]: sums of dz and dz xhat over the positions
-template <class IO, int ACT, int NP>
-__global__ void __launch_bounds__(HT)
-gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __restrict__ x, const float* __restrict__ mean,
-                      const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta, float* __restrict__ part,
-                      typename IO::T* __restrict__ dx, uint32_t B, int64_t S, int64_t C, uint32_t G, float inv, Hold h)
-{
-    __shared__ float all[HT * VE], ca[HSLAB * VE], ch[HSLAB * VE], g1[HSLAB * VE], g2[HSLAB * VE];
-    const Held p = held<IO>(h, B, S, C);
-    if (!p.any) return;
-    const uint32_t D = (uint32_t)(C / G);
-    Raw8<IO> rx[NP], rg[NP];
-#pragma unroll
-    for (int u = 0; u < NP; ++u) {
-        rx[u].load(p.at(x + p.base, p.piece(u)));
-        rg[u].load(p.at(dy + p.base, p.piece(u)));
-    }
-    Channels k;
-    k.load(p, p.b, mean, rstd, gamma, beta, G, D);
-    float a[VE] = {}, b[VE] = {};
-#pragma unroll
-    for (int u = 0; u < NP; ++u) {
-        if (!p.has(p.piece(u))) break;
-        float v[VE], g[VE];
-        rx[u].get(v);
-        rg[u].get(g);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            const float xh = (v[j] - k.mean[j]) * k.rstd[j];
-            const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(xh, k.gamma[j], k.beta[j]));
-            a[j] += dz;
-            b[j] = __builtin_fmaf(dz, xh, b[j]);
-        }
-    }
-    const uint32_t K = sum_rows(a, all, ca, h, p);
-    sum_rows(b, all, ch, h, p);
-    for (uint32_t i = threadIdx.x; i < p.W && p.first + (int)i < C; i += blockDim.x) {
-        float ta = 0.f, tb = 0.f;
-        for (uint32_t q = 0; q < K; ++q) {
-            ta += ca[q * p.W + i];
-            tb += ch[q * p.W + i];
-        }
-        float* q = part + (size_t)p.b * 2 * C + p.first + i;
-        q[0] = ta;
-        q[C] = tb;
-    }
-    if (!dx) return;
-    const auto weight = [&](uint32_t c) { return gamma && p.first + (int)c < C ? gamma[p.first + c] : 1.f; };
-    const auto mean_of = [&](float s) { return s * inv; };
-    sum_groups(ca, g1, K, D, p.W, weight, mean_of);
-    sum_groups(ch, g2, K, D, p.W, weight, mean_of);
-    float c1[VE], c2[VE];
-    in_slab(p, G, D, [&](int j, uint32_t g) {
-        c1[j] = g1[g];
-        c2[j] = g2[g];
-    });
-#pragma unroll
-    for (int u = 0; u < NP; ++u) {
-        if (!p.has(p.piece(u)) || !p.on) break;
-        float v[VE], g[VE];
-        rx[u].get(v);
-        rg[u].get(g);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            const float xh = (v[j] - k.mean[j]) * k.rstd[j];
-            const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(xh, k.gamma[j], k.beta[j]));
-            v[j] = k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - xh * c2[j]);
-        }
-        put<IO>(p.at(dx + p.base, p.piece(u)), p, v);
-    }
-}
-
-size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
-
-template <class IO, int ACT>
-hipError_t forward(const GnormArgs& a, const void* x, void* y, float* mean, float* rstd, float eps, void* ws, hipStream_t st)
-{
-    using T = typename IO::T;
-    dim3 g, gg;
-    const Hold h = hold(a.B, a.S, a.C, a.G, sizeof(T), 64 / Raw8<IO>::W);
-    if (h.blocks) {
-        const hipError_t e = launch_grid(h.blocks, HT, &g);
-        if (e != hipSuccess) return e;
-        const auto go = [&](auto np) {
-            hipLaunchKernelGGL((gnorm_hold_fwd_kernel<IO, ACT, decltype(np)::value>), g, dim3((h.slices * h.rows + 63) / 64 * 64), 0, st, (const T*)x,
-                               a.gamma, a.beta, (T*)y, mean, rstd, (uint32_t)a.B, a.S, a.C, (uint32_t)a.G, (float)(a.S * (a.C / a.G)), eps, h);
-        };
-        if (h.np == 1) go(std::integral_constant<int, 1>());
-        else if (h.np == 2) go(std::integral_constant<int, 2>());
-        else if (h.np == 4) go(std::integral_constant<int, 4>());
-        else if (h.np == 8) go(std::integral_constant<int, 8>());
-        else if constexpr (Raw8<IO>::W == 4) go(std::integral_constant<int, 16>());
-        return hipGetLastError();
-    }
-    const Walk w = walk(a.B, a.S, a.C);
-    hipError_t e = launch_grid((uint64_t)a.B * w.parts * w.slabs, GT, &g);
-    if (e == hipSuccess) e = launch_grid((uint64_t)a.B * a.G, 64, &gg);
-    if (e != hipSuccess) return e;
-    float* part = (float*)ws;
-    if (a.C < VE) hipLaunchKernelGGL((gnorm_stats_kernel<IO, true>), g, dim3(GT), 0, st, (const T*)x, part, a.S, a.C, w);
-    else hipLaunchKernelGGL((gnorm_stats_kernel<IO, false>), g, dim3(GT), 0, st, (const T*)x, part, a.S, a.C, w);
-    hipLaunchKernelGGL(gnorm_group_kernel, gg, dim3(64), 0, st, (const float*)part, mean, rstd, a.S, a.C, (uint32_t)a.G, w.parts, w.per, eps);
-    const auto apply = [&](auto narrow) {
-        hipLaunchKernelGGL((gnorm_apply_kernel<IO, ACT, decltype(narrow)::value>), g, dim3(GT), 0, st, (const T*)x, (T*)y, (const float*)mean,
-                           (const float*)rstd, a.gamma, a.beta, a.S, a.C, (uint32_t)a.G, w);
-    };
-    if (a.C < VE) apply(std::true_type());
-    else apply(std::false_type());
-    return hipGetLastError();
-}
-
-template <class IO, int ACT>
-hipError_t backward(const GnormArgs& a, const void* dy, const void* x, const float* mean, const float* rstd, void* dx, float* dgamma,
-                    float* dbeta, void* ws, hipStream_t st)
-{
-    using T = typename IO::T;
-    dim3 g, gg;
-    const float inv = (float)(1.0 / ((double)a.S * (a.C / a.G)));
-    const Hold h = hold(a.B, a.S, a.C, a.G, sizeof(T), 32 / Raw8<IO>::W);
-    if (h.blocks) {
-        const hipError_t e = launch_grid(h.blocks, HT, &g);
-        if (e != hipSuccess) return e;
-        const auto go = [&](auto np) {
-            hipLaunchKernelGGL((gnorm_hold_bwd_kernel<IO, ACT, decltype(np)::value>), g, dim3((h.slices * h.rows + 63) / 64 * 64), 0, st,
-                               (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta, (float*)ws, (T*)dx, (uint32_t)a.B, a.S, a.C, (uint32_t)a.G,
-                               inv, h);
-        };
-        if (h.np == 1) go(std::integral_constant<int, 1>());
-        else if (h.np == 2) go(std::integral_constant<int, 2>());
-        else if (h.np == 4) go(std::integral_constant<int, 4>());
-        else if constexpr (Raw8<IO>::W == 4) go(std::integral_constant<int, 8>());
-        if (dgamma || dbeta)
-            hipLaunchKernelGGL(gnorm_gather_kernel, dim3((unsigned)((a.C + RC - 1) / RC)), dim3(RT), 0, st, (const float*)ws, a.gamma, (float*)nullptr,
-                               (float*)nullptr, dgamma, dbeta, a.B, a.C, (uint32_t)a.G, 1u);
-        return hipGetLastError();
-    }
-    const Walk w = walk(a.B, a.S, a.C);
-    hipError_t e = launch_grid((uint64_t)a.B * w.parts * w.slabs, GT, &g);
-    if (e == hipSuccess) e = launch_grid((uint64_t)(a.C + RC - 1) / RC + ((uint64_t)a.B * a.G + RT / 64 - 1) / (RT / 64), RT, &gg);
-    if (e != hipSuccess) return e;
-    float* part = (float*)ws;
-    float* s1 = (float*)((char*)ws + up256(part_rows(a.B, a.S, a.C) * 2 * a.C * sizeof(float)));
-    float* s2 = s1 + a.B * a.G;
-    const auto go = [&](auto narrow) {
-        constexpr bool N = decltype(narrow)::value;
-        hipLaunchKernelGGL((gnorm_sums_kernel<IO, ACT, N>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta, part, a.S,
-                           a.C, (uint32_t)a.G, w);
-        hipLaunchKernelGGL(gnorm_gather_kernel, gg, dim3(RT), 0, st, (const float*)part, a.gamma, s1, s2, dgamma, dbeta, a.B, a.C, (uint32_t)a.G,
-                           w.parts);
-        if (dx)
-            hipLaunchKernelGGL((gnorm_dx_kernel<IO, ACT, N>), g, dim3(GT), 0, st, (const T*)dy, (const T*)x, mean, rstd, a.gamma, a.beta,
-                               (const float*)s1, (const float*)s2, (T*)dx, a.S, a.C, (uint32_t)a.G, inv, w);
-    };
-    if (a.C < VE) go(std::true_type());
-    else go(std::false_type());
-    return hipGetLastError();
-}
-
-template <class IO, class F>
-hipError_t by_act(int act, F&& f)
-{
-    switch (act) {
-        case LONGCONV_ACT_SILU: return f(std::integral_constant<int, LONGCONV_ACT_SILU>());
-        case LONGCONV_ACT_GELU: return f(std::integral_constant<int, LONGCONV_ACT_GELU>());
-        case LONGCONV_ACT_RELU: return f(std::integral_constant<int, LONGCONV_ACT_RELU>());
-        default: return f(std::integral_constant<int, LONGCONV_ACT_NONE>());
-    }
-}
-
-}  // namespace
+extern template hipError_t gnorm_fwd_io<IoF16>(const GnormArgs&, const void*, void*, float*, float*, float, void*, hipStream_t);
+extern template hipError_t gnorm_fwd_io<IoBF16>(const GnormArgs&, const void*, void*, float*, float*, float, void*, hipStream_t);
+extern template hipError_t gnorm_bwd_io<IoF16>(const GnormArgs&, const void*, const void*, const float*, const float*, void*, float*, float*, void*,
+                                               hipStream_t);
+extern template hipError_t gnorm_bwd_io<IoBF16>(const GnormArgs&, const void*, const void*, const float*, const float*, void*, float*, float*, void*,
+                                                hipStream_t);
 
 size_t gnorm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t G, int io, int backward)
 {
@@ -840,22 +18,17 @@ size_t gnorm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t G, int io,
 
 hipError_t gnorm_fwd(const GnormArgs& a, const void* x, void* y, float* mean, float* rstd, float eps, void* ws, hipStream_t st)
 {
-    const auto run = [&](auto io) {
-        using IO = decltype(io);
-        return by_act<IO>(a.act, [&](auto act) { return forward<IO, decltype(act)::value>(a, x, y, mean, rstd, eps, ws, st); });
-    };
-    return a.io == LONGCONV_F32 ? run(IoF32()) : a.io == LONGCONV_F16 ? run(IoF16()) : run(IoBF16());
+    if (a.io == LONGCONV_F32) return gnorm_fwd_io<IoF32>(a, x, y, mean, rstd, eps, ws, st);
+    return a.io == LONGCONV_F16 ? gnorm_fwd_io<IoF16>(a, x, y, mean, rstd, eps, ws, st)
+                                : gnorm_fwd_io<IoBF16>(a, x, y, mean, rstd, eps, ws, st);
 }
 
 hipError_t gnorm_bwd(const GnormArgs& a, const void* dy, const void* x, const float* mean, const float* rstd, void* dx, float* dgamma,
                      float* dbeta, void* ws, hipStream_t st)
 {
-    const auto run = [&](auto io) {
-        using IO = decltype(io);
-        return by_act<IO>(a.act,
-                          [&](auto act) { return backward<IO, decltype(act)::value>(a, dy, x, mean, rstd, dx, dgamma, dbeta, ws, st); });
-    };
-    return a.io == LONGCONV_F32 ? run(IoF32()) : a.io == LONGCONV_F16 ? run(IoF16()) : run(IoBF16());
+    if (a.io == LONGCONV_F32) return gnorm_bwd_io<IoF32>(a, dy, x, mean, rstd, dx, dgamma, dbeta, ws, st);
+    return a.io == LONGCONV_F16 ? gnorm_bwd_io<IoF16>(a, dy, x, mean, rstd, dx, dgamma, dbeta, ws, st)
+                                : gnorm_bwd_io<IoBF16>(a, dy, x, mean, rstd, dx, dgamma, dbeta, ws, st);
 }
 
 }  // namespace lc
