@@ -740,11 +740,12 @@ hipError_t embed_fwd(const EmbedArgs& a, const void* E, int table, void* y, hipS
 
 size_t embed_workspace_bytes(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
 {
-    return lay_out(B, N, V, H, io, layout).total;
+    return embed_is_small(N, V, io, layout) ? embed_small_workspace_bytes(B, N, H) : lay_out(B, N, V, H, io, layout).total;
 }
 
 hipError_t embed_bwd(const EmbedArgs& a, const void* dy, float* dE, void* ws, hipStream_t st)
 {
+    if (embed_is_small(a.N, a.V, a.io, a.layout)) return embed_small_bwd(a, dy, dE, ws, st);
     if (a.io == LONGCONV_F32) return backward<IoF32>(a, dy, dE, (char*)ws, st);
     return a.io == LONGCONV_F16 ? backward<IoF16>(a, dy, dE, (char*)ws, st) : backward<IoBF16>(a, dy, dE, (char*)ws, st);
 }

@@ -1,0 +1,252 @@
+// Gradient of an embedding whose table has at most 256 rows (bytes), 16-bit rows in the convolution's layout [B,H,N]: a product with
+// the tokens' one-hot matrix on the matrix cores,
+//     dE[v,h] = f . sum over (b,t) of dy[b,h,t] [ids[b,t] = v],
+// where dy's rows are the left operand as they lie in memory and the right one is made in registers from the tokens.  Its entries are 0
+// and 1, so the products are exact and the sums those of fp32; dy is read once, nothing is sorted and nothing transposed.  A wave keeps 32 channels by
+// 256 tokens of dE (128 accumulators, two waves a SIMD), its workgroup's four waves share out a range of 32-place steps, and the
+// ranges' sums are added in order by a second kernel.
+// What is not finite would reach every token of its channel (0 times infinity): a wave that finds such a sum takes its range's places
+// one by one instead, so that it stays with its token.
+#include "vec8.hpp"
+
+namespace lc {
+namespace {
+
+constexpr int VT = 16, MT = 2, CH = 16 * MT, WAVES = 4, PAD = 4;      // tiles of 16 tokens; tiles of 16 channels; channels of a workgroup; its waves
+constexpr int ROOM = SMALL_TABLE * (CH + PAD);                        // LDS floats of a workgroup's sums, [token][channel]
+constexpr int PIECES = 512;                                           // workgroups wanted: two on each of 256 compute units
+
+struct Steps {
+    uint32_t of_row, all, each, ranges, blocks;      // steps of a sequence; of all; of a range; ranges; blocks of 32 channels
+    uint32_t most;                                   // ranges there may be: does not fall as B grows
+};
+Steps steps(int64_t B, int64_t N, int64_t H)
+{
+    Steps s;
+    s.of_row = (uint32_t)((N + 31) / 32);
+    s.all = (uint32_t)B * s.of_row;
+    s.blocks = (uint32_t)((H + CH - 1) / CH);
+    const uint32_t wanted = PIECES / s.blocks > 1 ? PIECES / s.blocks : 1, worth = (s.all + 4 * WAVES - 1) / (4 * WAVES);      // four steps of a wave at least
+    s.most = worth < wanted ? worth : wanted;
+    s.each = (s.all + s.most - 1) / s.most;
+    s.ranges = (s.all + s.each - 1) / s.each;
+    return s;
+}
+__host__ __device__ inline size_t range_floats(const Steps& s) { return (size_t)SMALL_TABLE * s.blocks * CH; }
+
+typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+union Frag {
+    uint32_t w[4];
+    mu::h8 h;
+    b8 b;
+};
+template <class IO>
+__device__ __forceinline__ mu::f4 product(const Frag& a, const Frag& b, mu::f4 c)
+{
+    if constexpr (mu::IsBf<IO>::v) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, b.h, c, 0, 0, 0);
+}
+
+// A lane's eight places of a step: 8 (lane / 16) .. + 7, or, at a sequence's end, its last eight, those of other lanes left out.
+struct Places {
+    uint32_t b, t;       // sequence, first place loaded
+    uint32_t valid;      // bit j: place t + j is the lane's
+    __device__ __forceinline__ void set(uint32_t step, const Steps& s, uint32_t N, int group)
+    {
+        b = step / s.of_row;
+        const uint32_t want = (step - b * s.of_row) * 32 + (uint32_t)group * VE;
+        t = want < N - VE ? want : N - VE;
+        valid = want < N ? 0xffu & (0xffu << (want - t)) : 0u;
+    }
+};
+template <class ID>
+struct Ids {
+    typedef ID two __attribute__((ext_vector_type(16 / sizeof(ID)), aligned(sizeof(ID))));
+    static constexpr int PER = 16 / sizeof(ID);
+    two v[VE / PER];
+    __device__ __forceinline__ void load(const ID* p)
+    {
+#pragma unroll
+        for (int i = 0; i < VE / PER; ++i) v[i] = reinterpret_cast<const two*>(p)[i];
+    }
+    __device__ __forceinline__ ID operator[](int j) const { return v[j / PER][j % PER]; }
+};
+// bits 2 i, 2 i + 1 as masks of a word's halves
+__device__ __forceinline__ uint32_t half_masks(uint32_t bits, int i)
+{
+    return (bits >> (2 * i) & 1u ? 0xffffu : 0u) | (bits >> (2 * i + 1) & 1u ? 0xffff0000u : 0u);
+}
+
+template <class IO, class ID, bool DROP>
+__global__ void __launch_bounds__(64 * WAVES, 2)
+embed_small_kernel(const typename IO::T* __restrict__ dy, const ID* __restrict__ ids, float* __restrict__ part, uint32_t N, uint32_t H, uint32_t V,
+                   Steps s, Drop d)
+{
+    __shared__ float sums[ROOM];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, group = lane >> 4;
+    const uint32_t block = blockIdx.x % s.blocks, range = blockIdx.x / s.blocks, h0 = block * CH;
+    const uint32_t begin = range * s.each, stop = begin + s.each < s.all ? begin + s.each : s.all, each = (stop - begin + WAVES - 1) / WAVES;
+    const uint32_t from = begin + wave * each < stop ? begin + wave * each : stop, to = from + each < stop ? from + each : stop;
+    const uint64_t call = DROP ? call_of(d) : 0;
+    uint32_t h[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) h[m] = h0 + 16 * m + n < H ? h0 + 16 * m + n : H - 1;      // (channels there are not: nobody takes their sums)
+    mu::f4 acc[MT][VT] = {};
+    const uint32_t me = (uint32_t)n * 0x10001u, one = mu::IsBf<IO>::v ? 0x3f80u : 0x3c00u;
+    Places next;
+    Ids<ID> id;
+    Raw8<IO> raw[MT];
+    const auto ask = [&](uint32_t step) {
+        next.set(step, s, N, group);
+        id.load(ids + (size_t)next.b * N + next.t);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) raw[m].load(dy + ((size_t)next.b * H + h[m]) * N + next.t);
+    };
+    if (from < to) ask(from);
+    for (uint32_t step = from; step < to; ++step) {
+        const Places at = next;
+        Frag a[MT];
+        uint32_t x[4], valid = at.valid;
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+            if (!(id[j] >= 0 && id[j] < (ID)V)) valid &= ~(1u << j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // (what counts for nothing names no token: 256 and more)
+            const uint32_t lo = valid >> (2 * i) & 1u ? (uint32_t)id[2 * i] : 0x7fffu, hi = valid >> (2 * i + 1) & 1u ? (uint32_t)id[2 * i + 1] : 0x7fffu;
+            x[i] = (lo | hi << 16) ^ me;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const uint32_t bits = DROP ? valid & kept8_at(((size_t)at.b * H + h[m]) * N + at.t, d, call) : valid;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[m].w[i] = raw[m].w[i] & half_masks(bits, i);
+        }
+        if (step + 1 < to) ask(step + 1);
+#pragma unroll
+        for (int j = 0; j < VT; ++j) {
+            Frag b;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const us2 differ = __builtin_bit_cast(us2, x[i] ^ (uint32_t)j * 0x100010u), unit = {1, 1}, as = {(uint16_t)one, (uint16_t)one};
+                b.w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(unit, differ) * as);
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[m][j] = product<IO>(a[m], b, acc[m][j]);
+        }
+    }
+    float zero = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < VT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(acc[m][j][r], 0.f, zero);
+    const bool clean = __ballot(!(zero == 0.f)) == 0;
+    for (int w = 0; w < WAVES; ++w) {      // (every wave comes here as often)
+        if (w == wave) {
+            if (clean) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int j = 0; j < VT; ++j) {
+                        float4* q = reinterpret_cast<float4*>(sums + (16 * j + n) * (CH + PAD) + 16 * m + 4 * group);
+                        float4 t = make_float4(acc[m][j][0], acc[m][j][1], acc[m][j][2], acc[m][j][3]);
+                        if (w) {
+                            const float4 o = *q;
+                            t = make_float4(o.x + t.x, o.y + t.y, o.z + t.z, o.w + t.w);
+                        }
+                        *q = t;
+                    }
+            } else {
+                if (w == 0)
+                    for (int i = lane; i < ROOM; i += 64) sums[i] = 0.f;
+                __threadfence_block();
+                for (uint32_t step = from; step < to; ++step) {
+                    const uint32_t b = step / s.of_row, t0 = (step - b * s.of_row) * 32;
+                    for (uint32_t t = t0; t < t0 + 32 && t < N; ++t) {
+                        const ID v = ids[(size_t)b * N + t];
+                        if (!(v >= 0 && v < (ID)V) || lane >= CH || h0 + lane >= H) continue;
+                        const size_t e = ((size_t)b * H + h0 + lane) * N + t;
+                        if (!DROP || (kept8(e >> 3, d, call) >> (e & 7u) & 1u)) sums[(uint32_t)v * (CH + PAD) + lane] += IO::ld(dy, e);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+    float* out = part + range * range_floats(s);
+    for (uint32_t i = threadIdx.x; i < V * (CH / 4); i += 64 * WAVES) {
+        const uint32_t v = i / (CH / 4), c = i % (CH / 4) * 4;
+        *reinterpret_cast<float4*>(out + (size_t)v * s.blocks * CH + h0 + c) = *reinterpret_cast<const float4*>(sums + v * (CH + PAD) + c);
+    }
+}
+
+constexpr int SUM_T = 256, SHARES = 4;
+
+// dE = f times the ranges' sums, four shares of the ranges side by side and then in order
+__global__ void __launch_bounds__(SUM_T)
+embed_small_sum_kernel(const float* __restrict__ part, float* __restrict__ dE, uint32_t H, uint32_t V, float f, Steps s)
+{
+    __shared__ float4 sums[SHARES][64];
+    const uint32_t share = threadIdx.x / 64, lane = threadIdx.x % 64, wide = s.blocks * CH / 4, i = blockIdx.x * 64 + lane;
+    const uint32_t each = (s.ranges + SHARES - 1) / SHARES, from = share * each, to = from + each < s.ranges ? from + each : s.ranges;
+    const size_t stride = (size_t)SMALL_TABLE * wide;
+    const bool there = i < V * wide;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (there) {
+        const float4* p = reinterpret_cast<const float4*>(part) + i;
+#pragma unroll 8
+        for (uint32_t r = from; r < to; ++r) {
+            const float4 v = p[r * stride];
+            t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+        }
+    }
+    sums[share][lane] = t;
+    __syncthreads();
+    if (share || !there) return;
+#pragma unroll
+    for (int w = 1; w < SHARES; ++w) {
+        const float4 v = sums[w][lane];
+        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    }
+    const float o[4] = {t.x * f, t.y * f, t.z * f, t.w * f};
+    const uint32_t v = i / wide, c = (i - v * wide) * 4;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+        if (c + j < H) dE[(size_t)v * H + c + j] = o[j];
+}
+
+template <class IO, class ID>
+hipError_t run(const EmbedArgs& a, const void* dy, float* dE, float* part, hipStream_t st)
+{
+    const Steps s = steps(a.B, a.N, a.H);
+    dim3 g, gs;
+    hipError_t e = launch_grid((uint64_t)s.ranges * s.blocks, 64 * WAVES, &g);
+    if (e == hipSuccess) e = launch_grid(((uint64_t)a.V * s.blocks * (CH / 4) + 63) / 64, SUM_T, &gs);
+    if (e != hipSuccess) return e;
+    const auto kernel = a.drop.threshold ? embed_small_kernel<IO, ID, true> : embed_small_kernel<IO, ID, false>;
+    hipLaunchKernelGGL(kernel, g, dim3(64 * WAVES), 0, st, (const typename IO::T*)dy, (const ID*)a.ids, part, (uint32_t)a.N, (uint32_t)a.H,
+                       (uint32_t)a.V, s, a.drop);
+    hipLaunchKernelGGL(embed_small_sum_kernel, gs, dim3(SUM_T), 0, st, (const float*)part, dE, (uint32_t)a.H, (uint32_t)a.V, a.scale * a.drop.scale, s);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t embed_small_workspace_bytes(int64_t B, int64_t N, int64_t H)
+{
+    const Steps s = steps(B, N, H);
+    return s.most * range_floats(s) * sizeof(float);
+}
+
+hipError_t embed_small_bwd(const EmbedArgs& a, const void* dy, float* dE, void* ws, hipStream_t st)
+{
+    float* part = (float*)ws;
+    if (a.io == LONGCONV_F16)
+        return a.id_bytes == 8 ? run<IoF16, int64_t>(a, dy, dE, part, st) : run<IoF16, int32_t>(a, dy, dE, part, st);
+    return a.id_bytes == 8 ? run<IoBF16, int64_t>(a, dy, dE, part, st) : run<IoBF16, int32_t>(a, dy, dE, part, st);
+}
+
+}  // namespace lc

@@ -43,6 +43,14 @@ struct EmbedArgs {
 hipError_t embed_fwd(const EmbedArgs& a, const void* E, int table, void* y, hipStream_t st);
 size_t embed_workspace_bytes(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout);
 hipError_t embed_bwd(const EmbedArgs& a, const void* dy, float* dE, void* ws, hipStream_t st);
+// the gradient of a table of few rows on the matrix cores (embed_small.hip)
+constexpr int SMALL_TABLE = 256;
+inline bool embed_is_small(int64_t N, int64_t V, int io, int layout)
+{
+    return V <= SMALL_TABLE && N >= 8 && io != LONGCONV_F32 && layout == LONGCONV_CHANNELS_FIRST;
+}
+size_t embed_small_workspace_bytes(int64_t B, int64_t N, int64_t H);
+hipError_t embed_small_bwd(const EmbedArgs& a, const void* dy, float* dE, void* ws, hipStream_t st);
 
 struct GnormArgs {
     const float *gamma, *beta;      // may be null: ones, zeros

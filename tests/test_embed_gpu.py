@@ -133,6 +133,38 @@ def test_a_gradient_that_is_not_finite_stays_with_its_token():
     assert torch.equal(torch.nan_to_num(dE.cpu(), 99.0), torch.nan_to_num(want, 99.0))
 
 
+@pytest.mark.parametrize("io", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_columns_that_are_not_finite_stay_with_their_tokens(io, p):
+    # what is not finite at a place without a token, or dropped, reaches nothing; elsewhere its own token and channel
+    B, N, V, H = 2, 700, 90, 40
+    ids = _ids(B, N, V, "heavy", 3)
+    dy = _randn((B, H, N), DT[io], 4)
+    m = dropout.mask((B, H, N), p, 5, 6)
+    gone = (ids < 0) | (ids >= V)
+    dy.masked_fill_(gone[:, None, :], float("nan"))
+    dy.masked_fill_(torch.from_numpy(m).cuda() == 0, float("inf"))
+    kept = np.argwhere((m[1, 7] != 0) & ~gone[1].cpu().numpy())[:, 0]
+    dy[1, 7, int(kept[11])] = float("inf")
+    dy[1, 7, int(kept[30])] = float("nan")
+    dE = torch.full((V, H), 3.0, device="cuda")
+    ws = lc.new_workspace_embed(B, N, V, H, lc.dtype_code(dy), lc.CHANNELS_FIRST)
+    lc.longconv_embed_bwd(dy, ids, dE, 1.0, lc.CHANNELS_FIRST, ws, p, 5, 6)
+    ids64 = _np(ids).astype(np.int64)
+    clean = np.nan_to_num(_np(dy), nan=0.0, posinf=0.0)
+    want, size = (embed.embed_bwd(a, ids64, V, 1.0, True, m) for a in (clean, np.abs(clean)))
+    bad = {int(ids64[1, int(kept[i])]) for i in (11, 30)}
+    got = _np(dE)
+    for v in range(V):
+        for h in range(H):
+            if v in bad and h == 7:
+                assert not np.isfinite(got[v, h])
+    ok = np.ones((V, H), bool)
+    ok[list(bad), 7] = False
+    most = np.bincount(ids64[(ids64 >= 0) & (ids64 < V)], minlength=V).max()
+    assert (np.abs(got - want)[ok] <= ((most + 3) * U * size)[ok]).all()
+
+
 @pytest.mark.parametrize("first", [False, True])
 def test_offsets_past_32_bits(first):
     B, N, V, H = 3, 1 << 20, 8, 1030                                   # 3.2e9 elements
