@@ -34,18 +34,36 @@ dropout_kernel(const typename IO::T* x, const typename IO::T* r, typename IO::T*
     if (e >= n) return;
     const int here = n - e < (I)VE ? (int)(n - e) : VE;
     const uint64_t call = call_of(d);
+    Raw8<IO> rx, rr;
+    rr.zero();
+    if (here == VE) {
+        rx.load(x + e);
+        if (r) rr.load(r + e);
+    } else {
+        load_raw<IO>(x + e, here, rx);
+        if (r) load_raw<IO>(r + e, here, rr);
+    }
+    uint4 m;
+    if constexpr (TIED) {
+        const uint32_t bits = kept8_tied<I>(e, tie, d, call);
+        const auto word = [&](int i) { return (bits >> (2 * i) & 1u ? 0xffffu : 0u) | (bits >> (2 * i + 1) & 1u ? 0xffff0000u : 0u); };
+        m = make_uint4(word(0), word(1), word(2), word(3));
+    } else m = kept_words(e >> 3, d, call);
+    const uint32_t mask[4] = {m.x, m.y, m.z, m.w};
+    // (a dropped entry counts for nothing, whatever it holds: its bits become those of zero)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (Raw8<IO>::W == 4) rx.w[i] &= mask[i];
+        else {
+            rx.w[2 * i] &= (uint32_t)((int32_t)(mask[i] << 16) >> 16);
+            rx.w[2 * i + 1] &= (uint32_t)((int32_t)mask[i] >> 16);
+        }
+    }
     float v[VE], s[VE];
-    load8<IO>(x + e, here, v);
-    if (r) load8<IO>(r + e, here, s);
-    else
+    rx.get(v);
+    rr.get(s);
 #pragma unroll
-        for (int i = 0; i < VE; ++i) s[i] = 0.f;
-    uint32_t m;
-    if constexpr (TIED) m = kept8_tied<I>(e, tie, d, call);
-    else m = kept8(e >> 3, d, call);
-    // (a dropped entry counts for nothing, whatever it holds)
-#pragma unroll
-    for (int i = 0; i < VE; ++i) v[i] = m >> i & 1u ? __builtin_fmaf(v[i], d.scale, s[i]) : s[i];
+    for (int i = 0; i < VE; ++i) v[i] = __builtin_fmaf(v[i], d.scale, s[i]);
     store8<IO, true>(y + e, here, v);
 }
 

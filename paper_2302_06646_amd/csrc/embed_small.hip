@@ -2,7 +2,9 @@
 // the tokens' one-hot matrix on the matrix cores,
 //     dE[v,h] = f . sum over (b,t) of dy[b,h,t] [ids[b,t] = v],
 // where dy's rows are the left operand as they lie in memory and the right one is made in registers from the tokens.  Its entries are 0
-// and 1, so the products are exact and the sums those of fp32; dy is read once, nothing is sorted and nothing transposed.  A wave keeps 32 channels by
+// and 2 (taken back with f), so the products are exact and the sums those of fp32; dy is read once, nothing is sorted and nothing
+// transposed.  For a tile of tokens 16 j .. 16 j + 15 a lane needs [token = 16 j + lane mod 16] at eight places: a word of two halves that
+// are 0x4000 (2.0 in both types) where the low four bits agree, once for all tiles, and a bit of the set of high four bits, moved under it.  A wave keeps 32 channels by
 // 256 tokens of dE (128 accumulators, two waves a SIMD), its workgroup's four waves share out a range of 32-place steps, and the
 // ranges' sums are added in order by a second kernel.
 // What is not finite would reach every token of its channel (0 times infinity): a wave that finds such a sum takes its range's places
@@ -14,6 +16,7 @@ namespace {
 
 constexpr int VT = 16, MT = 2, CH = 16 * MT, WAVES = 4, PAD = 4;      // tiles of 16 tokens; tiles of 16 channels; channels of a workgroup; its waves
 constexpr int ROOM = SMALL_TABLE * (CH + PAD);                        // LDS floats of a workgroup's sums, [token][channel]
+constexpr int AHEAD = 2;                                              // steps whose rows are asked for ahead
 constexpr int PIECES = 512;                                           // workgroups wanted: two on each of 256 compute units
 
 struct Steps {
@@ -48,18 +51,25 @@ __device__ __forceinline__ mu::f4 product(const Frag& a, const Frag& b, mu::f4 c
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, b.h, c, 0, 0, 0);
 }
 
-// A lane's eight places of a step: 8 (lane / 16) .. + 7, or, at a sequence's end, its last eight, those of other lanes left out.
-struct Places {
-    uint32_t b, t;       // sequence, first place loaded
-    uint32_t valid;      // bit j: place t + j is the lane's
-    __device__ __forceinline__ void set(uint32_t step, const Steps& s, uint32_t N, int group)
+// A lane's eight places of a step are 8 (lane / 16) .. + 7 of it, or, at a sequence's end, the last eight, those of other lanes left
+// out.  `element`: of the row's first place of the step and the lane's group, moved on by whole steps.
+struct Cursor {
+    uint32_t t;            // the step's first place
+    int64_t element;
+    __device__ __forceinline__ void next(uint32_t N, int64_t wrap)      // wrap: from behind a row's steps to the next row's first
     {
-        b = step / s.of_row;
-        const uint32_t want = (step - b * s.of_row) * 32 + (uint32_t)group * VE;
-        t = want < N - VE ? want : N - VE;
-        valid = want < N ? 0xffu & (0xffu << (want - t)) : 0u;
+        t += 32;
+        element += 32;
+        if (t >= N) { t = 0; element += wrap; }
+    }
+    // how far the lane's eight places lie before those of its group (0 but at a sequence's end)
+    __device__ __forceinline__ uint32_t early(uint32_t N, uint32_t in_step) const
+    {
+        const uint32_t want = t + in_step, last = N - VE;
+        return want > last ? want - last : 0u;
     }
 };
+
 template <class ID>
 struct Ids {
     typedef ID two __attribute__((ext_vector_type(16 / sizeof(ID)), aligned(sizeof(ID))));
@@ -77,6 +87,20 @@ __device__ __forceinline__ uint32_t half_masks(uint32_t bits, int i)
 {
     return (bits >> (2 * i) & 1u ? 0xffffu : 0u) | (bits >> (2 * i + 1) & 1u ? 0xffff0000u : 0u);
 }
+// two tokens in the halves of a word, any that is not in 0 .. 65535 as 65535
+__device__ __forceinline__ uint32_t both(int32_t a, int32_t b)
+{
+    const uint32_t lo = (uint32_t)a < 0xffffu ? (uint32_t)a : 0xffffu, hi = (uint32_t)b < 0xffffu ? (uint32_t)b : 0xffffu;
+    return lo | hi << 16;
+}
+__device__ __forceinline__ uint32_t both(int64_t a, int64_t b)
+{
+    const auto low = [](int64_t v) {      // the upper half not zero: 2^31 and more
+        const uint32_t up = (uint32_t)((uint64_t)v >> 32);
+        return (int32_t)((uint32_t)v | (up < 1u ? up : 1u) << 31);
+    };
+    return both(low(a), low(b));
+}
 
 template <class IO, class ID, bool DROP>
 __global__ void __launch_bounds__(64 * WAVES, 2)
@@ -84,7 +108,7 @@ embed_small_kernel(const typename IO::T* __restrict__ dy, const ID* __restrict__
                    Steps s, Drop d)
 {
     __shared__ float sums[ROOM];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, group = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, group = lane >> 4;
     const uint32_t block = blockIdx.x % s.blocks, range = blockIdx.x / s.blocks, h0 = block * CH;
     const uint32_t begin = range * s.each, stop = begin + s.each < s.all ? begin + s.each : s.all, each = (stop - begin + WAVES - 1) / WAVES;
     const uint32_t from = begin + wave * each < stop ? begin + wave * each : stop, to = from + each < stop ? from + each : stop;
@@ -93,48 +117,82 @@ embed_small_kernel(const typename IO::T* __restrict__ dy, const ID* __restrict__
 #pragma unroll
     for (int m = 0; m < MT; ++m) h[m] = h0 + 16 * m + n < H ? h0 + 16 * m + n : H - 1;      // (channels there are not: nobody takes their sums)
     mu::f4 acc[MT][VT] = {};
-    const uint32_t me = (uint32_t)n * 0x10001u, one = mu::IsBf<IO>::v ? 0x3f80u : 0x3c00u;
-    Places next;
+    const uint32_t me = (uint32_t)n * 0x10001u;
+    const us2 unit = {1, 1}, two = {0x4000, 0x4000}, top = {(uint16_t)(V - 1), (uint16_t)(V - 1)};
+    const uint32_t row0 = from / s.of_row, in_step = (uint32_t)group * VE;
+    const int64_t past = (int64_t)s.of_row * 32;
+    // of the next step's tokens; of the rows asked for AHEAD steps before their use; of the step worked on
+    Cursor tokens{(from - row0 * s.of_row) * 32, 0};
+    tokens.element = (int64_t)row0 * N + tokens.t + in_step;
+    Cursor rows = tokens, now = tokens;
+    rows.element = now.element = ((int64_t)row0 * H + h[0]) * N + tokens.t + in_step;
+    const int64_t wrap = (int64_t)H * N - past;
+    int64_t apart[MT];      // from the first tile's row to the others'
+#pragma unroll
+    for (int m = 0; m < MT; ++m) apart[m] = (int64_t)(h[m] - h[0]) * N;
     Ids<ID> id;
-    Raw8<IO> raw[MT];
-    const auto ask = [&](uint32_t step) {
-        next.set(step, s, N, group);
-        id.load(ids + (size_t)next.b * N + next.t);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) raw[m].load(dy + ((size_t)next.b * H + h[m]) * N + next.t);
+    Raw8<IO> raw[AHEAD][MT];
+    const auto ask_tokens = [&] {
+        id.load(ids + tokens.element - tokens.early(N, in_step));
+        tokens.next(N, (int64_t)N - past);
     };
-    if (from < to) ask(from);
-    for (uint32_t step = from; step < to; ++step) {
-        const Places at = next;
-        Frag a[MT];
-        uint32_t x[4], valid = at.valid;
+    const auto ask_rows = [&](Raw8<IO>(&to_raw)[MT]) {
+        const typename IO::T* p = dy + rows.element - rows.early(N, in_step);
 #pragma unroll
-        for (int j = 0; j < VE; ++j)
-            if (!(id[j] >= 0 && id[j] < (ID)V)) valid &= ~(1u << j);
+        for (int m = 0; m < MT; ++m) to_raw[m].load(p + apart[m]);
+        rows.next(N, wrap);
+    };
+    if (from < to) ask_tokens();
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (from + u < to) ask_rows(raw[u]);
+    const auto work = [&](uint32_t step, Raw8<IO>(&mine)[MT]) {
+        const uint32_t early = now.early(N, in_step);
+        const int64_t element = now.element - early;
+        now.next(N, wrap);
+        Frag a[MT];
+        uint32_t low[4], high[4], there[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            // (what counts for nothing names no token: 256 and more)
-            const uint32_t lo = valid >> (2 * i) & 1u ? (uint32_t)id[2 * i] : 0x7fffu, hi = valid >> (2 * i + 1) & 1u ? (uint32_t)id[2 * i + 1] : 0x7fffu;
-            x[i] = (lo | hi << 16) ^ me;
+            const uint32_t pair = both(id[2 * i], id[2 * i + 1]);
+            const us2 over = __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(us2, pair), top), unit);
+            there[i] = __builtin_bit_cast(uint32_t, (us2)(over - unit));      // a token of the table (what is not, multiplies zeros)
+            low[i] = __builtin_bit_cast(uint32_t, (us2)(two << (__builtin_bit_cast(us2, pair ^ me) & (us2){15, 15}))) & 0x40004000u;
+            high[i] = __builtin_bit_cast(uint32_t, (us2)(unit << (__builtin_bit_cast(us2, pair >> 4) & (us2){15, 15})));
         }
+        if (step + 1 < to) ask_tokens();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("" : "+v"(low[i]));      // (or the mask above is taken again for every tile, in slower instructions)
+        if (__ballot(early)) {      // the first `early` of the eight are another lane's (all, where the group has none)
+            const uint32_t valid = early < VE ? 0xffu << early & 0xffu : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) there[i] &= half_masks(valid, i);
+        }
+        uint32_t keep[MT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            const uint32_t bits = DROP ? valid & kept8_at(((size_t)at.b * H + h[m]) * N + at.t, d, call) : valid;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[m].w[i] = raw[m].w[i] & half_masks(bits, i);
+            uint4 k = make_uint4(~0u, ~0u, ~0u, ~0u);
+            if constexpr (DROP) k = kept_words_at((uint64_t)(element + apart[m]), d, call);
+            keep[m][0] = k.x; keep[m][1] = k.y; keep[m][2] = k.z; keep[m][3] = k.w;
         }
-        if (step + 1 < to) ask(step + 1);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[m].w[i] = mine[m].w[i] & there[i] & keep[m][i];
+        if (step + AHEAD < to) ask_rows(mine);
 #pragma unroll
         for (int j = 0; j < VT; ++j) {
             Frag b;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const us2 differ = __builtin_bit_cast(us2, x[i] ^ (uint32_t)j * 0x100010u), unit = {1, 1}, as = {(uint16_t)one, (uint16_t)one};
-                b.w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(unit, differ) * as);
-            }
+            for (int i = 0; i < 4; ++i) b.w[i] = (j <= 14 ? high[i] << (14 - j) : high[i] >> 1) & low[i];
 #pragma unroll
             for (int m = 0; m < MT; ++m) acc[m][j] = product<IO>(a[m], b, acc[m][j]);
         }
+    };
+    for (uint32_t step = from; step < to; step += AHEAD) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (step + u < to) work(step + u, raw[u]);
     }
     float zero = 0.f;
 #pragma unroll
@@ -169,7 +227,7 @@ embed_small_kernel(const typename IO::T* __restrict__ dy, const ID* __restrict__
                         const ID v = ids[(size_t)b * N + t];
                         if (!(v >= 0 && v < (ID)V) || lane >= CH || h0 + lane >= H) continue;
                         const size_t e = ((size_t)b * H + h0 + lane) * N + t;
-                        if (!DROP || (kept8(e >> 3, d, call) >> (e & 7u) & 1u)) sums[(uint32_t)v * (CH + PAD) + lane] += IO::ld(dy, e);
+                        if (!DROP || (kept8(e >> 3, d, call) >> (e & 7u) & 1u)) sums[(uint32_t)v * (CH + PAD) + lane] += 2.f * IO::ld(dy, e);
                     }
                 }
             }
@@ -229,7 +287,7 @@ hipError_t run(const EmbedArgs& a, const void* dy, float* dE, float* part, hipSt
     const auto kernel = a.drop.threshold ? embed_small_kernel<IO, ID, true> : embed_small_kernel<IO, ID, false>;
     hipLaunchKernelGGL(kernel, g, dim3(64 * WAVES), 0, st, (const typename IO::T*)dy, (const ID*)a.ids, part, (uint32_t)a.N, (uint32_t)a.H,
                        (uint32_t)a.V, s, a.drop);
-    hipLaunchKernelGGL(embed_small_sum_kernel, gs, dim3(SUM_T), 0, st, (const float*)part, dE, (uint32_t)a.H, (uint32_t)a.V, a.scale * a.drop.scale, s);
+    hipLaunchKernelGGL(embed_small_sum_kernel, gs, dim3(SUM_T), 0, st, (const float*)part, dE, (uint32_t)a.H, (uint32_t)a.V, 0.5f * a.scale * a.drop.scale, s);
     return hipGetLastError();
 }
 

@@ -145,18 +145,25 @@ __device__ __forceinline__ uint4 philox(uint64_t block, uint64_t call, uint64_t 
     return make_uint4(c0, c1, c2, c3);
 }
 
+// The kept entries of a block as masks of the halves of four words, as 16-bit data lie in memory: 0xffff kept, 0 dropped.
+__device__ __forceinline__ uint4 kept_words(uint64_t block, const Drop& d, uint64_t call)
+{
+    typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+    if (d.threshold > 0xffffu) return make_uint4(0, 0, 0, 0);
+    const uint4 r = philox(block, call, d.seed);
+    const uint16_t t = (uint16_t)d.threshold;
+    const us2 least = {t, t}, one = {1, 1};
+    const auto mask = [&](uint32_t w) {      // what a half lacks of the threshold, as 0 or 1; less 1
+        const us2 lacks = __builtin_elementwise_sub_sat(least, __builtin_bit_cast(us2, w));
+        return __builtin_bit_cast(uint32_t, (us2)(__builtin_elementwise_min(lacks, one) - one));
+    };
+    return make_uint4(mask(r.x), mask(r.y), mask(r.z), mask(r.w));
+}
 // bit j: entry 8 block + j is kept
 __device__ __forceinline__ uint32_t kept8(uint64_t block, const Drop& d, uint64_t call)
 {
-    const uint4 r = philox(block, call, d.seed);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        m |= (w[i] & 0xffffu) >= d.threshold ? 1u << (2 * i) : 0u;
-        m |= (w[i] >> 16) >= d.threshold ? 2u << (2 * i) : 0u;
-    }
-    return m;
+    const uint4 w = kept_words(block, d, call);
+    return (w.x & 1u) | (w.x >> 16 & 2u) | (w.y & 4u) | (w.y >> 16 & 8u) | (w.z & 16u) | (w.z >> 16 & 32u) | (w.w & 64u) | (w.w >> 16 & 128u);
 }
 // bit j: entry e + j is kept
 __device__ __forceinline__ uint32_t kept8_at(uint64_t e, const Drop& d, uint64_t call)
@@ -165,6 +172,29 @@ __device__ __forceinline__ uint32_t kept8_at(uint64_t e, const Drop& d, uint64_t
     uint32_t m = kept8(e >> 3, d, call);
     if (at) m = (m | kept8((e >> 3) + 1, d, call) << 8) >> at;
     return m & 0xffu;
+}
+
+// the masks of entries e .. e + 7
+__device__ __forceinline__ uint4 kept_words_at(uint64_t e, const Drop& d, uint64_t call)
+{
+    const uint32_t at = (uint32_t)e & 7u;
+    uint4 a = kept_words(e >> 3, d, call);
+    if (at) {
+        const uint4 b = kept_words((e >> 3) + 1, d, call);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        uint32_t v[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {      // words at / 2 ..
+            v[i] = w[i];
+#pragma unroll
+            for (int k = 1; k < 4; ++k)
+                if (at / 2 == (uint32_t)k && i + k < 8) v[i] = w[i + k];
+        }
+        const uint32_t by = at % 2 * 16;
+        const auto pick = [&](int i) { return by ? v[i] >> 16 | v[i + 1] << 16 : v[i]; };
+        a = make_uint4(pick(0), pick(1), pick(2), pick(3));
+    }
+    return a;
 }
 
 inline hipError_t launch_grid(uint64_t blocks, uint32_t threads, dim3* g)      // 1-D grid; a launch holds fewer than 2^32 threads
