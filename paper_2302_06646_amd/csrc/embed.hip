@@ -16,7 +16,8 @@ constexpr int TILE_MIN = 1024, TILES_MAX = 64, ROWS = TILE_MIN / SORT_T;        
 constexpr int ALONE = 4096, ALONE_T = 1024;                                     // tokens that one workgroup sorts by itself, its threads
 constexpr int CHUNK_MIN = 8;                                                    // sorted places of a thread, at least
 constexpr int AHEAD = 8;                                                        // rows of dy that a thread asks for before it adds the first
-constexpr int JOIN_T = 1024;                                                    // threads of a workgroup that joins a run's partial sums
+constexpr int JOIN_GROUPS = 256;                                                // workgroups that join a run's partial sums
+constexpr int JOIN_T = 1024;                                                    // and their threads
 
 // a token's row, or V for one that names none
 template <class ID>
@@ -446,7 +447,7 @@ sort_alone_kernel(Tokens<ID> in, uint32_t* __restrict__ key, uint32_t* __restric
 }
 
 // Sums of runs.  Partial sums lie at part[2 chunk + w]: w = 0 of a run that came in from the chunk before, 1 of one that began here
-// and goes on, which is noted down in `joins` (how many, then their chunks; in any order, they have nothing to do with each other).
+// and goes on, which is noted down in `joins` (how many, from the third word on their chunks and tokens; in any order, they have nothing to do with each other).
 // A thread's columns are eight from c on; where the row's end is not a multiple of eight the last thread begins `skip` columns early
 // (NARROW: rows of fewer than eight).  key, pos: readable up to a whole chunk.
 template <class IO, bool DROP, bool NARROW>
@@ -521,53 +522,85 @@ embed_sum_kernel(const typename IO::T* __restrict__ dy, const uint32_t* __restri
     if (cur >= V) return;
     if (to < M && key[to] == cur) {
         keep(came_in ? 0 : 1);
-        if (!came_in && slice == 0) joins[1 + atomicAdd(joins, 1u)] = chunk;
+        if (!came_in && slice == 0) reinterpret_cast<uint2*>(joins + 2)[atomicAdd(joins, 1u)] = make_uint2(chunk, cur);
     } else finish();
 }
 
-// Runs over several chunks: their partial sums, by the waves of a workgroup in turn and the waves' sums in order.  A lane takes four
-// columns.
+// Runs over several chunks: their partial sums added in the chunks' order, four columns a lane.  Most runs are of two or three chunks: a
+// wave takes one for 256 columns.  Those of more than LONG_RUN chunks (common tokens) it leaves to its whole workgroup, whose waves take
+// the chunks in turn and whose sums are then added in order.
+constexpr uint32_t LONG_RUN = 8;
 __global__ void __launch_bounds__(JOIN_T)
 embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ part, const uint32_t* __restrict__ joins, float* __restrict__ dE,
                   uint32_t M, uint32_t H, uint32_t P, uint32_t chunk_size, float f)
 {
-    constexpr int WAVES = JOIN_T / 64;
+    constexpr uint32_t WAVES = JOIN_T / 64, LIST = 256;
     __shared__ float4 sums[WAVES][64];
-    const uint32_t n = joins[0], blocks = (P * 2 + 63) / 64, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    for (uint32_t item = blockIdx.x; item < n * blocks; item += gridDim.x) {
-        const uint32_t chunk = joins[1 + item / blocks], col = item % blocks * 64 + lane, to = (chunk + 1) * chunk_size, k = key[to];
-        // the run's end: the first place behind `to` with another token; the lanes of a wave look at 64 places at once
-        uint32_t lo = to + 1, hi = M;
-        while (lo < hi) {
-            const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-            const uint32_t same = (uint32_t)__popcll(__ballot(at < hi && key[at] == k));      // (the first so many lanes)
-            const uint32_t end = lo + same * step;
-            if (same) lo = end - step + 1;
-            if (end < hi) hi = end;
+    __shared__ uint32_t longs[LIST], count;
+    const uint32_t blocks = (P * 2 + 63) / 64, items = joins[0] * blocks, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    // the last chunk of a run: the chunks that begin with its token; the lanes look at 64 of them at once
+    const auto last_chunk = [&](uint2 run) {
+        for (uint32_t last = run.x;; last += 64) {
+            const uint64_t at = (uint64_t)(last + 1 + lane) * chunk_size;
+            const uint32_t more = (uint32_t)__popcll(__ballot(at < M && key[at] == run.y));
+            if (more < 64) return last + more;
         }
-        const uint32_t last = (lo - 1) / chunk_size;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (col < P * 2) {
+    };
+    const auto add = [&](float4& s, uint32_t chunk, uint32_t from, uint32_t last, uint32_t by, uint32_t col) {
+        if (col >= P * 2) return;
 #pragma unroll 4
-            for (uint32_t q = chunk + wave; q <= last; q += WAVES) {
-                const float4 v = *reinterpret_cast<const float4*>(part + ((size_t)q * 2 + (q == chunk)) * (P * VE) + col * 4);
-                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        for (uint32_t q = from; q <= last; q += by) {
+            const float4 v = *reinterpret_cast<const float4*>(part + ((size_t)q * 2 + (q == chunk)) * (P * VE) + col * 4);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+    };
+    const auto write = [&](const float4& s, uint32_t k, uint32_t col) {
+        if (col >= P * 2) return;
+        const float v[4] = {s.x * f, s.y * f, s.z * f, s.w * f};
+        const uint32_t slice = col / 2, from = slice * VE, at = H > VE ? (from < H - VE ? from : H - VE) : 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {      // (column at + i; those before `from` are the slice's before)
+            const uint32_t i = col % 2 * 4 + j;
+            if (at + i >= from && at + i < H) dE[(size_t)k * H + at + i] = v[j];
+        }
+    };
+    const uint2* runs = reinterpret_cast<const uint2*>(joins + 2);
+    for (uint32_t item = wave * gridDim.x + blockIdx.x; item < items; item += gridDim.x * WAVES) {      // (a run's columns to several workgroups)
+        const uint2 run = runs[item / blocks];
+        const uint32_t chunk = run.x, col = item % blocks * 64 + lane;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        add(s, chunk, chunk, chunk + 1, 1, col);      // (the two there always are, asked for beside the search)
+        const uint32_t last = last_chunk(run);
+        if (last - chunk > LONG_RUN) {
+            uint32_t slot = 0;
+            if (lane == 0) slot = atomicAdd(&count, 1u);
+            slot = (uint32_t)__shfl((int)slot, 0);
+            if (slot < LIST) {
+                if (lane == 0) longs[slot] = item;
+                continue;
             }
         }
+        add(s, chunk, chunk + 2, last, 1, col);
+        write(s, run.y, col);
+    }
+    __syncthreads();
+    const uint32_t n = count < LIST ? count : LIST;
+    for (uint32_t i = 0; i < n; ++i) {
+        const uint32_t item = longs[i], col = item % blocks * 64 + lane;
+        const uint2 run = runs[item / blocks];
+        const uint32_t chunk = run.x, last = last_chunk(run);
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        add(s, chunk, chunk + wave, last, WAVES, col);
         sums[wave][lane] = s;
         __syncthreads();
-        if (wave == 0 && col < P * 2) {
-            for (uint32_t w = 1; w < WAVES && w <= last - chunk; ++w) {
+        if (wave == 0) {
+            for (uint32_t w = 1; w < WAVES; ++w) {
                 const float4 v = sums[w][lane];
                 s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
-            const float v[4] = {s.x * f, s.y * f, s.z * f, s.w * f};
-            const uint32_t slice = col / 2, from = slice * VE, at = H > VE ? (from < H - VE ? from : H - VE) : 0;
-#pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) {      // (column at + i; those before `from` are the slice's before)
-                const uint32_t i = col % 2 * 4 + j;
-                if (at + i >= from && at + i < H) dE[(size_t)k * H + at + i] = v[j];
-            }
+            write(s, run.y, col);
         }
         __syncthreads();
     }
@@ -609,7 +642,7 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
     // (room for the number of chunks that grows with M: those of 32 places, or so many shorter ones that there are 2^17 threads and twice that)
     const int64_t most = (l.M + CHUNK_MIN - 1) / CHUNK_MIN, some = (l.M + 31) / 32 + ((1 << 18) + l.P - 1) / l.P + 1;
     l.part = take((size_t)(most < some ? most : some) * 2 * l.P * VE * sizeof(float));
-    l.joins = take((size_t)((most < some ? most : some) + 1) * sizeof(uint32_t));
+    l.joins = take((size_t)((most < some ? most : some) + 1) * 2 * sizeof(uint32_t));
     l.rows = take(layout == LONGCONV_CHANNELS_FIRST ? (size_t)l.M * l.P * VE * (io == LONGCONV_F32 ? 4 : 2) : 0);
     l.total = off;
     return l;
@@ -717,7 +750,7 @@ hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hip
     if (a.H < VE) drop ? sum(std::true_type(), std::true_type()) : sum(std::false_type(), std::true_type());
     else drop ? sum(std::true_type(), std::false_type()) : sum(std::false_type(), std::false_type());
     if (l.chunks > 1)
-        hipLaunchKernelGGL(embed_join_kernel, dim3(512), dim3(JOIN_T), 0, st, key, (const float*)part, (const uint32_t*)joins, dE, (uint32_t)l.M,
+        hipLaunchKernelGGL(embed_join_kernel, dim3(JOIN_GROUPS), dim3(JOIN_T), 0, st, key, (const float*)part, (const uint32_t*)joins, dE, (uint32_t)l.M,
                            (uint32_t)a.H, l.P, (uint32_t)l.chunk, a.scale * a.drop.scale);
     return hipGetLastError();
 }
