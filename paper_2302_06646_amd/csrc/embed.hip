@@ -716,6 +716,13 @@ hipError_t forward(const EmbedArgs& a, const void* E, void* y, hipStream_t st)
     return hipGetLastError();
 }
 
+// a wave for every 256 columns of every run that there may be, up to JOIN_GROUPS workgroups
+unsigned join_groups(const Layout& l)
+{
+    const uint64_t waves = (uint64_t)l.chunks * ((l.P * 2 + 63) / 64), groups = (waves + JOIN_T / 64 - 1) / (JOIN_T / 64);
+    return (unsigned)(groups < JOIN_GROUPS ? groups : JOIN_GROUPS);
+}
+
 template <class IO>
 hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hipStream_t st)
 {
@@ -750,7 +757,7 @@ hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hip
     if (a.H < VE) drop ? sum(std::true_type(), std::true_type()) : sum(std::false_type(), std::true_type());
     else drop ? sum(std::true_type(), std::false_type()) : sum(std::false_type(), std::false_type());
     if (l.chunks > 1)
-        hipLaunchKernelGGL(embed_join_kernel, dim3(JOIN_GROUPS), dim3(JOIN_T), 0, st, key, (const float*)part, (const uint32_t*)joins, dE, (uint32_t)l.M,
+        hipLaunchKernelGGL(embed_join_kernel, dim3(join_groups(l)), dim3(JOIN_T), 0, st, key, (const float*)part, (const uint32_t*)joins, dE, (uint32_t)l.M,
                            (uint32_t)a.H, l.P, (uint32_t)l.chunk, a.scale * a.drop.scale);
     return hipGetLastError();
 }
