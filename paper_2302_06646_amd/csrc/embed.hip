@@ -12,7 +12,7 @@ namespace lc {
 namespace {
 
 constexpr int RADIX = 512, SORT_T = 256, SORT_W = SORT_T / 64;                  // digits of at most nine bits; threads and waves of a tile
-constexpr int TILE_MIN = 1024, TILES_MAX = 64, ROWS = TILE_MIN / SORT_T;        // tiles of a sorting pass; rows of 64 that a wave asks for at once
+constexpr int TILE_MIN = 1024, TILES_MAX = 128, ROWS = TILE_MIN / SORT_T;        // tiles of a sorting pass; rows of 64 that a wave asks for at once
 constexpr int ALONE = 4096, ALONE_T = 1024;                                     // tokens that one workgroup sorts by itself, its threads
 constexpr int CHUNK_MIN = 8;                                                    // sorted places of a thread, at least
 constexpr int AHEAD = 8;                                                        // rows of dy that a thread asks for before it adds the first
@@ -526,38 +526,53 @@ embed_sum_kernel(const typename IO::T* __restrict__ dy, const uint32_t* __restri
     } else finish();
 }
 
-// Runs over several chunks: their partial sums added in the chunks' order, four columns a lane.  Most runs are of two or three chunks: a
-// wave takes one for 256 columns.  Those of more than LONG_RUN chunks (common tokens) it leaves to its whole workgroup, whose waves take
-// the chunks in turn and whose sums are then added in order.
+// Runs over several chunks: their partial sums, four columns a lane and, where a row has fewer than 256, several chunks side by side in
+// a wave; in an order that the run's length alone gives.  Most runs are of two or three chunks: a wave takes one (of 256 columns).
+// Those that would take it more than LONG_RUN steps (common tokens) it leaves to its whole workgroup, whose waves take the chunks in
+// turn and whose sums are then added in order.
 constexpr uint32_t LONG_RUN = 8;
 __global__ void __launch_bounds__(JOIN_T)
 embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ part, const uint32_t* __restrict__ joins, float* __restrict__ dE,
-                  uint32_t M, uint32_t H, uint32_t P, uint32_t chunk_size, float f)
+                  uint32_t M, uint32_t H, uint32_t P, uint32_t chunk_size, uint32_t wide, float f)
 {
     constexpr uint32_t WAVES = JOIN_T / 64, LIST = 256;
     __shared__ float4 sums[WAVES][64];
     __shared__ uint32_t longs[LIST], count;
-    const uint32_t blocks = (P * 2 + 63) / 64, items = joins[0] * blocks, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const uint32_t blocks = (P * 2 + wide - 1) / wide, items = joins[0] * blocks, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const uint32_t side = 64 / wide, mine = lane / wide;      // chunks of a wave at once; the lane's among them
     if (threadIdx.x == 0) count = 0;
     __syncthreads();
-    // the last chunk of a run: the chunks that begin with its token; the lanes look at 64 of them at once
+    // the last chunk of a run, the last that begins with its token: the lanes look at the next 64, and, if all do, at 64 places of what is
+    // left at a time
     const auto last_chunk = [&](uint2 run) {
-        for (uint32_t last = run.x;; last += 64) {
-            const uint64_t at = (uint64_t)(last + 1 + lane) * chunk_size;
-            const uint32_t more = (uint32_t)__popcll(__ballot(at < M && key[at] == run.y));
-            if (more < 64) return last + more;
+        const auto begins = [&](uint32_t q, uint32_t end) { return (uint32_t)__popcll(__ballot(q < end && key[(size_t)q * chunk_size] == run.y)); };
+        uint32_t end = (M + chunk_size - 1) / chunk_size, last = run.x + begins(run.x + 1 + lane, end);
+        if (last < run.x + 64) return last;
+        while (last + 1 < end) {
+            const uint32_t step = (end - last - 1 + 63) / 64;
+            last += step * begins(last + step * (lane + 1), end);
+            if (last + step < end) end = last + step;
         }
+        return last;
     };
-    const auto add = [&](float4& s, uint32_t chunk, uint32_t from, uint32_t last, uint32_t by, uint32_t col) {
+    const auto add = [&](float4& s, uint32_t chunk, uint32_t& q, uint32_t last, uint32_t by, uint32_t col) {
         if (col >= P * 2) return;
 #pragma unroll 4
-        for (uint32_t q = from; q <= last; q += by) {
+        for (; q <= last; q += by) {
             const float4 v = *reinterpret_cast<const float4*>(part + ((size_t)q * 2 + (q == chunk)) * (P * VE) + col * 4);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
     };
+    const auto side_by_side = [&](float4& s) {
+        for (uint32_t m = wide; m < 64; m <<= 1) {
+            s.x += __shfl_xor(s.x, (int)m);
+            s.y += __shfl_xor(s.y, (int)m);
+            s.z += __shfl_xor(s.z, (int)m);
+            s.w += __shfl_xor(s.w, (int)m);
+        }
+    };
     const auto write = [&](const float4& s, uint32_t k, uint32_t col) {
-        if (col >= P * 2) return;
+        if (mine || col >= P * 2) return;
         const float v[4] = {s.x * f, s.y * f, s.z * f, s.w * f};
         const uint32_t slice = col / 2, from = slice * VE, at = H > VE ? (from < H - VE ? from : H - VE) : 0;
 #pragma unroll
@@ -569,11 +584,12 @@ embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ pa
     const uint2* runs = reinterpret_cast<const uint2*>(joins + 2);
     for (uint32_t item = wave * gridDim.x + blockIdx.x; item < items; item += gridDim.x * WAVES) {      // (a run's columns to several workgroups)
         const uint2 run = runs[item / blocks];
-        const uint32_t chunk = run.x, col = item % blocks * 64 + lane;
+        const uint32_t chunk = run.x, col = item % blocks * wide + lane % wide;
+        uint32_t q = chunk + mine;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        add(s, chunk, chunk, chunk + 1, 1, col);      // (the two there always are, asked for beside the search)
+        add(s, chunk, q, chunk + 1, side, col);      // (the two there always are, asked for beside the search)
         const uint32_t last = last_chunk(run);
-        if (last - chunk > LONG_RUN) {
+        if (last - chunk > LONG_RUN * side) {
             uint32_t slot = 0;
             if (lane == 0) slot = atomicAdd(&count, 1u);
             slot = (uint32_t)__shfl((int)slot, 0);
@@ -582,17 +598,20 @@ embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ pa
                 continue;
             }
         }
-        add(s, chunk, chunk + 2, last, 1, col);
+        add(s, chunk, q, last, side, col);
+        side_by_side(s);
         write(s, run.y, col);
     }
     __syncthreads();
     const uint32_t n = count < LIST ? count : LIST;
     for (uint32_t i = 0; i < n; ++i) {
-        const uint32_t item = longs[i], col = item % blocks * 64 + lane;
+        const uint32_t item = longs[i], col = item % blocks * wide + lane % wide;
         const uint2 run = runs[item / blocks];
         const uint32_t chunk = run.x, last = last_chunk(run);
+        uint32_t q = chunk + wave * side + mine;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        add(s, chunk, chunk + wave, last, WAVES, col);
+        add(s, chunk, q, last, WAVES * side, col);
+        side_by_side(s);
         sums[wave][lane] = s;
         __syncthreads();
         if (wave == 0) {
@@ -619,7 +638,7 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
 {
     Layout l;
     l.M = B * N;
-    // a pass reads the counts of every tile in every tile: no more than 64 of them, however many tokens there are
+    // a pass reads the counts of every tile in every tile: no more than 128 of them, however many tokens there are
     l.tile = TILE_MIN * ((l.M + (int64_t)TILE_MIN * TILES_MAX - 1) / ((int64_t)TILE_MIN * TILES_MAX));
     l.tiles = (l.M + l.tile - 1) / l.tile;
     l.P = (uint32_t)((H + VE - 1) / VE);
@@ -716,6 +735,13 @@ hipError_t forward(const EmbedArgs& a, const void* E, void* y, hipStream_t st)
     return hipGetLastError();
 }
 
+// lanes of a wave for a row's columns, four each: as many as it takes, in powers of two, and 64 at most
+uint32_t join_width(const Layout& l)
+{
+    uint32_t w = 64;
+    while (w / 2 >= l.P * 2) w /= 2;
+    return w;
+}
 // a wave for every 256 columns of every run that there may be, up to JOIN_GROUPS workgroups
 unsigned join_groups(const Layout& l)
 {
@@ -758,7 +784,7 @@ hipError_t backward(const EmbedArgs& a, const void* dy, float* dE, char* ws, hip
     else drop ? sum(std::true_type(), std::false_type()) : sum(std::false_type(), std::false_type());
     if (l.chunks > 1)
         hipLaunchKernelGGL(embed_join_kernel, dim3(join_groups(l)), dim3(JOIN_T), 0, st, key, (const float*)part, (const uint32_t*)joins, dE, (uint32_t)l.M,
-                           (uint32_t)a.H, l.P, (uint32_t)l.chunk, a.scale * a.drop.scale);
+                           (uint32_t)a.H, l.P, (uint32_t)l.chunk, join_width(l), a.scale * a.drop.scale);
     return hipGetLastError();
 }
 

@@ -65,11 +65,11 @@ __device__ __forceinline__ float slope_of(float z)
     return 1.f;
 }
 
-// (n, mean, m2) <- both sets together
+// (n, mean, m2) <- both sets together (the share to the last bit: means of channels differ by as much as the data do)
 __device__ __forceinline__ void merge(float& n, float& mean, float& m2, float n2, float mean2, float m22)
 {
     if (n2 == 0.f) return;
-    const float all = n + n2, d = mean2 - mean, f = n2 * __builtin_amdgcn_rcpf(all);
+    const float all = n + n2, d = mean2 - mean, f = n2 / all;
     mean = __builtin_fmaf(d, f, mean);
     m2 += m22 + d * d * n * f;
     n = all;
@@ -79,6 +79,7 @@ __device__ __forceinline__ void merge(float& n, float& mean, float& m2, float n2
 // are `rows` positions by `slices`.
 struct Walk {
     uint32_t P, slices, slabs, rows, parts;
+    uint32_t half;      // the largest power of two below `rows`, 0 for one row
     int64_t per;
 };
 Walk walk(int64_t B, int64_t S, int64_t C)
@@ -88,6 +89,7 @@ Walk walk(int64_t B, int64_t S, int64_t C)
     w.slices = w.P < SLAB ? w.P : SLAB;
     w.slabs = (w.P + w.slices - 1) / w.slices;
     w.rows = GT / w.slices;
+    for (w.half = w.rows > 1; 2 * w.half && 2 * w.half < w.rows; w.half *= 2) {}
     int64_t parts = GROUPS_WANTED / (B * w.slabs);
     const int64_t most = (S + 4 * w.rows - 1) / (4 * w.rows);      // four positions of a thread at least
     if (parts > most) parts = most;
@@ -281,7 +283,7 @@ gnorm_stats_kernel(const typename IO::T* __restrict__ x, float* __restrict__ par
                 float v[VE];
                 raw[u].get(v);
                 n += 1.f;
-                const float f = __builtin_amdgcn_rcpf(n);
+                const float g = __builtin_amdgcn_rcpf(n), f = __builtin_fmaf(g, __builtin_fmaf(-n, g, 1.f), g);      // 1 / n
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
                     const float d = v[j] - mean[j];
@@ -290,44 +292,78 @@ gnorm_stats_kernel(const typename IO::T* __restrict__ x, float* __restrict__ par
                 }
             }
         }
-    const int t = threadIdx.x;
-    to_slots(sm + t * VE, p, mean);
-    to_slots(s2 + t * VE, p, m2);
-    sn[t] = n;
-    __syncthreads();
-    const int wide = (int)w.slices * VE;
-    for (int i = t; i < wide; i += GT) {
-        const int64_t c = (int64_t)p.slab * wide + i;
-        if (c >= C) break;
-        float an = 0.f, am = 0.f, a2 = 0.f;
-        for (uint32_t r = 0; r < w.rows; ++r) {
-            const int from = (int)(r * w.slices);
-            merge(an, am, a2, sn[from + i / VE], sm[from * VE + i], s2[from * VE + i]);
+    // the rows' results together, half of them at a time
+    for (uint32_t half = w.half; half; half >>= 1) {
+        __syncthreads();
+        if (p.r >= half && p.r < 2 * half && p.r < w.rows) {
+            to_slots(sm + threadIdx.x * VE, p, mean);
+            to_slots(s2 + threadIdx.x * VE, p, m2);
+            sn[threadIdx.x] = n;
         }
-        float* q = part + ((size_t)p.b * w.parts + p.part) * 2 * C;
-        q[c] = am;
-        q[C + c] = a2;
+        __syncthreads();
+        if (p.r < half && p.r + half < w.rows) {
+            const uint32_t other = threadIdx.x + half * w.slices;
+            const float n2 = sn[other];
+            if (n2 != 0.f) {
+                const float all = n + n2, f = n2 / all, nf = n * f;
+#pragma unroll
+                for (int j = 0; j < VE; ++j) {
+                    const uint32_t slot = other * VE + ((j - p.skip) & (VE - 1));
+                    const float d = sm[slot] - mean[j];
+                    mean[j] = __builtin_fmaf(d, f, mean[j]);
+                    m2[j] += __builtin_fmaf(d * d, nf, s2[slot]);
+                }
+                n = all;
+            }
+        }
+    }
+    if (p.r == 0 && p.on) {
+        float* q = part + ((size_t)p.b * w.parts + p.part) * 2 * C + p.c;
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+            if (p.mine(j)) {
+                q[j] = mean[j];
+                q[C + j] = m2[j];
+            }
     }
 }
 
-// a wave for each group: its channels' and parts' results together
-__global__ void __launch_bounds__(64)
+// Entries first, first + T, ... of the parts' results of a group of D channels: f(row of part, channel of the group)
+template <int T, class F>
+__device__ __forceinline__ void each_entry(uint32_t first, uint32_t parts, uint32_t D, F&& f)
+{
+    const uint32_t dq = T / D, dc = T - dq * D;
+    uint32_t q = first / D, c = first - q * D;
+#pragma unroll 4
+    while (q < parts) {
+        f(q, c);
+        q += dq;
+        c += dc;
+        if (c >= D) { c -= D; ++q; }
+    }
+}
+constexpr int FEW = 1024;      // results of a group that one wave puts together; for more a workgroup of sixteen does
+
+// T threads for each group: its channels' and parts' results together
+template <int T>
+__global__ void __launch_bounds__(T)
 gnorm_group_kernel(const float* __restrict__ part, float* __restrict__ mean, float* __restrict__ rstd, int64_t S, int64_t C, uint32_t G,
                    uint32_t parts, int64_t per, float eps)
 {
-    const uint32_t b = blockIdx.x / G, g = blockIdx.x % G, D = (uint32_t)(C / G);
+    __shared__ float sn[T / 64], sm[T / 64], s2[T / 64];
+    const uint32_t b = blockIdx.x / G, g = blockIdx.x % G, D = (uint32_t)(C / G), lane = threadIdx.x % 64;
     float n = 0.f, m = 0.f, m2 = 0.f;
-    for (uint64_t i = threadIdx.x; i < (uint64_t)parts * D; i += 64) {
-        const uint32_t q = (uint32_t)(i / D), c = g * D + (uint32_t)(i - (uint64_t)q * D);
-        const float* row = part + ((size_t)b * parts + q) * 2 * C;
+    const float* first = part + (size_t)b * parts * 2 * C + (size_t)g * D;
+    each_entry<T>(threadIdx.x, parts, D, [&](uint32_t q, uint32_t c) {
+        const float* row = first + (size_t)q * 2 * C + c;
         const int64_t here = S - q * per < per ? S - q * per : per;
-        merge(n, m, m2, (float)here, row[c], row[C + c]);
-    }
+        merge(n, m, m2, (float)here, row[0], row[C]);
+    });
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
         // the lower lane of a pair first, on both sides: every lane ends with the same numbers
         float n2 = __shfl_xor(n, s), a2 = __shfl_xor(m, s), b2 = __shfl_xor(m2, s);
-        if (threadIdx.x & s) {
+        if (lane & s) {
             float t;
             t = n; n = n2; n2 = t;
             t = m; m = a2; a2 = t;
@@ -335,6 +371,16 @@ gnorm_group_kernel(const float* __restrict__ part, float* __restrict__ mean, flo
         }
         if (n == 0.f) { n = n2; m = a2; m2 = b2; }
         else merge(n, m, m2, n2, a2, b2);
+    }
+    if constexpr (T > 64) {
+        if (lane == 0) {
+            sn[threadIdx.x / 64] = n;
+            sm[threadIdx.x / 64] = m;
+            s2[threadIdx.x / 64] = m2;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0)
+            for (int w = 1; w < T / 64; ++w) merge(n, m, m2, sn[w], sm[w], s2[w]);
     }
     if (threadIdx.x == 0) {
         mean[blockIdx.x] = m;
@@ -405,29 +451,37 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
             }
         }
     }
-    const int t = threadIdx.x;
-    to_slots(sa + t * VE, p, a);
-    to_slots(sb + t * VE, p, b);
-    __syncthreads();
-    const int wide = (int)w.slices * VE;
-    for (int i = t; i < wide; i += GT) {
-        const int64_t c = (int64_t)p.slab * wide + i;
-        if (c >= C) break;
-        float ta = 0.f, tb = 0.f;
-        for (uint32_t r = 0; r < w.rows; ++r) {
-            ta += sa[r * wide + i];
-            tb += sb[r * wide + i];
+    for (uint32_t half = w.half; half; half >>= 1) {
+        __syncthreads();
+        if (p.r >= half && p.r < 2 * half && p.r < w.rows) {
+            to_slots(sa + threadIdx.x * VE, p, a);
+            to_slots(sb + threadIdx.x * VE, p, b);
         }
-        float* q = part + ((size_t)p.b * w.parts + p.part) * 2 * C;
-        q[c] = ta;
-        q[C + c] = tb;
+        __syncthreads();
+        if (p.r < half && p.r + half < w.rows) {
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                const uint32_t slot = (threadIdx.x + half * w.slices) * VE + ((j - p.skip) & (VE - 1));
+                a[j] += sa[slot];
+                b[j] += sb[slot];
+            }
+        }
+    }
+    if (p.r == 0 && p.on) {
+        float* q = part + ((size_t)p.b * w.parts + p.part) * 2 * C + p.c;
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+            if (p.mine(j)) {
+                q[j] = a[j];
+                q[C + j] = b[j];
+            }
     }
 }
 
 constexpr int RT = 1024, RC = 16;      // threads of a workgroup that sums channels, and channels of it
 
 // workgroups 0 .. ceil(C / 16) - 1: dgamma and dbeta of sixteen channels, the rows of partial results spread over the threads; behind
-// them sixteen groups each, s1 and s2 by a wave for every group
+// them s1 and s2, by a wave for every group where its results are few, else by a workgroup
 __global__ void __launch_bounds__(RT)
 gnorm_gather_kernel(const float* __restrict__ part, const float* __restrict__ gamma, float* __restrict__ s1, float* __restrict__ s2,
                     float* __restrict__ dgamma, float* __restrict__ dbeta, int64_t B, int64_t C, uint32_t G, uint32_t parts)
@@ -436,19 +490,34 @@ gnorm_gather_kernel(const float* __restrict__ part, const float* __restrict__ ga
     const uint32_t D = (uint32_t)(C / G), blocks = (uint32_t)((C + RC - 1) / RC);
     float a = 0.f, h = 0.f;
     if (blockIdx.x >= blocks) {
-        const uint32_t id = (blockIdx.x - blocks) * (RT / 64) + threadIdx.x / 64;
+        const bool few = (uint64_t)parts * D <= FEW;
+        const uint32_t id = few ? (blockIdx.x - blocks) * (RT / 64) + threadIdx.x / 64 : blockIdx.x - blocks;
         if (id >= (uint32_t)B * G) return;
         const uint32_t b = id / G, g = id % G;
-        for (uint32_t i = threadIdx.x % 64; i < parts * D; i += 64) {
-            const uint32_t q = i / D, c = g * D + (i - q * D);
-            const float* row = part + ((size_t)b * parts + q) * 2 * C;
-            const float ga = gamma ? gamma[c] : 1.f;
-            a = __builtin_fmaf(ga, row[c], a);
-            h = __builtin_fmaf(ga, row[C + c], h);
-        }
+        const float* first = part + (size_t)b * parts * 2 * C + (size_t)g * D;
+        const auto entry = [&](uint32_t q, uint32_t c) {
+            const float* row = first + (size_t)q * 2 * C + c;
+            const float ga = gamma ? gamma[g * D + c] : 1.f;
+            a = __builtin_fmaf(ga, row[0], a);
+            h = __builtin_fmaf(ga, row[C], h);
+        };
+        if (few) each_entry<64>(threadIdx.x % 64, parts, D, entry);
+        else each_entry<RT>(threadIdx.x, parts, D, entry);
         a = wave_sum(a);
         h = wave_sum(h);
-        if (threadIdx.x % 64 == 0) {
+        if (!few) {
+            if (threadIdx.x % 64 == 0) {
+                sa[threadIdx.x / 64] = a;
+                sh[threadIdx.x / 64] = h;
+            }
+            __syncthreads();
+            if (threadIdx.x == 0)
+                for (int w = 1; w < RT / 64; ++w) {
+                    a += sa[w];
+                    h += sh[w];
+                }
+        }
+        if (threadIdx.x % (few ? 64 : RT) == 0) {
             s1[id] = a;
             s2[id] = h;
         }
@@ -802,7 +871,10 @@ hipError_t forward(const GnormArgs& a, const void* x, void* y, float* mean, floa
     float* part = (float*)ws;
     if (a.C < VE) hipLaunchKernelGGL((gnorm_stats_kernel<IO, NARROW>), g, dim3(GT), 0, st, (const T*)x, part, a.S, a.C, w);
     else hipLaunchKernelGGL((gnorm_stats_kernel<IO, ANYHOW>), g, dim3(GT), 0, st, (const T*)x, part, a.S, a.C, w);
-    hipLaunchKernelGGL(gnorm_group_kernel, gg, dim3(64), 0, st, (const float*)part, mean, rstd, a.S, a.C, (uint32_t)a.G, w.parts, w.per, eps);
+    if ((uint64_t)w.parts * (a.C / a.G) <= FEW)
+        hipLaunchKernelGGL(gnorm_group_kernel<64>, gg, dim3(64), 0, st, (const float*)part, mean, rstd, a.S, a.C, (uint32_t)a.G, w.parts, w.per, eps);
+    else
+        hipLaunchKernelGGL(gnorm_group_kernel<1024>, gg, dim3(1024), 0, st, (const float*)part, mean, rstd, a.S, a.C, (uint32_t)a.G, w.parts, w.per, eps);
     by_mode(a, [&](auto mode) {
         hipLaunchKernelGGL((gnorm_apply_kernel<IO, ACT, decltype(mode)::value>), g, dim3(GT), 0, st, (const T*)x, (T*)y, (const float*)mean,
                            (const float*)rstd, a.gamma, a.beta, a.S, a.C, (uint32_t)a.G, w);
@@ -839,7 +911,7 @@ hipError_t backward(const GnormArgs& a, const void* dy, const void* x, const flo
     }
     const Walk w = walk(a.B, a.S, a.C);
     hipError_t e = launch_grid((uint64_t)a.B * w.parts * w.slabs, GT, &g);
-    if (e == hipSuccess) e = launch_grid((uint64_t)(a.C + RC - 1) / RC + ((uint64_t)a.B * a.G + RT / 64 - 1) / (RT / 64), RT, &gg);
+    if (e == hipSuccess) e = launch_grid((uint64_t)(a.C + RC - 1) / RC + ((uint64_t)w.parts * (a.C / a.G) <= FEW ? ((uint64_t)a.B * a.G + RT / 64 - 1) / (RT / 64) : (uint64_t)a.B * a.G), RT, &gg);
     if (e != hipSuccess) return e;
     float* part = (float*)ws;
     float* s1 = (float*)((char*)ws + up256(part_rows(a.B, a.S, a.C) * 2 * a.C * sizeof(float)));
