@@ -18,38 +18,48 @@ constexpr int SLAB = 64;             // pieces of eight channels of a workgroup,
 constexpr int GROUPS_WANTED = 1024;  // workgroups of a pass over the tensor
 constexpr int AHEAD = 4;             // pieces that a thread asks for before it uses the first
 
-// The normal distribution function, and e = exp(-z^2 / 2) beside it.  erfc(x) exp(x^2) is t Q(t), t = 1 / (1 + 0.4 x), for x >= 0, Q the
-// polynomial of degree eight of the least largest relative error (fitted by weighted least squares): 1.3e-7, and 2.2e-7 absolute in
-// fp32.  Below zero the result is not a difference, so its relative error is that of e, 8e-7 down to z = -4.
+// The normal distribution function, and e = exp(-z^2 / 2) beside it.  erfc(x) exp(x^2) is t Q(t), t = 1 / (1 + p x), for x >= 0, Q the
+// polynomial of the least largest relative error (fitted by weighted least squares).  FINE: of degree eight, p = 0.4, 1.3e-7, and 2.2e-7
+// absolute in fp32; below zero the result is not a difference, so its relative error is that of e, 8e-7 down to z = -4.  Otherwise, for
+// results that are rounded to sixteen bits (a relative 4.9e-4 and more): of degree five, p = 0.46, 1.7e-5.
+template <bool FINE>
 __device__ __forceinline__ float normal_cdf(float z, float& e)
 {
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.28284271247461901f, fabsf(z), 1.f));
-    float q = 0.0502542145550251f;
-    q = __builtin_fmaf(q, t, -0.18287357687950134f);
-    q = __builtin_fmaf(q, t, 0.16904595494270325f);
-    q = __builtin_fmaf(q, t, -0.0055788299068808556f);
-    q = __builtin_fmaf(q, t, 0.14142005145549774f);
-    q = __builtin_fmaf(q, t, 0.16854438185691833f);
-    q = __builtin_fmaf(q, t, 0.20784245431423187f);
-    q = __builtin_fmaf(q, t, 0.22566960752010345f);
-    q = __builtin_fmaf(q, t, 0.22567586600780487f);
+    float q;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(FINE ? 0.28284271247461901f : 0.3252691328525543f, fabsf(z), 1.f));
+    if constexpr (FINE) {
+        q = __builtin_fmaf(0.025127103552222252f, t, -0.09143677353858948f);
+        q = __builtin_fmaf(q, t, 0.08452295511960983f);
+        q = __builtin_fmaf(q, t, -0.0027893988881260157f);
+        q = __builtin_fmaf(q, t, 0.07071001827716827f);
+        q = __builtin_fmaf(q, t, 0.08427219092845917f);
+        q = __builtin_fmaf(q, t, 0.10392122715711594f);
+        q = __builtin_fmaf(q, t, 0.11283480376005173f);
+        q = __builtin_fmaf(q, t, 0.11283793300390244f);
+    } else {
+        q = __builtin_fmaf(-0.06317603588104248f, t, 0.12090080231428146f);
+        q = __builtin_fmaf(q, t, 0.06272530555725098f);
+        q = __builtin_fmaf(q, t, 0.12026208639144897f);
+        q = __builtin_fmaf(q, t, 0.12951715290546417f);
+        q = __builtin_fmaf(q, t, 0.1297658532857895f);
+    }
     e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
-    const float h = 0.5f * q * t * e;
+    const float h = q * t * e;      // (half of erfc: the factor is in Q)
     return z < 0.f ? h : 1.f - h;
 }
 
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float act_of(float z)
 {
     if constexpr (ACT == LONGCONV_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
     if constexpr (ACT == LONGCONV_ACT_GELU) {
         float e;
-        return z * normal_cdf(z, e);
+        return z * normal_cdf<FINE>(z, e);
     }
     if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
     return z;
 }
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float slope_of(float z)
 {
     if constexpr (ACT == LONGCONV_ACT_SILU) {
@@ -58,7 +68,7 @@ __device__ __forceinline__ float slope_of(float z)
     }
     if constexpr (ACT == LONGCONV_ACT_GELU) {
         float e;
-        const float c = normal_cdf(z, e);
+        const float c = normal_cdf<FINE>(z, e);
         return __builtin_fmaf(z * 0.39894228040143268f, e, c);
     }
     if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? 1.f : 0.f;
@@ -217,30 +227,67 @@ __device__ __forceinline__ void each_group(int c, uint32_t G, uint32_t D, F&& f)
         }
 }
 
-// xhat = (x - mean) rstd; where x has sixteen bits, the fp32 product and sum x rstd - mean rstd, whose rounding is far below x's own
+// xhat = (x - mean) rstd and z = gamma xhat + beta of a thread's channels.  Where x has sixteen bits, each is one fp32 multiply-add of x,
+// xhat = x rstd - mean rstd and z = x (gamma rstd) + (beta - mean gamma rstd), whose rounding is far below x's own.
 template <class IO, int MODE>
-struct Standard {
-    Groups<MODE> mean, rstd;      // (16 bits: mean holds -mean rstd)
-    __device__ __forceinline__ void set(int j, float m, float r)
-    {
-        rstd[j] = r;
-        mean[j] = sizeof(typename IO::T) == 2 ? -m * r : m;
-    }
-    __device__ __forceinline__ float operator()(int j, float x) const
-    {
-        return sizeof(typename IO::T) == 2 ? __builtin_fmaf(x, rstd[j], mean[j]) : (x - mean[j]) * rstd[j];
-    }
-};
-template <class IO, int MODE>
-struct Channels {      // of a thread's piece
-    Standard<IO, MODE> xhat;
-    float gamma[VE], beta[VE];
-    __device__ __forceinline__ void load(const Piece& p, size_t b, const float* mn, const float* rs, const float* ga, const float* be, uint32_t G,
-                                         uint32_t D)
+struct Channels {
+    static constexpr bool HALF = sizeof(typename IO::T) == 2;
+    Groups<MODE> mean, rstd;             // HALF: mean holds -mean rstd
+    float gamma[VE], beta[VE];           // HALF: gamma rstd, beta - mean gamma rstd
+    __device__ __forceinline__ void params(const Piece& p, const float* ga, const float* be)
     {
         load_params(ga, p, 1.f, gamma);
         load_params(be, p, 0.f, beta);
-        each_group<MODE>(p.c, G, D, [&](int j, uint32_t g) { xhat.set(j, mn[b * G + g], rs[b * G + g]); });
+    }
+    __device__ __forceinline__ void set(int j, float m, float r)
+    {
+        rstd[j] = r;
+        mean[j] = HALF ? -m * r : m;
+    }
+    __device__ __forceinline__ void combine()      // after params and set
+    {
+        if constexpr (HALF)
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                beta[j] = __builtin_fmaf(mean[j], gamma[j], beta[j]);
+                gamma[j] *= rstd[j];
+            }
+    }
+    __device__ __forceinline__ void load(const Piece& p, size_t b, const float* mn, const float* rs, const float* ga, const float* be, uint32_t G,
+                                         uint32_t D)
+    {
+        params(p, ga, be);
+        each_group<MODE>(p.c, G, D, [&](int j, uint32_t g) { set(j, mn[b * G + g], rs[b * G + g]); });
+        combine();
+    }
+    __device__ __forceinline__ float xhat(int j, float x) const
+    {
+        return HALF ? __builtin_fmaf(x, rstd[j], mean[j]) : (x - mean[j]) * rstd[j];
+    }
+    __device__ __forceinline__ float z(int j, float x) const
+    {
+        return HALF ? __builtin_fmaf(x, gamma[j], beta[j]) : __builtin_fmaf(xhat(j, x), gamma[j], beta[j]);
+    }
+};
+// dx = rstd (gamma dz - c1 - xhat c2), c1 and c2 the group's means of gamma dz and gamma dz xhat; for sixteen bits as
+// dz (gamma rstd) + x a + b
+template <class IO, int MODE>
+struct Slope {
+    Groups<MODE> a, b;                   // HALF: as above; else c1, c2
+    __device__ __forceinline__ void set(int j, float c1, float c2, const Channels<IO, MODE>& k)
+    {
+        if constexpr (Channels<IO, MODE>::HALF) {
+            a[j] = -k.rstd[j] * k.rstd[j] * c2;
+            b[j] = -k.rstd[j] * __builtin_fmaf(k.mean[j], c2, c1);
+        } else {
+            a[j] = c1;
+            b[j] = c2;
+        }
+    }
+    __device__ __forceinline__ float dx(int j, float x, float dz, const Channels<IO, MODE>& k) const
+    {
+        if constexpr (Channels<IO, MODE>::HALF) return __builtin_fmaf(dz, k.gamma[j], __builtin_fmaf(x, a[j], b[j]));
+        else return k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -a[j]) - k.xhat(j, x) * b[j]);
     }
 };
 
@@ -408,8 +455,7 @@ gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restr
             float v[VE];
             raw[u].get(v);
 #pragma unroll
-            for (int j = 0; j < VE; ++j)
-                v[j] = act_of<ACT>(__builtin_fmaf(k.xhat(j, v[j]), k.gamma[j], k.beta[j]));
+            for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
             put<IO, MODE>(p.at(y + p.base, o + u * p.step), p, v);
         }
     }
@@ -443,10 +489,9 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
                 rg[u].get(g);
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
-                    const float h = k.xhat(j, v[j]);
-                    const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
+                    const float dz = g[j] * slope_of<ACT, true>(k.z(j, v[j]));
                     a[j] += dz;
-                    b[j] = __builtin_fmaf(dz, h, b[j]);
+                    b[j] = __builtin_fmaf(dz, k.xhat(j, v[j]), b[j]);
                 }
             }
         }
@@ -557,11 +602,8 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
     const uint32_t D = (uint32_t)(C / G);
     Channels<IO, MODE> k;
     k.load(p, p.b, mean, rstd, gamma, beta, G, D);
-    Groups<MODE> c1, c2;
-    each_group<MODE>(p.c, G, D, [&](int j, uint32_t g) {
-        c1[j] = s1[(size_t)p.b * G + g] * inv;
-        c2[j] = s2[(size_t)p.b * G + g] * inv;
-    });
+    Slope<IO, MODE> of_group;
+    each_group<MODE>(p.c, G, D, [&](int j, uint32_t g) { of_group.set(j, s1[(size_t)p.b * G + g] * inv, s2[(size_t)p.b * G + g] * inv, k); });
     for (uint32_t o = p.off; p.has(o); o += AHEAD / 2 * p.step) {
         Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
 #pragma unroll
@@ -577,9 +619,8 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
             rg[u].get(g);
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                const float h = k.xhat(j, v[j]);
-                const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(h, k.gamma[j], k.beta[j]));
-                v[j] = k.xhat.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - h * c2[j]);
+                const float dz = g[j] * slope_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
+                v[j] = of_group.dx(j, v[j], dz, k);
             }
             put<IO, MODE>(p.at(dx + p.base, o + u * p.step), p, v);
         }
@@ -701,9 +742,8 @@ gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restr
     Raw8<IO> raw[NP];
 #pragma unroll
     for (int u = 0; u < NP; ++u) raw[u].load(p.at(x + p.base, p.piece(u)));
-    float ga[VE], be[VE];
-    load_params(gamma, p, 1.f, ga);
-    load_params(beta, p, 0.f, be);
+    Channels<IO, MODE> k;
+    k.params(p, gamma, beta);
     const auto one = [](uint32_t) { return 1.f; };
     float t[VE] = {};
     Groups<MODE> mn, rs;
@@ -734,9 +774,9 @@ gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restr
     K = sum_rows(t, all, cols, h, p);
     sum_groups(cols, group, K, D, p.W, one, [&](float s) { return 1.f / sqrtf(s / n + eps); });
     in_slab<MODE>(p, G, D, [&](int j, uint32_t g) { rs[j] = group[g]; });
-    Standard<IO, MODE> xhat;
 #pragma unroll
-    for (int j = 0; j < (MODE == ONE ? 1 : VE); ++j) xhat.set(j, mn[j], rs[j]);
+    for (int j = 0; j < (MODE == ONE ? 1 : VE); ++j) k.set(j, mn[j], rs[j]);
+    k.combine();
     if (p.r == 0) {      // the first channel of a group writes its numbers
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
@@ -753,7 +793,7 @@ gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restr
         float v[VE];
         raw[u].get(v);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT>(__builtin_fmaf(xhat(j, v[j]), ga[j], be[j]));
+        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
         put<IO, MODE>(p.at(y + p.base, p.piece(u)), p, v);
     }
 }
@@ -786,10 +826,9 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
         rg[u].get(g);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-            const float xh = k.xhat(j, v[j]);
-            const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(xh, k.gamma[j], k.beta[j]));
+            const float dz = g[j] * slope_of<ACT, true>(k.z(j, v[j]));
             a[j] += dz;
-            b[j] = __builtin_fmaf(dz, xh, b[j]);
+            b[j] = __builtin_fmaf(dz, k.xhat(j, v[j]), b[j]);
         }
     }
     const uint32_t K = sum_rows(a, all, ca, h, p);
@@ -809,11 +848,8 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
     const auto mean_of = [&](float s) { return s * inv; };
     sum_groups(ca, g1, K, D, p.W, weight, mean_of);
     sum_groups(ch, g2, K, D, p.W, weight, mean_of);
-    Groups<MODE> c1, c2;
-    in_slab<MODE>(p, G, D, [&](int j, uint32_t g) {
-        c1[j] = g1[g];
-        c2[j] = g2[g];
-    });
+    Slope<IO, MODE> of_group;
+    in_slab<MODE>(p, G, D, [&](int j, uint32_t g) { of_group.set(j, g1[g], g2[g], k); });
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
         if (!p.has(p.piece(u)) || !p.on) break;
@@ -822,9 +858,8 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
         rg[u].get(g);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-            const float xh = k.xhat(j, v[j]);
-            const float dz = g[j] * slope_of<ACT>(__builtin_fmaf(xh, k.gamma[j], k.beta[j]));
-            v[j] = k.xhat.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -c1[j]) - xh * c2[j]);
+            const float dz = g[j] * slope_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
+            v[j] = of_group.dx(j, v[j], dz, k);
         }
         put<IO, MODE>(p.at(dx + p.base, p.piece(u)), p, v);
     }
