@@ -13,8 +13,10 @@ namespace {
 
 constexpr int RADIX = 512, SORT_T = 256, SORT_W = SORT_T / 64;                  // digits of at most nine bits; threads and waves of a tile
 constexpr int TILE_MIN = 1024, TILES_MAX = 128, ROWS = TILE_MIN / SORT_T;        // tiles of a sorting pass; rows of 64 that a wave asks for at once
-constexpr int ALONE = 4096, ALONE_T = 1024;                                     // tokens that one workgroup sorts by itself, its threads
-constexpr int CHUNK_MIN = 8;                                                    // sorted places of a thread, at least
+// Tokens that one workgroup sorts by itself, and its threads.  8192 (V = 32768, with 100 MB of zeros beside the sort): 20 us, four launches of
+// tiles 30 and the gaps between them; 16384 do not fit its LDS, and took 53 us through memory (tiles 24).
+constexpr int ALONE = 8192, ALONE_T = 1024;
+constexpr int CHUNK_MIN = 8;                                                    // sorted places of a thread, at least (a whole number of AHEADs)
 constexpr int AHEAD = 8;                                                        // rows of dy that a thread asks for before it adds the first
 constexpr int JOIN_GROUPS = 256;                                                // workgroups that join a run's partial sums
 constexpr int JOIN_T = 1024;                                                    // and their threads
@@ -642,9 +644,10 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
     l.tile = TILE_MIN * ((l.M + (int64_t)TILE_MIN * TILES_MAX - 1) / ((int64_t)TILE_MIN * TILES_MAX));
     l.tiles = (l.M + l.tile - 1) / l.tile;
     l.P = (uint32_t)((H + VE - 1) / VE);
-    // long chunks leave few partial sums, short ones make enough threads: at least 2^17 where there are so many
+    // long chunks leave few partial sums, short ones make enough threads: at least 2^16 where there are so many.  Sums and joins, us:
+    // 16384 tokens x 768 16 + 7 in chunks of 16 (98304 threads), 16 + 9 of 8; 2695 x 193 7.8 + 5.7 of 16, 5.8 + 6.8 of 8
     l.chunk = 32;
-    while (l.chunk > CHUNK_MIN && l.M / l.chunk * l.P < (1 << 17)) l.chunk /= 2;
+    while (l.chunk > CHUNK_MIN && l.M / l.chunk * l.P < (1 << 16)) l.chunk /= 2;
     l.chunks = (l.M + l.chunk - 1) / l.chunk;
     int need = 0;
     while (V >> need) ++need;                       // bits of V, the number of no token
@@ -658,8 +661,9 @@ Layout lay_out(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout)
         l.key[i] = take((size_t)(l.M + 32) * sizeof(uint32_t));
         l.pos[i] = take((size_t)(l.M + 32) * sizeof(uint32_t));
     }
-    // (room for the number of chunks that grows with M: those of 32 places, or so many shorter ones that there are 2^17 threads and twice that)
-    const int64_t most = (l.M + CHUNK_MIN - 1) / CHUNK_MIN, some = (l.M + 31) / 32 + ((1 << 18) + l.P - 1) / l.P + 1;
+    // (room for a number of chunks that grows with M: those of 32 places, or shorter ones, that are fewer than 2^17 threads)
+    static_assert(CHUNK_MIN % AHEAD == 0, "a chunk that is not the last has no places left over");
+    const int64_t most = (l.M + CHUNK_MIN - 1) / CHUNK_MIN, some = (l.M + 31) / 32 + ((1 << 17) + l.P - 1) / l.P + 1;
     l.part = take((size_t)(most < some ? most : some) * 2 * l.P * VE * sizeof(float));
     l.joins = take((size_t)((most < some ? most : some) + 1) * 2 * sizeof(uint32_t));
     l.rows = take(layout == LONGCONV_CHANNELS_FIRST ? (size_t)l.M * l.P * VE * (io == LONGCONV_F32 ? 4 : 2) : 0);
