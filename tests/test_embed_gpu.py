@@ -118,6 +118,14 @@ def test_small_vocabularies_in_the_convolutions_layout(io, kind, B, N, V, H, p):
     _backward(_ids(B, N, V, kind, N), V, H, True, io, p, 3)
 
 
+# what one workgroup sorts and what tiles do; runs of few chunks and of many, in rows of one column to rows of several waves
+@pytest.mark.parametrize("M,V,H,io", [(8191, 2000, 9, "fp32"), (8192, 40, 1, "fp32"), (8193, 600, 20, "bf16"), (16384, 3, 70, "fp16"),
+                                      (12000, 5000, 300, "bf16"), (20000, 2, 33, "fp32"), (3000, 2, 515, "bf16")])
+@pytest.mark.parametrize("kind", ["all", "heavy", "one"])
+def test_sorts_and_joins(M, V, H, io, kind):
+    _backward(_ids(1, M, V, kind, M), V, H, False, io, 0.1, 4)
+
+
 def test_wide_rows():
     _backward(_ids(2, 40, 6, "heavy", 1), 6, 5000, False, "bf16", 0.1, 1)
     _backward(_ids(2, 40, 6, "heavy", 1), 6, 5000, True, "bf16", 0.1, 1)

@@ -97,6 +97,20 @@ def test_sizes(io, B, S, C, G):
     r.check()
 
 
+# groups that just fit a workgroup's registers and just do not (pieces of eight channels: 16 of 512 threads forward, 8 backward), and
+# partial results of a group that one wave puts together and that a workgroup does
+@pytest.mark.parametrize("io,act,B,S,C,G", [("bf16", "silu", 1, 2048, 32, 4), ("fp16", "gelu", 2, 2049, 32, 1), ("fp32", "silu", 1, 1024, 16, 1),
+                                            ("fp32", "gelu", 1, 1025, 24, 3), ("bf16", "gelu", 1, 8192, 8, 1), ("bf16", "none", 1, 8193, 8, 1),
+                                            ("fp16", "silu", 1, 3000, 130, 1), ("fp32", "silu", 2, 1500, 104, 2), ("bf16", "silu", 3, 5000, 3, 1),
+                                            ("fp32", "gelu", 1, 4097, 1, 1), ("fp16", "relu", 2, 700, 7, 7), ("bf16", "silu", 1, 2, 1030, 1),
+                                            ("fp32", "none", 1, 1, 2056, 257)])
+def test_where_the_way_through_changes(io, act, B, S, C, G):
+    r = Run(B, S, C, G, io, act, seed=3)
+    r.fwd()
+    r.bwd()
+    r.check()
+
+
 def test_without_parameters():
     r = Run(2, 30, 48, 4, "fp32", "gelu", params=False)
     r.fwd()
