@@ -3,8 +3,9 @@
 // mask value in runs of `tie` (the rows of [B,H,N]: one value for a head's whole sequence).
 //
 // Bound by memory: a thread takes the eight entries of one generator block, sixteen bytes of each tensor (thirty-two in fp32), all asked
-// for before the generator's hundred instructions.  64 x 1024 x 4096 in bf16: 260 us with the residual sum, 168 without, 6.2 and 6.4 TB/s; workgroups
-// of 128, 512 and 1024 threads the same, stores without the nt hint 269 and 165, and 14.2 for 11.8 at 16 x 768 x 1024.
+// for before the generator's hundred instructions.  64 x 1024 x 4096 in bf16: 263 us with the residual sum, 169 without, 6.1 and 6.4 TB/s;
+// workgroups of 128, 512 and 1024 threads within 3 percent.  Stores without the nt hint take 273 and 168 there, and at 16 x 768 x 1024, tied,
+// 15.3 and 11.7 for 12.4 and 9.7.
 #include "vec8.hpp"
 
 namespace lc {

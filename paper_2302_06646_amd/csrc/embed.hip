@@ -5,7 +5,7 @@
 // takes eight columns of a chunk of consecutive sorted places and sums runs of one token in fp32; a run that crosses chunks leaves
 // a partial sum in each, which are added in an order that the run's length gives.  Every row of dy is read once.
 // 16384 tokens x 768 in bf16, V = 32768, dropout 0.1: 46 us, 25 for the bytes (126 MB, most of them zeros of dE): four sorting launches of
-// 5 to 7, bound by their chains of loads, the sums 15 (scattered rows, and the generator), the joins 7.  Small tables of 16-bit rows in
+// 5 to 7, bound by their chains of loads, the sums 16 (scattered rows, and the generator), the joins 7.  Small tables of 16-bit rows in
 // [B,H,N] go through the matrix cores instead (embed_small.hip).
 #include <type_traits>
 

@@ -7,10 +7,10 @@
 // are 0x4000 (2.0 in both types) where the low four bits agree, once for all tiles, and a bit of the set of high four bits, moved under
 // it: two plain instructions a word.  A wave keeps 32 channels by 256 tokens of dE (128 accumulators, two waves a SIMD), its workgroup's
 // four waves share out a range of 32-place steps, and the ranges' sums are added in order by a second kernel.
-// 8 x 16384 tokens x 256 in fp16: 41 us with dropout 0.1, 37 without (sorted: 55); 1024 tokens x 64: 16 (sorted 18).  Bound by vector
-// issue, 450 instructions a step with the generator's two blocks for every lane, 270 without, beside 32 matrix instructions, at two
-// waves a SIMD; 12 us of it are the first loads, the sums in LDS and the ranges' sums (17 MB out and in).  Rows asked for one to four
-// steps ahead make no difference.
+// 8 x 16384 tokens x 256 in fp16: kernels of 44 us with dropout 0.1, 36 without (sorted, with it: 57); 1024 tokens x 64: 16.5 (sorted 17.6).
+// Bound by vector issue, 445 instructions a step with the generator's two blocks for every lane, 311 without, 32 of them matrix instructions,
+// at two waves a SIMD.  About 12 us do not grow with the length (22 and 32 at half and whole length, without dropout): first loads, sums
+// in LDS, the ranges' sums (17 MB out and in).  With rows asked for one to four steps ahead this kernel takes 38.9 to 40.5.
 // What is not finite would reach every token of its channel (0 times infinity): a wave that finds such a sum takes its range's places
 // one by one instead, so that it stays with its token.
 #include "vec8.hpp"
