@@ -233,31 +233,30 @@ __device__ __forceinline__ void each_group(int c, uint32_t G, uint32_t D, F&& f)
         }
 }
 
-// xhat = (x - mean) rstd and z = gamma xhat + beta of a thread's channels.  Where x has sixteen bits, each is one fp32 multiply-add of x,
-// xhat = x rstd - mean rstd and z = x (gamma rstd) + (beta - mean gamma rstd), whose rounding is far below x's own.
-template <class IO, int MODE>
+// d = x - mean, z = (gamma rstd) d + beta and xhat = rstd d of a thread's channels.  The difference comes first, so that an entry that is
+// the mean gives zero and beta: with x rstd - mean rstd, an instruction fewer, a group of one value would leave half a rounding of
+// |mean| rstd, which is 316 |mean| where the variance is zero and eps 1e-5, and relu's slope would be chance.
+template <int MODE>
 struct Channels {
-    static constexpr bool HALF = sizeof(typename IO::T) == 2;
-    Groups<MODE> mean, rstd;             // HALF: mean holds -mean rstd
-    float gamma[VE], beta[VE];           // HALF: gamma rstd, beta - mean gamma rstd
+    Groups<MODE> mean, rstd;
+    float scale[VE], beta[VE];           // scale: gamma, and gamma rstd after combine()
+    float one;                           // 1, which the compiler is not to know: a multiply-add takes a half as it lies, a difference does not
     __device__ __forceinline__ void params(const Piece& p, const float* ga, const float* be)
     {
-        load_params(ga, p, 1.f, gamma);
+        load_params(ga, p, 1.f, scale);
         load_params(be, p, 0.f, beta);
     }
     __device__ __forceinline__ void set(int j, float m, float r)
     {
+        mean[j] = m;
         rstd[j] = r;
-        mean[j] = HALF ? -m * r : m;
     }
     __device__ __forceinline__ void combine()      // after params and set
     {
-        if constexpr (HALF)
 #pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                beta[j] = __builtin_fmaf(mean[j], gamma[j], beta[j]);
-                gamma[j] *= rstd[j];
-            }
+        for (int j = 0; j < VE; ++j) scale[j] *= rstd[j];
+        one = 1.f;
+        asm("" : "+v"(one));
     }
     __device__ __forceinline__ void load(const Piece& p, size_t b, const float* mn, const float* rs, const float* ga, const float* be, uint32_t G,
                                          uint32_t D)
@@ -266,34 +265,32 @@ struct Channels {
         each_group<MODE>(p.c, G, D, [&](int j, uint32_t g) { set(j, mn[b * G + g], rs[b * G + g]); });
         combine();
     }
-    __device__ __forceinline__ float xhat(int j, float x) const
+    __device__ __forceinline__ float d(int j, float x) const { return __builtin_fmaf(x, one, -mean[j]); }
+    __device__ __forceinline__ float z(int j, float x) const { return __builtin_fmaf(d(j, x), scale[j], beta[j]); }
+    // a and b: sums of dz and dz xhat, b until finish() of dz d
+    __device__ __forceinline__ void add(int j, float x, float dz, float (&a)[VE], float (&b)[VE]) const
     {
-        return HALF ? __builtin_fmaf(x, rstd[j], mean[j]) : (x - mean[j]) * rstd[j];
+        a[j] += dz;
+        b[j] = __builtin_fmaf(dz, d(j, x), b[j]);
     }
-    __device__ __forceinline__ float z(int j, float x) const
+    __device__ __forceinline__ void finish(float (&b)[VE]) const
     {
-        return HALF ? __builtin_fmaf(x, gamma[j], beta[j]) : __builtin_fmaf(xhat(j, x), gamma[j], beta[j]);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) b[j] *= rstd[j];
     }
 };
-// dx = rstd (gamma dz - c1 - xhat c2), c1 and c2 the group's means of gamma dz and gamma dz xhat; for sixteen bits as
-// dz (gamma rstd) + x a + b
-template <class IO, int MODE>
+// dx = rstd (gamma dz - c1 - xhat c2), c1 and c2 the group's means of gamma dz and gamma dz xhat
+template <int MODE>
 struct Slope {
-    Groups<MODE> a, b;                   // HALF: as above; else c1, c2
-    __device__ __forceinline__ void set(int j, float c1, float c2, const Channels<IO, MODE>& k)
+    Groups<MODE> c1, c2;                 // times -rstd
+    __device__ __forceinline__ void set(int j, float a, float b, const Channels<MODE>& k)
     {
-        if constexpr (Channels<IO, MODE>::HALF) {
-            a[j] = -k.rstd[j] * k.rstd[j] * c2;
-            b[j] = -k.rstd[j] * __builtin_fmaf(k.mean[j], c2, c1);
-        } else {
-            a[j] = c1;
-            b[j] = c2;
-        }
+        c1[j] = -k.rstd[j] * a;
+        c2[j] = -k.rstd[j] * b;
     }
-    __device__ __forceinline__ float dx(int j, float x, float dz, const Channels<IO, MODE>& k) const
+    __device__ __forceinline__ float dx(int j, float x, float dz, const Channels<MODE>& k) const
     {
-        if constexpr (Channels<IO, MODE>::HALF) return __builtin_fmaf(dz, k.gamma[j], __builtin_fmaf(x, a[j], b[j]));
-        else return k.rstd[j] * (__builtin_fmaf(dz, k.gamma[j], -a[j]) - k.xhat(j, x) * b[j]);
+        return __builtin_fmaf(dz, k.scale[j], __builtin_fmaf(k.d(j, x) * k.rstd[j], c2[j], c1[j]));
     }
 };
 
@@ -449,7 +446,7 @@ gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restr
 {
     const Place p = place<IO>(w, S, C);
     if (!p.on) return;
-    Channels<IO, MODE> k;
+    Channels<MODE> k;
     k.load(p, p.b, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
     for (uint32_t o = p.off; p.has(o); o += AHEAD * p.step) {
         Raw8<IO> raw[AHEAD];
@@ -461,7 +458,7 @@ gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restr
             float v[VE];
             raw[u].get(v);
 #pragma unroll
-            for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
+            for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
             put<IO, MODE>(p.at(y + p.base, o + u * p.step), p, v);
         }
     }
@@ -478,7 +475,7 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
     const Place p = place<IO>(w, S, C);
     float a[VE] = {}, b[VE] = {};
     if (p.on) {
-        Channels<IO, MODE> k;
+        Channels<MODE> k;
         k.load(p, p.b, mean, rstd, gamma, beta, G, (uint32_t)(C / G));
         for (uint32_t o = p.off; p.has(o); o += AHEAD / 2 * p.step) {
             Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
@@ -496,11 +493,11 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
                     const float dz = g[j] * slope_of<ACT, true>(k.z(j, v[j]));
-                    a[j] += dz;
-                    b[j] = __builtin_fmaf(dz, k.xhat(j, v[j]), b[j]);
+                    k.add(j, v[j], dz, a, b);
                 }
             }
         }
+        k.finish(b);
     }
     for (uint32_t half = w.half; half; half >>= 1) {
         __syncthreads();
@@ -606,9 +603,9 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
     const Place p = place<IO>(w, S, C);
     if (!p.on) return;
     const uint32_t D = (uint32_t)(C / G);
-    Channels<IO, MODE> k;
+    Channels<MODE> k;
     k.load(p, p.b, mean, rstd, gamma, beta, G, D);
-    Slope<IO, MODE> of_group;
+    Slope<MODE> of_group;
     each_group<MODE>(p.c, G, D, [&](int j, uint32_t g) { of_group.set(j, s1[(size_t)p.b * G + g] * inv, s2[(size_t)p.b * G + g] * inv, k); });
     for (uint32_t o = p.off; p.has(o); o += AHEAD / 2 * p.step) {
         Raw8<IO> rx[AHEAD / 2], rg[AHEAD / 2];
@@ -625,7 +622,7 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
             rg[u].get(g);
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                const float dz = g[j] * slope_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
+                const float dz = g[j] * slope_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
                 v[j] = of_group.dx(j, v[j], dz, k);
             }
             put<IO, MODE>(p.at(dx + p.base, o + u * p.step), p, v);
@@ -750,7 +747,7 @@ gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restr
     Raw8<IO> raw[NP];
 #pragma unroll
     for (int u = 0; u < NP; ++u) raw[u].load(p.at(x + p.base, p.piece(u)));
-    Channels<IO, MODE> k;
+    Channels<MODE> k;
     k.params(p, gamma, beta);
     const auto one = [](uint32_t) { return 1.f; };
     float t[VE] = {};
@@ -801,7 +798,7 @@ gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restr
         float v[VE];
         raw[u].get(v);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
+        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
         put<IO, MODE>(p.at(y + p.base, p.piece(u)), p, v);
     }
 }
@@ -823,7 +820,7 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
         rx[u].load(p.at(x + p.base, p.piece(u)));
         rg[u].load(p.at(dy + p.base, p.piece(u)));
     }
-    Channels<IO, MODE> k;
+    Channels<MODE> k;
     k.load(p, p.b, mean, rstd, gamma, beta, G, D);
     float a[VE] = {}, b[VE] = {};
 #pragma unroll
@@ -835,10 +832,10 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
             const float dz = g[j] * slope_of<ACT, true>(k.z(j, v[j]));
-            a[j] += dz;
-            b[j] = __builtin_fmaf(dz, k.xhat(j, v[j]), b[j]);
+            k.add(j, v[j], dz, a, b);
         }
     }
+    k.finish(b);
     const uint32_t K = sum_rows(a, all, ca, h, p);
     sum_rows(b, all, ch, h, p);
     for (uint32_t i = threadIdx.x; i < p.W && p.first + (int)i < C; i += blockDim.x) {
@@ -856,7 +853,7 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
     const auto mean_of = [&](float s) { return s * inv; };
     sum_groups(ca, g1, K, D, p.W, weight, mean_of);
     sum_groups(ch, g2, K, D, p.W, weight, mean_of);
-    Slope<IO, MODE> of_group;
+    Slope<MODE> of_group;
     in_slab<MODE>(p, G, D, [&](int j, uint32_t g) { of_group.set(j, g1[g], g2[g], k); });
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
@@ -866,7 +863,7 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
         rg[u].get(g);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-            const float dz = g[j] * slope_of<ACT, !Channels<IO, MODE>::HALF>(k.z(j, v[j]));
+            const float dz = g[j] * slope_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
             v[j] = of_group.dx(j, v[j], dz, k);
         }
         put<IO, MODE>(p.at(dx + p.base, p.piece(u)), p, v);

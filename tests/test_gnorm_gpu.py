@@ -229,3 +229,22 @@ def test_every_way_through_the_binding_gives_the_same_bits():
         setattr(r, name, bad)
         with pytest.raises(lc.LongconvError):
             r.fwd()
+
+
+# groups of one value, however large: each entry is the mean, so xhat is zero and z is beta, to the last bit (sums of so few equal
+# numbers of so few bits are exact); both ways through, and groups of a single entry
+@pytest.mark.parametrize("io", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("value", [100.0, 300.0, -60000.0])
+@pytest.mark.parametrize("B,S,C,G", [(2, 16, 32, 2), (1, 9000, 16, 2), (5, 1, 24, 24), (1, 16, 30, 5)])
+def test_groups_of_one_value_give_beta(io, value, B, S, C, G):
+    r = Run(B, S, C, G, io, "none")
+    r.x.fill_(value)
+    r.fwd()
+    assert torch.equal(r.mean, r.x[:, 0, ::C // G].float())
+    assert torch.equal(r.y, r.beta.to(r.x.dtype).expand(B, S, C))
+    r = Run(B, S, C, G, io, "relu", params=False)
+    r.x.fill_(value)
+    r.fwd()
+    r.bwd()
+    for t in (r.y, r.dx, r.dgamma, r.dbeta):                            # z is zero, where the slope is zero
+        assert (t == 0).all()
