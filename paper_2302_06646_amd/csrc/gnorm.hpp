@@ -24,48 +24,37 @@ constexpr int SLAB = 64;             // pieces of eight channels of a workgroup,
 constexpr int GROUPS_WANTED = 1024;  // workgroups of a pass over the tensor
 constexpr int AHEAD = 4;             // pieces that a thread asks for before it uses the first
 
-// The normal distribution function, and e = exp(-z^2 / 2) beside it.  erfc(x) exp(x^2) is t Q(t), t = 1 / (1 + p x), for x >= 0, Q the
-// polynomial of the least largest relative error (fitted by weighted least squares).  FINE: of degree eight, p = 0.4, 1.3e-7, and 2.2e-7
-// absolute in fp32; below zero the result is not a difference, so its relative error is that of e, 8e-7 down to z = -4.  Otherwise, for
-// results that are rounded to sixteen bits (a relative 4.9e-4 and more): of degree five, p = 0.46, 1.7e-5.
-template <bool FINE>
+// The normal distribution function, and e = exp(-z^2 / 2) beside it.  erfc(x) exp(x^2) is t Q(t), t = 1 / (1 + 0.4 x), for x >= 0, Q the
+// polynomial of degree eight of the least largest relative error (fitted by weighted least squares): 1.3e-7, and 2.2e-7 absolute in
+// fp32.  Below zero the result is not a difference, so its relative error is that of e, 8e-7 down to z = -4.
 __device__ __forceinline__ float normal_cdf(float z, float& e)
 {
-    float q;
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(FINE ? 0.28284271247461901f : 0.3252691328525543f, fabsf(z), 1.f));
-    if constexpr (FINE) {
-        q = __builtin_fmaf(0.025127103552222252f, t, -0.09143677353858948f);
-        q = __builtin_fmaf(q, t, 0.08452295511960983f);
-        q = __builtin_fmaf(q, t, -0.0027893988881260157f);
-        q = __builtin_fmaf(q, t, 0.07071001827716827f);
-        q = __builtin_fmaf(q, t, 0.08427219092845917f);
-        q = __builtin_fmaf(q, t, 0.10392122715711594f);
-        q = __builtin_fmaf(q, t, 0.11283480376005173f);
-        q = __builtin_fmaf(q, t, 0.11283793300390244f);
-    } else {
-        q = __builtin_fmaf(-0.06317603588104248f, t, 0.12090080231428146f);
-        q = __builtin_fmaf(q, t, 0.06272530555725098f);
-        q = __builtin_fmaf(q, t, 0.12026208639144897f);
-        q = __builtin_fmaf(q, t, 0.12951715290546417f);
-        q = __builtin_fmaf(q, t, 0.1297658532857895f);
-    }
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.28284271247461901f, fabsf(z), 1.f));
+    float q = __builtin_fmaf(0.025127103552222252f, t, -0.09143677353858948f);
+    q = __builtin_fmaf(q, t, 0.08452295511960983f);
+    q = __builtin_fmaf(q, t, -0.0027893988881260157f);
+    q = __builtin_fmaf(q, t, 0.07071001827716827f);
+    q = __builtin_fmaf(q, t, 0.08427219092845917f);
+    q = __builtin_fmaf(q, t, 0.10392122715711594f);
+    q = __builtin_fmaf(q, t, 0.11283480376005173f);
+    q = __builtin_fmaf(q, t, 0.11283793300390244f);
     e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
     const float h = q * t * e;      // (half of erfc: the factor is in Q)
     return z < 0.f ? h : 1.f - h;
 }
 
-template <int ACT, bool FINE>
+template <int ACT>
 __device__ __forceinline__ float act_of(float z)
 {
     if constexpr (ACT == LONGCONV_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
     if constexpr (ACT == LONGCONV_ACT_GELU) {
         float e;
-        return z * normal_cdf<FINE>(z, e);
+        return z * normal_cdf(z, e);
     }
     if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
     return z;
 }
-template <int ACT, bool FINE>
+template <int ACT>
 __device__ __forceinline__ float slope_of(float z)
 {
     if constexpr (ACT == LONGCONV_ACT_SILU) {
@@ -74,7 +63,7 @@ __device__ __forceinline__ float slope_of(float z)
     }
     if constexpr (ACT == LONGCONV_ACT_GELU) {
         float e;
-        const float c = normal_cdf<FINE>(z, e);
+        const float c = normal_cdf(z, e);
         return __builtin_fmaf(z * 0.39894228040143268f, e, c);
     }
     if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? 1.f : 0.f;
@@ -458,7 +447,7 @@ gnorm_apply_kernel(const typename IO::T* __restrict__ x, typename IO::T* __restr
             float v[VE];
             raw[u].get(v);
 #pragma unroll
-            for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
+            for (int j = 0; j < VE; ++j) v[j] = act_of<ACT>(k.z(j, v[j]));
             put<IO, MODE>(p.at(y + p.base, o + u * p.step), p, v);
         }
     }
@@ -492,7 +481,7 @@ gnorm_sums_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* _
                 rg[u].get(g);
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
-                    const float dz = g[j] * slope_of<ACT, true>(k.z(j, v[j]));
+                    const float dz = g[j] * slope_of<ACT>(k.z(j, v[j]));
                     k.add(j, v[j], dz, a, b);
                 }
             }
@@ -622,7 +611,7 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
             rg[u].get(g);
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                const float dz = g[j] * slope_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
+                const float dz = g[j] * slope_of<ACT>(k.z(j, v[j]));
                 v[j] = of_group.dx(j, v[j], dz, k);
             }
             put<IO, MODE>(p.at(dx + p.base, o + u * p.step), p, v);
@@ -798,7 +787,7 @@ gnorm_hold_fwd_kernel(const typename IO::T* __restrict__ x, const float* __restr
         float v[VE];
         raw[u].get(v);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
+        for (int j = 0; j < VE; ++j) v[j] = act_of<ACT>(k.z(j, v[j]));
         put<IO, MODE>(p.at(y + p.base, p.piece(u)), p, v);
     }
 }
@@ -831,7 +820,7 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
         rg[u].get(g);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-            const float dz = g[j] * slope_of<ACT, true>(k.z(j, v[j]));
+            const float dz = g[j] * slope_of<ACT>(k.z(j, v[j]));
             k.add(j, v[j], dz, a, b);
         }
     }
@@ -863,7 +852,7 @@ gnorm_hold_bwd_kernel(const typename IO::T* __restrict__ dy, const typename IO::
         rg[u].get(g);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-            const float dz = g[j] * slope_of<ACT, sizeof(typename IO::T) == 4>(k.z(j, v[j]));
+            const float dz = g[j] * slope_of<ACT>(k.z(j, v[j]));
             v[j] = of_group.dx(j, v[j], dz, k);
         }
         put<IO, MODE>(p.at(dx + p.base, p.piece(u)), p, v);

@@ -248,3 +248,15 @@ def test_groups_of_one_value_give_beta(io, value, B, S, C, G):
     r.bwd()
     for t in (r.y, r.dx, r.dgamma, r.dbeta):                            # z is zero, where the slope is zero
         assert (t == 0).all()
+
+
+@pytest.mark.parametrize("S", [64, 20000])
+def test_results_in_sixteen_bits_are_rounded_once(S):
+    # Data of mean zero: z is good to a few roundings of fp32, and so is gelu(z).  A result with a relative error of 8 U before its one
+    # rounding differs from the exact value's rounding if that lies within 8 U of a midpoint of fp16 (2^-11 apart at least): 16 U / 2^-11.
+    half = torch.randn(1, S // 2, 64, generator=torch.Generator().manual_seed(5))
+    r = Run(1, S, 64, 8, "fp16", "gelu", params=False)
+    r.x = torch.cat([half, -half], 1).half().cuda()
+    r.fwd()
+    want = gnorm.gnorm_fwd(_np(r.x), np.ones(64), np.zeros(64), 8, EPS, "gelu")[0].astype(np.float16)
+    assert (r.y.cpu().numpy() != want).mean() <= 16 * U * 2 ** 11
