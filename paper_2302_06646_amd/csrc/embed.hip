@@ -536,7 +536,7 @@ embed_sum_kernel(const typename IO::T* __restrict__ dy, const uint32_t* __restri
 // Runs over several chunks: their partial sums, four columns a lane and, where a row has fewer than 256, several chunks side by side in
 // a wave; in an order that the run's length alone gives.  Most runs are of two or three chunks: a wave takes one (of 256 columns).
 // Those that would take it more than LONG_RUN steps (common tokens) it leaves to its whole workgroup, whose waves take the chunks in
-// turn and whose sums are then added in order.
+// turn and whose sums are then added in order.  All that are long go that way: the workgroup's list is emptied before it can overflow.
 constexpr uint32_t LONG_RUN = 8;
 __global__ void __launch_bounds__(JOIN_T)
 embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ part, const uint32_t* __restrict__ joins, float* __restrict__ dE,
@@ -547,8 +547,6 @@ embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ pa
     __shared__ uint32_t longs[LIST], count;
     const uint32_t blocks = (P * 2 + wide - 1) / wide, items = joins[0] * blocks, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     const uint32_t side = 64 / wide, mine = lane / wide;      // chunks of a wave at once; the lane's among them
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
     // the last chunk of a run, the last that begins with its token: the lanes look at the next 64, and, if all do, at 64 places of what is
     // left at a time
     const auto last_chunk = [&](uint2 run) {
@@ -589,46 +587,48 @@ embed_join_kernel(const uint32_t* __restrict__ key, const float* __restrict__ pa
         }
     };
     const uint2* runs = reinterpret_cast<const uint2*>(joins + 2);
-    for (uint32_t item = wave * gridDim.x + blockIdx.x; item < items; item += gridDim.x * WAVES) {      // (a run's columns to several workgroups)
-        const uint2 run = runs[item / blocks];
-        const uint32_t chunk = run.x, col = item % blocks * wide + lane % wide;
-        uint32_t q = chunk + mine;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        add(s, chunk, q, chunk + 1, side, col);      // (the two there always are, asked for beside the search)
-        const uint32_t last = last_chunk(run);
-        if (last - chunk > LONG_RUN * side) {
-            uint32_t slot = 0;
-            if (lane == 0) slot = atomicAdd(&count, 1u);
-            slot = (uint32_t)__shfl((int)slot, 0);
-            if (slot < LIST) {
-                if (lane == 0) longs[slot] = item;
+    const uint32_t round = gridDim.x * LIST;      // items of all workgroups in a round: LIST of each, so that its list holds all that are long
+    for (uint32_t begin = 0; begin < items; begin += round) {
+        const uint32_t end = items - begin < round ? items : begin + round;
+        if (threadIdx.x == 0) count = 0;
+        __syncthreads();
+        for (uint32_t item = begin + wave * gridDim.x + blockIdx.x; item < end; item += gridDim.x * WAVES) {      // (a run's columns to several workgroups)
+            const uint2 run = runs[item / blocks];
+            const uint32_t chunk = run.x, col = item % blocks * wide + lane % wide;
+            uint32_t q = chunk + mine;
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            add(s, chunk, q, chunk + 1, side, col);      // (the two there always are, asked for beside the search)
+            const uint32_t last = last_chunk(run);
+            if (last - chunk > LONG_RUN * side) {
+                if (lane == 0) longs[atomicAdd(&count, 1u)] = item;
                 continue;
             }
-        }
-        add(s, chunk, q, last, side, col);
-        side_by_side(s);
-        write(s, run.y, col);
-    }
-    __syncthreads();
-    const uint32_t n = count < LIST ? count : LIST;
-    for (uint32_t i = 0; i < n; ++i) {
-        const uint32_t item = longs[i], col = item % blocks * wide + lane % wide;
-        const uint2 run = runs[item / blocks];
-        const uint32_t chunk = run.x, last = last_chunk(run);
-        uint32_t q = chunk + wave * side + mine;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        add(s, chunk, q, last, WAVES * side, col);
-        side_by_side(s);
-        sums[wave][lane] = s;
-        __syncthreads();
-        if (wave == 0) {
-            for (uint32_t w = 1; w < WAVES; ++w) {
-                const float4 v = sums[w][lane];
-                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-            }
+            add(s, chunk, q, last, side, col);
+            side_by_side(s);
             write(s, run.y, col);
         }
         __syncthreads();
+        const uint32_t n = count;
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t item = longs[i], col = item % blocks * wide + lane % wide;
+            const uint2 run = runs[item / blocks];
+            const uint32_t chunk = run.x, last = last_chunk(run);
+            uint32_t q = chunk + wave * side + mine;
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            add(s, chunk, q, last, WAVES * side, col);
+            side_by_side(s);
+            sums[wave][lane] = s;
+            __syncthreads();
+            if (wave == 0) {
+                for (uint32_t w = 1; w < WAVES; ++w) {
+                    const float4 v = sums[w][lane];
+                    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+                }
+                write(s, run.y, col);
+            }
+            __syncthreads();
+        }
+        __syncthreads();      // (the list is read before the next round's begins)
     }
 }
 

@@ -244,3 +244,21 @@ def test_every_way_through_the_binding_gives_the_same_bits():
         lc.longconv_embed_fwd(ids, E.half(), dy, 1.0)                   # neither fp32 nor the rows' type
     with pytest.raises(lc.LongconvError):
         lc.longconv_embed_bwd(dy, ids, E, 1.0, lc.CHANNELS_LAST, ws[:100])
+
+
+def test_more_long_runs_than_a_workgroup_notes_down():
+    # 288 tokens of 640 places each (20 chunks of 32 and the ends of one), in rows of 255 pieces of 256 columns: about 287 long runs for
+    # each workgroup that joins them.  The order of a sum is that of its run's length alone, whatever else is joined: that of the first
+    # 256 columns by themselves, where no workgroup has more than two.
+    V, each, H = 288, 640, 255 * 256
+    ids = (torch.randperm(V * each, generator=torch.Generator().manual_seed(1)) % V)[None].cuda()
+    dy = torch.empty(1, V * each, H, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(2))
+    dE = torch.empty(V, H, device="cuda")
+    ws = lc.new_workspace_embed(1, V * each, V, H, lc.BF16)
+    lc.longconv_embed_bwd(dy, ids, dE, 1.0, lc.CHANNELS_LAST, ws)
+    for at in (0, 256 * 100, H - 256):
+        narrow = torch.empty(V, 256, device="cuda")
+        lc.longconv_embed_bwd(dy[:, :, at:at + 256].contiguous(), ids, narrow, 1.0, lc.CHANNELS_LAST, ws)
+        assert torch.equal(dE[:, at:at + 256], narrow)
+    del dy, ws
+    torch.cuda.empty_cache()
