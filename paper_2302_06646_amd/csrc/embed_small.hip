@@ -2,17 +2,17 @@
 // the tokens' one-hot matrix on the matrix cores,
 //     dE[v,h] = f . sum over (b,t) of dy[b,h,t] [ids[b,t] = v],
 // where dy's rows are the left operand as they lie in memory and the right one is made in registers from the tokens.  Its entries are 0
-// and 2 (taken back with f), so the products are exact and the sums those of fp32; dy is read once, nothing is sorted and nothing
-// transposed.  For a tile of tokens 16 j .. 16 j + 15 a lane needs [token = 16 j + lane mod 16] at eight places: a word of two halves that
-// are 0x4000 (2.0 in both types) where the low four bits agree, once for all tiles, and a bit of the set of high four bits, moved under
-// it: two plain instructions a word.  A wave keeps 32 channels by 256 tokens of dE (128 accumulators, two waves a SIMD), its workgroup's
-// four waves share out a range of 32-place steps, and the ranges' sums are added in order by a second kernel.
+// and 2 (the sums are halved as they leave the registers), so the products are exact and the sums those of fp32; dy is read once, nothing
+// is sorted and nothing transposed.  For a tile of tokens 16 j .. 16 j + 15 a lane needs [token = 16 j + lane mod 16] at eight places: a
+// word of two halves that are 0x4000 (2.0 in both types) where the low four bits agree, once for all tiles, and a bit of the set of high
+// four bits, moved under it: two plain instructions a word.  A wave keeps 32 channels by 256 tokens of dE (128 accumulators, two waves a
+// SIMD), its workgroup's four waves share out a range of 32-place steps, and the ranges' sums are added in order by a second kernel.
 // 8 x 16384 tokens x 256 in fp16: kernels of 44 us with dropout 0.1, 36 without (sorted, with it: 57); 1024 tokens x 64: 16.5 (sorted 17.6).
 // Bound by vector issue, 445 instructions a step with the generator's two blocks for every lane, 311 without, 32 of them matrix instructions,
 // at two waves a SIMD.  About 12 us do not grow with the length (22 and 32 at half and whole length, without dropout): first loads, sums
 // in LDS, the ranges' sums (17 MB out and in).  With rows asked for one to four steps ahead this kernel takes 38.9 to 40.5.
-// What is not finite would reach every token of its channel (0 times infinity): a wave that finds such a sum takes its range's places
-// one by one instead, so that it stays with its token.
+// What is not finite would reach every token of its channel (0 times infinity), and twice a sum may pass the range of bf16 and fp32 where
+// the sum does not: a wave that finds such a sum takes its range's places one by one instead, so that it stays with its token.
 #include "vec8.hpp"
 
 namespace lc {
@@ -214,7 +214,8 @@ embed_small_kernel(const typename IO::T* __restrict__ dy, const ID* __restrict__
 #pragma unroll
                     for (int j = 0; j < VT; ++j) {
                         float4* q = reinterpret_cast<float4*>(sums + (16 * j + n) * (CH + PAD) + 16 * m + 4 * group);
-                        float4 t = make_float4(acc[m][j][0], acc[m][j][1], acc[m][j][2], acc[m][j][3]);
+                        const mu::f4 half = acc[m][j] * 0.5f;      // (exact: they are multiples of 2^-132, twice bf16's smallest number)
+                        float4 t = make_float4(half[0], half[1], half[2], half[3]);
                         if (w) {
                             const float4 o = *q;
                             t = make_float4(o.x + t.x, o.y + t.y, o.z + t.z, o.w + t.w);
@@ -231,7 +232,7 @@ embed_small_kernel(const typename IO::T* __restrict__ dy, const ID* __restrict__
                         const ID v = ids[(size_t)b * N + t];
                         if (!(v >= 0 && v < (ID)V) || lane >= CH || h0 + lane >= H) continue;
                         const size_t e = ((size_t)b * H + h0 + lane) * N + t;
-                        if (!DROP || (kept8(e >> 3, d, call) >> (e & 7u) & 1u)) sums[(uint32_t)v * (CH + PAD) + lane] += 2.f * IO::ld(dy, e);
+                        if (!DROP || (kept8(e >> 3, d, call) >> (e & 7u) & 1u)) sums[(uint32_t)v * (CH + PAD) + lane] += IO::ld(dy, e);
                     }
                 }
             }
@@ -291,7 +292,7 @@ hipError_t run(const EmbedArgs& a, const void* dy, float* dE, float* part, hipSt
     const auto kernel = a.drop.threshold ? embed_small_kernel<IO, ID, true> : embed_small_kernel<IO, ID, false>;
     hipLaunchKernelGGL(kernel, g, dim3(64 * WAVES), 0, st, (const typename IO::T*)dy, (const ID*)a.ids, part, (uint32_t)a.N, (uint32_t)a.H,
                        (uint32_t)a.V, s, a.drop);
-    hipLaunchKernelGGL(embed_small_sum_kernel, gs, dim3(SUM_T), 0, st, (const float*)part, dE, (uint32_t)a.H, (uint32_t)a.V, 0.5f * a.scale * a.drop.scale, s);
+    hipLaunchKernelGGL(embed_small_sum_kernel, gs, dim3(SUM_T), 0, st, (const float*)part, dE, (uint32_t)a.H, (uint32_t)a.V, a.scale * a.drop.scale, s);
     return hipGetLastError();
 }
 

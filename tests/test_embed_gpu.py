@@ -262,3 +262,17 @@ def test_more_long_runs_than_a_workgroup_notes_down():
         assert torch.equal(dE[:, at:at + 256], narrow)
     del dy, ws
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("V", [40, 300])
+@pytest.mark.parametrize("size", [1.1e38, 3e-39])
+def test_gradients_at_the_ends_of_the_range(first, V, size):
+    # sums of two that fit fp32, though twice as much would not; and of two below the normal range
+    ids = torch.arange(16, device="cuda").remainder_(8)[None]
+    shape = (1, 24, 16) if first else (1, 16, 24)
+    dy = (size * (0.5 + torch.rand(*shape, generator=torch.Generator().manual_seed(1)))).to(torch.bfloat16).cuda()
+    dE = torch.empty(V, 24, device="cuda")
+    lc.longconv_embed_bwd(dy, ids, dE, 1.0, _layout(first), lc.new_workspace_embed(1, 16, V, 24, lc.BF16, _layout(first)))
+    want = embed.embed_bwd(_np(dy), _np(ids).astype(np.int64), V, 1.0, first)
+    assert (np.abs(_np(dE) - want) <= 2 * U * np.abs(want) + 2.0 ** -149).all()
