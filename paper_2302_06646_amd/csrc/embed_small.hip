@@ -13,6 +13,7 @@
 // in LDS, the ranges' sums (17 MB out and in).  With rows asked for one to four steps ahead this kernel takes 38.9 to 40.5.
 // What is not finite would reach every token of its channel (0 times infinity), and twice a sum may pass the range of bf16 and fp32 where
 // the sum does not: a wave that finds such a sum takes its range's places one by one instead, so that it stays with its token.
+// 228 us where every wave does so, 71 where one of them does, for 43.
 #include "vec8.hpp"
 
 namespace lc {
@@ -225,14 +226,33 @@ embed_small_kernel(const typename IO::T* __restrict__ dy, const ID* __restrict__
             } else {
                 if (w == 0)
                     for (int i = lane; i < ROOM; i += 64) sums[i] = 0.f;
-                __threadfence_block();
+                // Tokens and rows of a step are asked for before the first is added; then a lane adds to its channel's column of the
+                // table, place by place: LDS takes a wave's additions in order, and none waits for another.
+                const bool there = lane < CH && h0 + lane < H;
                 for (uint32_t step = from; step < to; ++step) {
-                    const uint32_t b = step / s.of_row, t0 = (step - b * s.of_row) * 32;
-                    for (uint32_t t = t0; t < t0 + 32 && t < N; ++t) {
-                        const ID v = ids[(size_t)b * N + t];
-                        if (!(v >= 0 && v < (ID)V) || lane >= CH || h0 + lane >= H) continue;
-                        const size_t e = ((size_t)b * H + h0 + lane) * N + t;
-                        if (!DROP || (kept8(e >> 3, d, call) >> (e & 7u) & 1u)) sums[(uint32_t)v * (CH + PAD) + lane] += IO::ld(dy, e);
+                    const uint32_t b = step / s.of_row, t0 = (step - b * s.of_row) * 32, here = N - t0 < 32 ? N - t0 : 32;
+                    const ID v = ids[(size_t)b * N + t0 + (lane & 31u) % here];
+                    const uint32_t token = v >= 0 && v < (ID)V ? (uint32_t)v : V;
+                    const size_t e = ((size_t)b * H + h0 + (there ? lane : 0)) * N + t0;
+                    float x[32];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        Raw8<IO> r;
+                        load_raw<IO>(dy + e + VE * q, (int)here - VE * q, r);
+                        if constexpr (DROP) {
+                            const uint4 k = kept_words_at(e + VE * q, d, call);
+                            r.w[0] &= k.x; r.w[1] &= k.y; r.w[2] &= k.z; r.w[3] &= k.w;
+                        }
+                        float y[VE];
+                        r.get(y);
+#pragma unroll
+                        for (int j = 0; j < VE; ++j) x[VE * q + j] = y[j];
+                    }
+#pragma unroll
+                    for (uint32_t i = 0; i < 32; ++i) {
+                        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)token, (int)i);
+                        if (i < here && at < V && there)
+                            __hip_atomic_fetch_add(sums + at * (CH + PAD) + lane, x[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     }
                 }
             }

@@ -276,3 +276,31 @@ def test_gradients_at_the_ends_of_the_range(first, V, size):
     lc.longconv_embed_bwd(dy, ids, dE, 1.0, _layout(first), lc.new_workspace_embed(1, 16, V, 24, lc.BF16, _layout(first)))
     want = embed.embed_bwd(_np(dy), _np(ids).astype(np.int64), V, 1.0, first)
     assert (np.abs(_np(dE) - want) <= 2 * U * np.abs(want) + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("bad", ["one for each channel", "all"])
+def test_columns_that_are_not_finite_cost_a_few_times_as_much(bad):
+    # An overflow under loss scaling is an ordinary step.  Places taken one by one from memory, a workgroup's waves in turn, would wait
+    # for it two thousand times here, about a hundred times the product's time.
+    B, N, V, H = 8, 16384, 256, 256
+    ids = torch.randint(0, V, (B, N), generator=torch.Generator().manual_seed(1)).cuda()
+    clean = _randn((B, H, N), torch.float16, 2)
+    dy = clean.clone()
+    if bad == "all":
+        dy.fill_(float("nan"))
+    else:
+        dy[:, :, 5::512] = float("inf")                                 # in every wave's share of every channel
+    dE = torch.empty(V, H, device="cuda")
+    ws = lc.new_workspace_embed(B, N, V, H, lc.F16, lc.CHANNELS_FIRST)
+
+    def time(t):
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
+        for _ in range(5):
+            lc.longconv_embed_bwd(t, ids, dE, 1.0, lc.CHANNELS_FIRST, ws, 0.1, 1, 2)
+        end.record()
+        end.synchronize()
+        return start.elapsed_time(end) / 5
+
+    times = [(time(clean), time(dy)) for _ in range(6)][1:]
+    assert min(t[1] for t in times) < 8 * min(t[0] for t in times), times
