@@ -310,7 +310,7 @@ typedef enum {
  * neighbouring channels each, statistics over a group's channels and all positions of one b:
  *     y = act(gamma[c] (x - mean[b,g]) rstd[b,g] + beta[c]),      rstd = 1 / sqrt(variance + eps)
  * gamma, beta [C] float32, each may be NULL (ones, zeros).  mean, rstd [B,G] float32 are written and are what the backward pass
- * reads.  eps >= 0 and finite.  1 <= G, G divides C, C <= 65535, B C <= 2^25, B S C <= 2^34. */
+ * reads.  eps >= 0 and finite.  1 <= G, G divides C, C <= 65535, B < 2^23, B C <= 2^25, B S C <= 2^34. */
 size_t longconv_gnorm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t G, int io, int backward);
 int longconv_gnorm_fwd(const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, int64_t B, int64_t S,
                        int64_t C, int64_t G, float eps, int act, int io, void* workspace, size_t workspace_bytes, void* stream);

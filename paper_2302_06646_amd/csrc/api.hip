@@ -972,6 +972,7 @@ static int check_gnorm(int64_t B, int64_t S, int64_t C, int64_t G, int io)
 {
     if (bad_dtype(io)) return LONGCONV_ERR_DTYPE;
     if (B < 1 || S < 1 || C < 1 || C > 65535 || G < 1 || G > C || C % G) return LONGCONV_ERR_SHAPE;
+    if (B >= (int64_t(1) << 23)) return LONGCONV_ERR_SHAPE;      // (a workgroup of 512 threads for each where C < 8, in one launch)
     if (B > (int64_t(1) << 25) / C || S > MAX_ELEMENTS / (B * C)) return LONGCONV_ERR_SHAPE;
     return LONGCONV_OK;
 }

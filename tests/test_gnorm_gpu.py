@@ -260,3 +260,29 @@ def test_results_in_sixteen_bits_are_rounded_once(S):
     r.fwd()
     want = gnorm.gnorm_fwd(_np(r.x), np.ones(64), np.zeros(64), 8, EPS, "gelu")[0].astype(np.float16)
     assert (r.y.cpu().numpy() != want).mean() <= 16 * U * 2 ** 11
+
+
+def test_as_many_sequences_as_a_launch_takes():
+    B, S, C, G = (1 << 23) - 1, 2, 4, 2
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.randn(B, S, C, generator=gen, device="cuda") for _ in range(2))
+
+    def step(x, dy):
+        out = [torch.full_like(x, 7.0) for _ in range(2)] + [torch.full((len(x), G), 7.0, device="cuda") for _ in range(2)]
+        sums = [torch.empty(C, device="cuda") for _ in range(2)]
+        ws = lc.new_workspace_gnorm(len(x), S, C, G, lc.F32, True)
+        lc.longconv_gnorm_fwd(x, None, None, out[0], *out[2:], EPS, "silu", ws)
+        lc.longconv_gnorm_bwd(dy, x, None, None, *out[2:], out[1], *sums, "silu", ws)
+        return out, sums
+
+    out, (dgamma, dbeta) = step(x, dy)
+    for at in (slice(0, 1000), slice(B // 2, B // 2 + 1000), slice(B - 1000, B)):      # each of the B by itself
+        few, _ = step(x[at].clone(), dy[at].clone())
+        assert all(torch.equal(a[at], b) for a, b in zip(out, few))
+    # a thread adds 2^17 numbers of both signs: as in test_gradients_past_32_bits, about one U of the sum of magnitudes; 64 are allowed
+    each = lambda t: t.double().repeat_interleave(C // G, 1)[:, None]  # noqa: E731
+    xhat = (x.double() - each(out[2])) * each(out[3])
+    q = torch.sigmoid(xhat)
+    dz = dy.double() * q * (1 + xhat * (1 - q))
+    assert ((dbeta - dz.sum((0, 1))).abs() <= 64 * U * dy.abs().double().sum((0, 1)) * 1.13).all()
+    assert ((dgamma - (dz * xhat).sum((0, 1))).abs() <= 64 * U * (dy.double() * (1 + xhat.abs())).abs().sum((0, 1)) * 1.13).all()

@@ -109,3 +109,14 @@ def test_the_binding_refuses_host_tensors_and_unknown_names():
         lc.longconv_gnorm_fwd(x, None, None, x, s, s, 1e-5, "silu", s)
     with pytest.raises(KeyError):
         lc.longconv_gnorm_fwd(x, None, None, x, s, s, 1e-5, "tanh", s)
+
+
+def test_group_norm_takes_as_many_sequences_as_a_launch_does():
+    # a launch has fewer than 2^32 threads, and rows of fewer than eight channels take a workgroup of 512 for each of the B
+    L = lc.lib()
+    for C, G in ((1, 1), (3, 1), (4, 2)):
+        assert lc.longconv_gnorm_workspace_bytes((1 << 23) - 1, 2, C, G, lc.F32, True) > 0
+        for B in (1 << 23, 1 << 24):
+            assert lc.longconv_gnorm_workspace_bytes(B, 2, C, G, lc.F32, True) == 0
+            assert L.longconv_gnorm_fwd(A, A, A, A, A, A, B, 2, C, G, 1e-5, 1, 0, A, BIG, None) == SHAPE
+            assert L.longconv_gnorm_bwd(A, A, A, A, A, A, A, A, A, B, 2, C, G, 1, 0, A, BIG, None) == SHAPE
