@@ -61,7 +61,7 @@ class Classifier:
         lc.longconv_dropout_fwd(self.y, self.x1, self.tied_drop, self.seed, call + 2, residual=self.x0, tie=self.N)
         self.t = self.x1.transpose(1, 2).contiguous()
         lc.longconv_gnorm_fwd(self.t, p["gamma"], p["beta"], self.z, self.mean, self.rstd, self.eps, "silu", self.ws_gnorm)
-        self.there = (tokens >= 0).float() / (tokens >= 0).sum(1, keepdim=True)
+        self.there = (tokens >= 0).float() / (tokens >= 0).sum(1, keepdim=True).clamp(min=1)      # (none: nothing is pooled)
         self.pooled = (self.z.float() * self.there[..., None]).sum(1)
         return self.pooled @ p["head"]
 

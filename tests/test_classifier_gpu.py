@@ -50,3 +50,21 @@ def test_a_step_against_the_oracles():
 
 def test_it_learns():
     assert classifier.main(["--steps", "60", "--batch", "16", "--length", "512", "--width", "32"]) < 0.7
+
+
+def test_a_sequence_without_a_byte():
+    B, N, H = 3, 256, 16
+    runs = []
+    for rows in (slice(0, 3), slice(0, 2)):                             # with the empty sequence, and without it
+        m = classifier.Classifier(len(range(B)[rows]), N, H, 4, 2, dtype=torch.float32, seed=7, drop=0.0, kernel_drop=0.0, tied_drop=0.0)
+        tokens, _ = classifier.batch(B, N, 4, torch.Generator(device="cuda").manual_seed(2))
+        tokens[2] = -1
+        tokens = tokens[rows].contiguous()
+        logits = m.forward(tokens, 0)
+        dlogits = torch.randn(B, 4, generator=torch.Generator().manual_seed(3)).cuda()[rows].contiguous()
+        m.backward(dlogits, tokens, 0)
+        runs.append((logits, {k: p.grad.clone() for k, p in m.p.items()}))
+    (logits, grads), (logits2, grads2) = runs
+    assert (logits[2] == 0).all() and _rel(_np(logits[:2]), _np(logits2)) < 1e-5      # nothing is pooled, and the others do not notice
+    for name in grads:
+        assert _rel(_np(grads[name]), _np(grads2[name])) < 1e-5, name
