@@ -286,3 +286,51 @@ def test_as_many_sequences_as_a_launch_takes():
     dz = dy.double() * q * (1 + xhat * (1 - q))
     assert ((dbeta - dz.sum((0, 1))).abs() <= 64 * U * dy.abs().double().sum((0, 1)) * 1.13).all()
     assert ((dgamma - (dz * xhat).sum((0, 1))).abs() <= 64 * U * (dy.double() * (1 + xhat.abs())).abs().sum((0, 1)) * 1.13).all()
+
+
+@pytest.mark.parametrize("io", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("B,S,C,G", [(2, 64, 24, 3), (1, 9000, 16, 2), (3, 50, 195, 5)])
+def test_relu_gradients_where_no_entry_is_near_zero(io, B, S, C, G):
+    r = Run(B, S, C, G, io, "relu", seed=6)
+    sign = torch.where(torch.rand(r.x.shape, generator=torch.Generator().manual_seed(7)) < 0.5, -1.0, 1.0)
+    r.x = (sign * (1.5 + torch.rand(r.x.shape, generator=torch.Generator().manual_seed(8)))).to(r.x.dtype).cuda()
+    r.gamma, r.beta = (torch.where(r.gamma < 1, -1.0, 1.0) * (0.5 + (r.gamma - 1).abs())).contiguous(), torch.zeros_like(r.beta)
+    x = _np(r.x)
+    mean, rstd = (np.repeat(a, C // G, 1)[:, None] for a in gnorm.statistics(x, G, EPS))
+    assert np.abs((x - mean) * rstd * _np(r.gamma)).min() > 0.1         # (check() passes over gradients where one is near)
+    r.fwd()
+    r.bwd()
+    r.check()
+
+
+def test_gradients_past_32_bits():
+    B, S, C, G = 3, 1 << 20, 1376, 8                                    # 4.3e9 elements
+    D, tail = C // G, 4096
+    x, dy = (torch.zeros(B, S, C, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t, seed in ((x, 1), (dy, 2)):
+        t[B - 1].normal_(generator=torch.Generator(device="cuda").manual_seed(seed))
+    y, dx = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    mean, rstd, dgamma, dbeta = (torch.empty(*s, device="cuda") for s in ((B, G), (B, G), (C,), (C,)))
+    ws = lc.new_workspace_gnorm(B, S, C, G, lc.BF16, True)
+    lc.longconv_gnorm_fwd(x, None, None, y, mean, rstd, EPS, "none", ws)
+    lc.longconv_gnorm_bwd(dy, x, None, None, mean, rstd, dx, dgamma, dbeta, "none", ws)
+    assert all((t[:B - 1] == 0).all() for t in (y, dx))
+    # Sums in 64 bits, a group at a time.  A thread adds about 1200 numbers one by one, of both signs: their sums stay near the root of
+    # their number, so the roundings come to about one U of the sum of magnitudes; 64 are allowed, as in check().
+    for g in range(G):
+        c = slice(g * D, g * D + D)
+        xg, dg = x[B - 1, :, c].double(), dy[B - 1, :, c].double()
+        m, v = xg.mean(), xg.var(unbiased=False)
+        xhat = (xg - m) * (v + EPS) ** -0.5
+        K = 64 * U
+        assert ((dbeta[c].double() - dg.sum(0)).abs() <= K * dg.abs().sum(0)).all()
+        assert ((dgamma[c].double() - (dg * xhat).sum(0)).abs() <= K * (dg.abs() * (1 + xhat.abs())).sum(0)).all()
+        want = (v + EPS) ** -0.5 * (dg - dg.mean() - xhat * (dg * xhat).mean())
+        size = dg.abs() + dg.abs().mean() + xhat.abs() * (dg * xhat).abs().mean()
+        for rows in (slice(0, tail), slice(S - tail, S)):
+            for got, exact, slack in ((y, xhat, K * (1 + xhat.abs())), (dx, want, K * 2 * size)):
+                off = (got[B - 1, rows, c].double() - exact[rows]).abs()
+                assert (off <= slack[rows] + UNIT["bf16"] * exact[rows].abs()).all()
+        del xg, dg, xhat, want, size
+    del x, dy, y, dx
+    torch.cuda.empty_cache()
