@@ -292,7 +292,7 @@ int longconv_embed_fwd(const void* ids, int id_bytes, const void* E, int table, 
 
 /* Its gradient, every row of dE [V,H] float32 written (zeros where no token names it):
  *     dE[v,:] = scale . sum over ids[b,t] = v of m . dy[b,t,:]
- * The tokens' places are sorted in the workspace, and each token's gradients added up in the order of their places.
+ * Each token's gradients are added up in a fixed order that the tokens' places give, by way of the workspace.
  * longconv_embed_workspace_bytes (0 on bad arguments) does not fall as B grows. */
 size_t longconv_embed_workspace_bytes(int64_t B, int64_t N, int64_t V, int64_t H, int io, int layout);
 int longconv_embed_bwd(const void* dy, const void* ids, int id_bytes, float* dE, int64_t B, int64_t N, int64_t V, int64_t H, int io,

@@ -7,8 +7,8 @@
 // word of two halves that are 0x4000 (2.0 in both types) where the low four bits agree, once for all tiles, and a bit of the set of high
 // four bits, moved under it: two plain instructions a word.  A wave keeps 32 channels by 256 tokens of dE (128 accumulators, two waves a
 // SIMD), its workgroup's four waves share out a range of 32-place steps, and the ranges' sums are added in order by a second kernel.
-// 8 x 16384 tokens x 256 in fp16: kernels of 44 us with dropout 0.1, 36 without (sorted, with it: 57); 1024 tokens x 64: 16.5 (sorted 17.6).
-// Bound by vector issue, 445 instructions a step with the generator's two blocks for every lane, 311 without, 32 of them matrix instructions,
+// 8 x 16384 tokens x 256 in fp16: kernels of 44 us with dropout 0.1, 36 without (sorted, with it: 58).
+// Bound by vector issue, 453 instructions a step with the generator's two blocks for every lane, 320 without, 32 of them matrix instructions,
 // at two waves a SIMD.  About 12 us do not grow with the length (22 and 32 at half and whole length, without dropout): first loads, sums
 // in LDS, the ranges' sums (17 MB out and in).  With rows asked for one to four steps ahead this kernel takes 38.9 to 40.5.
 // What is not finite would reach every token of its channel (0 times infinity), and twice a sum may pass the range of bf16 and fp32 where

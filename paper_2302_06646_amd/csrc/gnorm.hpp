@@ -8,11 +8,12 @@
 // and the group's sums come from the same numbers.  Mean and variance are carried as (mean, sum of squared differences), merged
 // pairwise, so a mean that is large against the deviation costs nothing.  All in fp32, in a fixed order.
 //
-// Forward and backward, 64 x 1024 x 256 in bf16, 32 groups, silu: 50 us (33 for the bytes), groups held by workgroups: kernels of 17 + 32
-// + 5; in the backward one loads, vector issue (8.7 million instructions: 16 us at four cycles and 2.1 GHz) and stores follow each other
+// Forward and backward, 64 x 1024 x 256 in bf16, 32 groups, silu: 51 us (33 for the bytes), groups held by workgroups: kernels of 17 + 33
+// + 5; in the backward one loads, vector issue (9.2 million instructions: 17 us at four cycles and 2.1 GHz) and stores follow each other
 // in the one workgroup that a compute unit has registers for.
-// 16 x 16384 x 256 in fp16, gelu: 213 us, in passes that read x twice and x, dy twice (1.07 GB, 210 us at a copy's rate): kernels of 30
-// for the statistics, apply 46 (5.8 TB/s), sums 66 (bound by issue, 30 million vector instructions), dx 67 (6.0 TB/s).
+// 16 x 16384 x 256 in fp16, gelu: 216 us, in passes that read x twice and x, dy twice (1.07 GB, 210 us at a copy's rate): kernels of 30
+// for the statistics, apply 52 (5.1 TB/s, issue takes 44: 24 million vector instructions), sums 63 (bound by issue, 30 million), dx 69
+// (5.9 TB/s).
 #pragma once
 #include "vec8.hpp"
 
@@ -621,9 +622,12 @@ gnorm_dx_kernel(const typename IO::T* __restrict__ dy, const typename IO::T* __r
 
 // ---- groups that fit a workgroup -------------------------------------------------------------------------------------
 // A workgroup holds a slab of whole groups of one b in registers, as it came from memory: one read, one launch.  Its threads are `rows`
-// positions by `slices` pieces; a thread has NP pieces, `rows` positions apart.  Whatever fits goes this way: 64 x 1024 x 256 both ways 54
-// us of kernels against 69 in passes, 3 x 49 x 195 fp32 forward 8.5 against 14.2.  512 threads of eight pieces take 17 us forward where 1024 of four take 24
-// (what a thread does once), and segments of 64 bytes and more matter (32 bytes: 40 us).
+// positions by `slices` pieces; a thread has NP pieces, `rows` positions apart.  Whatever fits goes this way: 64 x 1024 x 256
+// both ways 55 us of kernels against 69 in passes, 3 x 49 x 195 fp32 forward 8.7 against 14.1.  512 threads of eight pieces take 17 us forward
+// where 1024 of four take 24 (what a thread does once).  A slab has segments of 64 bytes of a row, or fewer where those of 64 do not fit, down
+// to its groups: from 2049 positions on forward and 1025 on backward (16-bit rows, C / G = 8).  What that costs, us of kernels held and in
+// passes: 16 x 4096 x 256 forward (32 bytes) 40 and 30, backward (16 bytes) 83 and 41; 32 x 2048 x 256 backward (32 bytes) 54 and 41;
+// 8 x 8192 x 256 forward (16 bytes) 76 and 33; 1 x 4096 x 256 14 and 16, 23 and 18: narrow segments pay in small forward passes alone.
 constexpr int HT = 512, HSLAB = 128;      // threads, and pieces of a slab, at most
 
 struct Hold {
