@@ -321,6 +321,81 @@ int longconv_gnorm_bwd(const void* dy, const void* x, const float* gamma, const 
                        void* dx, float* dgamma, float* dbeta, int64_t B, int64_t S, int64_t C, int64_t G, int act, int io,
                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- operators beside the convolution --------------------------------------------------------------------------------------
+ * What a block of today puts beside a long convolution: a short one, a recurrence whose coefficients depend on the input, and the dense
+ * products between them; for training, for prompts and for single tokens.  Conventions as for the operators above.  Parameters are
+ * float32 (W of longconv_linear_fwd has the I/O dtype).
+ *   lengths: [B] int64 on the device, or NULL (every sequence has N places).  Places at and behind a sequence's length (taken as 0 or N
+ *   where it is outside 0 .. N) count for nothing, whatever the inputs hold there, NaN included; results are zero there, and the last
+ *   state is that behind the sequence's own last place.  The lengths are read when the kernels run.
+ *   State in, state out: a sequence may come in parts, each call taking the state that the one before left; the gradients go the same
+ *   way back (dlast in, dstate out).  A call for one place alone (_step) works on the state in place. */
+
+/* Short causal convolution of each head, x, y [B,H,N]:
+ *     y[b,h,t] = act(bias[h] + sum_{j < taps} k[h,j] x[b,h,t-j])
+ * k [H,taps] float32, 1 <= taps <= 8; bias [H] float32 or NULL.  state [B,H,taps-1] in the I/O dtype or NULL (zeros): the inputs before
+ * the first place, oldest first; last (or NULL): the same behind the last place, may be `state` itself.  act: longconv_act_t.
+ * 1 <= B, H, N; H <= 65535, B H N <= 2^34 (with N rounded up to a multiple of eight). */
+int longconv_short_fwd(const void* x, const float* k, const float* bias, const void* state, void* y, void* last, const int64_t* lengths,
+                       int64_t B, int64_t H, int64_t N, int taps, int act, int io, void* stream);
+
+/* Backward: dx, dstate in the I/O dtype, dk [H,taps], dbias [H] float32, each of which may be NULL; dlast (or NULL) is the gradient of
+ * `last`.  state and dlast as the forward call had them.  longconv_short_workspace_bytes (0 on bad arguments) does not fall as B grows. */
+size_t longconv_short_workspace_bytes(int64_t B, int64_t H, int64_t N, int taps, int io);
+int longconv_short_bwd(const void* dy, const void* x, const float* k, const float* bias, const void* state, const void* dlast, void* dx,
+                       float* dk, float* dbias, void* dstate, const int64_t* lengths, int64_t B, int64_t H, int64_t N, int taps, int act,
+                       int io, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One new place of each sequence: x, y [B,H]; state [B,H,taps-1] (may be NULL if taps is 1) is read and moved on. */
+int longconv_short_step(const void* x, const float* k, const float* bias, void* state, void* y, int64_t B, int64_t H, int taps, int act,
+                        int io, void* stream);
+
+/* Selective state space scan, u, delta, z, y [B,H,N], B, C [B,G,S,N] in the I/O dtype (G divides H; head h reads group h / (H / G)):
+ *     dt = softplus(delta + bias[h])   (delta + bias[h] if softplus is 0)
+ *     h[t,s] = exp(dt[t] A[h,s]) h[t-1,s] + dt[t] B[t,s] u[t],      y[t] = (sum_s C[t,s] h[t,s] + D[h] u[t]) silu(z[t])
+ * A [H,S] float32; D, bias [H] float32, z: each may be NULL (0, 0, no gate).  state [B,H,S] float32 or NULL (zeros); last (or NULL) may
+ * be `state`.  marks (or NULL) [B,H,ceil(N / LONGCONV_SCAN_SPAN),S] float32: the states that the backward pass begins from.
+ * States are float32 throughout.  The recurrence is cut into pieces whose decays, products of exp(dt A), are multiplied up first: meant
+ * for A <= 0 and dt >= 0; where a product over a sequence's part overflows float32, so may the result.
+ * 1 <= S <= 64, H <= 65535, B H N <= 2^34, B H S <= 2^31, B G S N <= 2^33, and fewer than 2^22 blocks of 8 heads of a group. */
+#define LONGCONV_SCAN_SPAN 512
+size_t longconv_scan_workspace_bytes(int64_t B, int64_t H, int64_t N, int64_t S, int64_t G, int io, int backward);
+int longconv_scan_fwd(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
+                      const float* bias, const float* state, void* y, float* last, float* marks, const int64_t* lengths, int64_t B,
+                      int64_t H, int64_t N, int64_t S, int64_t G, int softplus, int io, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* Backward, from the marks of the forward call: du, ddelta, dB, dC, dz in the I/O dtype (dB, dC summed over a group's heads in float32),
+ * dA [H,S], dD, dbias [H], dstate [B,H,S] float32, each of which may be NULL; dlast [B,H,S] float32 or NULL is the gradient of `last`.
+ * longconv_scan_workspace_bytes (backward = 1; it serves the forward call too; 0 on bad arguments) does not fall as B grows. */
+int longconv_scan_bwd(const void* dy, const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D,
+                      const void* z, const float* bias, const float* marks, const float* dlast, void* du, void* ddelta, float* dA,
+                      void* dB, void* dC, float* dD, void* dz, float* dbias, float* dstate, const int64_t* lengths, int64_t B, int64_t H,
+                      int64_t N, int64_t S, int64_t G, int softplus, int io, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One new place of each sequence: u, delta, z, y [B,H], B, C [B,G,S]; state [B,H,S] float32 is read and moved on. */
+int longconv_scan_step(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
+                       const float* bias, float* state, void* y, int64_t B, int64_t H, int64_t S, int64_t G, int softplus, int io,
+                       void* stream);
+
+/* Dense product between layers, from and to either layout (longconv_layout_t: x is [B,N,K] or [B,K,N], y and residual [B,N,M] or [B,M,N]):
+ *     y = act(x W^T + bias) + residual          at every place
+ * W [M,K] in the I/O dtype, bias [M] float32 or NULL, residual in the I/O dtype or NULL; y may be `residual`.  16-bit products on the
+ * matrix cores, fp32 ones there too, all sums in fp32.
+ * 1 <= K, M <= 65535, B N <= 2^26, B N K <= 2^34, B N M <= 2^34, and fewer than 2^24 tiles of 128 places by 128 columns. */
+size_t longconv_linear_workspace_bytes(int64_t B, int64_t N, int64_t K, int64_t M, int io, int backward);
+int longconv_linear_fwd(const void* x, const void* W, const float* bias, const void* residual, void* y, int64_t B, int64_t N, int64_t K,
+                        int64_t M, int act, int x_layout, int y_layout, int io, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward (the residual's gradient is dy): with z = x W^T + bias made again and dz = dy act'(z),
+ *     dx = dz W,      dW = sum over places of dz^T x,      dbias = sum over places of dz
+ * dx in the I/O dtype, dW in dtype dW_type (float32 or the I/O dtype), dbias float32; each may be NULL.  Behind an activation dz is
+ * rounded to the I/O dtype on its way into dx and dW (the matrix cores' operands are that wide); dbias sums it before that.
+ * longconv_linear_workspace_bytes (backward = 1; it serves the forward call too; 0 on bad arguments) does not fall as B grows. */
+int longconv_linear_bwd(const void* dy, const void* x, const void* W, const float* bias, void* dx, void* dW, int dW_type, float* dbias,
+                        int64_t B, int64_t N, int64_t K, int64_t M, int act, int x_layout, int y_layout, int io, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
 /* Debug and test switches (process-wide; not needed in normal use).  Each selects among
  * kernels that compute the same result: "engine" (0 by dtype, 1 fp32 vector-ALU engine,
  * 2 fp16 matrix-core engine), "inner_log2" (0, or n: cap the on-chip transform at 2^n

@@ -20,7 +20,10 @@ Functions mirror the C ABI of ``include/longconv.h``:
     longconv_lbfly_bwd, longconv_blocksize_fwd,
     longconv_dropout_fwd, longconv_dropout_bwd, longconv_kreg_fwd_seeded, longconv_kreg_bwd_seeded,
     longconv_embed_workspace_bytes, longconv_embed_fwd, longconv_embed_bwd,
-    longconv_gnorm_workspace_bytes, longconv_gnorm_fwd, longconv_gnorm_bwd
+    longconv_gnorm_workspace_bytes, longconv_gnorm_fwd, longconv_gnorm_bwd,
+    longconv_short_workspace_bytes, longconv_short_fwd, longconv_short_bwd, longconv_short_step,
+    longconv_scan_workspace_bytes, longconv_scan_fwd, longconv_scan_bwd, longconv_scan_step,
+    longconv_linear_workspace_bytes, longconv_linear_fwd, longconv_linear_bwd
 """
 from __future__ import annotations
 
@@ -49,7 +52,10 @@ EXPORTS = ("longconv_init", "longconv_kspec_bytes", "longconv_workspace_bytes",
            "longconv_lbfly_fwd", "longconv_lbfly_bwd", "longconv_blocksize_fwd",
            "longconv_dropout_fwd", "longconv_dropout_bwd", "longconv_kreg_fwd_seeded", "longconv_kreg_bwd_seeded",
            "longconv_embed_workspace_bytes", "longconv_embed_fwd", "longconv_embed_bwd",
-           "longconv_gnorm_workspace_bytes", "longconv_gnorm_fwd", "longconv_gnorm_bwd")
+           "longconv_gnorm_workspace_bytes", "longconv_gnorm_fwd", "longconv_gnorm_bwd",
+           "longconv_short_workspace_bytes", "longconv_short_fwd", "longconv_short_bwd", "longconv_short_step",
+           "longconv_scan_workspace_bytes", "longconv_scan_fwd", "longconv_scan_bwd", "longconv_scan_step",
+           "longconv_linear_workspace_bytes", "longconv_linear_fwd", "longconv_linear_bwd")
 
 
 class LongconvError(RuntimeError):
@@ -119,12 +125,24 @@ def lib():
                 "longconv_embed_fwd": [vp, ci, vp, ci, vp, i64, i64, i64, i64, ci, ci, f32, *random, vp],
                 "longconv_embed_bwd": [vp, vp, ci, vp, i64, i64, i64, i64, ci, ci, f32, *random, vp, sz, vp],
                 "longconv_gnorm_fwd": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, f32, ci, ci, vp, sz, vp],
-                "longconv_gnorm_bwd": [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, sz, vp]}.items():
+                "longconv_gnorm_bwd": [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, sz, vp],
+                "longconv_short_fwd": [*[vp] * 7, i64, i64, i64, ci, ci, ci, vp],
+                "longconv_short_bwd": [*[vp] * 11, i64, i64, i64, ci, ci, ci, vp, sz, vp],
+                "longconv_short_step": [*[vp] * 5, i64, i64, ci, ci, ci, vp],
+                "longconv_scan_fwd": [*[vp] * 13, i64, i64, i64, i64, i64, ci, ci, vp, sz, vp],
+                "longconv_scan_bwd": [*[vp] * 21, i64, i64, i64, i64, i64, ci, ci, vp, sz, vp],
+                "longconv_scan_step": [*[vp] * 10, i64, i64, i64, i64, ci, ci, vp],
+                "longconv_linear_fwd": [*[vp] * 5, i64, i64, i64, i64, ci, ci, ci, ci, vp, sz, vp],
+                "longconv_linear_bwd": [*[vp] * 6, ci, vp, i64, i64, i64, i64, ci, ci, ci, ci, vp, sz, vp]}.items():
             getattr(L, name).restype, getattr(L, name).argtypes = ci, args
         L.longconv_embed_workspace_bytes.restype = sz
         L.longconv_embed_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, ci]
         L.longconv_gnorm_workspace_bytes.restype = sz
         L.longconv_gnorm_workspace_bytes.argtypes = [i64, i64, i64, i64, ci, ci]
+        for name, args in {"longconv_short_workspace_bytes": [i64, i64, i64, ci, ci],
+                           "longconv_scan_workspace_bytes": [i64, i64, i64, i64, i64, ci, ci],
+                           "longconv_linear_workspace_bytes": [i64, i64, i64, i64, ci, ci]}.items():
+            getattr(L, name).restype, getattr(L, name).argtypes = sz, args
         L.longconv_set_option.restype = ci
         L.longconv_set_option.argtypes = [ctypes.c_char_p, ci]
         _lib = L
@@ -588,3 +606,229 @@ def longconv_gnorm_bwd(dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, act: s
     _check(lib().longconv_gnorm_bwd(_ptr(dy), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma),
                                     _ptr(dbeta), B, S, C, G, code, io, _ptr(workspace), workspace.numel(), _stream(stream)),
            "longconv_gnorm_bwd")
+
+
+# ---- operators beside the convolution ----------------------------------------------------------------------------------------
+
+SCAN_SPAN = 512                                           # places between two marks of a scan
+
+
+def _room(n, device):
+    if n == 0:
+        raise LongconvError("bad shape or dtype")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+class _on:
+    """The checks of a call whose tensors have to be on one device, which is made the current one for as long as the call takes."""
+
+    def __init__(self, t, name):
+        _need(t, name, t.dtype, t.shape)
+        if t.dtype not in _CODE:
+            raise LongconvError(f"{name}: expected float32, float16 or bfloat16, got {t.dtype}")
+        self.device, self.io, self.dtype = t.device, _CODE[t.dtype], t.dtype
+
+    def need(self, t, name, dtype, shape):
+        _need(t, name, dtype, shape)
+        self.here(t, name)
+
+    def here(self, t, name):
+        if t is not None and t.device != self.device:
+            raise LongconvError(f"{name} is on {t.device}, other tensors of the call on {self.device}")
+
+    def call(self, f, *args, stream=None):
+        with torch.cuda.device(self.device):
+            _check(getattr(lib(), f)(*args, _stream(stream)), f)
+
+    def room(self, workspace):
+        self.here(workspace, "workspace")
+        return _ptr(workspace), workspace.numel()
+
+
+def longconv_short_workspace_bytes(B: int, H: int, N: int, taps: int, io: int) -> int:
+    return int(lib().longconv_short_workspace_bytes(B, H, N, taps, io))
+
+
+def new_workspace_short(B, H, N, taps, io, device="cuda"):
+    """For longconv_short_bwd; the forward call needs none."""
+    return _room(longconv_short_workspace_bytes(B, H, N, taps, io), device)
+
+
+def longconv_short_fwd(x, k, bias, y, act: str, state=None, last=None, lengths=None, stream=None) -> None:
+    """y [B, H, N] <- act(bias + sum_j k[:, j] x[t - j]), k [H, taps] fp32, bias [H] or None.  state [B, H, taps - 1] in x's dtype (or
+    None): the inputs before the first, oldest first; last (or None, or state itself) <- those before what comes next.  lengths [B]
+    int64 (or None): places behind count for nothing and are zero in y."""
+    code = _ACT[act]
+    if _done((_bound or _fast()).short_fwd(x, k, bias, y, code, state, last, lengths, stream), "longconv_short_fwd"):
+        return
+    c = _on(x, "x")
+    B, H, N = x.shape
+    taps = k.shape[1]
+    c.need(k, "k", torch.float32, (H, taps)); c.need(bias, "bias", torch.float32, (H,))
+    c.need(y, "y", c.dtype, (B, H, N)); c.need(lengths, "lengths", torch.int64, (B,))
+    for t, name in ((state, "state"), (last, "last")):
+        c.need(t, name, c.dtype, (B, H, taps - 1))
+    c.call("longconv_short_fwd", _ptr(x), _ptr(k), _ptr(bias), _ptr(state), _ptr(y), _ptr(last), _ptr(lengths), B, H, N, taps, code, c.io,
+           stream=stream)
+
+
+def longconv_short_bwd(dy, x, k, bias, dx, dk, dbias, act: str, workspace, state=None, dlast=None, dstate=None, lengths=None,
+                       stream=None) -> None:
+    """dx, dk [H, taps], dbias [H], dstate <- gradients of longconv_short_fwd (any may be None); dlast: the gradient of `last`."""
+    code = _ACT[act]
+    if _done((_bound or _fast()).short_bwd(dy, x, k, bias, dx, dk, dbias, code, workspace, state, dlast, dstate, lengths, stream),
+             "longconv_short_bwd"):
+        return
+    c = _on(x, "x")
+    B, H, N = x.shape
+    taps = k.shape[1]
+    for t, name in ((dy, "dy"), (dx, "dx")):
+        c.need(t, name, c.dtype, (B, H, N))
+    for t, name in ((k, "k"), (dk, "dk")):
+        c.need(t, name, torch.float32, (H, taps))
+    for t, name in ((bias, "bias"), (dbias, "dbias")):
+        c.need(t, name, torch.float32, (H,))
+    for t, name in ((state, "state"), (dlast, "dlast"), (dstate, "dstate")):
+        c.need(t, name, c.dtype, (B, H, taps - 1))
+    c.need(lengths, "lengths", torch.int64, (B,))
+    c.call("longconv_short_bwd", _ptr(dy), _ptr(x), _ptr(k), _ptr(bias), _ptr(state), _ptr(dlast), _ptr(dx), _ptr(dk), _ptr(dbias), _ptr(dstate),
+           _ptr(lengths), B, H, N, taps, code, c.io, *c.room(workspace), stream=stream)
+
+
+def longconv_short_step(x, k, bias, state, y, act: str, stream=None) -> None:
+    """One new place of each sequence, x, y [B, H]; state [B, H, taps - 1] is moved on in place (None where taps is 1)."""
+    code = _ACT[act]
+    if _done((_bound or _fast()).short_step(x, k, bias, state, y, code, stream), "longconv_short_step"):
+        return
+    c = _on(x, "x")
+    B, H = x.shape
+    taps = k.shape[1]
+    c.need(k, "k", torch.float32, (H, taps)); c.need(bias, "bias", torch.float32, (H,))
+    c.need(y, "y", c.dtype, (B, H)); c.need(state, "state", c.dtype, (B, H, taps - 1))
+    c.call("longconv_short_step", _ptr(x), _ptr(k), _ptr(bias), _ptr(state), _ptr(y), B, H, taps, code, c.io, stream=stream)
+
+
+def longconv_scan_workspace_bytes(B: int, H: int, N: int, S: int, G: int, io: int, backward) -> int:
+    return int(lib().longconv_scan_workspace_bytes(B, H, N, S, G, io, int(bool(backward))))
+
+
+def new_workspace_scan(B, H, N, S, G, io, backward, device="cuda"):
+    return _room(longconv_scan_workspace_bytes(B, H, N, S, G, io, backward), device)
+
+
+def new_scan_marks(B, H, N, S, device="cuda"):
+    """States of a scan at every SCAN_SPAN-th place: what longconv_scan_fwd leaves for longconv_scan_bwd."""
+    return torch.empty(B, H, -(-N // SCAN_SPAN), S, device=device)
+
+
+def _scan_args(u, delta, A, Bm, Cm, D, z, bias):
+    c = _on(u, "u")
+    B, H, *N = u.shape
+    S, G = A.shape[1], Bm.shape[1]
+    for t, name in ((u, "u"), (delta, "delta"), (z, "z")):
+        c.need(t, name, c.dtype, (B, H, *N))
+    c.need(A, "A", torch.float32, (H, S))
+    for t, name in ((Bm, "Bm"), (Cm, "Cm")):
+        c.need(t, name, c.dtype, (B, G, S, *N))
+    for t, name in ((D, "D"), (bias, "bias")):
+        c.need(t, name, torch.float32, (H,))
+    return c, (B, H, *N, S, G)
+
+
+def longconv_scan_fwd(u, delta, A, Bm, Cm, y, workspace, D=None, z=None, bias=None, softplus: bool = True, state=None, last=None,
+                      marks=None, lengths=None, stream=None) -> None:
+    """y [B, H, N] <- (C_t h_t + D u) silu(z), h_t = exp(dt A) h_{t-1} + dt B_t u, dt = softplus(delta + bias).  A [H, S] fp32; Bm, Cm
+    [B, G, S, N] in u's dtype, shared by the heads of a group; state, last [B, H, S] fp32 (last may be state); marks: new_scan_marks,
+    for the backward pass; lengths [B] int64: places behind count for nothing and are zero in y."""
+    if _done((_bound or _fast()).scan_fwd(u, delta, A, Bm, Cm, y, workspace, D, z, bias, int(softplus), state, last, marks, lengths, stream),
+             "longconv_scan_fwd"):
+        return
+    c, (B, H, N, S, G) = _scan_args(u, delta, A, Bm, Cm, D, z, bias)
+    c.need(y, "y", c.dtype, (B, H, N)); c.need(lengths, "lengths", torch.int64, (B,))
+    for t, name in ((state, "state"), (last, "last")):
+        c.need(t, name, torch.float32, (B, H, S))
+    c.need(marks, "marks", torch.float32, (B, H, -(-N // SCAN_SPAN), S))
+    c.call("longconv_scan_fwd", _ptr(u), _ptr(delta), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(bias), _ptr(state), _ptr(y), _ptr(last),
+           _ptr(marks), _ptr(lengths), B, H, N, S, G, int(softplus), c.io, *c.room(workspace), stream=stream)
+
+
+def longconv_scan_bwd(dy, u, delta, A, Bm, Cm, marks, du, ddelta, dA, dB, dC, workspace, D=None, z=None, bias=None, dD=None, dz=None,
+                      dbias=None, softplus: bool = True, dlast=None, dstate=None, lengths=None, stream=None) -> None:
+    """du, ddelta, dA, dB, dC, dD, dz, dbias, dstate <- gradients of longconv_scan_fwd (any may be None), from the marks it left;
+    dlast [B, H, S]: the gradient of `last`."""
+    if _done((_bound or _fast()).scan_bwd(dy, u, delta, A, Bm, Cm, marks, du, ddelta, dA, dB, dC, workspace, D, z, bias, dD, dz, dbias,
+                                          int(softplus), dlast, dstate, lengths, stream), "longconv_scan_bwd"):
+        return
+    c, (B, H, N, S, G) = _scan_args(u, delta, A, Bm, Cm, D, z, bias)
+    for t, name in ((dy, "dy"), (du, "du"), (ddelta, "ddelta"), (dz, "dz")):
+        c.need(t, name, c.dtype, (B, H, N))
+    for t, name in ((dB, "dB"), (dC, "dC")):
+        c.need(t, name, c.dtype, (B, G, S, N))
+    for t, name in ((dlast, "dlast"), (dstate, "dstate")):
+        c.need(t, name, torch.float32, (B, H, S))
+    for t, name in ((dD, "dD"), (dbias, "dbias")):
+        c.need(t, name, torch.float32, (H,))
+    c.need(dA, "dA", torch.float32, (H, S)); c.need(lengths, "lengths", torch.int64, (B,))
+    c.need(marks, "marks", torch.float32, (B, H, -(-N // SCAN_SPAN), S))
+    c.call("longconv_scan_bwd", _ptr(dy), _ptr(u), _ptr(delta), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(bias), _ptr(marks), _ptr(dlast),
+           _ptr(du), _ptr(ddelta), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dz), _ptr(dbias), _ptr(dstate), _ptr(lengths), B, H, N, S, G,
+           int(softplus), c.io, *c.room(workspace), stream=stream)
+
+
+def longconv_scan_step(u, delta, A, Bm, Cm, state, y, D=None, z=None, bias=None, softplus: bool = True, stream=None) -> None:
+    """One new place of each sequence, u, delta, z, y [B, H], Bm, Cm [B, G, S]; state [B, H, S] fp32 is moved on in place."""
+    if _done((_bound or _fast()).scan_step(u, delta, A, Bm, Cm, state, y, D, z, bias, int(softplus), stream), "longconv_scan_step"):
+        return
+    c, (B, H, S, G) = _scan_args(u, delta, A, Bm, Cm, D, z, bias)
+    c.need(state, "state", torch.float32, (B, H, S)); c.need(y, "y", c.dtype, (B, H))
+    c.call("longconv_scan_step", _ptr(u), _ptr(delta), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(bias), _ptr(state), _ptr(y), B, H, S, G,
+           int(softplus), c.io, stream=stream)
+
+
+def longconv_linear_workspace_bytes(B: int, N: int, K: int, M: int, io: int, backward) -> int:
+    return int(lib().longconv_linear_workspace_bytes(B, N, K, M, io, int(bool(backward))))
+
+
+def new_workspace_linear(B, N, K, M, io, backward, device="cuda"):
+    return _room(longconv_linear_workspace_bytes(B, N, K, M, io, backward), device)
+
+
+def _linear_args(x, W, x_layout, y_layout):
+    c = _on(x, "x")
+    if x_layout not in (CHANNELS_LAST, CHANNELS_FIRST) or y_layout not in (CHANNELS_LAST, CHANNELS_FIRST):
+        raise LongconvError("layouts are CHANNELS_LAST or CHANNELS_FIRST")
+    M, K = W.shape
+    B, N = x.shape[0], x.shape[2 if x_layout == CHANNELS_FIRST else 1]
+    of_x = (B, K, N) if x_layout == CHANNELS_FIRST else (B, N, K)
+    of_y = (B, M, N) if y_layout == CHANNELS_FIRST else (B, N, M)
+    c.need(x, "x", c.dtype, of_x); c.need(W, "W", c.dtype, (M, K))
+    return c, B, N, K, M, of_x, of_y
+
+
+def longconv_linear_fwd(x, W, bias, y, act: str, workspace, x_layout: int = CHANNELS_LAST, y_layout: int = CHANNELS_LAST, residual=None,
+                        stream=None) -> None:
+    """y <- act(x W^T + bias) + residual at every place: x [B, N, K] (or [B, K, N] for CHANNELS_FIRST), y and residual [B, N, M] (or
+    [B, M, N]), W [M, K] in x's dtype, bias [M] fp32 or None.  y may be residual."""
+    code = _ACT[act]
+    if _done((_bound or _fast()).linear_fwd(x, W, bias, y, code, workspace, x_layout, y_layout, residual, stream), "longconv_linear_fwd"):
+        return
+    c, B, N, K, M, _, of_y = _linear_args(x, W, x_layout, y_layout)
+    c.need(y, "y", c.dtype, of_y); c.need(residual, "residual", c.dtype, of_y); c.need(bias, "bias", torch.float32, (M,))
+    c.call("longconv_linear_fwd", _ptr(x), _ptr(W), _ptr(bias), _ptr(residual), _ptr(y), B, N, K, M, code, int(x_layout), int(y_layout), c.io,
+           *c.room(workspace), stream=stream)
+
+
+def longconv_linear_bwd(dy, x, W, bias, dx, dW, dbias, act: str, workspace, x_layout: int = CHANNELS_LAST, y_layout: int = CHANNELS_LAST,
+                        stream=None) -> None:
+    """dx, dW [M, K] (fp32 or x's dtype), dbias [M] fp32 <- gradients of longconv_linear_fwd (any may be None; the residual's is dy).
+    Behind an activation the product is made again, and dz = dy act'(z) rounded to x's dtype on its way into dx and dW."""
+    code = _ACT[act]
+    if _done((_bound or _fast()).linear_bwd(dy, x, W, bias, dx, dW, dbias, code, workspace, x_layout, y_layout, stream), "longconv_linear_bwd"):
+        return
+    c, B, N, K, M, of_x, of_y = _linear_args(x, W, x_layout, y_layout)
+    c.need(dy, "dy", c.dtype, of_y); c.need(dx, "dx", c.dtype, of_x)
+    c.need(dW, "dW", torch.float32 if dW is not None and dW.dtype == torch.float32 else c.dtype, (M, K))
+    for t, name in ((bias, "bias"), (dbias, "dbias")):
+        c.need(t, name, torch.float32, (M,))
+    c.call("longconv_linear_bwd", _ptr(dy), _ptr(x), _ptr(W), _ptr(bias), _ptr(dx), _ptr(dW), F32 if dW is None else dtype_code(dW), _ptr(dbias),
+           B, N, K, M, code, int(x_layout), int(y_layout), c.io, *c.room(workspace), stream=stream)

@@ -4,11 +4,13 @@
 // multipass.hip (outer passes), engine_valu.hip (fp32 I/O), engine_mfma.hip (first-generation in-place kernel, kept as a
 // cross-check behind a switch and for 256-point inner transforms), kreg.hip (kernel regularisers), gate.hip (the gate's streaming
 // pass) and conv2d.hip (row padding of the 2-D convolution), lbfly.hip (learned Butterfly extension), bsize.hip (block-size
-// study); dropout.hip, embed.hip and gnorm.hip hold the operators around the convolution.  Nothing here computes on the host.
+// study); dropout.hip, embed.hip and gnorm.hip hold the operators around the convolution, short.hip, scan.hip with scan_bwd.hip and linear.hip
+// those beside it.  Nothing here computes on the host.
 #include <atomic>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 
 #include "operators.hpp"
@@ -1016,6 +1018,178 @@ int longconv_gnorm_bwd(const void* dy, const void* x, const float* gamma, const 
     return note(gnorm_bwd(a, dy, x, mean, rstd, dx, dgamma, dbeta, workspace, (hipStream_t)stream), "gnorm bwd") == hipSuccess
                ? LONGCONV_OK
                : LONGCONV_ERR_HIP;
+}
+
+// ---- operators beside the convolution ----------------------------------------------------------------------------------
+
+static bool misaligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) != 0; }
+static bool any_misaligned(std::initializer_list<const void*> ps)
+{
+    for (const void* p : ps)
+        if (misaligned(p)) return true;
+    return false;
+}
+// B H rows of N (rounded up to `unit`) elements
+static bool bad_rows(int64_t B, int64_t H, int64_t N, int64_t unit)
+{
+    if (B < 1 || H < 1 || N < 1 || H > 65535 || B > MAX_ELEMENTS / H || N > MAX_ELEMENTS) return true;
+    return (N + unit - 1) / unit * unit > MAX_ELEMENTS / (B * H);
+}
+
+static int check_short(int64_t B, int64_t H, int64_t N, int taps, int io)
+{
+    if (bad_dtype(io)) return LONGCONV_ERR_DTYPE;
+    return taps < 1 || taps > SHORT_TAPS || bad_rows(B, H, N, 8) ? LONGCONV_ERR_SHAPE : LONGCONV_OK;
+}
+
+size_t longconv_short_workspace_bytes(int64_t B, int64_t H, int64_t N, int taps, int io)
+{
+    return check_short(B, H, N, taps, io) == LONGCONV_OK ? short_workspace_bytes(B, H, N) : 0;
+}
+
+int longconv_short_fwd(const void* x, const float* k, const float* bias, const void* state, void* y, void* last, const int64_t* lengths, int64_t B,
+                       int64_t H, int64_t N, int taps, int act, int io, void* stream)
+{
+    const int s = check_short(B, H, N, taps, io);
+    if (s != LONGCONV_OK) return s;
+    if (bad_act(act)) return LONGCONV_ERR_SHAPE;
+    if (!x || !k || !y) return LONGCONV_ERR_NULL;
+    if (any_misaligned({x, k, bias, state, y, last}) || misaligned8(lengths)) return LONGCONV_ERR_ALIGN;
+    const ShortArgs a{k, bias, lengths, B, H, N, taps, act, io};
+    return note(short_fwd(a, x, state, y, last, (hipStream_t)stream), "short fwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+int longconv_short_bwd(const void* dy, const void* x, const float* k, const float* bias, const void* state, const void* dlast, void* dx, float* dk,
+                       float* dbias, void* dstate, const int64_t* lengths, int64_t B, int64_t H, int64_t N, int taps, int act, int io,
+                       void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int s = check_short(B, H, N, taps, io);
+    if (s != LONGCONV_OK) return s;
+    if (bad_act(act)) return LONGCONV_ERR_SHAPE;
+    if (!dy || !x || !k) return LONGCONV_ERR_NULL;
+    if (any_misaligned({dy, x, k, bias, state, dlast, dx, dk, dbias, dstate, workspace}) || misaligned8(lengths)) return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < short_workspace_bytes(B, H, N)) return LONGCONV_ERR_WORKSPACE;
+    if (!dx && !dk && !dbias && !dstate) return LONGCONV_OK;
+    const ShortArgs a{k, bias, lengths, B, H, N, taps, act, io};
+    const ShortGrads d{dy, x, state, dlast, dx, dstate, dk, dbias};
+    return note(short_bwd(a, d, workspace, (hipStream_t)stream), "short bwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+int longconv_short_step(const void* x, const float* k, const float* bias, void* state, void* y, int64_t B, int64_t H, int taps, int act, int io,
+                        void* stream)
+{
+    const int s = check_short(B, H, 1, taps, io);
+    if (s != LONGCONV_OK) return s;
+    if (bad_act(act)) return LONGCONV_ERR_SHAPE;
+    if (!x || !k || !y || (!state && taps > 1)) return LONGCONV_ERR_NULL;
+    if (any_misaligned({x, k, bias, state, y})) return LONGCONV_ERR_ALIGN;
+    const ShortArgs a{k, bias, nullptr, B, H, 1, taps, act, io};
+    return note(short_step(a, x, state, y, (hipStream_t)stream), "short step") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+static int check_scan(int64_t B, int64_t H, int64_t N, int64_t S, int64_t G, int io)
+{
+    if (bad_dtype(io)) return LONGCONV_ERR_DTYPE;
+    if (bad_rows(B, H, N, 1) || S < 1 || S > SCAN_STATES || G < 1 || G > H || H % G) return LONGCONV_ERR_SHAPE;
+    if (B * H > (int64_t(1) << 31) / S || B * G * S > MAX_ELEMENTS / 2 / N) return LONGCONV_ERR_SHAPE;
+    return B * G * ((H / G + 7) / 8) >= (int64_t(1) << 22) ? LONGCONV_ERR_SHAPE : LONGCONV_OK;      // (workgroups of a launch)
+}
+
+size_t longconv_scan_workspace_bytes(int64_t B, int64_t H, int64_t N, int64_t S, int64_t G, int io, int backward)
+{
+    return check_scan(B, H, N, S, G, io) == LONGCONV_OK ? scan_workspace_bytes(B, H, N, (int)S, G, backward) : 0;
+}
+
+int longconv_scan_fwd(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
+                      const float* bias, const float* state, void* y, float* last, float* marks, const int64_t* lengths, int64_t B, int64_t H,
+                      int64_t N, int64_t S, int64_t G, int softplus, int io, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int s = check_scan(B, H, N, S, G, io);
+    if (s != LONGCONV_OK) return s;
+    if (!u || !delta || !A || !Bm || !Cm || !y) return LONGCONV_ERR_NULL;
+    if (any_misaligned({u, delta, A, Bm, Cm, D, z, bias, state, y, last, marks, workspace}) || misaligned8(lengths)) return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < scan_workspace_bytes(B, H, N, (int)S, G, 0)) return LONGCONV_ERR_WORKSPACE;
+    const ScanArgs a{u, delta, Bm, Cm, z, A, D, bias, lengths, B, H, N, G, (int)S, softplus, io};
+    return note(scan_fwd(a, state, y, last, marks, workspace, (hipStream_t)stream), "scan fwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+int longconv_scan_bwd(const void* dy, const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D,
+                      const void* z, const float* bias, const float* marks, const float* dlast, void* du, void* ddelta, float* dA, void* dB,
+                      void* dC, float* dD, void* dz, float* dbias, float* dstate, const int64_t* lengths, int64_t B, int64_t H, int64_t N,
+                      int64_t S, int64_t G, int softplus, int io, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int s = check_scan(B, H, N, S, G, io);
+    if (s != LONGCONV_OK) return s;
+    if (!dy || !u || !delta || !A || !Bm || !Cm || !marks || (dz && !z)) return LONGCONV_ERR_NULL;
+    if (any_misaligned({dy, u, delta, A, Bm, Cm, D, z, bias, marks, dlast, du, ddelta, dA, dB, dC, dD, dz, dbias, dstate, workspace}) ||
+        misaligned8(lengths))
+        return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < scan_workspace_bytes(B, H, N, (int)S, G, 1)) return LONGCONV_ERR_WORKSPACE;
+    if (!du && !ddelta && !dA && !dB && !dC && !dD && !dz && !dbias && !dstate) return LONGCONV_OK;
+    const ScanArgs a{u, delta, Bm, Cm, z, A, D, bias, lengths, B, H, N, G, (int)S, softplus, io};
+    const ScanGrads d{dy, marks, dlast, du, ddelta, dB, dC, dz, dA, dD, dbias, dstate};
+    return note(scan_bwd(a, d, workspace, (hipStream_t)stream), "scan bwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+int longconv_scan_step(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
+                       const float* bias, float* state, void* y, int64_t B, int64_t H, int64_t S, int64_t G, int softplus, int io, void* stream)
+{
+    const int s = check_scan(B, H, 1, S, G, io);
+    if (s != LONGCONV_OK) return s;
+    if (!u || !delta || !A || !Bm || !Cm || !state || !y) return LONGCONV_ERR_NULL;
+    if (any_misaligned({u, delta, A, Bm, Cm, D, z, bias, state, y})) return LONGCONV_ERR_ALIGN;
+    const ScanArgs a{u, delta, Bm, Cm, z, A, D, bias, nullptr, B, H, 1, G, (int)S, softplus, io};
+    return note(scan_step(a, state, y, (hipStream_t)stream), "scan step") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+static int check_linear(int64_t B, int64_t N, int64_t K, int64_t M, int io)
+{
+    if (bad_dtype(io)) return LONGCONV_ERR_DTYPE;
+    if (B < 1 || N < 1 || K < 1 || M < 1 || K > 65535 || M > 65535) return LONGCONV_ERR_SHAPE;
+    const int64_t wide = K > M ? K : M;
+    if (B > (int64_t(1) << 26) || N > (int64_t(1) << 26) / B || B * N > MAX_ELEMENTS / wide) return LONGCONV_ERR_SHAPE;
+    return B * ((N + 127) / 128) * ((wide + 127) / 128) >= (int64_t(1) << 24) ? LONGCONV_ERR_SHAPE : LONGCONV_OK;
+}
+
+size_t longconv_linear_workspace_bytes(int64_t B, int64_t N, int64_t K, int64_t M, int io, int backward)
+{
+    return check_linear(B, N, K, M, io) == LONGCONV_OK ? linear_workspace_bytes(B, N, K, M, io, backward) : 0;
+}
+
+static int check_linear_call(int64_t B, int64_t N, int64_t K, int64_t M, int act, int x_layout, int y_layout, int io)
+{
+    const int s = check_linear(B, N, K, M, io);
+    if (s != LONGCONV_OK) return s;
+    const auto bad_layout = [](int l) { return l != LONGCONV_CHANNELS_LAST && l != LONGCONV_CHANNELS_FIRST; };
+    return bad_act(act) || bad_layout(x_layout) || bad_layout(y_layout) ? LONGCONV_ERR_SHAPE : LONGCONV_OK;
+}
+
+int longconv_linear_fwd(const void* x, const void* W, const float* bias, const void* residual, void* y, int64_t B, int64_t N, int64_t K, int64_t M,
+                        int act, int x_layout, int y_layout, int io, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int s = check_linear_call(B, N, K, M, act, x_layout, y_layout, io);
+    if (s != LONGCONV_OK) return s;
+    if (!x || !W || !y) return LONGCONV_ERR_NULL;
+    if (any_misaligned({x, W, bias, residual, y, workspace})) return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < linear_workspace_bytes(B, N, K, M, io, 0)) return LONGCONV_ERR_WORKSPACE;
+    const LinearArgs a{W, bias, B, N, K, M, act, io, x_layout == LONGCONV_CHANNELS_FIRST, y_layout == LONGCONV_CHANNELS_FIRST};
+    return note(linear_fwd(a, x, residual, y, workspace, (hipStream_t)stream), "linear fwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
+}
+
+int longconv_linear_bwd(const void* dy, const void* x, const void* W, const float* bias, void* dx, void* dW, int dW_type, float* dbias, int64_t B,
+                        int64_t N, int64_t K, int64_t M, int act, int x_layout, int y_layout, int io, void* workspace, size_t workspace_bytes,
+                        void* stream)
+{
+    const int s = check_linear_call(B, N, K, M, act, x_layout, y_layout, io);
+    if (s != LONGCONV_OK) return s;
+    if (dW_type != LONGCONV_F32 && dW_type != io) return LONGCONV_ERR_DTYPE;
+    if (!dy || !x || !W) return LONGCONV_ERR_NULL;
+    if (any_misaligned({dy, x, W, bias, dx, dW, dbias, workspace})) return LONGCONV_ERR_ALIGN;
+    if (!workspace || workspace_bytes < linear_workspace_bytes(B, N, K, M, io, 1)) return LONGCONV_ERR_WORKSPACE;
+    if (!dx && !dW && !dbias) return LONGCONV_OK;
+    const LinearArgs a{W, bias, B, N, K, M, act, io, x_layout == LONGCONV_CHANNELS_FIRST, y_layout == LONGCONV_CHANNELS_FIRST};
+    const LinearGrads d{dy, x, dx, dW, dbias, dW_type == LONGCONV_F32};
+    return note(linear_bwd(a, d, workspace, (hipStream_t)stream), "linear bwd") == hipSuccess ? LONGCONV_OK : LONGCONV_ERR_HIP;
 }
 
 int longconv_set_option(const char* name, int value)

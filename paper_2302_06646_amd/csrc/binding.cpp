@@ -39,6 +39,14 @@ struct Api {
     decltype(&longconv_embed_bwd) embed_bwd;
     decltype(&longconv_gnorm_fwd) gnorm_fwd;
     decltype(&longconv_gnorm_bwd) gnorm_bwd;
+    decltype(&longconv_short_fwd) short_fwd;
+    decltype(&longconv_short_bwd) short_bwd;
+    decltype(&longconv_short_step) short_step;
+    decltype(&longconv_scan_fwd) scan_fwd;
+    decltype(&longconv_scan_bwd) scan_bwd;
+    decltype(&longconv_scan_step) scan_step;
+    decltype(&longconv_linear_fwd) linear_fwd;
+    decltype(&longconv_linear_bwd) linear_bwd;
 } g_api = {};
 
 // a plain device tensor: torch.Tensor or Parameter, strided, its own storage, no functional transform around it
@@ -56,6 +64,15 @@ const at::Tensor* plain(PyObject* o)
 struct Args {
     PyObject* const* a;
     bool ok = true;
+    int device = -1;                               // of all tensors, where a function has set it (on())
+    bool elsewhere(const at::Tensor& t) const { return device >= 0 && t.get_device() != device; }
+    // the call's device is that of argument i, and has to be the current one: everything else is left to the binding's Python part
+    void on(int i)
+    {
+        const at::Tensor* t = plain(a[i]);
+        if (!t || t->get_device() != (int)c10::hip::current_device()) ok = false;
+        else device = t->get_device();
+    }
     const at::Tensor* first(int i, int dims)       // the tensor that names the shape
     {
         const at::Tensor* t = plain(a[i]);
@@ -67,7 +84,7 @@ struct Args {
         if (!ok) return nullptr;
         if (may_be_none && a[i] == Py_None) return nullptr;
         const at::Tensor* t = plain(a[i]);
-        if (!t || t->scalar_type() != dt || t->sizes() != shape || !t->is_contiguous()) { ok = false; return nullptr; }
+        if (!t || t->scalar_type() != dt || t->sizes() != shape || !t->is_contiguous() || elsewhere(*t)) { ok = false; return nullptr; }
         return t->data_ptr();
     }
     // workspace or stored spectrum: any device tensor, taken by its address (and its number of elements)
@@ -77,7 +94,7 @@ struct Args {
         if (!ok) return nullptr;
         if (may_be_none && a[i] == Py_None) return nullptr;
         const at::Tensor* t = plain(a[i]);
-        if (!t) { ok = false; return nullptr; }
+        if (!t || elsewhere(*t)) { ok = false; return nullptr; }
         if (n) *n = (size_t)t->numel();
         return t->data_ptr();
     }
@@ -540,6 +557,244 @@ PyObject* gnorm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)   // dy, x, gam
     });
 }
 
+const c10::ScalarType L = at::kLong;
+
+PyObject* short_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)   // x, k, bias, y, act, state, last, lengths, stream
+{
+    return guarded(a, n, 9, g_api.short_fwd, [&](Args& A, auto& call) {
+        A.on(0);
+        const Rows r(A, 0, 3);
+        const at::Tensor* kt = A.first(1, 2);
+        if (!A.ok || !kt) return;
+        const int64_t taps = kt->size(1);
+        const void* x = A.ptr(0, r.dt, {r.B, r.H, r.N});
+        const auto k = (const float*)A.ptr(1, F, {r.H, taps}), bias = (const float*)A.ptr(2, F, {r.H});
+        void *y = A.ptr(3, r.dt, {r.B, r.H, r.N}), *last = A.ptr(6, r.dt, {r.B, r.H, taps - 1});
+        const int act = (int)A.number(4);
+        const void* state = A.ptr(5, r.dt, {r.B, r.H, taps - 1});
+        const auto lengths = (const int64_t*)A.ptr(7, L, {r.B});
+        void* st = A.stream(8);
+        call([&] { return g_api.short_fwd(x, k, bias, state, y, last, lengths, r.B, r.H, r.N, (int)taps, act, r.io, st); });
+    });
+}
+
+// dy, x, k, bias, dx, dk, dbias, act, workspace, state, dlast, dstate, lengths, stream
+PyObject* short_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(a, n, 14, g_api.short_bwd, [&](Args& A, auto& call) {
+        A.on(1);
+        const Rows r(A, 1, 3);
+        const at::Tensor* kt = A.first(2, 2);
+        if (!A.ok || !kt) return;
+        const int64_t taps = kt->size(1);
+        size_t wb;
+        const void *dy = A.ptr(0, r.dt, {r.B, r.H, r.N}), *x = A.ptr(1, r.dt, {r.B, r.H, r.N});
+        const auto k = (const float*)A.ptr(2, F, {r.H, taps}), bias = (const float*)A.ptr(3, F, {r.H});
+        void* dx = A.ptr(4, r.dt, {r.B, r.H, r.N});
+        const auto dk = (float*)A.ptr(5, F, {r.H, taps}), dbias = (float*)A.ptr(6, F, {r.H});
+        const int act = (int)A.number(7);
+        void* ws = A.raw(8, &wb, false);
+        const void *state = A.ptr(9, r.dt, {r.B, r.H, taps - 1}), *dlast = A.ptr(10, r.dt, {r.B, r.H, taps - 1});
+        void* dstate = A.ptr(11, r.dt, {r.B, r.H, taps - 1});
+        const auto lengths = (const int64_t*)A.ptr(12, L, {r.B});
+        void* st = A.stream(13);
+        call([&] {
+            return g_api.short_bwd(dy, x, k, bias, state, dlast, dx, dk, dbias, dstate, lengths, r.B, r.H, r.N, (int)taps, act, r.io, ws, wb, st);
+        });
+    });
+}
+
+PyObject* short_step(PyObject*, PyObject* const* a, Py_ssize_t n)  // x, k, bias, state, y, act, stream
+{
+    return guarded(a, n, 7, g_api.short_step, [&](Args& A, auto& call) {
+        A.on(0);
+        const at::Tensor *t = A.first(0, 2), *kt = A.first(1, 2);
+        if (!A.ok || !t || !kt) return;
+        const int64_t B = t->size(0), H = t->size(1), taps = kt->size(1);
+        const c10::ScalarType dt = t->scalar_type();
+        const int io = io_code(dt);
+        if (io < 0) { A.ok = false; return; }
+        const void* x = A.ptr(0, dt, {B, H});
+        const auto k = (const float*)A.ptr(1, F, {H, taps}), bias = (const float*)A.ptr(2, F, {H});
+        void *state = A.ptr(3, dt, {B, H, taps - 1}), *y = A.ptr(4, dt, {B, H});
+        const int act = (int)A.number(5);
+        void* st = A.stream(6);
+        call([&] { return g_api.short_step(x, k, bias, state, y, B, H, (int)taps, act, io, st); });
+    });
+}
+
+// What the scan's calls share: u, delta, A, B, C from argument i on (`dims` of u); steps have no N
+struct Scan {
+    int64_t B = 0, H = 0, N = 1, S = 0, G = 0;
+    c10::ScalarType dt = at::kFloat;
+    int io = -1;
+    const void *u = nullptr, *delta = nullptr, *Bm = nullptr, *Cm = nullptr;
+    const float* A_ = nullptr;
+    bool rows;
+    Scan(Args& A, int i, int dims) : rows(dims == 3)
+    {
+        A.on(i);
+        const at::Tensor *t = A.first(i, dims), *at_ = A.first(i + 2, 2), *bt = A.first(i + 3, dims + 1);
+        if (!A.ok || !t || !at_ || !bt) { A.ok = false; return; }
+        dt = t->scalar_type();
+        io = io_code(dt);
+        if (io < 0) { A.ok = false; return; }
+        B = t->size(0);
+        H = t->size(1);
+        N = rows ? t->size(2) : 1;
+        S = at_->size(1);
+        G = bt->size(1);
+        u = row(A, i);
+        delta = row(A, i + 1);
+        A_ = (const float*)A.ptr(i + 2, F, {H, S}, false);
+        Bm = group(A, i + 3);
+        Cm = group(A, i + 4);
+    }
+    void* row(Args& A, int i) const { return rows ? A.ptr(i, dt, {B, H, N}) : A.ptr(i, dt, {B, H}); }
+    void* group(Args& A, int i) const { return rows ? A.ptr(i, dt, {B, G, S, N}) : A.ptr(i, dt, {B, G, S}); }
+    float* heads(Args& A, int i) const { return (float*)A.ptr(i, F, {H}); }
+    float* state(Args& A, int i) const { return (float*)A.ptr(i, F, {B, H, S}); }
+    float* marks(Args& A, int i, bool may_be_none) const
+    {
+        return (float*)A.ptr(i, F, {B, H, (N + LONGCONV_SCAN_SPAN - 1) / LONGCONV_SCAN_SPAN, S}, may_be_none);
+    }
+};
+
+// u, delta, A, B, C, y, workspace, D, z, bias, softplus, state, last, marks, lengths, stream
+PyObject* scan_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(a, n, 16, g_api.scan_fwd, [&](Args& A, auto& call) {
+        const Scan s(A, 0, 3);
+        if (!A.ok) return;
+        size_t wb;
+        void *y = s.row(A, 5), *ws = A.raw(6, &wb, false);
+        const float *D = s.heads(A, 7), *bias = s.heads(A, 9);
+        const void* z = s.row(A, 8);
+        const int softplus = (int)A.number(10);
+        const float* state = s.state(A, 11);
+        float *last = s.state(A, 12), *marks = s.marks(A, 13, true);
+        const auto lengths = (const int64_t*)A.ptr(14, L, {s.B});
+        void* st = A.stream(15);
+        call([&] {
+            return g_api.scan_fwd(s.u, s.delta, s.A_, s.Bm, s.Cm, D, z, bias, state, y, last, marks, lengths, s.B, s.H, s.N, s.S, s.G, softplus, s.io,
+                                  ws, wb, st);
+        });
+    });
+}
+
+// dy, u, delta, A, B, C, marks, du, ddelta, dA, dB, dC, workspace, D, z, bias, dD, dz, dbias, softplus, dlast, dstate, lengths, stream
+PyObject* scan_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(a, n, 24, g_api.scan_bwd, [&](Args& A, auto& call) {
+        const Scan s(A, 1, 3);
+        if (!A.ok) return;
+        size_t wb;
+        const void* dy = s.row(A, 0);
+        const float* marks = s.marks(A, 6, false);
+        void *du = s.row(A, 7), *ddelta = s.row(A, 8);
+        const auto dA = (float*)A.ptr(9, F, {s.H, s.S});
+        void *dB = s.group(A, 10), *dC = s.group(A, 11), *ws = A.raw(12, &wb, false);
+        const float *D = s.heads(A, 13), *bias = s.heads(A, 15);
+        const void* z = s.row(A, 14);
+        float *dD = s.heads(A, 16), *dbias = s.heads(A, 18);
+        void* dz = s.row(A, 17);
+        const int softplus = (int)A.number(19);
+        const float* dlast = s.state(A, 20);
+        float* dstate = s.state(A, 21);
+        const auto lengths = (const int64_t*)A.ptr(22, L, {s.B});
+        void* st = A.stream(23);
+        call([&] {
+            return g_api.scan_bwd(dy, s.u, s.delta, s.A_, s.Bm, s.Cm, D, z, bias, marks, dlast, du, ddelta, dA, dB, dC, dD, dz, dbias, dstate, lengths,
+                                  s.B, s.H, s.N, s.S, s.G, softplus, s.io, ws, wb, st);
+        });
+    });
+}
+
+PyObject* scan_step(PyObject*, PyObject* const* a, Py_ssize_t n)   // u, delta, A, B, C, state, y, D, z, bias, softplus, stream
+{
+    return guarded(a, n, 12, g_api.scan_step, [&](Args& A, auto& call) {
+        const Scan s(A, 0, 2);
+        if (!A.ok) return;
+        float* state = s.state(A, 5);
+        void* y = s.row(A, 6);
+        const float *D = s.heads(A, 7), *bias = s.heads(A, 9);
+        const void* z = s.row(A, 8);
+        const int softplus = (int)A.number(10);
+        void* st = A.stream(11);
+        call([&] { return g_api.scan_step(s.u, s.delta, s.A_, s.Bm, s.Cm, D, z, bias, state, y, s.B, s.H, s.S, s.G, softplus, s.io, st); });
+    });
+}
+
+// What the dense product's calls share: x in argument i, W in argument j, the layouts in arguments l and l + 1
+struct Dense {
+    int64_t B = 0, N = 0, K = 0, M = 0;
+    c10::ScalarType dt = at::kFloat;
+    int io = -1, x_layout = 0, y_layout = 0;
+    const void *x = nullptr, *W = nullptr;
+    Dense(Args& A, int i, int j, int l)
+    {
+        A.on(i);
+        const at::Tensor *t = A.first(i, 3), *wt = A.first(j, 2);
+        x_layout = (int)A.number(l);
+        y_layout = (int)A.number(l + 1);
+        if (!A.ok || !t || !wt || x_layout > 1 || y_layout > 1) { A.ok = false; return; }
+        dt = t->scalar_type();
+        io = io_code(dt);
+        if (io < 0) { A.ok = false; return; }
+        const bool first = x_layout == LONGCONV_CHANNELS_FIRST;
+        B = t->size(0);
+        N = t->size(first ? 2 : 1);
+        K = t->size(first ? 1 : 2);
+        M = wt->size(0);
+        x = of_x(A, i);
+        W = A.ptr(j, dt, {M, K}, false);
+    }
+    void* of_x(Args& A, int i) const { return x_layout == LONGCONV_CHANNELS_FIRST ? A.ptr(i, dt, {B, K, N}) : A.ptr(i, dt, {B, N, K}); }
+    void* of_y(Args& A, int i) const { return y_layout == LONGCONV_CHANNELS_FIRST ? A.ptr(i, dt, {B, M, N}) : A.ptr(i, dt, {B, N, M}); }
+};
+
+PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)  // x, W, bias, y, act, workspace, x_layout, y_layout, residual, stream
+{
+    return guarded(a, n, 10, g_api.linear_fwd, [&](Args& A, auto& call) {
+        const Dense d(A, 0, 1, 6);
+        if (!A.ok) return;
+        size_t wb;
+        const auto bias = (const float*)A.ptr(2, F, {d.M});
+        void* y = d.of_y(A, 3);
+        const int act = (int)A.number(4);
+        void* ws = A.raw(5, &wb, false);
+        const void* residual = d.of_y(A, 8);
+        void* st = A.stream(9);
+        call([&] { return g_api.linear_fwd(d.x, d.W, bias, residual, y, d.B, d.N, d.K, d.M, act, d.x_layout, d.y_layout, d.io, ws, wb, st); });
+    });
+}
+
+// dy, x, W, bias, dx, dW, dbias, act, workspace, x_layout, y_layout, stream
+PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(a, n, 12, g_api.linear_bwd, [&](Args& A, auto& call) {
+        const Dense d(A, 1, 2, 9);
+        if (!A.ok) return;
+        size_t wb;
+        const void* dy = d.of_y(A, 0);
+        const auto bias = (const float*)A.ptr(3, F, {d.M});
+        void* dx = d.of_x(A, 4);
+        c10::ScalarType wt = F;
+        if (a[5] != Py_None) {
+            const at::Tensor* t = plain(a[5]);
+            if (!t || (t->scalar_type() != F && t->scalar_type() != d.dt)) { A.ok = false; return; }
+            wt = t->scalar_type();
+        }
+        void* dW = A.ptr(5, wt, {d.M, d.K});
+        const auto dbias = (float*)A.ptr(6, F, {d.M});
+        const int act = (int)A.number(7);
+        void *ws = A.raw(8, &wb, false), *st = A.stream(11);
+        call([&] {
+            return g_api.linear_bwd(dy, d.x, d.W, bias, dx, dW, io_code(wt), dbias, d.B, d.N, d.K, d.M, act, d.x_layout, d.y_layout, d.io, ws, wb, st);
+        });
+    });
+}
+
 // bind({name: address}): the entry points of the library that the binding has loaded
 PyObject* bind(PyObject*, PyObject* arg)
 {
@@ -575,6 +830,14 @@ PyObject* bind(PyObject*, PyObject* arg)
     set(g_api.embed_bwd, "longconv_embed_bwd");
     set(g_api.gnorm_fwd, "longconv_gnorm_fwd");
     set(g_api.gnorm_bwd, "longconv_gnorm_bwd");
+    set(g_api.short_fwd, "longconv_short_fwd");
+    set(g_api.short_bwd, "longconv_short_bwd");
+    set(g_api.short_step, "longconv_short_step");
+    set(g_api.scan_fwd, "longconv_scan_fwd");
+    set(g_api.scan_bwd, "longconv_scan_bwd");
+    set(g_api.scan_step, "longconv_scan_step");
+    set(g_api.linear_fwd, "longconv_linear_fwd");
+    set(g_api.linear_bwd, "longconv_linear_bwd");
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "an entry point is missing");
         return nullptr;
@@ -587,7 +850,8 @@ PyMethodDef methods[] = {
     {"bind", bind, METH_O, nullptr}, FAST(kspec_compute), FAST(fwd), FAST(bwd), FAST(fwd_gated), FAST(bwd_gated), FAST(fwd2d),
     FAST(bwd2d), FAST(kreg_fwd), FAST(kreg_bwd), FAST(lbfly_spectrum), FAST(lbfly_spectrum_bwd), FAST(lbfly_fwd),
     FAST(lbfly_bwd), FAST(dropout_fwd), FAST(dropout_bwd), FAST(kreg_fwd_seeded), FAST(kreg_bwd_seeded), FAST(embed_fwd),
-    FAST(embed_bwd), FAST(gnorm_fwd), FAST(gnorm_bwd), {nullptr, nullptr, 0, nullptr}};
+    FAST(embed_bwd), FAST(gnorm_fwd), FAST(gnorm_bwd), FAST(short_fwd), FAST(short_bwd), FAST(short_step),
+    FAST(scan_fwd), FAST(scan_bwd), FAST(scan_step), FAST(linear_fwd), FAST(linear_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

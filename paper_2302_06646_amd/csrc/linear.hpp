@@ -1,0 +1,551 @@
+// Dense product between layers, y = act(x W^T + bias) + residual, x and y each as [B,N,.] or [B,.,N], and its backward pass
+//     dz = dy act'(z),   dx = dz W,   dW = dz^T x,   dbias = sum over places of dz,      z made again by the same product.
+//
+// All four products are one kernel: out[s][f] = sum_k F(f,k) S(s,k), f the index that is neighbouring in the result's memory.  Either operand
+// may have k neighbouring in its memory (its tile then lies in LDS as rows along k) or its own index (rows along that).
+#pragma once
+#include "act.hpp"
+#include "vec8.hpp"
+
+namespace lc {
+namespace {
+
+constexpr int LT = 256;               // threads: four waves, two by two
+constexpr int TF = 128, TS = 128;     // tile of the result
+
+// One operand: element (i, k) of batch b and segment q of the sum lies at p + b batch + q seg + i ld + k, or + k ld + i
+struct Side {
+    const void* p;
+    int64_t n, ld, batch, seg;        // n: values of i
+};
+// What becomes of the result: `rows` of n_f values, ld apart
+struct Product {
+    Side F, S;
+    int64_t K, segs, batches;         // the sum goes over `segs` segments of K
+    int64_t splits, per;              // shares of the sum, of `per` steps each
+    // EPI_OUT, EPI_DZ
+    void* out;
+    int64_t ld, batch;                // of out, residual, dy
+    const float* bias;
+    bool bias_f;                      // bias goes by f, not by s
+    int act;
+    const void* residual;             // EPI_OUT
+    const void* dy;                   // EPI_DZ: out = dy act'(z)
+    float* sums;                      // EPI_DZ: [batches tiles 2][n of the bias], sums of dz over a tile's places
+    // EPI_SUM: [splits][n_s][n_f]
+    float* part;
+};
+enum { EPI_OUT, EPI_DZ, EPI_SUM };
+
+__device__ __forceinline__ float act_by(int act, float z)
+{
+    switch (act) {
+        case LONGCONV_ACT_SILU: return act_of<LONGCONV_ACT_SILU>(z);
+        case LONGCONV_ACT_GELU: return act_of<LONGCONV_ACT_GELU>(z);
+        case LONGCONV_ACT_RELU: return act_of<LONGCONV_ACT_RELU>(z);
+        default: return z;
+    }
+}
+__device__ __forceinline__ float slope_by(int act, float z)
+{
+    switch (act) {
+        case LONGCONV_ACT_SILU: return slope_of<LONGCONV_ACT_SILU>(z);
+        case LONGCONV_ACT_GELU: return slope_of<LONGCONV_ACT_GELU>(z);
+        case LONGCONV_ACT_RELU: return slope_of<LONGCONV_ACT_RELU>(z);
+        default: return 1.f;
+    }
+}
+
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ mu::f4 mfma(IoF16, const uint4& a, const uint4& b, const mu::f4& c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(mu::h8, a), __builtin_bit_cast(mu::h8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ mu::f4 mfma(IoBF16, const uint4& a, const uint4& b, const mu::f4& c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ mu::f4 mfma(IoF32, const float4& a, const float4& b, const mu::f4& c)      // sixteen k: four of each of four lanes
+{
+    mu::f4 d = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, b.x, c, 0, 0, 0);
+    d = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y, b.y, d, 0, 0, 0);
+    d = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, b.z, d, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, b.w, d, 0, 0, 0);
+}
+
+// A tile of 128 values of i by BK values of k in LDS, KF: rows along k, else rows along i
+template <class IO, bool KF>
+struct Tile {
+    using T = typename IO::T;
+    static constexpr int E = sizeof(T), BK = E == 4 ? 16 : 64, STEP = E == 4 ? 16 : 32;      // k of a step of the loop, of a matrix instruction
+    static constexpr int ROW = KF ? BK + 16 / E : 128 + 32 / E, ROWS = KF ? 128 : BK;        // elements from row to row
+    static constexpr int BYTES = ROW * ROWS * E;
+    static constexpr int PER_ROW = (KF ? BK : 128) / VE, PIECES = 128 * BK / VE / LT;
+    using Frag = typename std::conditional<E == 4, float4, uint4>::type;
+
+    static __device__ __forceinline__ void load(const Side& d, int64_t off, int64_t i0, int64_t k0, int64_t K, Raw8<IO> (&r)[PIECES])
+    {
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            const int id = threadIdx.x + j * LT, line = id / PER_ROW, at = id % PER_ROW * VE;
+            const int64_t slow = (KF ? i0 : k0) + line, fast = (KF ? k0 : i0) + at, n_slow = KF ? d.n : K, n_fast = KF ? K : d.n;
+            if (slow < n_slow && fast < n_fast) {
+                const int64_t n = n_fast - fast;
+                load_raw<IO>((const T*)d.p + off + slow * d.ld + fast, n < VE ? (int)n : VE, r[j]);
+            } else r[j].zero();
+        }
+    }
+    static __device__ __forceinline__ void put(T* lds, const Raw8<IO> (&r)[PIECES])
+    {
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            const int id = threadIdx.x + j * LT, line = id / PER_ROW, at = id % PER_ROW * VE;
+            uint4* const to = reinterpret_cast<uint4*>(lds + line * ROW + at);
+#pragma unroll
+            for (int q = 0; q < Raw8<IO>::W / 4; ++q) to[q] = make_uint4(r[j].w[4 * q], r[j].w[4 * q + 1], r[j].w[4 * q + 2], r[j].w[4 * q + 3]);
+        }
+    }
+    // a lane's k of matrix step `m` for i = i0 + lane % 16: eight from 8 (lane / 16) on, fp32 four from 4 (lane / 16) on
+    static __device__ __forceinline__ Frag frag(const T* lds, int i0, int m)
+    {
+        const int i = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
+        if constexpr (KF) {
+            return *reinterpret_cast<const Frag*>(lds + (i0 + i) * ROW + m * STEP + g * (E == 4 ? 4 : 8));
+        } else if constexpr (E == 4) {
+            const T* p = lds + (m * STEP + 4 * g) * ROW + i0 + i;
+            return make_float4(p[0], p[ROW], p[2 * ROW], p[3 * ROW]);
+        } else {
+            // lane i of 16 gives the address of numbers 4 (i % 4) .. + 3 of row i / 4 and receives column i of the four rows
+            typedef __fp16 t4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) t4 lds_t4;
+            const T* p = lds + (m * STEP + 8 * g + i / 4) * ROW + i0 + i % 4 * 4;
+            const t4 a = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_t4*)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_t4*)(p + 4 * ROW));
+            const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+            return make_uint4(x.x, x.y, y.x, y.y);
+        }
+    }
+};
+
+template <class IO>
+__device__ __forceinline__ void store4(typename IO::T* p, int n, const float (&v)[4])
+{
+    if constexpr (sizeof(typename IO::T) == 4) {
+        if (n >= 4) {
+            const At4 w = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+            *reinterpret_cast<At4*>(p) = w;
+            return;
+        }
+    } else if (n >= 4) {
+        typedef uint32_t A2 __attribute__((ext_vector_type(2), aligned(2)));
+        const A2 w = mu::IsBf<IO>::v ? A2{mu::pack_bf2(v[0], v[1]), mu::pack_bf2(v[2], v[3])} : A2{mu::pack_h2(v[0], v[1]), mu::pack_h2(v[2], v[3])};
+        *reinterpret_cast<A2*>(p) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) IO::st(p, i, v[i]);
+}
+template <class IO>
+__device__ __forceinline__ void load4(const typename IO::T* p, int n, float (&v)[4])
+{
+    if (n >= 4) {
+        if constexpr (sizeof(typename IO::T) == 4) {
+            const At4 w = *reinterpret_cast<const At4*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+            typedef uint32_t A2 __attribute__((ext_vector_type(2), aligned(2)));
+            const A2 w = *reinterpret_cast<const A2*>(p);
+            unpack2<IO>(w[0], v[0], v[1]);
+            unpack2<IO>(w[1], v[2], v[3]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? IO::ld(p, i) : 0.f;
+}
+
+// Workgroup: one tile, of one batch and one share of the sum.  A wave has 64 by 64 of it, in tiles of 16 by 16.
+template <class IO, bool FK, bool SK, int EPI>
+__global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f, uint32_t tiles_s)
+{
+    using T = typename IO::T;
+    using TileF = Tile<IO, FK>;
+    using TileS = Tile<IO, SK>;
+    constexpr int BK = TileF::BK, STEP = TileF::STEP;
+    __shared__ __align__(16) unsigned char lds[TileF::BYTES + TileS::BYTES];
+    T *const lf = reinterpret_cast<T*>(lds), *const ls = reinterpret_cast<T*>(lds + TileF::BYTES);
+    uint32_t w = blockIdx.x;
+    const uint32_t tf = w % tiles_f;
+    w /= tiles_f;
+    const uint32_t ts = w % tiles_s;
+    w /= tiles_s;
+    const uint32_t split = w % (uint32_t)a.splits, batch = w / (uint32_t)a.splits;
+    const int64_t f0 = (int64_t)tf * TF, s0 = (int64_t)ts * TS, steps = (a.K + BK - 1) / BK;
+    const int64_t first = (int64_t)split * a.per, end = first + a.per < steps * a.segs ? first + a.per : steps * a.segs;
+    const int wave = threadIdx.x >> 6, wf = (wave & 1) * 64, ws = (wave >> 1) * 64;
+    mu::f4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = mu::f4{0.f, 0.f, 0.f, 0.f};
+    Raw8<IO> rf[TileF::PIECES], rs[TileS::PIECES];
+    const auto ask = [&](int64_t at) {
+        const int64_t q = at / steps, k0 = (at - q * steps) * BK;
+        TileF::load(a.F, batch * a.F.batch + q * a.F.seg, f0, k0, a.K, rf);
+        TileS::load(a.S, batch * a.S.batch + q * a.S.seg, s0, k0, a.K, rs);
+    };
+    if (first < end) ask(first);
+    for (int64_t at = first; at < end; ++at) {
+        __syncthreads();
+        TileF::put(lf, rf);
+        TileS::put(ls, rs);
+        __syncthreads();
+        if (at + 1 < end) ask(at + 1);
+#pragma unroll
+        for (int m = 0; m < BK / STEP; ++m) {
+            typename TileF::Frag x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = TileF::frag(lf, wf + 16 * i, m);
+                y[i] = TileS::frag(ls, ws + 16 * i, m);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = mfma(IO(), x[i], y[j], acc[i][j]);
+        }
+    }
+    // a lane has f = 4 (lane / 16) .. + 3 and s = lane % 16 of each tile of 16 by 16
+    const int col = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
+    if constexpr (EPI == EPI_SUM) {
+        float* const to = a.part + (size_t)split * a.S.n * a.F.n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t s = s0 + ws + 16 * j + col;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t f = f0 + wf + 16 * i + 4 * g, n = a.F.n - f;
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                if (s < a.S.n && n > 0) store4<IoF32>(to + s * a.F.n + f, n < 4 ? (int)n : 4, v);
+            }
+        }
+        return;
+    }
+    float by_f[4][4] = {}, by_s[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t f = f0 + wf + 16 * i + 4 * g, n_f = a.F.n - f;
+        const int n = n_f < 4 ? (int)n_f : 4;
+        float bf[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.bias && a.bias_f && n > 0) load4<IoF32>(a.bias + f, n, bf);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t s = s0 + ws + 16 * j + col;
+            if (s >= a.S.n || n <= 0) continue;
+            const size_t at = (size_t)batch * a.batch + s * a.ld + f;
+            const float bs = a.bias && !a.bias_f ? a.bias[s] : 0.f;
+            float v[4], r[4] = {0.f, 0.f, 0.f, 0.f};
+            if (EPI == EPI_DZ) load4<IO>((const T*)a.dy + at, n, r);
+            else if (a.residual) load4<IO>((const T*)a.residual + at, n, r);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float z = acc[i][j][q] + bf[q] + bs;
+                if (EPI == EPI_DZ) {
+                    v[q] = q < n ? r[q] * slope_by(a.act, z) : 0.f;
+                    by_f[i][q] += v[q];
+                    by_s[j] += v[q];
+                } else v[q] = act_by(a.act, z) + r[q];
+            }
+            store4<IO>((T*)a.out + at, n, v);
+        }
+    }
+    if constexpr (EPI == EPI_DZ) {
+        if (!a.sums) return;
+        if (a.bias_f) {      // places are s: over the lanes of a row of sixteen
+            float* const to = a.sums + ((size_t)(batch * tiles_s + ts) * 2 + (wave >> 1)) * a.F.n;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v = by_f[i][q];
+#pragma unroll
+                    for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
+                    const int64_t f = f0 + wf + 16 * i + 4 * g + q;
+                    if (col == 0 && f < a.F.n) to[f] = v;
+                }
+        } else {             // places are f: over the four rows of lanes
+            float* const to = a.sums + ((size_t)(batch * tiles_f + tf) * 2 + (wave & 1)) * a.S.n;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v = by_s[j];
+                v += __shfl_xor(v, 16);
+                v += __shfl_xor(v, 32);
+                const int64_t s = s0 + ws + 16 * j + col;
+                if (g == 0 && s < a.S.n) to[s] = v;
+            }
+        }
+    }
+}
+
+// out[i] = sum over the shares, in their order
+template <class IO>
+__global__ __launch_bounds__(256) void linear_join_kernel(const float* __restrict__ part, typename IO::T* __restrict__ out, int64_t n, int64_t shares)
+{
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= n) return;
+    const int here = n - at < 4 ? (int)(n - at) : 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t q = 0; q < shares; ++q) {
+        float w[4];
+        load4<IoF32>(part + q * n + at, here, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += w[i];
+    }
+    store4<IO>(out + at, here, v);
+}
+
+constexpr int COLUMN_ROWS = 256;      // places that a workgroup adds up
+
+// part[share][M] <- sums of dy over places: of [T,M], shares of COLUMN_ROWS places
+template <class IO>
+__global__ __launch_bounds__(256) void columns_last_kernel(const typename IO::T* __restrict__ dy, float* __restrict__ part, int64_t T, int64_t M,
+                                                           uint32_t wide)
+{
+    const uint32_t share = blockIdx.x / wide;
+    const int64_t m = (int64_t)(blockIdx.x - share * wide) * 256 + threadIdx.x, first = (int64_t)share * COLUMN_ROWS;
+    if (m >= M) return;
+    const int64_t end = first + COLUMN_ROWS < T ? first + COLUMN_ROWS : T;
+    float v = 0.f;
+    for (int64_t t = first; t < end; ++t) v += IO::ld(dy, t * M + m);
+    part[(size_t)share * M + m] = v;
+}
+// of [B,M,N]: a share for each sequence
+template <class IO>
+__global__ __launch_bounds__(256) void columns_first_kernel(const typename IO::T* __restrict__ dy, float* __restrict__ part, int64_t rows, int64_t N)
+{
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * 4) {
+        float v = 0.f;
+        for (int64_t t = threadIdx.x & 63; t < N; t += 64) v += IO::ld(dy, row * N + t);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+        if ((threadIdx.x & 63) == 0) part[row] = v;
+    }
+}
+// dbias[m] = the sum of shares, a workgroup of eight rows of 32 columns
+__global__ __launch_bounds__(256) void columns_join_kernel(const float* __restrict__ part, float* __restrict__ dbias, int64_t M, int64_t shares)
+{
+    __shared__ float lds[8][32];
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+    const int64_t m = (int64_t)blockIdx.x * 32 + c;
+    float v = 0.f;
+    if (m < M)
+        for (int64_t q = r; q < shares; q += 8) v += part[q * M + m];
+    lds[r][c] = v;
+    __syncthreads();
+    if (r == 0 && m < M) {
+        for (int q = 1; q < 8; ++q) v += lds[q][c];
+        dbias[m] = v;
+    }
+}
+
+template <class IO, int EPI>
+hipError_t launch_product(const Product& p, bool fk, bool sk, hipStream_t st)
+{
+    const uint64_t tf = (uint64_t)((p.F.n + TF - 1) / TF), ts = (uint64_t)((p.S.n + TS - 1) / TS);
+    dim3 g;
+    const hipError_t e = launch_grid(tf * ts * (uint64_t)p.splits * (uint64_t)p.batches, LT, &g);
+    if (e != hipSuccess) return e;
+    const uint32_t a = (uint32_t)tf, b = (uint32_t)ts;
+    if (fk && sk) hipLaunchKernelGGL((product_kernel<IO, true, true, EPI>), g, dim3(LT), 0, st, p, a, b);
+    else if (fk) hipLaunchKernelGGL((product_kernel<IO, true, false, EPI>), g, dim3(LT), 0, st, p, a, b);
+    else if (sk) hipLaunchKernelGGL((product_kernel<IO, false, true, EPI>), g, dim3(LT), 0, st, p, a, b);
+    else hipLaunchKernelGGL((product_kernel<IO, false, false, EPI>), g, dim3(LT), 0, st, p, a, b);
+    return hipGetLastError();
+}
+
+inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// How the places are cut: [B,.,N] by sequences, [B,N,.] not at all; rows of one place are both
+struct Cut {
+    bool x_first, y_first;
+    int64_t batches, places;      // of the products that have the places as an index
+    Cut(const LinearArgs& a)
+    {
+        x_first = a.x_first && a.N > 1;
+        y_first = a.y_first && a.N > 1;
+        batches = x_first || y_first ? a.B : 1;
+        places = x_first || y_first ? a.N : a.B * a.N;
+    }
+};
+// rows [place][c] or [c][place] of a batch
+inline Side rows_of(const void* p, bool first, const Cut& c, int64_t width)
+{
+    return Side{p, c.places, first ? c.places : width, c.places * width, 0};
+}
+
+// z = x W^T + bias and what follows it
+template <class IO, int EPI>
+hipError_t forward(const LinearArgs& a, const void* x, Product p, hipStream_t st)
+{
+    const Cut c(a);
+    const Side X = rows_of(x, c.x_first, c, a.K), W{a.W, a.M, a.K, 0, 0};
+    p.K = a.K;
+    p.segs = 1;
+    p.batches = c.batches;
+    p.splits = 1;
+    p.per = INT64_MAX / 4;
+    p.bias = a.bias;
+    p.act = a.act;
+    p.batch = c.places * a.M;
+    p.ld = c.y_first ? c.places : a.M;
+    p.bias_f = !c.y_first;
+    p.F = c.y_first ? X : W;
+    p.S = c.y_first ? W : X;
+    return launch_product<IO, EPI>(p, c.y_first ? !c.x_first : true, c.y_first ? true : !c.x_first, st);
+}
+
+// shares of the sum over places of dW: as many as make 512 workgroups, of four steps at least
+struct Shares {
+    int64_t shares, per;
+};
+template <class IO>
+Shares shares_of(int64_t B, int64_t N, int64_t K, int64_t M, bool by_batch)
+{
+    constexpr int BK = Tile<IO, true>::BK;
+    const int64_t tiles = ((K + TF - 1) / TF) * ((M + TS - 1) / TS);
+    const int64_t steps = by_batch ? B * ((N + BK - 1) / BK) : (B * N + BK - 1) / BK;
+    int64_t want = (512 + tiles - 1) / tiles;
+    if (want > (steps + 3) / 4) want = (steps + 3) / 4;
+    const int64_t per = (steps + want - 1) / want;
+    return Shares{(steps + per - 1) / per, per};
+}
+
+template <class IO>
+hipError_t linear_fwd_io(const LinearArgs& a, const void* x, const void* residual, void* y, void* ws, hipStream_t st)
+{
+    Product p = {};
+    p.out = y;
+    p.residual = residual;
+    return forward<IO, EPI_OUT>(a, x, p, st);
+}
+
+// shares of the sums of dbias: of a tile's halves (EPI_DZ), of sequences, of places
+inline int64_t bias_shares(int64_t B, int64_t N)
+{
+    const int64_t by_batch = 2 * B * ((N + 127) / 128), flat = 2 * ((B * N + 127) / 128);
+    return by_batch > flat ? by_batch : flat;
+}
+template <class IO>
+size_t linear_workspace_io(int64_t B, int64_t N, int64_t K, int64_t M, int backward)
+{
+    if (!backward) return 256;
+    const int64_t tiles = ((K + TF - 1) / TF) * ((M + TS - 1) / TS);
+    const int64_t want = (512 + tiles - 1) / tiles, steps = (B * ((N + 15) / 16) + 3) / 4;      // (never more shares than either)
+    return up256((size_t)B * N * M * sizeof(typename IO::T)) + up256((size_t)(want < steps ? want : steps) * K * M * sizeof(float)) +
+           up256((size_t)bias_shares(B, N) * M * sizeof(float));
+}
+
+template <class IO>
+hipError_t linear_bwd_io(const LinearArgs& a, const LinearGrads& d, void* ws, hipStream_t st)
+{
+    using T = typename IO::T;
+    const Cut c(a);
+    char* at = (char*)ws;
+    void* const dz_room = at;
+    at += up256((size_t)a.B * a.N * a.M * sizeof(T));
+    const bool by_batch = c.x_first || c.y_first;
+    const Shares sh = shares_of<IO>(a.B, a.N, a.K, a.M, by_batch);
+    float* const part = (float*)at;
+    at += up256((size_t)sh.shares * a.K * a.M * sizeof(float));
+    float* const sums = (float*)at;
+    const void* dz = d.dy;
+    hipError_t e = hipSuccess;
+    int64_t bias_parts = 0;
+    if (a.act != LONGCONV_ACT_NONE) {
+        Product p = {};
+        p.out = dz_room;
+        p.dy = d.dy;
+        p.sums = d.dbias ? sums : nullptr;
+        e = forward<IO, EPI_DZ>(a, d.x, p, st);
+        dz = dz_room;
+        bias_parts = c.batches * ((c.places + 127) / 128) * 2;
+    } else if (d.dbias) {
+        if (c.y_first) {
+            bias_parts = a.B;
+            const int64_t groups = (a.B * a.M + 3) / 4;
+            hipLaunchKernelGGL(columns_first_kernel<IO>, dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20)), dim3(256), 0, st, (const T*)d.dy, sums, a.B * a.M, a.N);
+        } else {
+            bias_parts = (a.B * a.N + COLUMN_ROWS - 1) / COLUMN_ROWS;
+            const uint32_t wide = (uint32_t)((a.M + 255) / 256);
+            hipLaunchKernelGGL(columns_last_kernel<IO>, dim3((unsigned)(bias_parts * wide)), dim3(256), 0, st, (const T*)d.dy, sums, a.B * a.N, a.M, wide);
+        }
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+    if (d.dbias) {
+        hipLaunchKernelGGL(columns_join_kernel, dim3((unsigned)((a.M + 31) / 32)), dim3(256), 0, st, sums, d.dbias, a.M, bias_parts);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (d.dx) {      // dx[place][k] = sum_m dz[place][m] W[m][k]
+        Product p = {};
+        const Side Z = rows_of(dz, c.y_first, c, a.M), W{a.W, a.K, a.K, 0, 0};
+        p.K = a.M;
+        p.segs = 1;
+        p.batches = c.batches;
+        p.splits = 1;
+        p.per = INT64_MAX / 4;
+        p.act = LONGCONV_ACT_NONE;
+        p.out = d.dx;
+        p.batch = c.places * a.K;
+        p.ld = c.x_first ? c.places : a.K;
+        p.F = c.x_first ? Z : W;
+        p.S = c.x_first ? W : Z;
+        e = launch_product<IO, EPI_OUT>(p, c.x_first ? !c.y_first : false, c.x_first ? false : !c.y_first, st);
+        if (e != hipSuccess) return e;
+    }
+    if (d.dW) {      // dW[m][k] = sum over places of dz[place][m] x[place][k]
+        Product p = {};
+        p.F = rows_of(d.x, c.x_first, c, a.K);
+        p.F.seg = p.F.batch;
+        p.F.n = a.K;
+        p.S = rows_of(dz, c.y_first, c, a.M);
+        p.S.seg = p.S.batch;
+        p.S.n = a.M;
+        p.K = c.places;
+        p.segs = c.batches;
+        p.batches = 1;
+        p.splits = sh.shares;
+        p.per = sh.per;
+        p.part = sh.shares == 1 && d.dW_f32 ? (float*)d.dW : part;
+        e = launch_product<IO, EPI_SUM>(p, c.x_first, c.y_first, st);
+        if (e != hipSuccess || p.part == d.dW) return e;
+        const int64_t n = a.K * a.M;
+        const dim3 g((unsigned)((n + 1023) / 1024));
+        if (d.dW_f32) hipLaunchKernelGGL(linear_join_kernel<IoF32>, g, dim3(256), 0, st, part, (float*)d.dW, n, sh.shares);
+        else hipLaunchKernelGGL(linear_join_kernel<IO>, g, dim3(256), 0, st, part, (T*)d.dW, n, sh.shares);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+}  // namespace
+
+template <class IO>
+size_t linear_workspace_of(int64_t B, int64_t N, int64_t K, int64_t M, int backward)
+{
+    return linear_workspace_io<IO>(B, N, K, M, backward);
+}
+template <class IO>
+hipError_t linear_fwd_of(const LinearArgs& a, const void* x, const void* residual, void* y, void* ws, hipStream_t st)
+{
+    return linear_fwd_io<IO>(a, x, residual, y, ws, st);
+}
+template <class IO>
+hipError_t linear_bwd_of(const LinearArgs& a, const LinearGrads& d, void* ws, hipStream_t st)
+{
+    return linear_bwd_io<IO>(a, d, ws, st);
+}
+
+}  // namespace lc

@@ -1,5 +1,5 @@
 // Launch interfaces of the operators around the convolution: dropout (dropout.hip, kreg.hip), embedding (embed.hip), group norm
-// (gnorm.hip).  Arguments are checked by the C-ABI layer.
+// (gnorm.hip), and beside it: short convolution (short.hip), selective scan (scan.hip), dense product (linear.hip).  Arguments are checked by the C-ABI layer.
 #pragma once
 #include "engines.hpp"
 
@@ -63,5 +63,63 @@ size_t gnorm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t G, int io,
 hipError_t gnorm_fwd(const GnormArgs& a, const void* x, void* y, float* mean, float* rstd, float eps, void* ws, hipStream_t st);
 hipError_t gnorm_bwd(const GnormArgs& a, const void* dy, const void* x, const float* mean, const float* rstd, void* dx, float* dgamma,
                      float* dbeta, void* ws, hipStream_t st);
+
+// ---- operators beside the convolution ----------------------------------------------------------------------------------
+
+// Short causal convolution (short.hip)
+constexpr int SHORT_TAPS = 8;      // at most
+struct ShortArgs {
+    const float *k, *bias;          // [H,taps], [H] or null
+    const int64_t* lengths;         // [B] on the device, or null: all N
+    int64_t B, H, N;
+    int taps, act, io;
+};
+struct ShortGrads {                 // state, dlast may be null, and so may any result
+    const void *dy, *x, *state, *dlast;
+    void *dx, *dstate;
+    float *dk, *dbias;
+};
+size_t short_workspace_bytes(int64_t B, int64_t H, int64_t N);
+hipError_t short_fwd(const ShortArgs& a, const void* x, const void* state, void* y, void* last, hipStream_t st);
+hipError_t short_bwd(const ShortArgs& a, const ShortGrads& d, void* ws, hipStream_t st);
+hipError_t short_step(const ShortArgs& a, const void* x, void* state, void* y, hipStream_t st);
+
+// Selective state space scan (scan.hip, scan_bwd.hip)
+constexpr int SCAN_STATES = 64;      // at most
+struct ScanArgs {
+    const void *u, *delta, *Bm, *Cm, *z;      // z may be null
+    const float *A, *D, *bias;                // [H,S], [H] or null, [H] or null
+    const int64_t* lengths;                   // [B] on the device, or null: all N
+    int64_t B, H, N, G;
+    int S, softplus, io;
+};
+struct ScanGrads {                            // dlast may be null, and so may any result
+    const void* dy;
+    const float *marks, *dlast;
+    void *du, *ddelta, *dB, *dC, *dz;
+    float *dA, *dD, *dbias, *dstate;
+};
+size_t scan_workspace_bytes(int64_t B, int64_t H, int64_t N, int S, int64_t G, int backward);
+hipError_t scan_fwd(const ScanArgs& a, const float* state, void* y, float* last, float* marks, void* ws, hipStream_t st);
+hipError_t scan_bwd(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st);
+hipError_t scan_step(const ScanArgs& a, float* state, void* y, hipStream_t st);
+
+// Dense product (linear.hip, linear.hpp)
+struct LinearArgs {
+    const void* W;                            // [M,K] in the I/O type
+    const float* bias;                        // [M] or null
+    int64_t B, N, K, M;
+    int act, io;
+    bool x_first, y_first;                    // [B,.,N], else [B,N,.]
+};
+struct LinearGrads {                          // any result may be null
+    const void *dy, *x;
+    void *dx, *dW;
+    float* dbias;
+    bool dW_f32;                              // dW is float32, not the I/O type
+};
+size_t linear_workspace_bytes(int64_t B, int64_t N, int64_t K, int64_t M, int io, int backward);
+hipError_t linear_fwd(const LinearArgs& a, const void* x, const void* residual, void* y, void* ws, hipStream_t st);
+hipError_t linear_bwd(const LinearArgs& a, const LinearGrads& d, void* ws, hipStream_t st);
 
 }  // namespace lc

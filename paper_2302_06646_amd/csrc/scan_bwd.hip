@@ -1,0 +1,392 @@
+// Backward pass of the selective scan (formulas of the forward pass: scan.hip).  With g_t the gradient of the state h_t, q_t = g_t a_t h_{t-1}:
+//     dy' = dy silu(z),   dz = dy (C h + D u) silu'(z),   g_t = C_t dy'_t + a_{t+1} g_{t+1}   (behind the last place: dlast),
+//     du = dt sum_s g B + D dy',   ddt = sum_s A q + u sum_s g B,   ddelta = ddt (1 - exp(-dt) with softplus),
+//     dA = sum_{b,t} dt q,   dB = sum over the group's heads of g dt u,   dC = ... of dy' h,   dD = sum dy' u,   dbias = sum ddelta.
+//
+// Chunks of SPAN places, from the last to the first.  A wave has NS states and walks over a block of heads: the sums over heads, dB and dC,
+// stay in its registers for the chunk; the sums over states, of every head, go through LDS between the NW waves.  h runs again from the
+// forward pass's marks, one for each chunk.
+#include "scan.hpp"
+
+namespace lc {
+namespace {
+
+constexpr int K = SPAN / 64;      // places of a lane
+
+// where place t of a chunk lies in LDS: a wave's reads of four places a lane are one run of memory
+__device__ __forceinline__ int place(int t) { return (t % K / 4 * 64 + t / K) * 4 + t % 4; }
+
+struct Parts {
+    float *dB, *dC;      // [blocks][B,G,S,N], or null: dB and dC are written themselves
+    float *dA;           // [B segs][H,S]
+    float *dDb;          // [B segs][H,2]: of D and of the bias
+};
+
+template <class IO, int NS, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void scan_bwd_kernel(ScanArgs a, ScanGrads d, Segments g, Parts parts, int blocks, int CB)
+{
+    using T = typename IO::T;
+    constexpr int TH = 64 * NW, SP = NS * NW, TPT = SPAN / TH;      // threads, states with those that are not there, places of a thread
+    extern __shared__ __align__(16) float lds[];
+    float* const stage = lds;                        // [3][SPAN]: dt, dt u, dy'
+    float* const part = stage + 3 * SPAN;            // [NW][3][SPAN]: sums over a wave's states of g B, A q, C h
+    float* const gcar = part + NW * 3 * SPAN;        // [CB][SP]: what the chunk behind hands on
+    float* const dAsum = gcar + CB * SP;             // [CB][SP]
+    float* const small = dAsum + CB * SP;            // [NW][CB][2]: of dD and dbias
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x;
+    int64_t w = blockIdx.x;
+    const int seg = (int)(w % g.segs);
+    w /= g.segs;
+    const int blk = (int)(w % blocks);
+    w /= blocks;
+    const int64_t grp = w % a.G, b = w / a.G, in_group = a.H / a.G;
+    const int64_t N = a.N, len = scan_length(a, b);
+    const int64_t begin = seg * g.len, stop = begin + g.len < N ? begin + g.len : N, end = stop < len ? stop : len;
+    const int64_t head0 = grp * in_group + (int64_t)blk * CB;
+    const int heads = (int)(in_group - (int64_t)blk * CB < CB ? in_group - (int64_t)blk * CB : CB);
+    const int S = a.S;
+    const int64_t n_marks = (N + SPAN - 1) / SPAN;
+    const size_t bg = (size_t)(b * a.G + grp) * S;      // rows of B, C
+    for (int i = tid; i < heads * SP; i += TH) {
+        const int c = i / SP, s = i % SP;
+        const size_t row = (size_t)b * a.H + head0 + c;
+        float from = 0.f;
+        if (s < S) from = entering<true>(g, row, seg, S, s, LOG2E * a.A[(head0 + c) * S + s], d.dlast ? d.dlast[row * S + s] : 0.f);
+        gcar[c * SP + s] = from;
+        dAsum[c * SP + s] = 0.f;
+    }
+    for (int i = tid; i < NW * CB * 2; i += TH) small[i] = 0.f;
+
+    const int64_t top = end > begin ? begin + (end - 1 - begin) / SPAN * SPAN : begin - SPAN;
+    for (int64_t t0 = top; t0 >= begin; t0 -= SPAN) {
+        float dBv[NS][K], dCv[NS][K];
+        constexpr bool HELD = NS <= 4;      // B and C in registers for all heads, or brought in for each
+        float Bv[HELD ? NS : 1][K], Cv[HELD ? NS : 1][K];
+        const auto bring = [&](int n, float (&Bq)[K], float (&Cq)[K]) {
+            const int s = wave * NS + n;
+#pragma unroll
+            for (int j = 0; j < K; j += 4) {
+                const float4 q = s < S ? load4<IO>((const T*)a.Bm + (bg + s) * N, t0 + lane * K + j, N, end) : make_float4(0.f, 0.f, 0.f, 0.f);
+                const float4 r = s < S ? load4<IO>((const T*)a.Cm + (bg + s) * N, t0 + lane * K + j, N, end) : make_float4(0.f, 0.f, 0.f, 0.f);
+                Bq[j] = q.x; Bq[j + 1] = q.y; Bq[j + 2] = q.z; Bq[j + 3] = q.w;
+                Cq[j] = r.x; Cq[j + 1] = r.y; Cq[j + 2] = r.z; Cq[j + 3] = r.w;
+            }
+        };
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            if constexpr (HELD) bring(n, Bv[n], Cv[n]);
+#pragma unroll
+            for (int i = 0; i < K; ++i) dBv[n][i] = dCv[n][i] = 0.f;
+        }
+        for (int c = 0; c < heads; ++c) {
+            const int64_t h = head0 + c;
+            const size_t row = (size_t)b * a.H + h;
+            const float bias = a.bias ? a.bias[h] : 0.f, D = a.D ? a.D[h] : 0.f;
+            // this thread's places, for all waves and for itself
+            float dt[TPT], u[TPT], dyg[TPT], dyz[TPT], rate[TPT];
+#pragma unroll
+            for (int i = 0; i < TPT; ++i) {
+                const int64_t t = t0 + tid * TPT + i;
+                dt[i] = u[i] = dyg[i] = dyz[i] = rate[i] = 0.f;
+                if (t < end) {
+                    const float x = IO::ld((const T*)a.delta + row * N, t) + bias;
+                    dt[i] = a.softplus ? softplus_of(x) : x;
+                    rate[i] = a.softplus ? logistic(x) : 1.f;
+                    u[i] = IO::ld((const T*)a.u + row * N, t);
+                    dyg[i] = IO::ld((const T*)d.dy + row * N, t);
+                    if (a.z) {
+                        const float z = IO::ld((const T*)a.z + row * N, t), q = logistic(z);
+                        dyz[i] = dyg[i] * (q * (1.f + z * (1.f - q)));
+                        dyg[i] *= z * q;
+                    }
+                }
+                const int to = place(tid * TPT + i);
+                stage[to] = dt[i];
+                stage[SPAN + to] = dt[i] * u[i];
+                stage[2 * SPAN + to] = dyg[i];
+            }
+            __syncthreads();
+            float e[K], x[K], f[K], gB[K], Aq[K], Ch[K], sum = 0.f;      // dt, dt u, dy' of the lane's places
+#pragma unroll
+            for (int j = 0; j < K / 4; ++j) {
+                const float4 q = reinterpret_cast<const float4*>(stage)[j * 64 + lane];
+                const float4 r = reinterpret_cast<const float4*>(stage + SPAN)[j * 64 + lane];
+                const float4 v = reinterpret_cast<const float4*>(stage + 2 * SPAN)[j * 64 + lane];
+                e[4 * j] = q.x; e[4 * j + 1] = q.y; e[4 * j + 2] = q.z; e[4 * j + 3] = q.w;
+                x[4 * j] = r.x; x[4 * j + 1] = r.y; x[4 * j + 2] = r.z; x[4 * j + 3] = r.w;
+                f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
+            }
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                sum += e[i];
+                gB[i] = Aq[i] = Ch[i] = 0.f;
+            }
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                const int s = wave * NS + n;
+                if (s >= S) continue;
+                if constexpr (!HELD) bring(n, Bv[0], Cv[0]);
+                const float(&B)[K] = Bv[HELD ? n : 0];
+                const float(&C)[K] = Cv[HELD ? n : 0];
+                const float A = a.A[h * S + s], A2 = LOG2E * A;
+                const float in = d.marks[(row * n_marks + t0 / SPAN) * S + s], back = gcar[c * SP + s];
+                float dec[K], q[K];
+                float v = lane == 0 ? in : 0.f;
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    dec[i] = exp2_of(A2 * e[i]);
+                    v = __builtin_fmaf(dec[i], v, x[i] * B[i]);
+                }
+                const float all = exp2_of(A2 * sum);
+                float p = all;
+                scan_up(p, v);
+                v = dpp<0x138>(v, in);      // the state in front of the lane
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    q[i] = dec[i] * v;
+                    v = __builtin_fmaf(x[i], B[i], q[i]);
+                    dCv[n][i] = __builtin_fmaf(f[i], v, dCv[n][i]);
+                    Ch[i] = __builtin_fmaf(C[i], v, Ch[i]);
+                }
+                v = lane == 63 ? back : 0.f;
+#pragma unroll
+                for (int i = K - 1; i >= 0; --i) v = dec[i] * __builtin_fmaf(C[i], f[i], v);
+                p = all;
+                scan_down(p, v);
+                v = dpp<0x130>(v, back);      // what the lane behind hands on
+                float dA = 0.f;
+#pragma unroll
+                for (int i = K - 1; i >= 0; --i) {
+                    const float gt = __builtin_fmaf(C[i], f[i], v);
+                    dBv[n][i] = __builtin_fmaf(gt, x[i], dBv[n][i]);
+                    gB[i] = __builtin_fmaf(gt, B[i], gB[i]);
+                    const float qt = gt * q[i];
+                    Aq[i] = __builtin_fmaf(A, qt, Aq[i]);
+                    dA = __builtin_fmaf(e[i], qt, dA);
+                    v = dec[i] * gt;
+                }
+                dA = sum_of_wave(dA);
+                if (lane == 0) {
+                    gcar[c * SP + s] = v;
+                    dAsum[c * SP + s] += dA;
+                }
+            }
+            float4* const to = reinterpret_cast<float4*>(part + wave * 3 * SPAN);
+#pragma unroll
+            for (int j = 0; j < K / 4; ++j) {
+                to[j * 64 + lane] = make_float4(gB[4 * j], gB[4 * j + 1], gB[4 * j + 2], gB[4 * j + 3]);
+                to[SPAN / 4 + j * 64 + lane] = make_float4(Aq[4 * j], Aq[4 * j + 1], Aq[4 * j + 2], Aq[4 * j + 3]);
+                if (d.dz) to[SPAN / 2 + j * 64 + lane] = make_float4(Ch[4 * j], Ch[4 * j + 1], Ch[4 * j + 2], Ch[4 * j + 3]);
+            }
+            __syncthreads();
+            float sD = 0.f, sb = 0.f;
+#pragma unroll
+            for (int i = 0; i < TPT; ++i) {
+                const int at = place(tid * TPT + i);
+                float wB = 0.f, wA = 0.f, wC = 0.f;
+#pragma unroll
+                for (int r = 0; r < NW; ++r) {
+                    wB += part[r * 3 * SPAN + at];
+                    wA += part[r * 3 * SPAN + SPAN + at];
+                    if (d.dz) wC += part[r * 3 * SPAN + 2 * SPAN + at];
+                }
+                const int64_t t = t0 + tid * TPT + i;
+                const float dw = __builtin_fmaf(wB, u[i], wA) * rate[i];
+                if (t < stop) {
+                    const bool is = t < end;
+                    if (d.du) IO::st((T*)d.du + row * N, t, is ? __builtin_fmaf(dt[i], wB, D * dyg[i]) : 0.f);
+                    if (d.ddelta) IO::st((T*)d.ddelta + row * N, t, is ? dw : 0.f);
+                    if (d.dz) IO::st((T*)d.dz + row * N, t, is ? __builtin_fmaf(D, u[i], wC) * dyz[i] : 0.f);
+                    if (is) {
+                        sD = __builtin_fmaf(dyg[i], u[i], sD);
+                        sb += dw;
+                    }
+                }
+            }
+            sD = sum_of_wave(sD);
+            sb = sum_of_wave(sb);
+            if (lane == 0) {
+                small[(wave * CB + c) * 2] += sD;
+                small[(wave * CB + c) * 2 + 1] += sb;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const int s = wave * NS + n;
+            if (s >= S) continue;
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                float(&v)[K] = which ? dCv[n] : dBv[n];
+                const int64_t t = t0 + lane * K;
+                const int64_t n_here = stop - t;
+#pragma unroll
+                for (int i = 0; i < K; ++i) v[i] = t + i < end ? v[i] : 0.f;
+                float* const f32 = which ? parts.dC : parts.dB;
+                T* const io = (T*)(which ? d.dC : d.dB);
+                if (f32) {
+                    if (n_here > 0) store8<IoF32>(f32 + ((size_t)blk * a.B * a.G * S + bg + s) * N + t, n_here < VE ? (int)n_here : VE, v);
+                } else if (io && n_here > 0) store8<IO, true>(io + (bg + s) * N + t, n_here < VE ? (int)n_here : VE, v);
+            }
+        }
+    }
+    // behind the sequence's end, from the first place that no chunk wrote
+    const int64_t zero = top + SPAN > begin ? top + SPAN : begin;
+    for (int c = 0; c < heads; ++c) {
+        const size_t row = (size_t)b * a.H + head0 + c;
+        for (int64_t t = zero + tid; t < stop; t += TH) {
+            if (d.du) IO::st((T*)d.du + row * N, t, 0.f);
+            if (d.ddelta) IO::st((T*)d.ddelta + row * N, t, 0.f);
+            if (d.dz) IO::st((T*)d.dz + row * N, t, 0.f);
+        }
+    }
+    if (!parts.dB)
+        for (int s = 0; s < S; ++s)
+            for (int64_t t = zero + tid; t < stop; t += TH) {
+                if (d.dB) IO::st((T*)d.dB + (bg + s) * N, t, 0.f);
+                if (d.dC) IO::st((T*)d.dC + (bg + s) * N, t, 0.f);
+            }
+    __syncthreads();
+    for (int i = tid; i < heads * S; i += TH) {
+        const int c = i / S, s = i % S;
+        const size_t h = head0 + c, row = (size_t)b * a.H + h;
+        parts.dA[((size_t)(b * g.segs + seg) * a.H + h) * S + s] = dAsum[c * SP + s];
+        if (d.dstate && seg == 0) d.dstate[row * S + s] = gcar[c * SP + s];
+    }
+    for (int i = tid; i < heads * 2; i += TH) {
+        float s = 0.f;
+        for (int r = 0; r < NW; ++r) s += small[r * CB * 2 + i];
+        parts.dDb[((size_t)(b * g.segs + seg) * a.H + head0) * 2 + i] = s;
+    }
+}
+
+// dB and dC from the blocks' sums
+template <class IO>
+__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Parts parts, typename IO::T* __restrict__ dB, typename IO::T* __restrict__ dC, int blocks)
+{
+    const int64_t P = (a.N + VE - 1) / VE, rows = a.B * a.G * a.S;
+    int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= 2 * rows * P) return;
+    const bool second = id >= rows * P;
+    if (second) id -= rows * P;
+    typename IO::T* const to = second ? dC : dB;
+    if (!to) return;
+    const int64_t row = id / P, t = (id - row * P) * VE, len = scan_length(a, row / (a.G * a.S));
+    const float* from = (second ? parts.dC : parts.dB) + row * a.N + t;
+    float v[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = 0.f;
+    const int n = a.N - t < VE ? (int)(a.N - t) : VE;
+    if (t < len)
+        for (int q = 0; q < blocks; ++q) {
+            float w[VE];
+            load8<IoF32>(from + (size_t)q * rows * a.N, n, w);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[i] += w[i];
+        }
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = t + i < len ? v[i] : 0.f;
+    store8<IO, true>(to + row * a.N + t, n, v);
+}
+
+// dA, dD, dbias from the sums of sequences and segments
+__global__ __launch_bounds__(256) void scan_sums_kernel(Parts parts, float* __restrict__ dA, float* __restrict__ dD, float* __restrict__ dbias, int64_t H,
+                                                        int S, int64_t shares)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id < H * S) {
+        if (!dA) return;
+        float s = 0.f;
+        for (int64_t q = 0; q < shares; ++q) s += parts.dA[q * H * S + id];
+        dA[id] = s;
+    } else if (id < H * S + 2 * H) {
+        const int64_t i = id - H * S;
+        float* const to = i & 1 ? dbias : dD;
+        if (!to) return;
+        float s = 0.f;
+        for (int64_t q = 0; q < shares; ++q) s += parts.dDb[q * 2 * H + i];
+        to[i >> 1] = s;
+    }
+}
+
+// Heads of a workgroup: as many as leave 256 workgroups (with the segments a sequence may be cut into), 32 at most
+int block_heads(int64_t B, int64_t H, int64_t N, int64_t G)
+{
+    int CB = 32;
+    while (CB > 8 && B * G * ((H / G + CB - 1) / CB) * ((N + 1023) / 1024) < 256) CB /= 2;
+    return CB;
+}
+
+template <class IO, int NS, int NW>
+hipError_t launch(const ScanArgs& a, const ScanGrads& d, const Segments& g, const Parts& parts, int blocks, int CB, hipStream_t st)
+{
+    dim3 grid;
+    hipError_t e = launch_grid((uint64_t)(a.B * a.G * blocks * g.segs), 64 * NW, &grid);
+    if (e != hipSuccess) return e;
+    const size_t bytes = ((3 + 3 * NW) * SPAN + 2 * CB * NS * NW + 2 * NW * CB) * sizeof(float);
+    if (bytes > 65536) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_bwd_kernel<IO, NS, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((scan_bwd_kernel<IO, NS, NW>), grid, dim3(64 * NW), bytes, st, a, d, g, parts, blocks, CB);
+    return hipGetLastError();
+}
+
+template <class IO>
+hipError_t run(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
+{
+    Segments g;
+    hipError_t e = scan_back(a, d.dy, ws, &g, st);
+    if (e != hipSuccess) return e;
+    const int CB = block_heads(a.B, a.H, a.N, a.G), blocks = (int)((a.H / a.G + CB - 1) / CB);
+    const size_t rows = (size_t)a.B * a.G * a.S;
+    Parts parts;
+    char* p = (char*)ws + scan_segment_bytes(a.B, a.H, a.N, a.S, a.G);
+    parts.dA = (float*)p;
+    p += up256((size_t)a.B * g.segs * a.H * a.S * sizeof(float));
+    parts.dDb = (float*)p;
+    p += up256((size_t)a.B * g.segs * a.H * 2 * sizeof(float));
+    parts.dB = parts.dC = nullptr;
+    if (blocks > 1) {
+        parts.dB = (float*)p;
+        parts.dC = parts.dB + blocks * rows * a.N;
+    }
+    if (a.S <= 4) e = launch<IO, 1, 4>(a, d, g, parts, blocks, CB, st);
+    else if (a.S <= 8) e = launch<IO, 2, 4>(a, d, g, parts, blocks, CB, st);
+    else if (a.S <= 16) e = launch<IO, 4, 4>(a, d, g, parts, blocks, CB, st);
+    else if (a.S <= 32) e = launch<IO, 4, 8>(a, d, g, parts, blocks, CB, st);
+    else e = launch<IO, 8, 8>(a, d, g, parts, blocks, CB, st);
+    if (e != hipSuccess) return e;
+    dim3 grid;
+    if (blocks > 1 && (d.dB || d.dC)) {
+        e = launch_grid((2 * rows * ((a.N + VE - 1) / VE) + 255) / 256, 256, &grid);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(scan_join_kernel<IO>, grid, dim3(256), 0, st, a, parts, (typename IO::T*)d.dB, (typename IO::T*)d.dC, blocks);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!d.dA && !d.dD && !d.dbias) return hipSuccess;
+    hipLaunchKernelGGL(scan_sums_kernel, dim3((unsigned)((a.H * (a.S + 2) + 255) / 256)), dim3(256), 0, st, parts, d.dA, d.dD, d.dbias, a.H, a.S,
+                       (int64_t)a.B * g.segs);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t scan_bwd_bytes(int64_t B, int64_t H, int64_t N, int S, int64_t G)
+{
+    // the most of any batch up to B.  Sequences times segments: as scan_segment_bytes says, with 512 workgroups at most where there are
+    // several segments.  Blocks: of 32 heads, or of 8 as long as those of twice as many are fewer than 256 workgroups.
+    const int64_t all = B * ((N + 1023) / 1024), some = 513 + (B < 256 ? B : 256), shares = all < some || B > some ? (all < some ? all : B) : some;
+    const int64_t in_group = H / G, narrow = B * G * ((in_group + 7) / 8), wide = B * G * ((in_group + 31) / 32);
+    const int64_t blocks = narrow < 512 ? narrow : wide < 512 ? 512 : wide;
+    return up256((size_t)shares * H * S * sizeof(float)) + up256((size_t)shares * H * 2 * sizeof(float)) +
+           (in_group > 8 ? up256((size_t)blocks * S * N * 2 * sizeof(float)) : 0);
+}
+
+hipError_t scan_bwd(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
+{
+    if (a.io == LONGCONV_F32) return run<IoF32>(a, d, ws, st);
+    return a.io == LONGCONV_F16 ? run<IoF16>(a, d, ws, st) : run<IoBF16>(a, d, ws, st);
+}
+
+}  // namespace lc
