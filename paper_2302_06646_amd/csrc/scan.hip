@@ -7,23 +7,23 @@
 namespace lc {
 namespace {
 
-constexpr int FW = 8, FT = FW * 64;      // waves and threads of a workgroup
-constexpr int FC = 2;                    // heads of a wave
-constexpr int FB = 2;                    // states whose B and C are brought in at a time
+constexpr int FW = 8, FT = FW * 64;      // waves of a workgroup, each with a head of its own; threads
+constexpr int FB = 8;                    // states whose B and C are brought in at a time, while those before are worked on
 
 enum Mode { WHOLE, STATES, BACK };
 
-// Workgroup: 16 heads of one group, one segment.  B and C of two states at a time are laid out in fp32 for all of them.
+// Workgroup: eight heads of one group, one segment.  B and C of FB states at a time are laid out in fp32 for all of them; a wave has two
+// states at a time.
 // WHOLE: y, marks and the last state.  STATES: what Segments holds of segments 0 .. segs - 2.  BACK: the same for the gradient of the state,
 // g_t = C_t dy_t + a_{t+1} g_{t+1}, as v_t = a_t (C_t dy_t + v_{t+1}) in reversed time, of segments 1 .. segs - 1.
+// A and the states between chunks are kept one in a lane, lane s for state s.
 template <class IO, int K, int MODE>
-__global__ __launch_bounds__(FT) void scan_kernel(ScanArgs a, const typename IO::T* __restrict__ dy, const float* state, typename IO::T* __restrict__ y,
+__global__ __launch_bounds__(FT, 4) void scan_kernel(ScanArgs a, const typename IO::T* __restrict__ dy, const float* state, typename IO::T* __restrict__ y,
                                                   float* last, float* __restrict__ marks, Segments g, int blocks)
 {
     using T = typename IO::T;
     constexpr int CH = 64 * K;
     __shared__ float4 lds[2][FB][2][CH / 4];           // [buffer][state][B or C][K / 4][lane]
-    __shared__ float carry[FW][FC][SCAN_STATES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int run_segs = MODE == WHOLE ? g.segs : g.segs - 1;
     int64_t w = blockIdx.x;
@@ -34,183 +34,197 @@ __global__ __launch_bounds__(FT) void scan_kernel(ScanArgs a, const typename IO:
     const int64_t grp = w % a.G, b = w / a.G, heads = a.H / a.G;
     const int64_t len = scan_length(a, b), N = a.N;
     const int64_t begin = seg * g.len, stop = begin + g.len < N ? begin + g.len : N, end = stop < len ? stop : len;
-    const int S = a.S, phases = (S + FB - 1) / FB;
+    const int S = a.S;
     const T* Bm = (const T*)a.Bm + (size_t)(b * a.G + grp) * S * N;
     const T* Cm = (const T*)a.Cm + (size_t)(b * a.G + grp) * S * N;
-    int64_t head[FC];
-    bool mine[FC];
-    size_t row[FC];
-    float bias[FC], D[FC], total[FC];
-#pragma unroll
-    for (int c = 0; c < FC; ++c) {
-        const int64_t i = (int64_t)blk * FW * FC + wave * FC + c;
-        mine[c] = i < heads;
-        head[c] = grp * heads + (mine[c] ? i : 0);
-        row[c] = (size_t)b * a.H + head[c];
-        bias[c] = a.bias ? a.bias[head[c]] : 0.f;
-        D[c] = a.D ? a.D[head[c]] : 0.f;
-        total[c] = 0.f;
-        if (lane < S) {
-            // (the given state is read here alone where one workgroup has the whole row: `last`, which it writes, may be `state`.  Where
-            // several have it the pass over STATES puts it in the place that no segment uses.)
-            const float given = MODE == BACK || !state ? 0.f : state[row[c] * S + lane];
-            float* const kept = g.ends + (row[c] * g.segs + g.segs - 1) * S + lane;
-            if (MODE == STATES && seg == 0 && mine[c]) *kept = given;
-            carry[wave][c][lane] =
-                MODE == WHOLE ? entering<false>(g, row[c], seg, S, lane, LOG2E * a.A[head[c] * S + lane], g.segs > 1 ? *kept : given) : 0.f;
-        }
+    // (a wave that has no head left runs along with the group's first one and writes nothing)
+    const int64_t mine_of = (int64_t)blk * FW + wave;
+    const bool mine = mine_of < heads;
+    const int64_t head = grp * heads + (mine ? mine_of : 0);
+    const size_t row = (size_t)b * a.H + head;
+    const T* const delta = (const T*)a.delta + row * N;
+    const T* const in = (MODE == BACK ? dy : (const T*)a.u) + row * N;
+    const T* const zr = a.z ? (const T*)a.z + row * N : nullptr;
+    const float bias = a.bias ? a.bias[head] : 0.f, D = a.D ? a.D[head] : 0.f;
+    float total = 0.f, A2 = 0.f, carry = 0.f;
+    if (lane < S) {
+        A2 = LOG2E * a.A[head * S + lane];
+        // (the given state is read here alone where one workgroup has the whole row: `last`, which it writes, may be `state`.  Where
+        // several have it the pass over STATES puts it in the place that no segment uses.)
+        const float given = MODE == BACK || !state ? 0.f : state[row * S + lane];
+        float* const kept = g.ends + (row * g.segs + g.segs - 1) * S + lane;
+        if (MODE == STATES && seg == 0 && mine) *kept = given;
+        if (MODE == WHOLE) carry = entering<false>(g, row, seg, S, lane, A2, g.segs > 1 ? *kept : given);
     }
-    // the four places 4 q .. of a chunk as they lie in `lds`: lane 4 q / K, group (4 q % K) / 4 (BACK: in reversed order)
-    const auto bring = [&](int64_t t0, int ph, int i, float4& v) {      // piece i of this thread
-        const int id = threadIdx.x + i * FT, q = id % (CH / 4), which = id / (CH / 4) % 2, s = ph * FB + id / (CH / 2);
-        v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (id >= FB * CH / 2 || s >= S || (MODE == STATES && which == 1) || (MODE == BACK && which == 0)) return;
-        const int64_t t = t0 + (MODE == BACK ? CH - 4 - 4 * q : 4 * q);
-        v = load4<IO>((which ? Cm : Bm) + (size_t)s * N, t, N, end);
-        if (MODE == BACK) v = make_float4(v.w, v.z, v.y, v.x);
-    };
-    const auto put = [&](int buf, int i, const float4& v) {
-        const int id = threadIdx.x + i * FT, q = id % (CH / 4), which = id / (CH / 4) % 2, st = id / (CH / 2);
-        if (st < FB) lds[buf][st][which][q % (K / 4) * 64 + q / (K / 4)] = v;
-    };
-    constexpr int PIECES = (FB * CH / 2 + FT - 1) / FT;
-    int64_t t0 = begin;
-    if (MODE == BACK) t0 = end <= begin ? begin - CH : begin + (end - 1 - begin) / CH * CH;
-    for (; MODE == BACK ? t0 >= begin : t0 < end; t0 += MODE == BACK ? -CH : CH) {
-        float dt[FC][K], x[FC][K], out[FC][K], sum[FC];
-        const int64_t at = t0 + (MODE == BACK ? 63 - lane : lane) * K;      // this lane's places
-#pragma unroll
-        for (int c = 0; c < FC; ++c) {
-            sum[c] = 0.f;
-            if (!mine[c]) continue;
-#pragma unroll
-            for (int j = 0; j < K; j += 4) {
-                const float4 d4 = load4<IO>((const T*)a.delta + row[c] * N, at + j, N, end);
-                const float4 u4 = MODE == BACK ? load4<IO>(dy + row[c] * N, at + j, N, end) : load4<IO>((const T*)a.u + row[c] * N, at + j, N, end);
-                const float d[4] = {d4.x, d4.y, d4.z, d4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
-                float z[4] = {0.f, 0.f, 0.f, 0.f};
-                if (MODE == BACK && a.z) {
-                    const float4 z4 = load4<IO>((const T*)a.z + row[c] * N, at + j, N, end);
-                    z[0] = z4.x; z[1] = z4.y; z[2] = z4.z; z[3] = z4.w;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float wv = d[i] + bias[c];
-                    const float v = at + j + i < end ? a.softplus ? softplus_of(wv) : wv : 0.f;
-                    const int to = MODE == BACK ? K - 1 - j - i : j + i;
-                    dt[c][to] = v;
-                    sum[c] += v;
-                    if (MODE == BACK) x[c][to] = a.z ? u[i] * z[i] * logistic(z[i]) : u[i];
-                    else x[c][to] = v * u[i];
-                    out[c][to] = D[c] * u[i];
-                }
-            }
-        }
-        __syncthreads();      // (the buffers of the chunk before are read, the carries written)
-        float4 next[PIECES];
+    // Pieces of four places of B and C: piece 4 q .. of a chunk lies in `lds` at lane 4 q / K, group (4 q % K) / 4 (BACK: in reversed order)
+    constexpr int PER = CH / 4, PIECES = FB * 2 * PER / FT;
+    static_assert(FB * 2 * PER % FT == 0 && FT % PER == 0, "whole rows of pieces a thread");
+    const int q4 = threadIdx.x % PER, line = threadIdx.x / PER;      // its rows of pieces: line, line + FT / PER, ...
+    Raw4<IO> raw[PIECES];
+    const int t4 = MODE == BACK ? CH - 4 - 4 * q4 : 4 * q4, tl = (MODE == BACK ? 63 - lane : lane) * K;      // places of a piece, of the lane
+    const auto left = [&](int64_t t0, int64_t to) { return (int)(to - t0 < CH ? to - t0 : CH); };
+    const auto whole = [&](int64_t t0) { return t0 + CH + VE <= N && t0 + CH <= end; };      // (a piece of eight may reach past a chunk of 256)
+    const auto bring = [&](int64_t t0, int s0) {
+        const int n = N - t0 < CH ? (int)(N - t0) : CH, lim = left(t0, end);
+        const bool full = whole(t0) && s0 + FB <= S;
+        const T *const Bt = Bm + t0, *const Ct = Cm + t0;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            bring(t0, 0, i, next[i]);
-            put(0, i, next[i]);
+            const int r = line + i * (FT / PER), s = s0 + r / 2, which = r % 2;      // B or C of a state
+            if ((MODE == STATES && which == 1) || (MODE == BACK && which == 0)) raw[i].zero();
+            else if (full || (s < S && t4 < lim)) raw[i].ask((which ? Ct : Bt) + (size_t)s * N, t4, n, full);
+            else raw[i].zero();
         }
-        __syncthreads();
-        for (int ph = 0; ph < phases; ++ph) {
-            const int buf = ph & 1;
-            if (ph + 1 < phases)
+    };
+    const auto put = [&](int buf, int64_t t0) {
+        const int lim = left(t0, end);
 #pragma unroll
-                for (int i = 0; i < PIECES; ++i) bring(t0, ph + 1, i, next[i]);
+        for (int i = 0; i < PIECES; ++i) {
+            const int r = line + i * (FT / PER);
+            const float4 v = raw[i].get(t4, lim, lim == CH);
+            lds[buf][r / 2][r % 2][q4 % (K / 4) * 64 + q4 / (K / 4)] = MODE == BACK ? make_float4(v.w, v.z, v.y, v.x) : v;
+        }
+    };
+    Raw8<IO> rd, ru, rz;      // a piece of eight of this chunk, asked for during the one before
+    const auto ask = [&](const T* from, int64_t t0, Raw8<IO>& r) {
+        int lim = left(t0, end);
+        if (K < VE && tl + K < lim) lim = tl + K;
+        ask8<IO>(from + t0, tl, N - t0 < CH + VE ? (int)(N - t0) : CH + VE, lim, r, whole(t0));
+    };
+    const auto ask_all = [&](int64_t t0) {
+        ask(delta, t0, rd);
+        ask(in, t0, ru);
+        if (MODE == BACK && zr) ask(zr, t0, rz);
+    };
+    int64_t t0 = begin;
+    if (MODE == BACK) t0 = end <= begin ? begin - CH : begin + (end - 1 - begin) / CH * CH;
+    const auto going = [&](int64_t t) { return MODE == BACK ? t >= begin : t < end; };
+    int buf = 0;
+    if (going(t0)) {
+        ask_all(t0);
+        bring(t0, 0);
+    }
+    for (; going(t0); t0 += MODE == BACK ? -CH : CH) {
+        float dt[K], x[K], out[K], sum = 0.f;
+        const int lim = left(t0, end);
+        {
+            float d[VE], u[VE], z[VE];
+            rd.get(d);
+            ru.get(u);
+            if (MODE == BACK && zr) rz.get(z);
 #pragma unroll
-            for (int st = 0; st < FB; ++st) {
-                const int s = ph * FB + st;
-                if (s >= S) continue;
-                float Bv[K], Cv[K];
+            for (int i = 0; i < K; ++i) d[i] += bias;
+            if (a.softplus) {
 #pragma unroll
-                for (int j = 0; j < K / 4; ++j) {
-                    if (MODE != BACK) {
-                        const float4 q = lds[buf][st][0][j * 64 + lane];
-                        Bv[4 * j] = q.x; Bv[4 * j + 1] = q.y; Bv[4 * j + 2] = q.z; Bv[4 * j + 3] = q.w;
-                    }
-                    if (MODE != STATES) {
-                        const float4 q = lds[buf][st][1][j * 64 + lane];
-                        Cv[4 * j] = q.x; Cv[4 * j + 1] = q.y; Cv[4 * j + 2] = q.z; Cv[4 * j + 3] = q.w;
-                    }
+                for (int i = 0; i < K; ++i) d[i] = softplus_of(d[i]);
+            }
+            if (MODE == BACK && zr) {
+#pragma unroll
+                for (int i = 0; i < K; ++i) u[i] *= z[i] * logistic(z[i]);
+            }
+            if (lim < CH) {
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    d[i] = tl + i < lim ? d[i] : 0.f;
+                    u[i] = tl + i < lim ? u[i] : 0.f;
                 }
+            }
 #pragma unroll
-                for (int c = 0; c < FC; ++c) {
-                    if (!mine[c]) continue;
-                    const float A2 = LOG2E * a.A[head[c] * S + s];
-                    const float in = carry[wave][c][s];
-                    float d[K], h = lane == 0 ? in : 0.f;
+            for (int i = 0; i < K; ++i) {
+                const int to = MODE == BACK ? K - 1 - i : i;
+                dt[to] = d[i];
+                sum += d[i];
+                x[to] = MODE == BACK ? u[i] : d[i] * u[i];
+                out[to] = D * u[i];
+            }
+        }
+        const int64_t t_next = t0 + (MODE == BACK ? -CH : CH);
+        if (going(t_next)) ask_all(t_next);
+        if (MODE == WHOLE && zr) ask(zr, t0, rz);
+        if (MODE == WHOLE && marks && t0 % SPAN == 0 && mine && lane < S) marks[(row * ((N + SPAN - 1) / SPAN) + t0 / SPAN) * S + lane] = carry;
+        for (int s0 = 0; s0 < S; s0 += FB, buf ^= 1) {
+            put(buf, t0);
+            __syncthreads();      // (the other buffer's readers are past it too: it is filled behind the next one of these)
+            if (s0 + FB < S) bring(t0, s0 + FB);
+            else if (going(t_next)) bring(t_next, 0);
+            const int here = S - s0 < FB ? S - s0 : FB;
+            for (int s1 = 0; s1 < here; s1 += 2) {      // (a state that is not there: B and C zero)
+                float Bv[2][K], Cv[2][K], d[2][K], h[2], p[2], was[2];
 #pragma unroll
-                    for (int i = 0; i < K; ++i) {
-                        d[i] = exp2_of(A2 * dt[c][i]);
-                        if (MODE == BACK) h = d[i] * __builtin_fmaf(x[c][i], Cv[i], h);
-                        else h = __builtin_fmaf(d[i], h, x[c][i] * Bv[i]);
-                    }
-                    float p = exp2_of(A2 * sum[c]);
-                    scan_up(p, h);
-                    if (MODE == WHOLE) {
-                        if (marks && t0 % SPAN == 0 && lane == 0) marks[(row[c] * ((N + SPAN - 1) / SPAN) + t0 / SPAN) * S + s] = in;
-                        float v = dpp<0x138>(h, in);      // of the lane before
+                for (int st = 0; st < 2; ++st) {
+                    const int s = s0 + s1 + st;
 #pragma unroll
-                        for (int i = 0; i < K; ++i) {
-                            v = __builtin_fmaf(d[i], v, x[c][i] * Bv[i]);
-                            out[c][i] = __builtin_fmaf(Cv[i], v, out[c][i]);
+                    for (int j = 0; j < K / 4; ++j) {
+                        if (MODE != BACK) {
+                            const float4 q = lds[buf][s1 + st][0][j * 64 + lane];
+                            Bv[st][4 * j] = q.x; Bv[st][4 * j + 1] = q.y; Bv[st][4 * j + 2] = q.z; Bv[st][4 * j + 3] = q.w;
+                        }
+                        if (MODE != STATES) {
+                            const float4 q = lds[buf][s1 + st][1][j * 64 + lane];
+                            Cv[st][4 * j] = q.x; Cv[st][4 * j + 1] = q.y; Cv[st][4 * j + 2] = q.z; Cv[st][4 * j + 3] = q.w;
                         }
                     }
-                    if (lane == 63) carry[wave][c][s] = h;
+                    const float A_s = lane_of(A2, s);
+                    was[st] = lane_of(carry, s);
+                    h[st] = lane == 0 ? was[st] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < K; ++i) {
+                        d[st][i] = exp2_of(A_s * dt[i]);
+                        if (MODE == BACK) h[st] = d[st][i] * __builtin_fmaf(x[i], Cv[st][i], h[st]);
+                        else h[st] = __builtin_fmaf(d[st][i], h[st], x[i] * Bv[st][i]);
+                    }
+                    p[st] = exp2_of(A_s * sum);
+                }
+                scan_up(p[0], h[0], p[1], h[1]);
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    carry = with_lane(carry, s0 + s1 + st, lane_of(h[st], 63));
+                    if (MODE == WHOLE) {
+                        float v = dpp<0x138>(h[st], was[st]);      // of the lane before
+#pragma unroll
+                        for (int i = 0; i < K; ++i) {
+                            v = __builtin_fmaf(d[st][i], v, x[i] * Bv[st][i]);
+                            out[i] = __builtin_fmaf(Cv[st][i], v, out[i]);
+                        }
+                    }
                 }
             }
-            if (ph + 1 < phases)
-#pragma unroll
-                for (int i = 0; i < PIECES; ++i) put(buf ^ 1, i, next[i]);
-            __syncthreads();
         }
+        if (MODE != WHOLE) {
+            total += sum_of_wave(sum);
+            continue;
+        }
+        if (!mine) continue;
+        T* const to = y + (row * N + t0) + (uint32_t)tl;
+        const int n = left(t0, N) - tl;
+        if (zr) {
+            float z[VE];
+            rz.get(z);
 #pragma unroll
-        for (int c = 0; c < FC; ++c) {
-            if (!mine[c]) continue;
-            if (MODE != WHOLE) {
-                total[c] += sum_of_wave(sum[c]);
-                continue;
-            }
-            if (a.z) {
+            for (int i = 0; i < K; ++i) out[i] *= z[i] * logistic(z[i]);
+        }
+        if (lim < CH) {
 #pragma unroll
-                for (int j = 0; j < K; j += 4) {
-                    const float4 z4 = load4<IO>((const T*)a.z + row[c] * N, at + j, N, end);
-                    const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+            for (int i = 0; i < K; ++i) out[i] = tl + i < lim ? out[i] : 0.f;
+        }
+        if constexpr (K == VE) {
+            if (lim == CH) store8<IO, true>(to, VE, out);
+            else if (n > 0) store8<IO, true>(to, n < VE ? n : VE, out);
+        } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) out[c][j + i] *= z[i] * logistic(z[i]);
-                }
-            }
-            T* to = y + row[c] * N;
-#pragma unroll
-            for (int i = 0; i < K; ++i) out[c][i] = at + i < end ? out[c][i] : 0.f;
-            if constexpr (K >= VE) {
-#pragma unroll
-                for (int j = 0; j < K; j += VE) {
-                    const int64_t n = N - at - j;
-                    if (n > 0) store8<IO, true>(to + at + j, n < VE ? (int)n : VE, reinterpret_cast<float(&)[VE]>(out[c][j]));
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < K; ++i)
-                    if (at + i < N) IO::st(to, at + i, out[c][i]);
-            }
+            for (int i = 0; i < K; ++i)
+                if (i < n) IO::st(to, i, out[i]);
         }
     }
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < FC; ++c) {
-        if (!mine[c]) continue;
-        if (MODE == WHOLE) {
-            // behind the sequence's end: zeros from the first place that no chunk wrote
-            const int64_t zero = end > begin ? begin + (end - begin + CH - 1) / CH * CH : begin;
-            for (int64_t t = zero + lane; t < stop; t += 64) IO::st(y + row[c] * N, t, 0.f);
-            if (last && seg == g.segs - 1 && lane < S) last[row[c] * S + lane] = carry[wave][c][lane];
-        } else {
-            if (lane < S) g.ends[(row[c] * g.segs + seg) * S + lane] = carry[wave][c][lane];
-            if (lane == 0) g.sums[row[c] * g.segs + seg] = total[c];
-        }
+    if (!mine) return;
+    if (MODE == WHOLE) {
+        // behind the sequence's end: zeros from the first place that no chunk wrote
+        const int64_t zero = end > begin ? begin + (end - begin + CH - 1) / CH * CH : begin;
+        for (int64_t t = zero + lane; t < stop; t += 64) IO::st(y + row * N, t, 0.f);
+        if (last && seg == g.segs - 1 && lane < S) last[row * S + lane] = carry;
+    } else {
+        if (lane < S) g.ends[(row * g.segs + seg) * S + lane] = carry;
+        if (lane == 0) g.sums[row * g.segs + seg] = total;
     }
 }
 
@@ -248,12 +262,12 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, float* __res
     }
 }
 
-int64_t row_blocks(const ScanArgs& a) { return (a.H / a.G + FW * FC - 1) / (FW * FC); }
+int64_t row_blocks(const ScanArgs& a) { return (a.H / a.G + FW - 1) / FW; }
 
 // Segments: none where the heads alone are 256 workgroups; else as many as make 512, of 1024 places at least.
 int segments(int64_t B, int64_t H, int64_t N, int64_t G)
 {
-    const int64_t groups = B * G * ((H / G + FW * FC - 1) / (FW * FC)), most = (N + 1023) / 1024;
+    const int64_t groups = B * G * ((H / G + FW - 1) / FW), most = (N + 1023) / 1024;
     if (groups >= 256) return 1;
     const int64_t want = (512 + groups - 1) / groups;
     return (int)(want < most ? want : most);
@@ -305,7 +319,7 @@ size_t scan_segment_bytes(int64_t B, int64_t H, int64_t N, int S, int64_t G)
 {
     // rows times segments of any batch up to B: at most one segment for each 1024 places, and where there are several at most 512 /
     // (workgroups of a sequence) + B, with B < 256
-    const int64_t blocks = G * ((H / G + FW * FC - 1) / (FW * FC)), all = B * ((N + 1023) / 1024), some = 512 / blocks + 1 + (B < 256 ? B : 256);
+    const int64_t blocks = G * ((H / G + FW - 1) / FW), all = B * ((N + 1023) / 1024), some = 512 / blocks + 1 + (B < 256 ? B : 256);
     return up256((size_t)(all < some ? all : some) * H * (S + 1) * sizeof(float));
 }
 size_t scan_workspace_bytes(int64_t B, int64_t H, int64_t N, int S, int64_t G, int backward)

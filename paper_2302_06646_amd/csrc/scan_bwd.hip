@@ -22,15 +22,15 @@ struct Parts {
     float *dDb;          // [B segs][H,2]: of D and of the bias
 };
 
-template <class IO, int NS, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void scan_bwd_kernel(ScanArgs a, ScanGrads d, Segments g, Parts parts, int blocks, int CB)
+template <class IO, int NS, int NW, bool GATED>
+__global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(ScanArgs a, ScanGrads d, Segments g, Parts parts, int blocks, int CB)
 {
     using T = typename IO::T;
     constexpr int TH = 64 * NW, SP = NS * NW, TPT = SPAN / TH;      // threads, states with those that are not there, places of a thread
     extern __shared__ __align__(16) float lds[];
-    float* const stage = lds;                        // [3][SPAN]: dt, dt u, dy'
-    float* const part = stage + 3 * SPAN;            // [NW][3][SPAN]: sums over a wave's states of g B, A q, C h
-    float* const gcar = part + NW * 3 * SPAN;        // [CB][SP]: what the chunk behind hands on
+    float* const stages = lds;                       // [2][3][SPAN]: dt, dt u, dy' of a head, and of the next one
+    float* const sums = stages + 2 * 3 * SPAN;       // [2][NW][3][SPAN]: sums over a wave's states of g B, A q, C h, and of the head before
+    float* const gcar = sums + 2 * NW * 3 * SPAN;    // [CB][SP]: what the chunk behind hands on
     float* const dAsum = gcar + CB * SP;             // [CB][SP]
     float* const small = dAsum + CB * SP;            // [NW][CB][2]: of dD and dbias
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x;
@@ -60,16 +60,22 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void scan_bwd_kernel(Scan
     const int64_t top = end > begin ? begin + (end - 1 - begin) / SPAN * SPAN : begin - SPAN;
     for (int64_t t0 = top; t0 >= begin; t0 -= SPAN) {
         float dBv[NS][K], dCv[NS][K];
-        constexpr bool HELD = NS <= 4;      // B and C in registers for all heads, or brought in for each
-        float Bv[HELD ? NS : 1][K], Cv[HELD ? NS : 1][K];
+        constexpr bool HELD = NS <= 2;      // B and C in registers for all heads, or brought in for each
+        float Bv[HELD ? NS : 2][K], Cv[HELD ? NS : 2][K];
+        const int lim = (int)(end - t0 < SPAN ? end - t0 : SPAN), left = (int)(N - t0 < SPAN ? N - t0 : SPAN);
         const auto bring = [&](int n, float (&Bq)[K], float (&Cq)[K]) {
             const int s = wave * NS + n;
+            Raw8<IO> rB, rC;
+            ask8<IO>((const T*)a.Bm + ((bg + s) * N + t0), lane * K, left, s < S ? lim : 0, rB, lim == SPAN && s < S);
+            ask8<IO>((const T*)a.Cm + ((bg + s) * N + t0), lane * K, left, s < S ? lim : 0, rC, lim == SPAN && s < S);
+            rB.get(Bq);
+            rC.get(Cq);
+            if (lim < SPAN) {
 #pragma unroll
-            for (int j = 0; j < K; j += 4) {
-                const float4 q = s < S ? load4<IO>((const T*)a.Bm + (bg + s) * N, t0 + lane * K + j, N, end) : make_float4(0.f, 0.f, 0.f, 0.f);
-                const float4 r = s < S ? load4<IO>((const T*)a.Cm + (bg + s) * N, t0 + lane * K + j, N, end) : make_float4(0.f, 0.f, 0.f, 0.f);
-                Bq[j] = q.x; Bq[j + 1] = q.y; Bq[j + 2] = q.z; Bq[j + 3] = q.w;
-                Cq[j] = r.x; Cq[j + 1] = r.y; Cq[j + 2] = r.z; Cq[j + 3] = r.w;
+                for (int i = 0; i < K; ++i) {
+                    Bq[i] = lane * K + i < lim ? Bq[i] : 0.f;
+                    Cq[i] = lane * K + i < lim ? Cq[i] : 0.f;
+                }
             }
         };
 #pragma unroll
@@ -78,34 +84,67 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void scan_bwd_kernel(Scan
 #pragma unroll
             for (int i = 0; i < K; ++i) dBv[n][i] = dCv[n][i] = 0.f;
         }
-        for (int c = 0; c < heads; ++c) {
-            const int64_t h = head0 + c;
-            const size_t row = (size_t)b * a.H + h;
-            const float bias = a.bias ? a.bias[h] : 0.f, D = a.D ? a.D[h] : 0.f;
-            // this thread's places, for all waves and for itself
-            float dt[TPT], u[TPT], dyg[TPT], dyz[TPT], rate[TPT];
+        // of this thread's places and of the wave's states (lane n for state wave NS + n), of head c, asked for during the one before
+        float nd[TPT], nu[TPT], ny[TPT], nz[TPT], nA = 0.f, nm = 0.f;
+        const auto ask = [&](int c) {
+            const size_t row = (size_t)b * a.H + head0 + c, at0 = row * N + t0;
 #pragma unroll
             for (int i = 0; i < TPT; ++i) {
-                const int64_t t = t0 + tid * TPT + i;
-                dt[i] = u[i] = dyg[i] = dyz[i] = rate[i] = 0.f;
-                if (t < end) {
-                    const float x = IO::ld((const T*)a.delta + row * N, t) + bias;
-                    dt[i] = a.softplus ? softplus_of(x) : x;
-                    rate[i] = a.softplus ? logistic(x) : 1.f;
-                    u[i] = IO::ld((const T*)a.u + row * N, t);
-                    dyg[i] = IO::ld((const T*)d.dy + row * N, t);
-                    if (a.z) {
-                        const float z = IO::ld((const T*)a.z + row * N, t), q = logistic(z);
-                        dyz[i] = dyg[i] * (q * (1.f + z * (1.f - q)));
-                        dyg[i] *= z * q;
-                    }
+                const uint32_t t = (uint32_t)(tid * TPT + i);
+                nd[i] = nu[i] = ny[i] = nz[i] = 0.f;
+                if (lim == SPAN || (int)t < lim) {
+                    nd[i] = IO::ld((const T*)a.delta + at0, t);
+                    nu[i] = IO::ld((const T*)a.u + at0, t);
+                    ny[i] = IO::ld((const T*)d.dy + at0, t);
+                    if (GATED) nz[i] = IO::ld((const T*)a.z + at0, t);
                 }
-                const int to = place(tid * TPT + i);
-                stage[to] = dt[i];
-                stage[SPAN + to] = dt[i] * u[i];
-                stage[2 * SPAN + to] = dyg[i];
             }
-            __syncthreads();
+            const int s = wave * NS + lane;
+            if (lane < NS && s < S) {
+                nA = a.A[(head0 + c) * S + s];
+                nm = d.marks[(row * n_marks + t0 / SPAN) * S + s];
+            }
+        };
+        // this thread's places: for all waves, and what it needs of them itself
+        struct Own {
+            float dt[TPT], u[TPT], dyg[TPT], dyz[TPT], rate[TPT], A, mark, D;
+        };
+        const auto lay = [&](int c) {
+            Own o;
+            o.A = nA;
+            o.mark = nm;
+            o.D = a.D ? a.D[head0 + c] : 0.f;
+            const float bias = a.bias ? a.bias[head0 + c] : 0.f;
+            float* const stage = stages + (c & 1) * 3 * SPAN;
+#pragma unroll
+            for (int i = 0; i < TPT; ++i) {
+                const bool is = tid * TPT + i < lim;
+                const float x = nd[i] + bias, z = nz[i], q = GATED ? logistic(z) : 1.f;
+                float rate;
+                const float sp = softplus_of(x, &rate), y = a.softplus ? sp : x;
+                o.dt[i] = is ? y : 0.f;
+                o.rate[i] = a.softplus ? rate : 1.f;
+                o.u[i] = nu[i];
+                o.dyg[i] = GATED ? ny[i] * (z * q) : ny[i];
+                o.dyz[i] = ny[i] * (q * (1.f + z * (1.f - q)));
+                const int to = place(tid * TPT + i);
+                stage[to] = o.dt[i];
+                stage[SPAN + to] = o.dt[i] * o.u[i];
+                stage[2 * SPAN + to] = o.dyg[i];
+            }
+            return o;
+        };
+        __syncthreads();      // (the chunk before is done with `stages`)
+        ask(0);
+        Own own = lay(0);
+        if (heads > 1) ask(1);
+        __syncthreads();
+        for (int c = 0; c < heads; ++c) {
+            const size_t at0 = ((size_t)b * a.H + head0 + c) * N + t0;
+            const int here = (int)(stop - t0 < SPAN ? stop - t0 : SPAN);
+            const float *const stage = stages + (c & 1) * 3 * SPAN, Al = own.A, ml = own.mark;
+            float* const part = sums + (c & 1) * NW * 3 * SPAN;
+            float cl = lane < NS ? gcar[c * SP + wave * NS + lane] : 0.f;
             float e[K], x[K], f[K], gB[K], Aq[K], Ch[K], sum = 0.f;      // dt, dt u, dy' of the lane's places
 #pragma unroll
             for (int j = 0; j < K / 4; ++j) {
@@ -117,66 +156,85 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void scan_bwd_kernel(Scan
                 f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
             }
 #pragma unroll
-            for (int i = 0; i < K; ++i) {
-                sum += e[i];
-                gB[i] = Aq[i] = Ch[i] = 0.f;
+            for (int i = 0; i < K; ++i) sum += e[i];
+            float dA[NS < 2 ? 2 : NS];
+            dA[1] = 0.f;
+            // two states at a time (a state that is not there: A, B, C and all that comes of them zero)
+            constexpr int P = NS < 2 ? 1 : 2;
+#pragma unroll
+            for (int n = 0; n < NS; n += P) {
+                if constexpr (!HELD) {
+#pragma unroll
+                    for (int r = 0; r < P; ++r) bring(n + r, Bv[r], Cv[r]);
+                }
+                float dec[P][K], q[P][K], v[P], p[P], all[P], A[P], in[P], back[P];
+#pragma unroll
+                for (int r = 0; r < P; ++r) {
+                    const float(&B)[K] = Bv[HELD ? n + r : r];
+                    A[r] = lane_of(Al, n + r);
+                    in[r] = lane_of(ml, n + r);
+                    back[r] = lane_of(cl, n + r);
+                    const float A2 = LOG2E * A[r];
+                    v[r] = lane == 0 ? in[r] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < K; ++i) {
+                        dec[r][i] = exp2_of(A2 * e[i]);
+                        v[r] = __builtin_fmaf(dec[r][i], v[r], x[i] * B[i]);
+                    }
+                    p[r] = all[r] = exp2_of(A2 * sum);
+                }
+                if constexpr (P == 2) scan_up(p[0], v[0], p[1], v[1]);
+                else scan_up(p[0], v[0]);
+#pragma unroll
+                for (int r = 0; r < P; ++r) {
+                    const float(&B)[K] = Bv[HELD ? n + r : r];
+                    const float(&C)[K] = Cv[HELD ? n + r : r];
+                    float w = dpp<0x138>(v[r], in[r]);      // the state in front of the lane
+#pragma unroll
+                    for (int i = 0; i < K; ++i) {
+                        q[r][i] = dec[r][i] * w;
+                        w = __builtin_fmaf(x[i], B[i], q[r][i]);
+                        dCv[n + r][i] = __builtin_fmaf(f[i], w, dCv[n + r][i]);
+                        if (GATED) Ch[i] = n + r ? __builtin_fmaf(C[i], w, Ch[i]) : C[i] * w;
+                    }
+                    v[r] = lane == 63 ? back[r] : 0.f;
+#pragma unroll
+                    for (int i = K - 1; i >= 0; --i) v[r] = dec[r][i] * __builtin_fmaf(C[i], f[i], v[r]);
+                    p[r] = all[r];
+                }
+                if constexpr (P == 2) scan_down(p[0], v[0], p[1], v[1]);
+                else scan_down(p[0], v[0]);
+#pragma unroll
+                for (int r = 0; r < P; ++r) {
+                    const float(&B)[K] = Bv[HELD ? n + r : r];
+                    const float(&C)[K] = Cv[HELD ? n + r : r];
+                    float w = dpp<0x130>(v[r], back[r]);      // what the lane behind hands on
+                    float s = 0.f;
+#pragma unroll
+                    for (int i = K - 1; i >= 0; --i) {
+                        const float gt = __builtin_fmaf(C[i], f[i], w), qt = gt * q[r][i];
+                        dBv[n + r][i] = __builtin_fmaf(gt, x[i], dBv[n + r][i]);
+                        gB[i] = n + r ? __builtin_fmaf(gt, B[i], gB[i]) : gt * B[i];
+                        Aq[i] = n + r ? __builtin_fmaf(A[r], qt, Aq[i]) : A[r] * qt;
+                        s = __builtin_fmaf(e[i], qt, s);
+                        w = dec[r][i] * gt;
+                    }
+                    dA[n + r] = s;
+                    cl = with_lane(cl, n + r, lane_of(w, 0));
+                }
             }
-#pragma unroll
-            for (int n = 0; n < NS; ++n) {
-                const int s = wave * NS + n;
-                if (s >= S) continue;
-                if constexpr (!HELD) bring(n, Bv[0], Cv[0]);
-                const float(&B)[K] = Bv[HELD ? n : 0];
-                const float(&C)[K] = Cv[HELD ? n : 0];
-                const float A = a.A[h * S + s], A2 = LOG2E * A;
-                const float in = d.marks[(row * n_marks + t0 / SPAN) * S + s], back = gcar[c * SP + s];
-                float dec[K], q[K];
-                float v = lane == 0 ? in : 0.f;
-#pragma unroll
-                for (int i = 0; i < K; ++i) {
-                    dec[i] = exp2_of(A2 * e[i]);
-                    v = __builtin_fmaf(dec[i], v, x[i] * B[i]);
-                }
-                const float all = exp2_of(A2 * sum);
-                float p = all;
-                scan_up(p, v);
-                v = dpp<0x138>(v, in);      // the state in front of the lane
-#pragma unroll
-                for (int i = 0; i < K; ++i) {
-                    q[i] = dec[i] * v;
-                    v = __builtin_fmaf(x[i], B[i], q[i]);
-                    dCv[n][i] = __builtin_fmaf(f[i], v, dCv[n][i]);
-                    Ch[i] = __builtin_fmaf(C[i], v, Ch[i]);
-                }
-                v = lane == 63 ? back : 0.f;
-#pragma unroll
-                for (int i = K - 1; i >= 0; --i) v = dec[i] * __builtin_fmaf(C[i], f[i], v);
-                p = all;
-                scan_down(p, v);
-                v = dpp<0x130>(v, back);      // what the lane behind hands on
-                float dA = 0.f;
-#pragma unroll
-                for (int i = K - 1; i >= 0; --i) {
-                    const float gt = __builtin_fmaf(C[i], f[i], v);
-                    dBv[n][i] = __builtin_fmaf(gt, x[i], dBv[n][i]);
-                    gB[i] = __builtin_fmaf(gt, B[i], gB[i]);
-                    const float qt = gt * q[i];
-                    Aq[i] = __builtin_fmaf(A, qt, Aq[i]);
-                    dA = __builtin_fmaf(e[i], qt, dA);
-                    v = dec[i] * gt;
-                }
-                dA = sum_of_wave(dA);
-                if (lane == 0) {
-                    gcar[c * SP + s] = v;
-                    dAsum[c * SP + s] += dA;
-                }
-            }
+            if (lane < NS) gcar[c * SP + wave * NS + lane] = cl;
             float4* const to = reinterpret_cast<float4*>(part + wave * 3 * SPAN);
 #pragma unroll
             for (int j = 0; j < K / 4; ++j) {
                 to[j * 64 + lane] = make_float4(gB[4 * j], gB[4 * j + 1], gB[4 * j + 2], gB[4 * j + 3]);
                 to[SPAN / 4 + j * 64 + lane] = make_float4(Aq[4 * j], Aq[4 * j + 1], Aq[4 * j + 2], Aq[4 * j + 3]);
-                if (d.dz) to[SPAN / 2 + j * 64 + lane] = make_float4(Ch[4 * j], Ch[4 * j + 1], Ch[4 * j + 2], Ch[4 * j + 3]);
+                if (GATED) to[SPAN / 2 + j * 64 + lane] = make_float4(Ch[4 * j], Ch[4 * j + 1], Ch[4 * j + 2], Ch[4 * j + 3]);
+            }
+            Own next = own;
+            if (c + 1 < heads) {
+                next = lay(c + 1);
+                if (c + 2 < heads) ask(c + 2);
             }
             __syncthreads();
             float sD = 0.f, sb = 0.f;
@@ -188,27 +246,33 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void scan_bwd_kernel(Scan
                 for (int r = 0; r < NW; ++r) {
                     wB += part[r * 3 * SPAN + at];
                     wA += part[r * 3 * SPAN + SPAN + at];
-                    if (d.dz) wC += part[r * 3 * SPAN + 2 * SPAN + at];
+                    if (GATED) wC += part[r * 3 * SPAN + 2 * SPAN + at];
                 }
-                const int64_t t = t0 + tid * TPT + i;
-                const float dw = __builtin_fmaf(wB, u[i], wA) * rate[i];
-                if (t < stop) {
-                    const bool is = t < end;
-                    if (d.du) IO::st((T*)d.du + row * N, t, is ? __builtin_fmaf(dt[i], wB, D * dyg[i]) : 0.f);
-                    if (d.ddelta) IO::st((T*)d.ddelta + row * N, t, is ? dw : 0.f);
-                    if (d.dz) IO::st((T*)d.dz + row * N, t, is ? __builtin_fmaf(D, u[i], wC) * dyz[i] : 0.f);
+                const uint32_t t = (uint32_t)(tid * TPT + i);
+                const float dw = __builtin_fmaf(wB, own.u[i], wA) * own.rate[i];
+                if ((int)t < here) {
+                    const bool is = (int)t < lim;
+                    if (d.du) put1<IO>((T*)d.du + at0, t, is ? __builtin_fmaf(own.dt[i], wB, own.D * own.dyg[i]) : 0.f);
+                    if (d.ddelta) put1<IO>((T*)d.ddelta + at0, t, is ? dw : 0.f);
+                    if (GATED && d.dz) put1<IO>((T*)d.dz + at0, t, is ? __builtin_fmaf(own.D, own.u[i], wC) * own.dyz[i] : 0.f);
                     if (is) {
-                        sD = __builtin_fmaf(dyg[i], u[i], sD);
+                        sD = __builtin_fmaf(own.dyg[i], own.u[i], sD);
                         sb += dw;
                     }
                 }
             }
-            sD = sum_of_wave(sD);
-            sb = sum_of_wave(sb);
-            if (lane == 0) {
-                small[(wave * CB + c) * 2] += sD;
-                small[(wave * CB + c) * 2 + 1] += sb;
+            // lanes 0, 1: dA of the first two states; 2, 3: the shares of dD and dbias
+            const float t = sums_of_wave(dA[0], dA[1], sD, sb);
+            if (lane < 2 && lane < NS) dAsum[c * SP + wave * NS + lane] += t;
+            if (lane == 2 || lane == 3) small[(wave * CB + c) * 2 + lane - 2] += t;
+            if constexpr (NS > 2) {
+#pragma unroll
+                for (int n = 2; n < NS; n += 2) {
+                    const float r = sums_of_wave(dA[n], dA[n + 1], 0.f, 0.f);
+                    if (lane < 2) dAsum[c * SP + wave * NS + n + lane] += r;
+                }
             }
+            own = next;
         }
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
@@ -316,19 +380,25 @@ int block_heads(int64_t B, int64_t H, int64_t N, int64_t G)
     return CB;
 }
 
-template <class IO, int NS, int NW>
-hipError_t launch(const ScanArgs& a, const ScanGrads& d, const Segments& g, const Parts& parts, int blocks, int CB, hipStream_t st)
+template <class IO, int NS, int NW, bool GATED>
+hipError_t launch_of(const ScanArgs& a, const ScanGrads& d, const Segments& g, const Parts& parts, int blocks, int CB, hipStream_t st)
 {
     dim3 grid;
     hipError_t e = launch_grid((uint64_t)(a.B * a.G * blocks * g.segs), 64 * NW, &grid);
     if (e != hipSuccess) return e;
-    const size_t bytes = ((3 + 3 * NW) * SPAN + 2 * CB * NS * NW + 2 * NW * CB) * sizeof(float);
+    const size_t bytes = (2 * (3 + 3 * NW) * SPAN + 2 * CB * NS * NW + 2 * NW * CB) * sizeof(float);
     if (bytes > 65536) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_bwd_kernel<IO, NS, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_bwd_kernel<IO, NS, NW, GATED>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((scan_bwd_kernel<IO, NS, NW>), grid, dim3(64 * NW), bytes, st, a, d, g, parts, blocks, CB);
+    hipLaunchKernelGGL((scan_bwd_kernel<IO, NS, NW, GATED>), grid, dim3(64 * NW), bytes, st, a, d, g, parts, blocks, CB);
     return hipGetLastError();
+}
+
+template <class IO, int NS, int NW>
+hipError_t launch(const ScanArgs& a, const ScanGrads& d, const Segments& g, const Parts& parts, int blocks, int CB, hipStream_t st)
+{
+    return a.z ? launch_of<IO, NS, NW, true>(a, d, g, parts, blocks, CB, st) : launch_of<IO, NS, NW, false>(a, d, g, parts, blocks, CB, st);
 }
 
 template <class IO>
@@ -352,7 +422,7 @@ hipError_t run(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
     }
     if (a.S <= 4) e = launch<IO, 1, 4>(a, d, g, parts, blocks, CB, st);
     else if (a.S <= 8) e = launch<IO, 2, 4>(a, d, g, parts, blocks, CB, st);
-    else if (a.S <= 16) e = launch<IO, 4, 4>(a, d, g, parts, blocks, CB, st);
+    else if (a.S <= 16) e = launch<IO, 2, 8>(a, d, g, parts, blocks, CB, st);
     else if (a.S <= 32) e = launch<IO, 4, 8>(a, d, g, parts, blocks, CB, st);
     else e = launch<IO, 8, 8>(a, d, g, parts, blocks, CB, st);
     if (e != hipSuccess) return e;
