@@ -23,6 +23,7 @@ struct Product {
     Side F, S;
     int64_t K, segs, batches;         // the sum goes over `segs` segments of K
     int64_t splits, per;              // shares of the sum, of `per` steps each
+    bool wide;                        // tiles of 256 by 256
     // EPI_OUT, EPI_DZ
     void* out;
     int64_t ld, batch;                // of out, residual, dy
@@ -54,6 +55,29 @@ __device__ __forceinline__ float slope_by(int act, float z)
         case LONGCONV_ACT_RELU: return slope_of<LONGCONV_ACT_RELU>(z);
         default: return 1.f;
     }
+}
+
+// of eight at a time, one decision for all
+__device__ __forceinline__ void acts_by(int act, float (&z)[VE])
+{
+    const auto each = [&](auto which) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) z[i] = act_of<decltype(which)::value>(z[i]);
+    };
+    if (act == LONGCONV_ACT_SILU) each(std::integral_constant<int, LONGCONV_ACT_SILU>());
+    else if (act == LONGCONV_ACT_GELU) each(std::integral_constant<int, LONGCONV_ACT_GELU>());
+    else if (act == LONGCONV_ACT_RELU) each(std::integral_constant<int, LONGCONV_ACT_RELU>());
+}
+__device__ __forceinline__ void slopes_by(int act, float (&z)[VE])
+{
+    const auto each = [&](auto which) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) z[i] = slope_of<decltype(which)::value>(z[i]);
+    };
+    if (act == LONGCONV_ACT_SILU) each(std::integral_constant<int, LONGCONV_ACT_SILU>());
+    else if (act == LONGCONV_ACT_GELU) each(std::integral_constant<int, LONGCONV_ACT_GELU>());
+    else if (act == LONGCONV_ACT_RELU) each(std::integral_constant<int, LONGCONV_ACT_RELU>());
+    else each(std::integral_constant<int, LONGCONV_ACT_NONE>());
 }
 
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
@@ -288,6 +312,272 @@ __global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f
     }
 }
 
+// ---- 16-bit operands whose rows are whole pieces of 16 bytes ---------------------------------------------------------------
+// The tile of an operand is brought into LDS by the memory instructions themselves, 1 KB of it a wave instruction, the next step's while
+// this one's is worked on.  They write LDS in the order of lanes, so where a piece of 16 bytes comes to lie is chosen by which piece a lane
+// asks for: rows along k (128 bytes) exchange their eight pieces by the row's number / 2, rows along i their pairs of pieces by bits 0, 1 and
+// 3 of it, so that sixteen lanes' reads of a fragment fall on all banks.  What lies beyond the operand reads as zero (the buffer's range).
+// (Written out, because the compiler takes every read of LDS for one of what such an instruction writes and waits for all of them first.)
+typedef uint32_t range_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ range_t make_range(const void* p, uint32_t bytes)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return range_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)),
+                   (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00027000u};
+}
+constexpr uint32_t BEYOND = 0x80000000u;
+// 16 bytes of each lane from byte `off` on to LDS byte `to` + 16 lane; they are there when vmcnt says so
+__device__ __forceinline__ void bring16(const range_t& r, uint32_t off, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(to) : "memory");
+}
+
+// rows (k fast) or columns (k slow) i0 .. i0 + BI - 1 of an operand, 64 values of k a step, by NW waves
+template <bool KF, int BI, int NW>
+struct Fast {
+    static constexpr int BK = 64, BYTES = BI * BK * 2, LOADS = BYTES / 1024 / NW;
+    static constexpr int SLOTS = KF ? 8 : BI / 8, LINES = 64 / SLOTS;      // pieces of a row in LDS, rows of a wave instruction
+    const char* base;
+    uint32_t off[LOADS], at_k;      // of this lane's pieces; the first one's k (KF)
+    int64_t ld;
+    int cols;
+
+    __device__ __forceinline__ void init(const Side& d, int64_t offset, int64_t i0)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t left = d.n - i0;
+        cols = (int)(left < BI ? left : BI);
+        ld = d.ld;
+        base = reinterpret_cast<const char*>(d.p) + (offset + (KF ? i0 * ld : i0)) * 2;
+        const int slot = lane % SLOTS;
+        at_k = 0;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int row = (j * NW + wave) * LINES + lane / SLOTS;
+            if (KF) {
+                const int c = slot ^ (row >> 1 & 7);
+                at_k = (uint32_t)c * 8;      // (the same for all j: NW LINES is a multiple of sixteen)
+                off[j] = row < cols ? (uint32_t)(row * ld * 2) + c * 16 : BEYOND;
+            } else {
+                const int c = ((slot >> 1) ^ ((row & 3) | (row >> 1 & 4))) * 2 + (slot & 1);
+                off[j] = c * 8 < cols ? (uint32_t)(row * ld * 2) + c * 16 : BEYOND;
+            }
+        }
+    }
+    // step: k0 .. k0 + 63 of a segment of K, whose elements begin `seg` elements behind the operand's
+    __device__ __forceinline__ void load(int64_t seg, int64_t k0, int64_t K, uint32_t lds) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t left = K - k0;
+        const uint32_t here = (uint32_t)(left < BK ? left : BK);
+        if (KF) {
+            const range_t r = make_range(base + (seg + k0) * 2, (uint32_t)((cols - 1) * ld + here) * 2);
+            const bool is = at_k < here;
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) bring16(r, is ? off[j] : BEYOND, lds + (j * NW + wave) * 1024);
+        } else {
+            const range_t r = make_range(base + (seg + k0 * ld) * 2, (uint32_t)((here - 1) * ld + cols) * 2);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) bring16(r, off[j], lds + (j * NW + wave) * 1024);
+        }
+    }
+    // a lane's eight k, from 32 m + 8 (lane / 16) on, for i = i0 + lane % 16
+    static __device__ __forceinline__ uint4 frag(const char* lds, int i0, int m)
+    {
+        const int i = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
+        if constexpr (KF) {
+            return *reinterpret_cast<const uint4*>(lds + (i0 + i) * 128 + (((m * 4 + g) ^ (i >> 1)) << 4));
+        } else {
+            typedef __fp16 t4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) t4 lds_t4;
+            const char* p = lds + (m * 32 + 8 * g + (i >> 2)) * (BI * 2) + (((i0 >> 4) ^ ((i >> 2) | (g & 1) << 2)) << 5) + (i & 3) * 8;
+            const t4 a = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_t4*)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_t4*)(p + 4 * BI * 2));
+            const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+            return make_uint4(x.x, x.y, y.x, y.y);
+        }
+    }
+};
+
+// Workgroup: a tile of BF by BS, WF by WS waves.  The result goes through LDS, each wave's part by itself, so that memory sees rows of f.
+template <class IO, bool FK, bool SK, int EPI, int BF, int BS, int WF, int WS>
+__global__ __launch_bounds__(64 * WF * WS, 2) void fast_product_kernel(Product a, uint32_t tiles_f, uint32_t tiles_s)
+{
+    using T = typename IO::T;
+    constexpr int NW = WF * WS, NF = BF / WF / 16, NS = BS / WS / 16;      // tiles of 16 of a wave
+    using SideF = Fast<FK, BF, NW>;
+    using SideS = Fast<SK, BS, NW>;
+    constexpr int STAGE = SideF::BYTES + SideS::BYTES;
+    __shared__ __align__(1024) char lds[2 * STAGE];
+    uint32_t w = blockIdx.x;
+    {   // workgroups go round the eight dies: each die gets a run of neighbouring tiles, which share operands in its cache
+        const uint32_t n = gridDim.x, each = n / 8, rest = n % 8, die = w % 8, at = w / 8;
+        w = die * each + (die < rest ? die : rest) + at;
+    }
+    const uint32_t tf = w % tiles_f;
+    w /= tiles_f;
+    const uint32_t ts = w % tiles_s;
+    w /= tiles_s;
+    const uint32_t split = w % (uint32_t)a.splits, batch = w / (uint32_t)a.splits;
+    const int64_t f0 = (int64_t)tf * BF, s0 = (int64_t)ts * BS, steps = (a.K + 63) / 64;
+    const int64_t first = (int64_t)split * a.per, end = first + a.per < steps * a.segs ? first + a.per : steps * a.segs;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wf = wave % WF * (BF / WF), ws = wave / WF * (BS / WS);
+    SideF sf;
+    SideS ss;
+    sf.init(a.F, batch * a.F.batch, f0);
+    ss.init(a.S, batch * a.S.batch, s0);
+    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
+    int64_t seg = first / steps, k0 = (first - seg * steps) * 64;      // of the step to be asked for next
+    const auto ask = [&](int buf) {
+        sf.load(seg * a.F.seg, k0, a.K, lds0 + buf * STAGE);
+        ss.load(seg * a.S.seg, k0, a.K, lds0 + buf * STAGE + SideF::BYTES);
+        k0 += 64;
+        if (k0 >= a.K) {
+            k0 = 0;
+            ++seg;
+        }
+    };
+    mu::f4 acc[NF][NS], ones[NS];
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+        ones[j] = mu::f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NF; ++i) acc[i][j] = ones[j];
+    }
+    const bool sums = EPI == EPI_SUM && a.sums && f0 == 0 && wf == 0;
+    const uint32_t one = mu::IsBf<IO>::v ? 0x3f803f80u : 0x3c003c00u;
+    const uint4 all_ones = make_uint4(one, one, one, one);
+    if (first < end) ask(0);
+    int buf = 0;
+    for (int64_t at = first; at < end; ++at, buf ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (at + 1 < end) ask(buf ^ 1);
+        const char *const lf = lds + buf * STAGE, *const ls = lf + SideF::BYTES;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            uint4 x[NF], y[NS];
+#pragma unroll
+            for (int i = 0; i < NF; ++i) x[i] = SideF::frag(lf, wf + 16 * i, m);
+#pragma unroll
+            for (int j = 0; j < NS; ++j) y[j] = SideS::frag(ls, ws + 16 * j, m);
+#pragma unroll
+            for (int i = 0; i < NF; ++i)
+#pragma unroll
+                for (int j = 0; j < NS; ++j) acc[i][j] = mfma(IO(), x[i], y[j], acc[i][j]);
+            if (EPI == EPI_SUM && sums) {
+#pragma unroll
+                for (int j = 0; j < NS; ++j) ones[j] = mfma(IO(), all_ones, y[j], ones[j]);
+            }
+        }
+    }
+    __syncthreads();
+    const int col = lane & 15, g = lane >> 4;
+    if constexpr (EPI == EPI_SUM) {
+        if (sums && g == 0) {
+#pragma unroll
+            for (int j = 0; j < NS; ++j) {
+                const int64_t s = s0 + ws + 16 * j + col;
+                if (s < a.S.n) a.sums[(size_t)split * a.S.n + s] = ones[j][0];
+            }
+        }
+    }
+    // 64 values of f by SP of s at a time in this wave's share of LDS, fp32, the sixteen pieces of a row exchanged by s
+    constexpr int MINE = 2 * STAGE / NW, FP = NF * 16 < 64 ? NF * 16 : 64, SP = MINE / (FP * 4) < NS * 16 ? MINE / (FP * 4) : NS * 16;
+    constexpr int LANES = FP / 8, ROWS = 64 / LANES;      // lanes of a row of f, rows of a wave instruction
+    static_assert(FP % 64 == 0 && SP % 16 == 0 && SP % ROWS == 0, "whole tiles");
+    float* const mine = reinterpret_cast<float*>(lds + wave * MINE);
+    const int q = lane % LANES, r0 = lane / LANES;
+    constexpr int ITS = SP / ROWS;
+    static_assert(NS * 16 % SP == 0, "whole passes");
+    const bool whole = f0 + BF <= a.F.n && s0 + BS <= a.S.n;
+    const T* const from = EPI == EPI_DZ ? (const T*)a.dy : EPI == EPI_OUT ? (const T*)a.residual : nullptr;
+#pragma unroll
+    for (int fp = 0; fp < NF * 16 / FP; ++fp) {
+        const int64_t f = f0 + wf + fp * FP + 8 * q;
+        const int n = whole || a.F.n - f >= 8 ? 8 : (int)(a.F.n - f);
+        float bf[8] = {}, by_f[8] = {};
+        if (EPI != EPI_SUM && a.bias && a.bias_f && n > 0) load8<IoF32>(a.bias + f, n, bf);
+#pragma unroll
+        for (int sp = 0; sp < NS * 16 / SP; ++sp) {
+            const int64_t sr = s0 + ws + sp * SP + r0;      // this lane's rows: sr, sr + ROWS, ...
+            Raw8<IO> other[EPI == EPI_SUM ? 1 : ITS];
+            float bs[EPI == EPI_SUM ? 1 : ITS];
+            if constexpr (EPI != EPI_SUM) {
+                const T* const at = from ? from + (size_t)batch * a.batch + sr * a.ld + f : nullptr;
+#pragma unroll
+                for (int it = 0; it < ITS; ++it) {
+                    const bool is = whole || (sr + it * ROWS < a.S.n && n > 0);
+                    bs[it] = 0.f;
+                    if (a.bias && !a.bias_f && is) bs[it] = a.bias[sr + it * ROWS];
+                    if (!from) continue;
+                    if (whole) other[it].load(at + it * ROWS * a.ld);
+                    else if (is) load_raw<IO>(at + it * ROWS * a.ld, n, other[it]);
+                    else other[it].zero();
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < SP / 16; ++j)
+#pragma unroll
+                for (int i = 0; i < FP / 16; ++i) {
+                    const int s = 16 * j + col;
+                    const mu::f4 v = acc[fp * (FP / 16) + i][sp * (SP / 16) + j];
+                    *reinterpret_cast<float4*>(mine + s * FP + (((4 * i + g) ^ (s & 15)) << 2)) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            mu::wave_lds_fence();
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) {
+                const int r = it * ROWS + r0;
+                const int64_t s = sr + it * ROWS;
+                const float4 u = *reinterpret_cast<const float4*>(mine + r * FP + (((2 * q) ^ (r & 15)) << 2));
+                const float4 t = *reinterpret_cast<const float4*>(mine + r * FP + (((2 * q + 1) ^ (r & 15)) << 2));
+                float v[8] = {u.x, u.y, u.z, u.w, t.x, t.y, t.z, t.w};
+                const bool is = whole || (s < a.S.n && n > 0);
+                if constexpr (EPI == EPI_SUM) {
+                    if (is) store8<IoF32>(a.part + (size_t)split * a.S.n * a.F.n + s * a.F.n + f, n, v);
+                } else {
+                    float o[8] = {}, by_s = 0.f;
+                    if (from) other[it].get(o);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += bf[e] + bs[it];
+                    if constexpr (EPI == EPI_DZ) slopes_by(a.act, v);
+                    else acts_by(a.act, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (EPI == EPI_DZ) {
+                            v[e] = is ? o[e] * v[e] : 0.f;
+                            if (!whole && e >= n) v[e] = 0.f;
+                            by_f[e] += v[e];
+                            by_s += v[e];
+                        } else v[e] += o[e];
+                    }
+                    if (is) store8<IO>((T*)a.out + (size_t)batch * a.batch + s * a.ld + f, n, v);
+                    if (EPI == EPI_DZ && a.sums && !a.bias_f) {      // places are f: over the lanes of a row
+#pragma unroll
+                        for (int d = 1; d < LANES; d *= 2) by_s += __shfl_xor(by_s, d);
+                        float* const at = a.sums + ((size_t)(batch * tiles_f + tf) * (BF / 64) + (wf / 64 + fp)) * a.S.n;
+                        if (q == 0 && s < a.S.n) at[s] = by_s;
+                    }
+                }
+            }
+            mu::wave_lds_fence();
+        }
+        if constexpr (EPI == EPI_DZ) {
+            if (a.sums && a.bias_f) {      // places are s: over the lanes that have the same f
+                float* const at = a.sums + ((size_t)(batch * tiles_s + ts) * WS + wave / WF) * a.F.n;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float v = by_f[e];
+#pragma unroll
+                    for (int d = LANES; d < 64; d *= 2) v += __shfl_xor(v, d);
+                    if (r0 == 0 && e < n) at[f + e] = v;
+                }
+            }
+        }
+    }
+}
+
 // out[i] = sum over the shares, in their order
 template <class IO>
 __global__ __launch_bounds__(256) void linear_join_kernel(const float* __restrict__ part, typename IO::T* __restrict__ out, int64_t n, int64_t shares)
@@ -332,36 +622,75 @@ __global__ __launch_bounds__(256) void columns_first_kernel(const typename IO::T
         if ((threadIdx.x & 63) == 0) part[row] = v;
     }
 }
-// dbias[m] = the sum of shares, a workgroup of eight rows of 32 columns
-__global__ __launch_bounds__(256) void columns_join_kernel(const float* __restrict__ part, float* __restrict__ dbias, int64_t M, int64_t shares)
+// dbias[m] = the sum of shares, a workgroup of 32 rows of 32 columns
+__global__ __launch_bounds__(1024) void columns_join_kernel(const float* __restrict__ part, float* __restrict__ dbias, int64_t M, int64_t shares)
 {
-    __shared__ float lds[8][32];
+    __shared__ float lds[32][33];
     const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
     const int64_t m = (int64_t)blockIdx.x * 32 + c;
     float v = 0.f;
-    if (m < M)
-        for (int64_t q = r; q < shares; q += 8) v += part[q * M + m];
+    if (m < M) {
+#pragma unroll 8
+        for (int64_t q = r; q < shares; q += 32) v += part[q * M + m];
+    }
     lds[r][c] = v;
     __syncthreads();
-    if (r == 0 && m < M) {
-        for (int q = 1; q < 8; ++q) v += lds[q][c];
-        dbias[m] = v;
-    }
+    v = lds[c][r];      // row c's sum of column r: each half wave adds up one column
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) v += __shfl_xor(v, d);
+    const int64_t to = (int64_t)blockIdx.x * 32 + r;
+    if (c == 0 && to < M) dbias[to] = v;
 }
 
-template <class IO, int EPI>
-hipError_t launch_product(const Product& p, bool fk, bool sk, hipStream_t st)
+// Whether an operand's rows are whole pieces of 16 bytes, wherever a tile begins
+inline bool whole_pieces(const Side& d, bool kf, int64_t K) { return d.ld % 8 == 0 && (kf ? K : d.n) % 8 == 0 && d.batch % 8 == 0 && d.seg % 8 == 0 && d.ld < (1 << 23); }
+
+template <class IO, int EPI, bool FK, bool SK, int BF, int BS, int WF, int WS>
+hipError_t launch_fast(const Product& p, int64_t* shares, hipStream_t st)
 {
-    const uint64_t tf = (uint64_t)((p.F.n + TF - 1) / TF), ts = (uint64_t)((p.S.n + TS - 1) / TS);
+    const uint32_t tf = (uint32_t)((p.F.n + BF - 1) / BF), ts = (uint32_t)((p.S.n + BS - 1) / BS);
     dim3 g;
-    const hipError_t e = launch_grid(tf * ts * (uint64_t)p.splits * (uint64_t)p.batches, LT, &g);
+    const hipError_t e = launch_grid((uint64_t)tf * ts * (uint64_t)p.splits * (uint64_t)p.batches, 64 * WF * WS, &g);
     if (e != hipSuccess) return e;
-    const uint32_t a = (uint32_t)tf, b = (uint32_t)ts;
-    if (fk && sk) hipLaunchKernelGGL((product_kernel<IO, true, true, EPI>), g, dim3(LT), 0, st, p, a, b);
-    else if (fk) hipLaunchKernelGGL((product_kernel<IO, true, false, EPI>), g, dim3(LT), 0, st, p, a, b);
-    else if (sk) hipLaunchKernelGGL((product_kernel<IO, false, true, EPI>), g, dim3(LT), 0, st, p, a, b);
-    else hipLaunchKernelGGL((product_kernel<IO, false, false, EPI>), g, dim3(LT), 0, st, p, a, b);
+    if (shares) *shares = EPI == EPI_SUM ? p.splits : p.batches * (p.bias_f ? (int64_t)ts * WS : (int64_t)tf * (BF / 64));
+    hipLaunchKernelGGL((fast_product_kernel<IO, FK, SK, EPI, BF, BS, WF, WS>), g, dim3(64 * WF * WS), 0, st, p, tf, ts);
     return hipGetLastError();
+}
+// Tiles of 256 by 256 (one workgroup a compute unit, half the operand traffic) where they fill the last round of 256 units to three quarters
+// and more, else of 128 by 128 (two workgroups a unit, one's epilogue beside the other's products).  us, 256 and 128: forward 16384 x 768 ->
+// 2048 bf16 66 and 72; its dx, 192 tiles of 256, 74 and 67; 16384 x 2048 -> 768 57 and 59; 8192^3 870 and 1010; 131072 x 256 -> 1024 with gelu
+// fp16 228 and 234.
+inline bool wide_tiles(int64_t f, int64_t s, int64_t batches)
+{
+    const int64_t tiles = ((f + 255) / 256) * ((s + 255) / 256) * batches, rounds = (tiles + 255) / 256;
+    return tiles > rounds * 192;
+}
+
+template <class IO, int EPI, bool FK, bool SK>
+hipError_t launch_sides(Product p, int64_t* shares, hipStream_t st)
+{
+    dim3 g;
+    if constexpr (sizeof(typename IO::T) == 2) {
+        if (whole_pieces(p.F, FK, p.K) && whole_pieces(p.S, SK, p.K)) {
+            if (p.wide) return launch_fast<IO, EPI, FK, SK, 256, 256, 2, 4>(p, shares, st);
+            return launch_fast<IO, EPI, FK, SK, 128, 128, 2, 2>(p, shares, st);
+        }
+    }
+    const uint32_t tf = (uint32_t)((p.F.n + TF - 1) / TF), ts = (uint32_t)((p.S.n + TS - 1) / TS);
+    const hipError_t e = launch_grid((uint64_t)tf * ts * (uint64_t)p.splits * (uint64_t)p.batches, LT, &g);
+    if (e != hipSuccess) return e;
+    if (shares) *shares = EPI == EPI_SUM ? 0 : p.batches * 2 * (p.bias_f ? ts : tf);
+    hipLaunchKernelGGL((product_kernel<IO, FK, SK, EPI>), g, dim3(LT), 0, st, p, tf, ts);
+    return hipGetLastError();
+}
+// shares: how many sums of dz's columns it leaves at p.sums (0: none)
+template <class IO, int EPI>
+hipError_t launch_product(const Product& p, bool fk, bool sk, int64_t* shares, hipStream_t st)
+{
+    if (fk && sk) return launch_sides<IO, EPI, true, true>(p, shares, st);
+    if (fk) return launch_sides<IO, EPI, true, false>(p, shares, st);
+    if (sk) return launch_sides<IO, EPI, false, true>(p, shares, st);
+    return launch_sides<IO, EPI, false, false>(p, shares, st);
 }
 
 inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -386,7 +715,7 @@ inline Side rows_of(const void* p, bool first, const Cut& c, int64_t width)
 
 // z = x W^T + bias and what follows it
 template <class IO, int EPI>
-hipError_t forward(const LinearArgs& a, const void* x, Product p, hipStream_t st)
+hipError_t forward(const LinearArgs& a, const void* x, Product p, int64_t* shares, hipStream_t st)
 {
     const Cut c(a);
     const Side X = rows_of(x, c.x_first, c, a.K), W{a.W, a.M, a.K, 0, 0};
@@ -402,23 +731,33 @@ hipError_t forward(const LinearArgs& a, const void* x, Product p, hipStream_t st
     p.bias_f = !c.y_first;
     p.F = c.y_first ? X : W;
     p.S = c.y_first ? W : X;
-    return launch_product<IO, EPI>(p, c.y_first ? !c.x_first : true, c.y_first ? true : !c.x_first, st);
+    p.wide = wide_tiles(p.F.n, p.S.n, p.batches);
+    return launch_product<IO, EPI>(p, c.y_first ? !c.x_first : true, c.y_first ? true : !c.x_first, shares, st);
 }
 
-// shares of the sum over places of dW: as many as make 512 workgroups, of four steps at least
+// Shares of the sum over places of dW, of four steps at least: as many as make 256 workgroups of 256 by 256 where that is four tiles or more
+// and 16 shares at most, else 512 of 128 by 128.
 struct Shares {
     int64_t shares, per;
+    bool wide;
 };
+inline int64_t shares_wanted(int64_t K, int64_t M, bool* wide)
+{
+    const int64_t large = ((K + 255) / 256) * ((M + 255) / 256), tiles = ((K + TF - 1) / TF) * ((M + TS - 1) / TS);
+    *wide = large >= 16;
+    return *wide ? (large >= 256 ? 1 : 256 / large) : (512 + tiles - 1) / tiles;
+}
 template <class IO>
 Shares shares_of(int64_t B, int64_t N, int64_t K, int64_t M, bool by_batch)
 {
     constexpr int BK = Tile<IO, true>::BK;
-    const int64_t tiles = ((K + TF - 1) / TF) * ((M + TS - 1) / TS);
+    Shares r;
+    int64_t want = shares_wanted(K, M, &r.wide);
     const int64_t steps = by_batch ? B * ((N + BK - 1) / BK) : (B * N + BK - 1) / BK;
-    int64_t want = (512 + tiles - 1) / tiles;
     if (want > (steps + 3) / 4) want = (steps + 3) / 4;
-    const int64_t per = (steps + want - 1) / want;
-    return Shares{(steps + per - 1) / per, per};
+    r.per = (steps + want - 1) / want;
+    r.shares = (steps + r.per - 1) / r.per;
+    return r;
 }
 
 template <class IO>
@@ -427,23 +766,20 @@ hipError_t linear_fwd_io(const LinearArgs& a, const void* x, const void* residua
     Product p = {};
     p.out = y;
     p.residual = residual;
-    return forward<IO, EPI_OUT>(a, x, p, st);
+    return forward<IO, EPI_OUT>(a, x, p, nullptr, st);
 }
 
-// shares of the sums of dbias: of a tile's halves (EPI_DZ), of sequences, of places
-inline int64_t bias_shares(int64_t B, int64_t N)
-{
-    const int64_t by_batch = 2 * B * ((N + 127) / 128), flat = 2 * ((B * N + 127) / 128);
-    return by_batch > flat ? by_batch : flat;
-}
+// the most shares that sums of dbias come in: two for each 128 places (a tile's halves), or as many as dW's sums
+inline int64_t bias_shares(int64_t B, int64_t N) { return 2 * B * ((N + 127) / 128); }
 template <class IO>
 size_t linear_workspace_io(int64_t B, int64_t N, int64_t K, int64_t M, int backward)
 {
     if (!backward) return 256;
-    const int64_t tiles = ((K + TF - 1) / TF) * ((M + TS - 1) / TS);
-    const int64_t want = (512 + tiles - 1) / tiles, steps = (B * ((N + 15) / 16) + 3) / 4;      // (never more shares than either)
-    return up256((size_t)B * N * M * sizeof(typename IO::T)) + up256((size_t)(want < steps ? want : steps) * K * M * sizeof(float)) +
-           up256((size_t)bias_shares(B, N) * M * sizeof(float));
+    bool wide;
+    const int64_t want = shares_wanted(K, M, &wide), steps = (B * ((N + 15) / 16) + 3) / 4;      // (never more shares than either)
+    const int64_t shares = want < steps ? want : steps, bias = bias_shares(B, N);
+    return up256((size_t)B * N * M * sizeof(typename IO::T)) + up256((size_t)shares * K * M * sizeof(float)) +
+           up256((size_t)(bias > shares ? bias : shares) * M * sizeof(float));
 }
 
 template <class IO>
@@ -461,49 +797,15 @@ hipError_t linear_bwd_io(const LinearArgs& a, const LinearGrads& d, void* ws, hi
     float* const sums = (float*)at;
     const void* dz = d.dy;
     hipError_t e = hipSuccess;
-    int64_t bias_parts = 0;
+    int64_t shares = 0;      // sums of dz's columns that wait at `sums`
     if (a.act != LONGCONV_ACT_NONE) {
         Product p = {};
         p.out = dz_room;
         p.dy = d.dy;
         p.sums = d.dbias ? sums : nullptr;
-        e = forward<IO, EPI_DZ>(a, d.x, p, st);
+        e = forward<IO, EPI_DZ>(a, d.x, p, &shares, st);
+        if (e != hipSuccess) return e;
         dz = dz_room;
-        bias_parts = c.batches * ((c.places + 127) / 128) * 2;
-    } else if (d.dbias) {
-        if (c.y_first) {
-            bias_parts = a.B;
-            const int64_t groups = (a.B * a.M + 3) / 4;
-            hipLaunchKernelGGL(columns_first_kernel<IO>, dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20)), dim3(256), 0, st, (const T*)d.dy, sums, a.B * a.M, a.N);
-        } else {
-            bias_parts = (a.B * a.N + COLUMN_ROWS - 1) / COLUMN_ROWS;
-            const uint32_t wide = (uint32_t)((a.M + 255) / 256);
-            hipLaunchKernelGGL(columns_last_kernel<IO>, dim3((unsigned)(bias_parts * wide)), dim3(256), 0, st, (const T*)d.dy, sums, a.B * a.N, a.M, wide);
-        }
-        e = hipGetLastError();
-    }
-    if (e != hipSuccess) return e;
-    if (d.dbias) {
-        hipLaunchKernelGGL(columns_join_kernel, dim3((unsigned)((a.M + 31) / 32)), dim3(256), 0, st, sums, d.dbias, a.M, bias_parts);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (d.dx) {      // dx[place][k] = sum_m dz[place][m] W[m][k]
-        Product p = {};
-        const Side Z = rows_of(dz, c.y_first, c, a.M), W{a.W, a.K, a.K, 0, 0};
-        p.K = a.M;
-        p.segs = 1;
-        p.batches = c.batches;
-        p.splits = 1;
-        p.per = INT64_MAX / 4;
-        p.act = LONGCONV_ACT_NONE;
-        p.out = d.dx;
-        p.batch = c.places * a.K;
-        p.ld = c.x_first ? c.places : a.K;
-        p.F = c.x_first ? Z : W;
-        p.S = c.x_first ? W : Z;
-        e = launch_product<IO, EPI_OUT>(p, c.x_first ? !c.y_first : false, c.x_first ? false : !c.y_first, st);
-        if (e != hipSuccess) return e;
     }
     if (d.dW) {      // dW[m][k] = sum over places of dz[place][m] x[place][k]
         Product p = {};
@@ -518,16 +820,57 @@ hipError_t linear_bwd_io(const LinearArgs& a, const LinearGrads& d, void* ws, hi
         p.batches = 1;
         p.splits = sh.shares;
         p.per = sh.per;
+        p.wide = sh.wide;
         p.part = sh.shares == 1 && d.dW_f32 ? (float*)d.dW : part;
-        e = launch_product<IO, EPI_SUM>(p, c.x_first, c.y_first, st);
-        if (e != hipSuccess || p.part == d.dW) return e;
-        const int64_t n = a.K * a.M;
-        const dim3 g((unsigned)((n + 1023) / 1024));
-        if (d.dW_f32) hipLaunchKernelGGL(linear_join_kernel<IoF32>, g, dim3(256), 0, st, part, (float*)d.dW, n, sh.shares);
-        else hipLaunchKernelGGL(linear_join_kernel<IO>, g, dim3(256), 0, st, part, (T*)d.dW, n, sh.shares);
-        e = hipGetLastError();
+        p.sums = d.dbias && !shares ? sums : nullptr;
+        int64_t left = 0;
+        e = launch_product<IO, EPI_SUM>(p, c.x_first, c.y_first, &left, st);
+        if (e != hipSuccess) return e;
+        if (p.sums) shares = left;
+        if (p.part != d.dW) {
+            const int64_t n = a.K * a.M;
+            const dim3 g((unsigned)((n + 1023) / 1024));
+            if (d.dW_f32) hipLaunchKernelGGL(linear_join_kernel<IoF32>, g, dim3(256), 0, st, part, (float*)d.dW, n, sh.shares);
+            else hipLaunchKernelGGL(linear_join_kernel<IO>, g, dim3(256), 0, st, part, (T*)d.dW, n, sh.shares);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
     }
-    return e;
+    if (d.dbias && !shares) {
+        if (c.y_first) {
+            shares = a.B;
+            const int64_t groups = (a.B * a.M + 3) / 4;
+            hipLaunchKernelGGL(columns_first_kernel<IO>, dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20)), dim3(256), 0, st, (const T*)dz, sums, a.B * a.M, a.N);
+        } else {
+            shares = (a.B * a.N + COLUMN_ROWS - 1) / COLUMN_ROWS;
+            const uint32_t wide = (uint32_t)((a.M + 255) / 256);
+            hipLaunchKernelGGL(columns_last_kernel<IO>, dim3((unsigned)(shares * wide)), dim3(256), 0, st, (const T*)dz, sums, a.B * a.N, a.M, wide);
+        }
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (d.dbias) {
+        hipLaunchKernelGGL(columns_join_kernel, dim3((unsigned)((a.M + 31) / 32)), dim3(1024), 0, st, sums, d.dbias, a.M, shares);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!d.dx) return hipSuccess;
+    // dx[place][k] = sum_m dz[place][m] W[m][k]
+    Product p = {};
+    const Side Z = rows_of(dz, c.y_first, c, a.M), W{a.W, a.K, a.K, 0, 0};
+    p.K = a.M;
+    p.segs = 1;
+    p.batches = c.batches;
+    p.splits = 1;
+    p.per = INT64_MAX / 4;
+    p.act = LONGCONV_ACT_NONE;
+    p.out = d.dx;
+    p.batch = c.places * a.K;
+    p.ld = c.x_first ? c.places : a.K;
+    p.F = c.x_first ? Z : W;
+    p.S = c.x_first ? W : Z;
+    p.wide = wide_tiles(p.F.n, p.S.n, p.batches);
+    return launch_product<IO, EPI_OUT>(p, c.x_first ? !c.y_first : false, c.x_first ? false : !c.y_first, nullptr, st);
 }
 
 }  // namespace
