@@ -11,7 +11,7 @@ namespace lc {
 namespace {
 
 constexpr int LT = 256;               // threads: four waves, two by two
-constexpr int TF = 128, TS = 128;     // tile of the result
+constexpr int TF = 128, TS = 128;     // tile of the result (there are smaller and larger ones)
 
 // One operand: element (i, k) of batch b and segment q of the sum lies at p + b batch + q seg + i ld + k, or + k ld + i
 struct Side {
@@ -97,14 +97,14 @@ __device__ __forceinline__ mu::f4 mfma(IoF32, const float4& a, const float4& b, 
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, b.w, d, 0, 0, 0);
 }
 
-// A tile of 128 values of i by BK values of k in LDS, KF: rows along k, else rows along i
-template <class IO, bool KF>
+// A tile of BT values of i by BK values of k in LDS, KF: rows along k, else rows along i
+template <class IO, bool KF, int BT = 128>
 struct Tile {
     using T = typename IO::T;
-    static constexpr int E = sizeof(T), BK = E == 4 ? 16 : 64, STEP = E == 4 ? 16 : 32;      // k of a step of the loop, of a matrix instruction
-    static constexpr int ROW = KF ? BK + 16 / E : 128 + 32 / E, ROWS = KF ? 128 : BK;        // elements from row to row
+    static constexpr int E = sizeof(T), BK = E == 4 ? 32 : 64, STEP = E == 4 ? 16 : 32;      // k of a step of the loop, of a matrix instruction
+    static constexpr int ROW = KF ? BK + 16 / E : BT + 32 / E, ROWS = KF ? BT : BK;        // elements from row to row
     static constexpr int BYTES = ROW * ROWS * E;
-    static constexpr int PER_ROW = (KF ? BK : 128) / VE, PIECES = 128 * BK / VE / LT;
+    static constexpr int PER_ROW = (KF ? BK : BT) / VE, PIECES = BT * BK / VE / LT;
     using Frag = typename std::conditional<E == 4, float4, uint4>::type;
 
     static __device__ __forceinline__ void load(const Side& d, int64_t off, int64_t i0, int64_t k0, int64_t K, Raw8<IO> (&r)[PIECES])
@@ -189,14 +189,15 @@ __device__ __forceinline__ void load4(const typename IO::T* p, int n, float (&v)
     for (int i = 0; i < 4; ++i) v[i] = i < n ? IO::ld(p, i) : 0.f;
 }
 
-// Workgroup: one tile, of one batch and one share of the sum.  A wave has 64 by 64 of it, in tiles of 16 by 16.
-template <class IO, bool FK, bool SK, int EPI>
-__global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f, uint32_t tiles_s)
+// Workgroup: one tile, of one batch and one share of the sum.  A wave has a quarter of it, in tiles of 16 by 16.  Operands are asked for into
+// registers two steps ahead, at any alignment.
+template <class IO, bool FK, bool SK, int EPI, int BT>
+__global__ __launch_bounds__(LT, 2) void product_kernel(Product a, uint32_t tiles_f, uint32_t tiles_s)
 {
     using T = typename IO::T;
-    using TileF = Tile<IO, FK>;
-    using TileS = Tile<IO, SK>;
-    constexpr int BK = TileF::BK, STEP = TileF::STEP;
+    using TileF = Tile<IO, FK, BT>;
+    using TileS = Tile<IO, SK, BT>;
+    constexpr int BK = TileF::BK, STEP = TileF::STEP, NT = BT / 32;
     __shared__ __align__(16) unsigned char lds[TileF::BYTES + TileS::BYTES];
     T *const lf = reinterpret_cast<T*>(lds), *const ls = reinterpret_cast<T*>(lds + TileF::BYTES);
     uint32_t w = blockIdx.x;
@@ -205,39 +206,51 @@ __global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f
     const uint32_t ts = w % tiles_s;
     w /= tiles_s;
     const uint32_t split = w % (uint32_t)a.splits, batch = w / (uint32_t)a.splits;
-    const int64_t f0 = (int64_t)tf * TF, s0 = (int64_t)ts * TS, steps = (a.K + BK - 1) / BK;
+    const int64_t f0 = (int64_t)tf * BT, s0 = (int64_t)ts * BT, steps = (a.K + BK - 1) / BK;
     const int64_t first = (int64_t)split * a.per, end = first + a.per < steps * a.segs ? first + a.per : steps * a.segs;
-    const int wave = threadIdx.x >> 6, wf = (wave & 1) * 64, ws = (wave >> 1) * 64;
-    mu::f4 acc[4][4];
+    const int wave = threadIdx.x >> 6, wf = (wave & 1) * (BT / 2), ws = (wave >> 1) * (BT / 2);
+    mu::f4 acc[NT][NT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mu::f4{0.f, 0.f, 0.f, 0.f};
-    Raw8<IO> rf[TileF::PIECES], rs[TileS::PIECES];
-    const auto ask = [&](int64_t at) {
-        const int64_t q = at / steps, k0 = (at - q * steps) * BK;
-        TileF::load(a.F, batch * a.F.batch + q * a.F.seg, f0, k0, a.K, rf);
-        TileS::load(a.S, batch * a.S.batch + q * a.S.seg, s0, k0, a.K, rs);
+        for (int j = 0; j < NT; ++j) acc[i][j] = mu::f4{0.f, 0.f, 0.f, 0.f};
+    Raw8<IO> rf[2][TileF::PIECES], rs[2][TileS::PIECES];
+    int64_t seg = first / steps, k0 = (first - seg * steps) * BK, asked = first;      // of the step to be asked for next
+    const auto ask = [&](int u) {
+        if (asked >= end) return;
+        TileF::load(a.F, batch * a.F.batch + seg * a.F.seg, f0, k0, a.K, rf[u]);
+        TileS::load(a.S, batch * a.S.batch + seg * a.S.seg, s0, k0, a.K, rs[u]);
+        ++asked;
+        k0 += BK;
+        if (k0 >= a.K) {
+            k0 = 0;
+            ++seg;
+        }
     };
-    if (first < end) ask(first);
-    for (int64_t at = first; at < end; ++at) {
-        __syncthreads();
-        TileF::put(lf, rf);
-        TileS::put(ls, rs);
-        __syncthreads();
-        if (at + 1 < end) ask(at + 1);
+    ask(0);
+    ask(1);
+    for (int64_t at = first; at < end; at += 2) {
 #pragma unroll
-        for (int m = 0; m < BK / STEP; ++m) {
-            typename TileF::Frag x[4], y[4];
+        for (int u = 0; u < 2; ++u) {
+            if (at + u >= end) break;
+            __syncthreads();
+            TileF::put(lf, rf[u]);
+            TileS::put(ls, rs[u]);
+            __syncthreads();
+            ask(u);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i] = TileF::frag(lf, wf + 16 * i, m);
-                y[i] = TileS::frag(ls, ws + 16 * i, m);
+            for (int m = 0; m < BK / STEP; ++m) {
+                typename TileF::Frag x[NT], y[NT];
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    x[i] = TileF::frag(lf, wf + 16 * i, m);
+                    y[i] = TileS::frag(ls, ws + 16 * i, m);
+                }
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma(IO(), x[i], y[j], acc[i][j]);
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = mfma(IO(), x[i], y[j], acc[i][j]);
         }
     }
     // a lane has f = 4 (lane / 16) .. + 3 and s = lane % 16 of each tile of 16 by 16
@@ -245,10 +258,10 @@ __global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f
     if constexpr (EPI == EPI_SUM) {
         float* const to = a.part + (size_t)split * a.S.n * a.F.n;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NT; ++j) {
             const int64_t s = s0 + ws + 16 * j + col;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < NT; ++i) {
                 const int64_t f = f0 + wf + 16 * i + 4 * g, n = a.F.n - f;
                 const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
                 if (s < a.S.n && n > 0) store4<IoF32>(to + s * a.F.n + f, n < 4 ? (int)n : 4, v);
@@ -256,15 +269,15 @@ __global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f
         }
         return;
     }
-    float by_f[4][4] = {}, by_s[4] = {};
+    float by_f[NT][4] = {}, by_s[NT] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NT; ++i) {
         const int64_t f = f0 + wf + 16 * i + 4 * g, n_f = a.F.n - f;
         const int n = n_f < 4 ? (int)n_f : 4;
         float bf[4] = {0.f, 0.f, 0.f, 0.f};
         if (a.bias && a.bias_f && n > 0) load4<IoF32>(a.bias + f, n, bf);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NT; ++j) {
             const int64_t s = s0 + ws + 16 * j + col;
             if (s >= a.S.n || n <= 0) continue;
             const size_t at = (size_t)batch * a.batch + s * a.ld + f;
@@ -289,7 +302,7 @@ __global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f
         if (a.bias_f) {      // places are s: over the lanes of a row of sixteen
             float* const to = a.sums + ((size_t)(batch * tiles_s + ts) * 2 + (wave >> 1)) * a.F.n;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float v = by_f[i][q];
@@ -301,7 +314,7 @@ __global__ __launch_bounds__(LT) void product_kernel(Product a, uint32_t tiles_f
         } else {             // places are f: over the four rows of lanes
             float* const to = a.sums + ((size_t)(batch * tiles_f + tf) * 2 + (wave & 1)) * a.S.n;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < NT; ++j) {
                 float v = by_s[j];
                 v += __shfl_xor(v, 16);
                 v += __shfl_xor(v, 32);
@@ -450,7 +463,7 @@ __global__ __launch_bounds__(64 * WF * WS, 2) void fast_product_kernel(Product a
     if (first < end) ask(0);
     int buf = 0;
     for (int64_t at = first; at < end; ++at, buf ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // this step's tiles are here, the last one's are read
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (at + 1 < end) ask(buf ^ 1);
@@ -586,6 +599,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const float* __restric
     if (at >= n) return;
     const int here = n - at < 4 ? (int)(n - at) : 4;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int64_t q = 0; q < shares; ++q) {
         float w[4];
         load4<IoF32>(part + q * n + at, here, w);
@@ -642,8 +656,82 @@ __global__ __launch_bounds__(1024) void columns_join_kernel(const float* __restr
     if (c == 0 && to < M) dbias[to] = v;
 }
 
-// Whether an operand's rows are whole pieces of 16 bytes, wherever a tile begins
-inline bool whole_pieces(const Side& d, bool kf, int64_t K) { return d.ld % 8 == 0 && (kf ? K : d.n) % 8 == 0 && d.batch % 8 == 0 && d.seg % 8 == 0 && d.ld < (1 << 23); }
+// ---- few places ------------------------------------------------------------------------------------------------------------
+// y = act(x W^T + bias) + residual for up to 16 NT rows of x: W is what is read, each piece of it once, straight into the matrix instructions'
+// operands.  Workgroup: 16 columns m; its eight waves take the sum's steps in turn and add up through LDS.
+constexpr int FEW = 64;      // places
+template <class IO, int NT>
+__global__ __launch_bounds__(512) void few_kernel(Product a)
+{
+    using T = typename IO::T;
+    constexpr bool F4 = sizeof(T) == 4;
+    constexpr int PER = F4 ? 4 : 8, STEP = 4 * PER, NW = 8;      // k of a lane, of a step
+    using Frag = typename std::conditional<F4, float4, uint4>::type;
+    __shared__ float lds[NW][NT][16][17];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int64_t m0 = (int64_t)blockIdx.x * 16;
+    const auto frag = [&](const Side& d, int64_t row, int64_t k) {
+        Frag r;
+        const T* const p = (const T*)d.p + row * d.ld + k;
+        const int64_t n = row < d.n ? a.K - k : 0;
+        if constexpr (F4) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (n > 0) load4<IoF32>(p, n < 4 ? (int)n : 4, v);
+            r = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+            Raw8<IO> q;
+            load_raw<IO>(p, n < 8 ? (int)n : 8, q);
+            r = make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]);
+        }
+        return r;
+    };
+    mu::f4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = mu::f4{0.f, 0.f, 0.f, 0.f};
+    constexpr int AHEAD = NT == 1 ? 4 : 2;      // steps whose operands are asked for at once
+    for (int64_t k0 = (int64_t)wave * STEP; k0 < a.K; k0 += (int64_t)AHEAD * NW * STEP) {
+        Frag w[AHEAD], x[AHEAD][NT];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) {
+            const int64_t k = k0 + (int64_t)s * NW * STEP + g * PER;
+            w[s] = frag(a.F, m0 + i, k);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) x[s][t] = frag(a.S, 16 * t + i, k);
+        }
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[t] = mfma(IO(), w[s], x[s][t], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) lds[wave][t][i][4 * g + r] = acc[t][r];
+    __syncthreads();
+    for (int id = threadIdx.x; id < NT * 256; id += 512) {
+        const int t = id >> 8, row = id >> 4 & 15, c = id & 15;
+        const int64_t s = 16 * t + row, m = m0 + c;
+        if (s >= a.S.n || m >= a.F.n) continue;
+        float z = a.bias ? a.bias[m] : 0.f;
+#pragma unroll
+        for (int r = 0; r < NW; ++r) z += lds[r][t][row][c];
+        z = act_by(a.act, z);
+        if (a.residual) z += IO::ld((const T*)a.residual, s * a.ld + m);
+        IO::st((T*)a.out, s * a.ld + m, z);
+    }
+}
+template <class IO>
+hipError_t launch_few(const Product& p, hipStream_t st)
+{
+    const dim3 g((unsigned)((p.F.n + 15) / 16));
+    if (p.S.n <= 16) hipLaunchKernelGGL((few_kernel<IO, 1>), g, dim3(512), 0, st, p);
+    else if (p.S.n <= 32) hipLaunchKernelGGL((few_kernel<IO, 2>), g, dim3(512), 0, st, p);
+    else hipLaunchKernelGGL((few_kernel<IO, 4>), g, dim3(512), 0, st, p);
+    return hipGetLastError();
+}
+
+// Whether an operand's rows are whole pieces of 16 bytes, wherever a tile begins, and a tile's 256 rows lie within 2 GB (BEYOND is beyond)
+inline bool whole_pieces(const Side& d, bool kf, int64_t K) { return d.ld % 8 == 0 && (kf ? K : d.n) % 8 == 0 && d.batch % 8 == 0 && d.seg % 8 == 0 && d.ld < (1 << 22); }
 
 template <class IO, int EPI, bool FK, bool SK, int BF, int BS, int WF, int WS>
 hipError_t launch_fast(const Product& p, int64_t* shares, hipStream_t st)
@@ -656,14 +744,14 @@ hipError_t launch_fast(const Product& p, int64_t* shares, hipStream_t st)
     hipLaunchKernelGGL((fast_product_kernel<IO, FK, SK, EPI, BF, BS, WF, WS>), g, dim3(64 * WF * WS), 0, st, p, tf, ts);
     return hipGetLastError();
 }
-// Tiles of 256 by 256 (one workgroup a compute unit, half the operand traffic) where they fill the last round of 256 units to three quarters
-// and more, else of 128 by 128 (two workgroups a unit, one's epilogue beside the other's products).  us, 256 and 128: forward 16384 x 768 ->
+// Tiles of 256 by 256 (one workgroup a compute unit, half the operand traffic) where they are full to three quarters and more, and so is
+// the last round of 256 units, else of 128 by 128 (two workgroups a unit, one's epilogue beside the other's products).  us, 256 and 128: forward 16384 x 768 ->
 // 2048 bf16 66 and 72; its dx, 192 tiles of 256, 74 and 67; 16384 x 2048 -> 768 57 and 59; 8192^3 870 and 1010; 131072 x 256 -> 1024 with gelu
 // fp16 228 and 234.
 inline bool wide_tiles(int64_t f, int64_t s, int64_t batches)
 {
     const int64_t tiles = ((f + 255) / 256) * ((s + 255) / 256) * batches, rounds = (tiles + 255) / 256;
-    return tiles > rounds * 192;
+    return tiles > rounds * 192 && f * s * batches >= tiles * (256 * 192);
 }
 
 template <class IO, int EPI, bool FK, bool SK>
@@ -676,11 +764,16 @@ hipError_t launch_sides(Product p, int64_t* shares, hipStream_t st)
             return launch_fast<IO, EPI, FK, SK, 128, 128, 2, 2>(p, shares, st);
         }
     }
-    const uint32_t tf = (uint32_t)((p.F.n + TF - 1) / TF), ts = (uint32_t)((p.S.n + TS - 1) / TS);
+    // smaller tiles where the larger ones leave units without work
+    const auto tiles = [&](int64_t n, int64_t t) { return (uint64_t)((n + t - 1) / t); };
+    const bool small = tiles(p.F.n, 128) * tiles(p.S.n, 128) * (uint64_t)p.splits * (uint64_t)p.batches < 512;
+    const int64_t t = small ? 64 : 128;
+    const uint32_t tf = (uint32_t)tiles(p.F.n, t), ts = (uint32_t)tiles(p.S.n, t);
     const hipError_t e = launch_grid((uint64_t)tf * ts * (uint64_t)p.splits * (uint64_t)p.batches, LT, &g);
     if (e != hipSuccess) return e;
     if (shares) *shares = EPI == EPI_SUM ? 0 : p.batches * 2 * (p.bias_f ? ts : tf);
-    hipLaunchKernelGGL((product_kernel<IO, FK, SK, EPI>), g, dim3(LT), 0, st, p, tf, ts);
+    if (small) hipLaunchKernelGGL((product_kernel<IO, FK, SK, EPI, 64>), g, dim3(LT), 0, st, p, tf, ts);
+    else hipLaunchKernelGGL((product_kernel<IO, FK, SK, EPI, 128>), g, dim3(LT), 0, st, p, tf, ts);
     return hipGetLastError();
 }
 // shares: how many sums of dz's columns it leaves at p.sums (0: none)
@@ -731,20 +824,23 @@ hipError_t forward(const LinearArgs& a, const void* x, Product p, int64_t* share
     p.bias_f = !c.y_first;
     p.F = c.y_first ? X : W;
     p.S = c.y_first ? W : X;
+    if (EPI == EPI_OUT && !c.x_first && !c.y_first && c.places <= FEW) return launch_few<IO>(p, st);
     p.wide = wide_tiles(p.F.n, p.S.n, p.batches);
     return launch_product<IO, EPI>(p, c.y_first ? !c.x_first : true, c.y_first ? true : !c.x_first, shares, st);
 }
 
-// Shares of the sum over places of dW, of four steps at least: as many as make 256 workgroups of 256 by 256 where that is four tiles or more
-// and 16 shares at most, else 512 of 128 by 128.
+// Shares of the sum over places of dW, of four steps at least: as many as make 256 workgroups of 256 by 256 where there are 16 such tiles and
+// more (fewer: more shares, and with them more sums to write and join), else 512 of 128 by 128.  us, the two: 768 x 2048 (24 tiles) 65 + 11 and
+// 98 + 8, 256 x 1024 (4 tiles) 133 and 104.
 struct Shares {
     int64_t shares, per;
     bool wide;
 };
-inline int64_t shares_wanted(int64_t K, int64_t M, bool* wide)
+inline int64_t shares_wanted(int64_t K, int64_t M, bool f32, bool* wide)
 {
-    const int64_t large = ((K + 255) / 256) * ((M + 255) / 256), tiles = ((K + TF - 1) / TF) * ((M + TS - 1) / TS);
-    *wide = large >= 16;
+    const int64_t t = f32 ? 64 : 128;      // (fp32: four workgroups a unit, of 64 by 64)
+    const int64_t large = ((K + 255) / 256) * ((M + 255) / 256), tiles = ((K + t - 1) / t) * ((M + t - 1) / t);
+    *wide = !f32 && large >= 16;
     return *wide ? (large >= 256 ? 1 : 256 / large) : (512 + tiles - 1) / tiles;
 }
 template <class IO>
@@ -752,7 +848,7 @@ Shares shares_of(int64_t B, int64_t N, int64_t K, int64_t M, bool by_batch)
 {
     constexpr int BK = Tile<IO, true>::BK;
     Shares r;
-    int64_t want = shares_wanted(K, M, &r.wide);
+    int64_t want = shares_wanted(K, M, sizeof(typename IO::T) == 4, &r.wide);
     const int64_t steps = by_batch ? B * ((N + BK - 1) / BK) : (B * N + BK - 1) / BK;
     if (want > (steps + 3) / 4) want = (steps + 3) / 4;
     r.per = (steps + want - 1) / want;
@@ -769,14 +865,15 @@ hipError_t linear_fwd_io(const LinearArgs& a, const void* x, const void* residua
     return forward<IO, EPI_OUT>(a, x, p, nullptr, st);
 }
 
-// the most shares that sums of dbias come in: two for each 128 places (a tile's halves), or as many as dW's sums
-inline int64_t bias_shares(int64_t B, int64_t N) { return 2 * B * ((N + 127) / 128); }
+// the most shares that sums of dbias come in: two for each 64 places (a tile's halves), or as many as dW's sums; a tile of 256 makes four,
+// however few its places
+inline int64_t bias_shares(int64_t B, int64_t N) { return B * (2 * ((N + 63) / 64) + 2); }
 template <class IO>
 size_t linear_workspace_io(int64_t B, int64_t N, int64_t K, int64_t M, int backward)
 {
     if (!backward) return 256;
     bool wide;
-    const int64_t want = shares_wanted(K, M, &wide), steps = (B * ((N + 15) / 16) + 3) / 4;      // (never more shares than either)
+    const int64_t want = shares_wanted(K, M, sizeof(typename IO::T) == 4, &wide), steps = (B * ((N + 15) / 16) + 3) / 4;      // (never more shares than either)
     const int64_t shares = want < steps ? want : steps, bias = bias_shares(B, N);
     return up256((size_t)B * N * M * sizeof(typename IO::T)) + up256((size_t)shares * K * M * sizeof(float)) +
            up256((size_t)(bias > shares ? bias : shares) * M * sizeof(float));

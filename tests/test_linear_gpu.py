@@ -177,3 +177,24 @@ def test_under_graph_capture_on_a_side_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, kept))
+
+
+# one sequence, or one place of each: what is few places in one layout is columns in another
+@pytest.mark.parametrize("B,N", [(1, 1), (1, 2), (1, 17), (1, 64), (5, 1), (64, 1)])
+@pytest.mark.parametrize("firsts", [(True, True), (False, True), (True, False)])
+@pytest.mark.parametrize("io", ["fp32", "bf16"])
+def test_few_places_in_other_layouts(B, N, firsts, io):
+    Run(B, N, 72, 136, io, "silu", residual=True, x_first=firsts[0], y_first=firsts[1], seed=11).fwd().bwd().check()
+
+
+# the sums' shares where places are few and tiles many, and where tiles are the largest; a workspace of just the size asked for
+@pytest.mark.parametrize("io,B,N,K,M,firsts", [("bf16", 200, 32, 64, 256, (False, True)), ("fp16", 260, 24, 256, 64, (True, True)), ("bf16", 1, 1, 16, 65528, (False, False)),
+                                               ("fp16", 1, 3300, 64, 4096, (False, False)), ("bf16", 2, 1600, 64, 4096, (False, True)),
+                                               ("fp32", 120, 8, 8, 72, (True, True)), ("bf16", 3, 200, 1024, 1032, (False, False))])
+def test_writes_stay_within_the_workspace(io, B, N, K, M, firsts):
+    for act in ("silu", "none"):
+        r = Run(B, N, K, M, io, act, x_first=firsts[0], y_first=firsts[1], seed=12)
+        room = torch.full((r.ws.numel() + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+        r.ws = room[:-65536]
+        r.fwd().bwd().check()
+        assert (room[-65536:] == 0x5A).all()
