@@ -1,5 +1,7 @@
 // Activations and their slopes, in fp32: group norm (gnorm.hpp), the short convolution (short.hip), the dense product (linear.hip).
 #pragma once
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace lc {
@@ -49,6 +51,51 @@ __device__ __forceinline__ float slope_of(float z)
     }
     if constexpr (ACT == LONGCONV_ACT_RELU) return z > 0.f ? 1.f : 0.f;
     return 1.f;
+}
+
+// by a value that is the same for all of a launch
+__device__ __forceinline__ float act_by(int act, float z)
+{
+    switch (act) {
+        case LONGCONV_ACT_SILU: return act_of<LONGCONV_ACT_SILU>(z);
+        case LONGCONV_ACT_GELU: return act_of<LONGCONV_ACT_GELU>(z);
+        case LONGCONV_ACT_RELU: return act_of<LONGCONV_ACT_RELU>(z);
+        default: return z;
+    }
+}
+__device__ __forceinline__ float slope_by(int act, float z)
+{
+    switch (act) {
+        case LONGCONV_ACT_SILU: return slope_of<LONGCONV_ACT_SILU>(z);
+        case LONGCONV_ACT_GELU: return slope_of<LONGCONV_ACT_GELU>(z);
+        case LONGCONV_ACT_RELU: return slope_of<LONGCONV_ACT_RELU>(z);
+        default: return 1.f;
+    }
+}
+
+// of N at a time, one decision for all
+template <int N>
+__device__ __forceinline__ void acts_by(int act, float (&z)[N])
+{
+    const auto each = [&](auto which) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = act_of<decltype(which)::value>(z[i]);
+    };
+    if (act == LONGCONV_ACT_SILU) each(std::integral_constant<int, LONGCONV_ACT_SILU>());
+    else if (act == LONGCONV_ACT_GELU) each(std::integral_constant<int, LONGCONV_ACT_GELU>());
+    else if (act == LONGCONV_ACT_RELU) each(std::integral_constant<int, LONGCONV_ACT_RELU>());
+}
+template <int N>
+__device__ __forceinline__ void slopes_by(int act, float (&z)[N])
+{
+    const auto each = [&](auto which) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = slope_of<decltype(which)::value>(z[i]);
+    };
+    if (act == LONGCONV_ACT_SILU) each(std::integral_constant<int, LONGCONV_ACT_SILU>());
+    else if (act == LONGCONV_ACT_GELU) each(std::integral_constant<int, LONGCONV_ACT_GELU>());
+    else if (act == LONGCONV_ACT_RELU) each(std::integral_constant<int, LONGCONV_ACT_RELU>());
+    else each(std::integral_constant<int, LONGCONV_ACT_NONE>());
 }
 
 }  // namespace

@@ -38,48 +38,6 @@ struct Product {
 };
 enum { EPI_OUT, EPI_DZ, EPI_SUM };
 
-__device__ __forceinline__ float act_by(int act, float z)
-{
-    switch (act) {
-        case LONGCONV_ACT_SILU: return act_of<LONGCONV_ACT_SILU>(z);
-        case LONGCONV_ACT_GELU: return act_of<LONGCONV_ACT_GELU>(z);
-        case LONGCONV_ACT_RELU: return act_of<LONGCONV_ACT_RELU>(z);
-        default: return z;
-    }
-}
-__device__ __forceinline__ float slope_by(int act, float z)
-{
-    switch (act) {
-        case LONGCONV_ACT_SILU: return slope_of<LONGCONV_ACT_SILU>(z);
-        case LONGCONV_ACT_GELU: return slope_of<LONGCONV_ACT_GELU>(z);
-        case LONGCONV_ACT_RELU: return slope_of<LONGCONV_ACT_RELU>(z);
-        default: return 1.f;
-    }
-}
-
-// of eight at a time, one decision for all
-__device__ __forceinline__ void acts_by(int act, float (&z)[VE])
-{
-    const auto each = [&](auto which) {
-#pragma unroll
-        for (int i = 0; i < VE; ++i) z[i] = act_of<decltype(which)::value>(z[i]);
-    };
-    if (act == LONGCONV_ACT_SILU) each(std::integral_constant<int, LONGCONV_ACT_SILU>());
-    else if (act == LONGCONV_ACT_GELU) each(std::integral_constant<int, LONGCONV_ACT_GELU>());
-    else if (act == LONGCONV_ACT_RELU) each(std::integral_constant<int, LONGCONV_ACT_RELU>());
-}
-__device__ __forceinline__ void slopes_by(int act, float (&z)[VE])
-{
-    const auto each = [&](auto which) {
-#pragma unroll
-        for (int i = 0; i < VE; ++i) z[i] = slope_of<decltype(which)::value>(z[i]);
-    };
-    if (act == LONGCONV_ACT_SILU) each(std::integral_constant<int, LONGCONV_ACT_SILU>());
-    else if (act == LONGCONV_ACT_GELU) each(std::integral_constant<int, LONGCONV_ACT_GELU>());
-    else if (act == LONGCONV_ACT_RELU) each(std::integral_constant<int, LONGCONV_ACT_RELU>());
-    else each(std::integral_constant<int, LONGCONV_ACT_NONE>());
-}
-
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ mu::f4 mfma(IoF16, const uint4& a, const uint4& b, const mu::f4& c)
 {

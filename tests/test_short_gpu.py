@@ -202,3 +202,24 @@ def test_under_graph_capture_on_a_side_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (r.y, r.last, r.dx, r.dk, r.dbias, r.dstate)))
+
+
+# rows that go by whole waves in the backward pass: around 64 pieces of eight, units of 128, and several units.  Few rows: a thread adds up one unit,
+# sixteen terms
+@pytest.mark.parametrize("N", [504, 505, 512, 513, 900, 1023, 1024, 1025, 1031, 1536, 2048, 2051, 4000])
+@pytest.mark.parametrize("taps,io,act", [(4, "bf16", "silu"), (8, "fp32", "gelu"), (2, "fp16", "none")])
+def test_long_rows(N, taps, io, act):
+    Run(3, 2, N, taps, io, act, carry=True, seed=6).run().check()
+
+
+@pytest.mark.parametrize("taps", [1, 4, 8])
+@pytest.mark.parametrize("carry", [False, True])
+def test_uneven_lengths_of_long_rows(taps, carry):
+    N, lengths = 2060, [0, 1, 3, 511, 512, 513, 1023, 1024, 1025, 1027, 1031, 1032, 2047, 2048, 2052, 2060]
+    r = Run(len(lengths), 2, N, taps, "fp32", "silu", carry=carry, lengths=lengths, seed=7)
+    for b, n in enumerate(lengths):
+        r.x[b, :, n:] = float("nan")
+        r.dy[b, :, n:] = float("inf")
+    r.run().check()
+    for b, n in enumerate(lengths):
+        assert not r.y[b, :, n:].any() and not r.dx[b, :, n:].any()
