@@ -323,53 +323,64 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
     }
 }
 
-// dB and dC from the blocks' sums
+// What the workgroups left, added up.  Workgroups 0 .. joins - 1: dB and dC from the sums of blocks of heads, 64 pieces of four places, each by four
+// threads that take every fourth block.  The others: dA, dD, dbias from the sums of sequences and segments.  (One launch: each of the two spends
+// most of its time on the way to what other dies wrote.)
 template <class IO>
-__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Parts parts, typename IO::T* __restrict__ dB, typename IO::T* __restrict__ dC, int blocks)
+__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, ScanGrads d, Parts parts, int blocks, int64_t joins, int64_t shares)
 {
-    const int64_t P = (a.N + VE - 1) / VE, rows = a.B * a.G * a.S;
-    int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= 2 * rows * P) return;
-    const bool second = id >= rows * P;
-    if (second) id -= rows * P;
-    typename IO::T* const to = second ? dC : dB;
-    if (!to) return;
-    const int64_t row = id / P, t = (id - row * P) * VE, len = scan_length(a, row / (a.G * a.S));
-    const float* from = (second ? parts.dC : parts.dB) + row * a.N + t;
-    float v[VE];
+    using T = typename IO::T;
+    if ((int64_t)blockIdx.x < joins) {
+        __shared__ float4 lds[3][64];
+        const int64_t P = (a.N + 3) / 4, rows = a.B * a.G * a.S;
+        const int lane = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+        int64_t id = (int64_t)blockIdx.x * 64 + lane;
+        const bool is = id < 2 * rows * P, second = id >= rows * P;
+        if (second) id -= rows * P;
+        if (!is) id = 0;
+        const int64_t row = id / P, t = (id - row * P) * 4, len = scan_length(a, row / (a.G * a.S));
+        const float* from = (second ? parts.dC : parts.dB) + row * a.N + t;
+        const int n = a.N - t < 4 ? (int)(a.N - t) : 4;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (t < len && n == 4) {
+#pragma unroll 8
+            for (int q = quarter; q < blocks; q += 4) {
+                const At4 w = *reinterpret_cast<const At4*>(from + (size_t)q * rows * a.N);
 #pragma unroll
-    for (int i = 0; i < VE; ++i) v[i] = 0.f;
-    const int n = a.N - t < VE ? (int)(a.N - t) : VE;
-    if (t < len)
-        for (int q = 0; q < blocks; ++q) {
-            float w[VE];
-            load8<IoF32>(from + (size_t)q * rows * a.N, n, w);
+                for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(w[i]);
+            }
+        } else if (t < len)
+            for (int q = quarter; q < blocks; q += 4)
 #pragma unroll
-            for (int i = 0; i < VE; ++i) v[i] += w[i];
+                for (int i = 0; i < 4; ++i)
+                    if (i < n) v[i] += from[(size_t)q * rows * a.N + i];
+        if (quarter) lds[quarter - 1][lane] = make_float4(v[0], v[1], v[2], v[3]);
+        __syncthreads();
+        T* const to = (T*)(second ? d.dC : d.dB);
+        if (quarter || !is || !to) return;
+#pragma unroll
+        for (int r = 0; r < 3; ++r) {
+            const float4 w = lds[r][lane];
+            v[0] += w.x;
+            v[1] += w.y;
+            v[2] += w.z;
+            v[3] += w.w;
         }
 #pragma unroll
-    for (int i = 0; i < VE; ++i) v[i] = t + i < len ? v[i] : 0.f;
-    store8<IO, true>(to + row * a.N + t, n, v);
-}
-
-// dA, dD, dbias from the sums of sequences and segments
-__global__ __launch_bounds__(256) void scan_sums_kernel(Parts parts, float* __restrict__ dA, float* __restrict__ dD, float* __restrict__ dbias, int64_t H,
-                                                        int S, int64_t shares)
-{
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id < H * S) {
-        if (!dA) return;
-        float s = 0.f;
-        for (int64_t q = 0; q < shares; ++q) s += parts.dA[q * H * S + id];
-        dA[id] = s;
-    } else if (id < H * S + 2 * H) {
-        const int64_t i = id - H * S;
-        float* const to = i & 1 ? dbias : dD;
-        if (!to) return;
-        float s = 0.f;
-        for (int64_t q = 0; q < shares; ++q) s += parts.dDb[q * 2 * H + i];
-        to[i >> 1] = s;
+        for (int i = 0; i < 4; ++i)
+            if (i < n) put1<IO>(to + row * a.N + t, i, t + i < len ? v[i] : 0.f);
+        return;
     }
+    const int64_t id = ((int64_t)blockIdx.x - joins) * 256 + threadIdx.x, in_A = a.H * a.S;
+    if (id >= in_A + 2 * a.H) return;
+    const int64_t i = id - in_A, each = id < in_A ? in_A : 2 * a.H;
+    const float* const from = id < in_A ? parts.dA + id : parts.dDb + i;
+    float* const to = id < in_A ? d.dA : i & 1 ? d.dbias : d.dD;
+    if (!to) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int64_t q = 0; q < shares; ++q) s += from[q * each];
+    to[id < in_A ? id : i >> 1] = s;
 }
 
 // Heads of a workgroup: as many as leave 256 workgroups (with the segments a sequence may be cut into), 32 at most
@@ -426,17 +437,13 @@ hipError_t run(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
     else if (a.S <= 32) e = launch<IO, 4, 8>(a, d, g, parts, blocks, CB, st);
     else e = launch<IO, 8, 8>(a, d, g, parts, blocks, CB, st);
     if (e != hipSuccess) return e;
+    const int64_t joins = blocks > 1 && (d.dB || d.dC) ? (int64_t)(2 * rows * ((a.N + 3) / 4) + 63) / 64 : 0;
+    const int64_t others = d.dA || d.dD || d.dbias ? (a.H * (a.S + 2) + 255) / 256 : 0;
+    if (joins + others == 0) return hipSuccess;
     dim3 grid;
-    if (blocks > 1 && (d.dB || d.dC)) {
-        e = launch_grid((2 * rows * ((a.N + VE - 1) / VE) + 255) / 256, 256, &grid);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(scan_join_kernel<IO>, grid, dim3(256), 0, st, a, parts, (typename IO::T*)d.dB, (typename IO::T*)d.dC, blocks);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (!d.dA && !d.dD && !d.dbias) return hipSuccess;
-    hipLaunchKernelGGL(scan_sums_kernel, dim3((unsigned)((a.H * (a.S + 2) + 255) / 256)), dim3(256), 0, st, parts, d.dA, d.dD, d.dbias, a.H, a.S,
-                       (int64_t)a.B * g.segs);
+    e = launch_grid((uint64_t)(joins + others), 256, &grid);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(scan_join_kernel<IO>, grid, dim3(256), 0, st, a, d, parts, blocks, joins, (int64_t)a.B * g.segs);
     return hipGetLastError();
 }
 
