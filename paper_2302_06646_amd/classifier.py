@@ -9,6 +9,8 @@ and computes the head and its loss):
     z    = silu(group norm(x1 transposed))                  longconv_gnorm_fwd, [B, N, H]
     logits = mean over the sequence's places of z, times the head
 
+With `--mixer scan` the block of selective.py stands in the convolution's place: x1 = x0 + dropout(selective(x0)), up to each sequence's end.
+
 No mask is stored: the backward pass draws each of them again from (seed, number of the call).  Sequences are of uneven lengths; their
 padding is token -1, which embeds to zeros and has no gradient.
 
@@ -22,6 +24,7 @@ import math
 import torch
 
 import paper_2302_06646_amd as lc
+from paper_2302_06646_amd.selective import Selective
 
 VOCABULARY = 256
 
@@ -29,7 +32,8 @@ VOCABULARY = 256
 class Classifier:
     """Parameters (fp32, float32 gradients in `.grad`), workspaces and activations for batches of B sequences of N tokens."""
 
-    def __init__(self, B, N, H=64, classes=4, groups=8, dtype=torch.bfloat16, drop=0.1, kernel_drop=0.2, tied_drop=0.1, seed=0):
+    def __init__(self, B, N, H=64, classes=4, groups=8, dtype=torch.bfloat16, drop=0.1, kernel_drop=0.2, tied_drop=0.1, seed=0,
+                 mixer="conv"):
         g = torch.Generator(device="cuda").manual_seed(seed)
         randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
         self.B, self.N, self.H, self.groups, self.seed = B, N, H, groups, seed
@@ -39,15 +43,24 @@ class Classifier:
         self.p = {"E": randn(VOCABULARY, H) / math.sqrt(H), "K": randn(H, N) / math.sqrt(N) * decay, "D": randn(H),
                   "gamma": torch.ones(H, device="cuda"), "beta": torch.zeros(H, device="cuda"),
                   "head": (randn(H, classes) / math.sqrt(H))}
+        self.block = None
+        if mixer == "scan":
+            del self.p["K"], self.p["D"]
+            self.block = Selective(B, N, H, dtype=dtype, generator=g)
+        elif mixer != "conv":
+            raise ValueError(f"mixer: expected conv or scan, got {mixer}")
         for t in self.p.values():
             t.grad = torch.zeros_like(t)
+        if self.block:
+            self.p.update(self.block.p)
         io = lc.dtype_code(torch.empty(0, dtype=dtype))
         new = lambda *s, dt=dtype: torch.empty(*s, dtype=dt, device="cuda")  # noqa: E731
         self.x0, self.y, self.x1, self.dx1, self.dy, self.dx0 = (new(B, H, N) for _ in range(6))
         self.z, self.dt = new(B, N, H), new(B, N, H)
-        self.kbar, self.dkbar = torch.empty_like(self.p["K"]), torch.empty_like(self.p["K"])
+        if mixer == "conv":
+            self.kbar, self.dkbar = torch.empty_like(self.p["K"]), torch.empty_like(self.p["K"])
+            self.ws = lc.new_workspace(B, H, N, io, True)
         self.mean, self.rstd = (new(B, groups, dt=torch.float32) for _ in range(2))
-        self.ws = lc.new_workspace(B, H, N, io, True)
         self.ws_embed = lc.new_workspace_embed(B, N, VOCABULARY, H, io, lc.CHANNELS_FIRST)
         self.ws_gnorm = lc.new_workspace_gnorm(B, N, H, groups, io, True)
         lc.longconv_init()
@@ -56,8 +69,13 @@ class Classifier:
         """Logits [B, classes] of tokens [B, N]; `step` numbers the training steps, and with them the masks."""
         p, call = self.p, 3 * step
         lc.longconv_embed_fwd(tokens, p["E"], self.x0, self.scale, lc.CHANNELS_FIRST, self.drop, self.seed, call)
-        lc.longconv_kreg_fwd_seeded(p["K"], self.kbar, self.width, self.squash, self.kernel_drop, self.seed, call + 1)
-        lc.longconv_fwd(self.x0, self.kbar, p["D"], self.y, self.ws)
+        if self.block:
+            self.lengths = (tokens >= 0).sum(1)               # (a sequence's padding is behind its end)
+            self.block.refresh()
+            self.block.forward(self.x0, self.y, self.lengths)
+        else:
+            lc.longconv_kreg_fwd_seeded(p["K"], self.kbar, self.width, self.squash, self.kernel_drop, self.seed, call + 1)
+            lc.longconv_fwd(self.x0, self.kbar, p["D"], self.y, self.ws)
         lc.longconv_dropout_fwd(self.y, self.x1, self.tied_drop, self.seed, call + 2, residual=self.x0, tie=self.N)
         self.t = self.x1.transpose(1, 2).contiguous()
         lc.longconv_gnorm_fwd(self.t, p["gamma"], p["beta"], self.z, self.mean, self.rstd, self.eps, "silu", self.ws_gnorm)
@@ -74,8 +92,11 @@ class Classifier:
                               self.ws_gnorm)
         self.dx1.copy_(self.dt.transpose(1, 2))
         lc.longconv_dropout_bwd(self.dx1, self.dy, self.tied_drop, self.seed, call + 2, tie=self.N)
-        lc.longconv_bwd(self.dy, self.x0, self.kbar, p["D"], self.dx0, self.dkbar, p["D"].grad, self.ws)
-        lc.longconv_kreg_bwd_seeded(p["K"], self.dkbar, p["K"].grad, self.width, self.squash, self.kernel_drop, self.seed, call + 1)
+        if self.block:
+            self.block.backward(self.dy, self.x0, self.dx0, self.lengths)
+        else:
+            lc.longconv_bwd(self.dy, self.x0, self.kbar, p["D"], self.dx0, self.dkbar, p["D"].grad, self.ws)
+            lc.longconv_kreg_bwd_seeded(p["K"], self.dkbar, p["K"].grad, self.width, self.squash, self.kernel_drop, self.seed, call + 1)
         self.dx0.add_(self.dx1)                               # the residual's gradient
         lc.longconv_embed_bwd(self.dx0, tokens, p["E"].grad, self.scale, lc.CHANNELS_FIRST, self.ws_embed, self.drop, self.seed, call)
 
@@ -105,8 +126,9 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=16)
     ap.add_argument("--length", type=int, default=2048, help="a power of two, 256 to 131072")
     ap.add_argument("--width", type=int, default=64)
+    ap.add_argument("--mixer", choices=("conv", "scan"), default="conv")
     a = ap.parse_args(argv)
-    model = Classifier(a.batch, a.length, a.width)
+    model = Classifier(a.batch, a.length, a.width, mixer=a.mixer)
     optimizer = torch.optim.Adam(list(model.p.values()), lr=3e-3)
     generator = torch.Generator(device="cuda").manual_seed(1)
     for i in range(a.steps):

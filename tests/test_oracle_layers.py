@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 import oracle
-from oracle import linear, scan, short
+from oracle import linear, scan, selective, short
 
 
 def _differences(f, args, grads, names, eps=1e-6):
@@ -111,3 +111,20 @@ def test_linear_by_hand():
     y = linear.linear_fwd(np.array([[[1.0, 2.0]]]), np.array([[1.0, 1.0], [-1.0, -1.0], [0.0, 2.0]]), np.array([0.5, 0.0, 0.0]), "relu",
                           residual=np.full((1, 1, 3), 10.0))
     assert (y == [[[13.5, 10.0, 14.0]]]).all()
+
+
+def test_the_selective_blocks_gradients_against_differences():
+    rng = np.random.default_rng(11)
+    B, N, H, E, R, S, G, taps = 2, 9, 3, 4, 2, 3, 2, 3
+    shapes = dict(W_u=(E, H), W_z=(E, H), W_r=(R, E), W_d=(E, R), W_B=(G * S, E), W_C=(G * S, E), W_y=(H, E), taps=(E, taps), taps_bias=(E,),
+                  rate=(E, S), D=(E,), dt_bias=(E,))
+    p = {k: rng.standard_normal(s) * 0.7 for k, s in shapes.items()}
+    x, dy, lengths = rng.standard_normal((B, H, N)), rng.standard_normal((B, H, N)), np.array([N, 6])
+    dx, grads = selective.backward(dy, p, selective.forward(x, p, S, G, lengths)[1], lengths)
+    value = lambda x, p: (dy * selective.forward(x, p, S, G, lengths)[0]).sum()  # noqa: E731
+    eps = 1e-5      # differences: eps^2 of third derivatives and 2^-53 / eps of values of some tens
+    for name in (*shapes, None):
+        d = rng.standard_normal(x.shape if name is None else shapes[name])
+        side = lambda s: value(x + s * d, p) if name is None else value(x, {**p, name: p[name] + s * d})  # noqa: E731
+        want = (d * (dx if name is None else grads[name])).sum()
+        assert abs((side(eps) - side(-eps)) / (2 * eps) - want) < 1e-6 * max(1.0, abs(want)), name
