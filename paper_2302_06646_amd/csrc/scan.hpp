@@ -147,8 +147,10 @@ __device__ __forceinline__ float sums_of_wave(float v0, float v1, float v2, floa
     float c = (high ? b : a) + dpp<0x4E>(high ? a : b, 0.f);
     c += dpp<0x124>(c, 0.f);
     c += dpp<0x128>(c, 0.f);
-    c += __shfl_xor(c, 16);
-    return c + __shfl_xor(c, 32);
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(c), __float_as_uint(c), false, false);      // of the other row of a pair
+    c = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(c), __float_as_uint(c), false, false);
+    return __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
 }
 
 // x, with `v` in one lane

@@ -85,20 +85,24 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
             for (int i = 0; i < K; ++i) dBv[n][i] = dCv[n][i] = 0.f;
         }
         // of this thread's places and of the wave's states (lane n for state wave NS + n), of head c, asked for during the one before
-        float nd[TPT], nu[TPT], ny[TPT], nz[TPT], nA = 0.f, nm = 0.f;
+        // (as they lie in memory: to convert them is to wait for them)
+        T nd[TPT], nu[TPT], ny[TPT], nz[TPT];
+        float nA = 0.f, nm = 0.f, nD = 0.f, nbias = 0.f;
         const auto ask = [&](int c) {
             const size_t row = (size_t)b * a.H + head0 + c, at0 = row * N + t0;
 #pragma unroll
             for (int i = 0; i < TPT; ++i) {
                 const uint32_t t = (uint32_t)(tid * TPT + i);
-                nd[i] = nu[i] = ny[i] = nz[i] = 0.f;
+                nd[i] = nu[i] = ny[i] = nz[i] = T();
                 if (lim == SPAN || (int)t < lim) {
-                    nd[i] = IO::ld((const T*)a.delta + at0, t);
-                    nu[i] = IO::ld((const T*)a.u + at0, t);
-                    ny[i] = IO::ld((const T*)d.dy + at0, t);
-                    if (GATED) nz[i] = IO::ld((const T*)a.z + at0, t);
+                    nd[i] = ((const T*)a.delta + at0)[t];
+                    nu[i] = ((const T*)a.u + at0)[t];
+                    ny[i] = ((const T*)d.dy + at0)[t];
+                    if (GATED) nz[i] = ((const T*)a.z + at0)[t];
                 }
             }
+            if (a.D) nD = a.D[head0 + c];
+            if (a.bias) nbias = a.bias[head0 + c];
             const int s = wave * NS + lane;
             if (lane < NS && s < S) {
                 nA = a.A[(head0 + c) * S + s];
@@ -113,20 +117,19 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
             Own o;
             o.A = nA;
             o.mark = nm;
-            o.D = a.D ? a.D[head0 + c] : 0.f;
-            const float bias = a.bias ? a.bias[head0 + c] : 0.f;
+            o.D = nD;
             float* const stage = stages + (c & 1) * 3 * SPAN;
 #pragma unroll
             for (int i = 0; i < TPT; ++i) {
                 const bool is = tid * TPT + i < lim;
-                const float x = nd[i] + bias, z = nz[i], q = GATED ? logistic(z) : 1.f;
+                const float x = IO::ld(nd, i) + nbias, u = IO::ld(nu, i), dy = IO::ld(ny, i), z = IO::ld(nz, i), q = GATED ? logistic(z) : 1.f;
                 float rate;
                 const float sp = softplus_of(x, &rate), y = a.softplus ? sp : x;
                 o.dt[i] = is ? y : 0.f;
                 o.rate[i] = a.softplus ? rate : 1.f;
-                o.u[i] = nu[i];
-                o.dyg[i] = GATED ? ny[i] * (z * q) : ny[i];
-                o.dyz[i] = ny[i] * (q * (1.f + z * (1.f - q)));
+                o.u[i] = u;
+                o.dyg[i] = GATED ? dy * (z * q) : dy;
+                o.dyz[i] = dy * (q * (1.f + z * (1.f - q)));
                 const int to = place(tid * TPT + i);
                 stage[to] = o.dt[i];
                 stage[SPAN + to] = o.dt[i] * o.u[i];
@@ -139,13 +142,9 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
         Own own = lay(0);
         if (heads > 1) ask(1);
         __syncthreads();
-        for (int c = 0; c < heads; ++c) {
-            const size_t at0 = ((size_t)b * a.H + head0 + c) * N + t0;
-            const int here = (int)(stop - t0 < SPAN ? stop - t0 : SPAN);
-            const float *const stage = stages + (c & 1) * 3 * SPAN, Al = own.A, ml = own.mark;
-            float* const part = sums + (c & 1) * NW * 3 * SPAN;
-            float cl = lane < NS ? gcar[c * SP + wave * NS + lane] : 0.f;
-            float e[K], x[K], f[K], gB[K], Aq[K], Ch[K], sum = 0.f;      // dt, dt u, dy' of the lane's places
+        float e[K], x[K], f[K], cl;      // dt, dt u, dy' of the lane's places; lane n: what the chunk behind hands on to state wave NS + n
+        const auto take = [&](int c) {
+            const float* const stage = stages + (c & 1) * 3 * SPAN;
 #pragma unroll
             for (int j = 0; j < K / 4; ++j) {
                 const float4 q = reinterpret_cast<const float4*>(stage)[j * 64 + lane];
@@ -155,6 +154,15 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
                 x[4 * j] = r.x; x[4 * j + 1] = r.y; x[4 * j + 2] = r.z; x[4 * j + 3] = r.w;
                 f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
             }
+            cl = lane < NS ? gcar[c * SP + wave * NS + lane] : 0.f;
+        };
+        take(0);
+        for (int c = 0; c < heads; ++c) {
+            const size_t at0 = ((size_t)b * a.H + head0 + c) * N + t0;
+            const int here = (int)(stop - t0 < SPAN ? stop - t0 : SPAN);
+            const float Al = own.A, ml = own.mark;
+            float* const part = sums + (c & 1) * NW * 3 * SPAN;
+            float gB[K], Aq[K], Ch[K], sum = 0.f;
 #pragma unroll
             for (int i = 0; i < K; ++i) sum += e[i];
             float dA[NS < 2 ? 2 : NS];
@@ -237,6 +245,7 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
                 if (c + 2 < heads) ask(c + 2);
             }
             __syncthreads();
+            if (c + 1 < heads) take(c + 1);      // (on its way while this head's end is made)
             float sD = 0.f, sb = 0.f;
 #pragma unroll
             for (int i = 0; i < TPT; ++i) {
