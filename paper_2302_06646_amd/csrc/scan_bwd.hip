@@ -16,6 +16,12 @@ constexpr int K = SPAN / 64;      // places of a lane
 // where place t of a chunk lies in LDS: a wave's reads of four places a lane are one run of memory
 __device__ __forceinline__ int place(int t) { return (t % K / 4 * 64 + t / K) * 4 + t % 4; }
 
+// to LDS, without waiting for what is there (one lane adds to a place, so the order is its program's)
+__device__ __forceinline__ void add(float* to, float v) { __hip_atomic_fetch_add(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+
+// v is made by here: the compiler otherwise puts off what is only needed later, and keeps what it is made of for as long
+__device__ __forceinline__ void made(float& v) { asm volatile("" : "+v"(v)); }
+
 struct Parts {
     float *dB, *dC;      // [blocks][B,G,S,N], or null: dB and dC are written themselves
     float *dA;           // [B segs][H,S]
@@ -84,30 +90,28 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
 #pragma unroll
             for (int i = 0; i < K; ++i) dBv[n][i] = dCv[n][i] = 0.f;
         }
-        // of this thread's places and of the wave's states (lane n for state wave NS + n), of head c, asked for during the one before
-        // (as they lie in memory: to convert them is to wait for them)
+        const auto one_of = [&](int c) { return c < heads ? c : heads - 1; };      // (the last head once more: nobody reads it)
+        // Of this thread's places and of the wave's states (lane n for state wave NS + n), of head c, asked for during the one before.  Nothing is
+        // asked for under a condition, and nothing converted: either would wait for it at once.  What is not there is asked for elsewhere and
+        // made zero in lay().
         T nd[TPT], nu[TPT], ny[TPT], nz[TPT];
-        float nA = 0.f, nm = 0.f, nD = 0.f, nbias = 0.f;
+        float nA, nm, nD, nbias;
+        const int s_mine = wave * NS + (lane < NS ? lane : 0), s_there = s_mine < S ? s_mine : 0;
+        const float *const Dr = a.D ? a.D : a.A, *const br = a.bias ? a.bias : a.A;
         const auto ask = [&](int c) {
             const size_t row = (size_t)b * a.H + head0 + c, at0 = row * N + t0;
 #pragma unroll
             for (int i = 0; i < TPT; ++i) {
-                const uint32_t t = (uint32_t)(tid * TPT + i);
-                nd[i] = nu[i] = ny[i] = nz[i] = T();
-                if (lim == SPAN || (int)t < lim) {
-                    nd[i] = ((const T*)a.delta + at0)[t];
-                    nu[i] = ((const T*)a.u + at0)[t];
-                    ny[i] = ((const T*)d.dy + at0)[t];
-                    if (GATED) nz[i] = ((const T*)a.z + at0)[t];
-                }
+                const uint32_t t = (uint32_t)(tid * TPT + i < lim ? tid * TPT + i : lim - 1);
+                nd[i] = ((const T*)a.delta + at0)[t];
+                nu[i] = ((const T*)a.u + at0)[t];
+                ny[i] = ((const T*)d.dy + at0)[t];
+                nz[i] = GATED ? ((const T*)a.z + at0)[t] : T();
             }
-            if (a.D) nD = a.D[head0 + c];
-            if (a.bias) nbias = a.bias[head0 + c];
-            const int s = wave * NS + lane;
-            if (lane < NS && s < S) {
-                nA = a.A[(head0 + c) * S + s];
-                nm = d.marks[(row * n_marks + t0 / SPAN) * S + s];
-            }
+            nD = Dr[head0 + c];
+            nbias = br[head0 + c];
+            nA = a.A[(head0 + c) * S + s_there];
+            nm = d.marks[(row * n_marks + t0 / SPAN) * S + s_there];
         };
         // this thread's places: for all waves, and what it needs of them itself
         struct Own {
@@ -115,14 +119,17 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
         };
         const auto lay = [&](int c) {
             Own o;
-            o.A = nA;
-            o.mark = nm;
-            o.D = nD;
+            o.A = s_mine < S ? nA : 0.f;
+            o.mark = s_mine < S ? nm : 0.f;
+            made(o.A);
+            made(o.mark);
+            o.D = a.D ? nD : 0.f;
+            const float bias = a.bias ? nbias : 0.f;
             float* const stage = stages + (c & 1) * 3 * SPAN;
 #pragma unroll
             for (int i = 0; i < TPT; ++i) {
                 const bool is = tid * TPT + i < lim;
-                const float x = IO::ld(nd, i) + nbias, u = IO::ld(nu, i), dy = IO::ld(ny, i), z = IO::ld(nz, i), q = GATED ? logistic(z) : 1.f;
+                const float x = IO::ld(nd, i) + bias, u = is ? IO::ld(nu, i) : 0.f, dy = is ? IO::ld(ny, i) : 0.f, z = is ? IO::ld(nz, i) : 0.f, q = GATED ? logistic(z) : 1.f;
                 float rate;
                 const float sp = softplus_of(x, &rate), y = a.softplus ? sp : x;
                 o.dt[i] = is ? y : 0.f;
@@ -140,7 +147,7 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
         __syncthreads();      // (the chunk before is done with `stages`)
         ask(0);
         Own own = lay(0);
-        if (heads > 1) ask(1);
+        ask(one_of(1));
         __syncthreads();
         float e[K], x[K], f[K], cl;      // dt, dt u, dy' of the lane's places; lane n: what the chunk behind hands on to state wave NS + n
         const auto take = [&](int c) {
@@ -154,7 +161,7 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
                 x[4 * j] = r.x; x[4 * j + 1] = r.y; x[4 * j + 2] = r.z; x[4 * j + 3] = r.w;
                 f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
             }
-            cl = lane < NS ? gcar[c * SP + wave * NS + lane] : 0.f;
+            cl = gcar[one_of(c) * SP + wave * NS + (lane < NS ? lane : 0)];
         };
         take(0);
         for (int c = 0; c < heads; ++c) {
@@ -232,6 +239,13 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
                 }
             }
             if (lane < NS) gcar[c * SP + wave * NS + lane] = cl;
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    made(dBv[n][i]);
+                    made(dCv[n][i]);
+                }
             float4* const to = reinterpret_cast<float4*>(part + wave * 3 * SPAN);
 #pragma unroll
             for (int j = 0; j < K / 4; ++j) {
@@ -239,13 +253,10 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
                 to[SPAN / 4 + j * 64 + lane] = make_float4(Aq[4 * j], Aq[4 * j + 1], Aq[4 * j + 2], Aq[4 * j + 3]);
                 if (GATED) to[SPAN / 2 + j * 64 + lane] = make_float4(Ch[4 * j], Ch[4 * j + 1], Ch[4 * j + 2], Ch[4 * j + 3]);
             }
-            Own next = own;
-            if (c + 1 < heads) {
-                next = lay(c + 1);
-                if (c + 2 < heads) ask(c + 2);
-            }
+            const Own next = lay(c + 1);
+            ask(one_of(c + 2));
             __syncthreads();
-            if (c + 1 < heads) take(c + 1);      // (on its way while this head's end is made)
+            take(c + 1);      // (on its way while this head's end is made)
             float sD = 0.f, sb = 0.f;
 #pragma unroll
             for (int i = 0; i < TPT; ++i) {
@@ -272,13 +283,13 @@ __global__ __launch_bounds__(64 * NW, NS <= 2 ? 2 : 2) void scan_bwd_kernel(Scan
             }
             // lanes 0, 1: dA of the first two states; 2, 3: the shares of dD and dbias
             const float t = sums_of_wave(dA[0], dA[1], sD, sb);
-            if (lane < 2 && lane < NS) dAsum[c * SP + wave * NS + lane] += t;
-            if (lane == 2 || lane == 3) small[(wave * CB + c) * 2 + lane - 2] += t;
+            if (lane < 2 && lane < NS) add(&dAsum[c * SP + wave * NS + lane], t);
+            if (lane == 2 || lane == 3) add(&small[(wave * CB + c) * 2 + lane - 2], t);
             if constexpr (NS > 2) {
 #pragma unroll
                 for (int n = 2; n < NS; n += 2) {
                     const float r = sums_of_wave(dA[n], dA[n + 1], 0.f, 0.f);
-                    if (lane < 2) dAsum[c * SP + wave * NS + n + lane] += r;
+                    if (lane < 2) add(&dAsum[c * SP + wave * NS + n + lane], r);
                 }
             }
             own = next;
