@@ -369,16 +369,16 @@ struct Fast {
     }
 };
 
-// Workgroup: a tile of BF by BS, WF by WS waves.  The result goes through LDS, each wave's part by itself, so that memory sees rows of f.
-template <class IO, bool FK, bool SK, int EPI, int BF, int BS, int WF, int WS>
-__global__ __launch_bounds__(64 * WF * WS, 2) void fast_product_kernel(Product a, uint32_t tiles_f, uint32_t tiles_s)
+// Workgroup: a tile of BF by BS, WF by WS waves, NB tiles of each operand in LDS at once.  The result goes through LDS, each wave's part by itself, so that memory sees rows of f.
+template <class IO, bool FK, bool SK, int EPI, int BF, int BS, int WF, int WS, int NB>
+__global__ __launch_bounds__(64 * WF * WS, NB == 1 ? 4 : 2) void fast_product_kernel(Product a, uint32_t tiles_f, uint32_t tiles_s)
 {
     using T = typename IO::T;
     constexpr int NW = WF * WS, NF = BF / WF / 16, NS = BS / WS / 16;      // tiles of 16 of a wave
     using SideF = Fast<FK, BF, NW>;
     using SideS = Fast<SK, BS, NW>;
     constexpr int STAGE = SideF::BYTES + SideS::BYTES;
-    __shared__ __align__(1024) char lds[2 * STAGE];
+    __shared__ __align__(1024) char lds[NB * STAGE];
     uint32_t w = blockIdx.x;
     {   // workgroups go round the eight dies: each die gets a run of neighbouring tiles, which share operands in its cache
         const uint32_t n = gridDim.x, each = n / 8, rest = n % 8, die = w % 8, at = w / 8;
@@ -418,13 +418,17 @@ __global__ __launch_bounds__(64 * WF * WS, 2) void fast_product_kernel(Product a
     const bool sums = EPI == EPI_SUM && a.sums && f0 == 0 && wf == 0;
     const uint32_t one = mu::IsBf<IO>::v ? 0x3f803f80u : 0x3c003c00u;
     const uint4 all_ones = make_uint4(one, one, one, one);
-    if (first < end) ask(0);
+    if (NB == 2 && first < end) ask(0);
     int buf = 0;
-    for (int64_t at = first; at < end; ++at, buf ^= 1) {
+    for (int64_t at = first; at < end; ++at, buf ^= NB - 1) {
+        if (NB == 1) {
+            __syncthreads();      // (the step before is read)
+            ask(0);
+        }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // this step's tiles are here, the last one's are read
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (at + 1 < end) ask(buf ^ 1);
+        if (NB == 2 && at + 1 < end) ask(buf ^ 1);
         const char *const lf = lds + buf * STAGE, *const ls = lf + SideF::BYTES;
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -455,7 +459,8 @@ __global__ __launch_bounds__(64 * WF * WS, 2) void fast_product_kernel(Product a
         }
     }
     // 64 values of f by SP of s at a time in this wave's share of LDS, fp32, the sixteen pieces of a row exchanged by s
-    constexpr int MINE = 2 * STAGE / NW, FP = NF * 16 < 64 ? NF * 16 : 64, SP = MINE / (FP * 4) < NS * 16 ? MINE / (FP * 4) : NS * 16;
+    constexpr int MINE = NB * STAGE / NW, FP = NF * 16 < 64 ? NF * 16 : 64, FIT = MINE / (FP * 4) < NS * 16 ? MINE / (FP * 4) : NS * 16;
+    constexpr int SP = NB == 1 && EPI == EPI_DZ ? 16 : FIT;      // (fewer registers)
     constexpr int LANES = FP / 8, ROWS = 64 / LANES;      // lanes of a row of f, rows of a wave instruction
     static_assert(FP % 64 == 0 && SP % 16 == 0 && SP % ROWS == 0, "whole tiles");
     float* const mine = reinterpret_cast<float*>(lds + wave * MINE);
@@ -691,7 +696,7 @@ hipError_t launch_few(const Product& p, hipStream_t st)
 // Whether an operand's rows are whole pieces of 16 bytes, wherever a tile begins, and a tile's 256 rows lie within 2 GB (BEYOND is beyond)
 inline bool whole_pieces(const Side& d, bool kf, int64_t K) { return d.ld % 8 == 0 && (kf ? K : d.n) % 8 == 0 && d.batch % 8 == 0 && d.seg % 8 == 0 && d.ld < (1 << 22); }
 
-template <class IO, int EPI, bool FK, bool SK, int BF, int BS, int WF, int WS>
+template <class IO, int EPI, bool FK, bool SK, int BF, int BS, int WF, int WS, int NB>
 hipError_t launch_fast(const Product& p, int64_t* shares, hipStream_t st)
 {
     const uint32_t tf = (uint32_t)((p.F.n + BF - 1) / BF), ts = (uint32_t)((p.S.n + BS - 1) / BS);
@@ -699,17 +704,18 @@ hipError_t launch_fast(const Product& p, int64_t* shares, hipStream_t st)
     const hipError_t e = launch_grid((uint64_t)tf * ts * (uint64_t)p.splits * (uint64_t)p.batches, 64 * WF * WS, &g);
     if (e != hipSuccess) return e;
     if (shares) *shares = EPI == EPI_SUM ? p.splits : p.batches * (p.bias_f ? (int64_t)ts * WS : (int64_t)tf * (BF / 64));
-    hipLaunchKernelGGL((fast_product_kernel<IO, FK, SK, EPI, BF, BS, WF, WS>), g, dim3(64 * WF * WS), 0, st, p, tf, ts);
+    hipLaunchKernelGGL((fast_product_kernel<IO, FK, SK, EPI, BF, BS, WF, WS, NB>), g, dim3(64 * WF * WS), 0, st, p, tf, ts);
     return hipGetLastError();
 }
-// Tiles of 256 by 256 (one workgroup a compute unit, half the operand traffic) where they are full to three quarters and more, and so is
-// the last round of 256 units, else of 128 by 128 (two workgroups a unit, one's epilogue beside the other's products).  us, 256 and 128: forward 16384 x 768 ->
-// 2048 bf16 66 and 72; its dx, 192 tiles of 256, 74 and 67; 16384 x 2048 -> 768 57 and 59; 8192^3 870 and 1010; 131072 x 256 -> 1024 with gelu
-// fp16 228 and 234.
-inline bool wide_tiles(int64_t f, int64_t s, int64_t batches)
+// Products over K with an epilogue.  Tiles of 256 by 256, two of each operand in LDS (one workgroup a compute unit, half the operand traffic), where
+// the sum is long, and where they are full to three quarters and more, and so is the last round of 256 units.  Else tiles of 128 by 128, one of
+// each operand (four workgroups a unit, whose loads, products and epilogues lie side by side).  us, 256 and 128, bf16: 16384 x K -> 2048: K = 768
+// 61 and 60, 1024 76 and 71 (in other layouts 78 to 81 and 78 to 85), 1536 101 and 108, 2048 121 and 129, 4096 217 and 241; 8192^3 957 and 1300;
+// 131072 x 256 -> 1024 with gelu, fp16, 220 and 187.  Two operands of 128 each in LDS, two workgroups a unit: K = 768 69, the last 234.
+inline bool wide_tiles(int64_t f, int64_t s, int64_t batches, int64_t K)
 {
     const int64_t tiles = ((f + 255) / 256) * ((s + 255) / 256) * batches, rounds = (tiles + 255) / 256;
-    return tiles > rounds * 192 && f * s * batches >= tiles * (256 * 192);
+    return K >= 1024 && tiles > rounds * 192 && f * s * batches >= tiles * (256 * 192);
 }
 
 template <class IO, int EPI, bool FK, bool SK>
@@ -718,8 +724,8 @@ hipError_t launch_sides(Product p, int64_t* shares, hipStream_t st)
     dim3 g;
     if constexpr (sizeof(typename IO::T) == 2) {
         if (whole_pieces(p.F, FK, p.K) && whole_pieces(p.S, SK, p.K)) {
-            if (p.wide) return launch_fast<IO, EPI, FK, SK, 256, 256, 2, 4>(p, shares, st);
-            return launch_fast<IO, EPI, FK, SK, 128, 128, 2, 2>(p, shares, st);
+            if (p.wide) return launch_fast<IO, EPI, FK, SK, 256, 256, 2, 4, 2>(p, shares, st);
+            return launch_fast<IO, EPI, FK, SK, 128, 128, 2, 2, EPI == EPI_SUM ? 2 : 1>(p, shares, st);
         }
     }
     // smaller tiles where the larger ones leave units without work
@@ -783,7 +789,7 @@ hipError_t forward(const LinearArgs& a, const void* x, Product p, int64_t* share
     p.F = c.y_first ? X : W;
     p.S = c.y_first ? W : X;
     if (EPI == EPI_OUT && !c.x_first && !c.y_first && c.places <= FEW) return launch_few<IO>(p, st);
-    p.wide = wide_tiles(p.F.n, p.S.n, p.batches);
+    p.wide = wide_tiles(p.F.n, p.S.n, p.batches, p.K);
     return launch_product<IO, EPI>(p, c.y_first ? !c.x_first : true, c.y_first ? true : !c.x_first, shares, st);
 }
 
@@ -924,7 +930,7 @@ hipError_t linear_bwd_io(const LinearArgs& a, const LinearGrads& d, void* ws, hi
     p.ld = c.x_first ? c.places : a.K;
     p.F = c.x_first ? Z : W;
     p.S = c.x_first ? W : Z;
-    p.wide = wide_tiles(p.F.n, p.S.n, p.batches);
+    p.wide = wide_tiles(p.F.n, p.S.n, p.batches, p.K);
     return launch_product<IO, EPI_OUT>(p, c.x_first ? !c.y_first : false, c.x_first ? false : !c.y_first, nullptr, st);
 }
 

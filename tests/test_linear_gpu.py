@@ -198,3 +198,10 @@ def test_writes_stay_within_the_workspace(io, B, N, K, M, firsts):
         r.ws = room[:-65536]
         r.fwd().bwd().check()
         assert (room[-65536:] == 0x5A).all()
+
+
+# long sums, whose tiles are the largest where they fill the card: with a remainder on each side, in each layout, and short sums beside
+@pytest.mark.parametrize("firsts", [(False, False), (True, True), (False, True), (True, False)])
+@pytest.mark.parametrize("K", [1016, 1032])
+def test_the_largest_tiles(K, firsts):
+    Run(1, 3400, K, 3544, "bf16", "silu", residual=True, x_first=firsts[0], y_first=firsts[1], dW="bf16", seed=13).fwd().bwd().check()
