@@ -33,7 +33,7 @@ struct Product {
     const void* residual;             // EPI_OUT
     const void* dy;                   // EPI_DZ: out = dy act'(z)
     float* sums;                      // EPI_DZ: [batches tiles 2][n of the bias], sums of dz over a tile's places
-    // EPI_SUM: [splits][n_s][n_f]
+    // EPI_SUM: [batches][splits][n_s][n_f]
     float* part;
 };
 enum { EPI_OUT, EPI_DZ, EPI_SUM };
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(LT, 2) void product_kernel(Product a, uint32_t tile
     // a lane has f = 4 (lane / 16) .. + 3 and s = lane % 16 of each tile of 16 by 16
     const int col = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
     if constexpr (EPI == EPI_SUM) {
-        float* const to = a.part + (size_t)split * a.S.n * a.F.n;
+        float* const to = a.part + (size_t)(batch * a.splits + split) * a.S.n * a.F.n;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const int64_t s = s0 + ws + 16 * j + col;
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(64 * WF * WS, NB == 1 ? 4 : 2) void fast_product_ke
 #pragma unroll
             for (int j = 0; j < NS; ++j) {
                 const int64_t s = s0 + ws + 16 * j + col;
-                if (s < a.S.n) a.sums[(size_t)split * a.S.n + s] = ones[j][0];
+                if (s < a.S.n) a.sums[(size_t)split * a.S.n + s] = ones[j][0];      // (dW: one batch)
             }
         }
     }
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(64 * WF * WS, NB == 1 ? 4 : 2) void fast_product_ke
                 float v[8] = {u.x, u.y, u.z, u.w, t.x, t.y, t.z, t.w};
                 const bool is = whole || (s < a.S.n && n > 0);
                 if constexpr (EPI == EPI_SUM) {
-                    if (is) store8<IoF32>(a.part + (size_t)split * a.S.n * a.F.n + s * a.F.n + f, n, v);
+                    if (is) store8<IoF32>(a.part + (size_t)(batch * a.splits + split) * a.S.n * a.F.n + s * a.F.n + f, n, v);
                 } else {
                     float o[8] = {}, by_s = 0.f;
                     if (from) other[it].get(o);
@@ -571,6 +571,78 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const float* __restric
         for (int i = 0; i < 4; ++i) v[i] += w[i];
     }
     store4<IO>(out + at, here, v);
+}
+
+// What EPI_OUT and EPI_DZ do, of the shares of a sum.  Workgroup: 256 values of f, four a lane, by FINISH rows of s, every fourth a wave's; EPI_DZ's sums
+// over its places.
+constexpr int FINISH = 16;
+template <class IO, int EPI>
+__global__ __launch_bounds__(256) void linear_finish_kernel(Product a, uint32_t blocks_f, uint32_t blocks_s)
+{
+    using T = typename IO::T;
+    __shared__ float4 lds[3][64];
+    uint32_t w = blockIdx.x;
+    const uint32_t bf = w % blocks_f;
+    w /= blocks_f;
+    const uint32_t bs = w % blocks_s;
+    const int64_t batch = w / blocks_s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t f = (int64_t)bf * 256 + 4 * lane, left = a.F.n - f, each = a.S.n * a.F.n;
+    const int n = left < 4 ? (int)left : 4;
+    float bias[4] = {0.f, 0.f, 0.f, 0.f}, by_f[4] = {0.f, 0.f, 0.f, 0.f};
+    if (a.bias && a.bias_f && n > 0) load4<IoF32>(a.bias + f, n, bias);
+#pragma unroll
+    for (int k = 0; k < FINISH / 4; ++k) {
+        const int64_t s = (int64_t)bs * FINISH + 4 * k + wave;
+        float by_s = 0.f;
+        if (s < a.S.n && n > 0) {
+            const float* const from = a.part + batch * a.splits * each + s * a.F.n + f;
+            const size_t at = (size_t)batch * a.batch + s * a.ld + f;
+            const float of_s = a.bias && !a.bias_f ? a.bias[s] : 0.f;
+            float v[4], r[4] = {0.f, 0.f, 0.f, 0.f};
+            if (EPI == EPI_DZ) load4<IO>((const T*)a.dy + at, n, r);
+            else if (a.residual) load4<IO>((const T*)a.residual + at, n, r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = bias[i] + of_s;
+#pragma unroll 4
+            for (int64_t q = 0; q < a.splits; ++q) {
+                float u[4];
+                load4<IoF32>(from + q * each, n, u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += u[i];
+            }
+            if (EPI == EPI_DZ) slopes_by(a.act, v);
+            else acts_by(a.act, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (EPI == EPI_DZ) {
+                    v[i] = i < n ? r[i] * v[i] : 0.f;
+                    by_f[i] += v[i];
+                    by_s += v[i];
+                } else v[i] += r[i];
+            }
+            store4<IO>((T*)a.out + at, n, v);
+        }
+        if (EPI == EPI_DZ && a.sums && !a.bias_f) {      // places are f
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) by_s += __shfl_xor(by_s, d);
+            if (lane == 0 && s < a.S.n) a.sums[(size_t)(batch * blocks_f + bf) * a.S.n + s] = by_s;
+        }
+    }
+    if (EPI == EPI_DZ && a.sums && a.bias_f) {      // places are s
+        if (wave) lds[wave - 1][lane] = make_float4(by_f[0], by_f[1], by_f[2], by_f[3]);
+        __syncthreads();
+        if (wave || n <= 0) return;
+#pragma unroll
+        for (int r = 0; r < 3; ++r) {
+            const float4 u = lds[r][lane];
+            by_f[0] += u.x;
+            by_f[1] += u.y;
+            by_f[2] += u.z;
+            by_f[3] += u.w;
+        }
+        store4<IoF32>(a.sums + (size_t)(batch * blocks_s + bs) * a.F.n + f, n, by_f);
+    }
 }
 
 constexpr int COLUMN_ROWS = 256;      // places that a workgroup adds up
@@ -773,17 +845,66 @@ inline Side rows_of(const void* p, bool first, const Cut& c, int64_t width)
     return Side{p, c.places, first ? c.places : width, c.places * width, 0};
 }
 
+// Shares of a long sum of few tiles: as many as make 256 workgroups of 128 by 128 (fp32: 512 of 64 by 64), of four steps at least.  us, cut and whole:
+// bf16, 128 x 4096 -> 4096 26 and 68, 512 x 2048 -> 2048 25 and 37, 300 x 2051 -> 777 21 and 25, 1024 x 1024 -> 1024 24 and 17.5 (not taken); fp32, 128
+// x 4096 -> 4096 60 and 126, 512 x 1024 -> 1024 26 and 35, 300 x 515 -> 777 17 and 20.
+template <class IO>
+struct Cuts {
+    static constexpr bool F4 = sizeof(typename IO::T) == 4;
+    static constexpr int64_t SIDE = F4 ? 64 : 128, BK = Tile<IO, true>::BK, WANT = F4 ? 512 : 256, LONG = F4 ? 512 : 2048;
+    static int64_t steps(int64_t K) { return (K + BK - 1) / BK; }
+    static int64_t of(int64_t f, int64_t s, int64_t batches, int64_t K, int64_t* per)
+    {
+        const int64_t tiles = ((f + SIDE - 1) / SIDE) * ((s + SIDE - 1) / SIDE) * batches;
+        if (K < LONG || tiles > 128) return 1;
+        const int64_t want = WANT / tiles, most = steps(K) / 4, n = want < most ? want : most;
+        if (n < 2) return 1;
+        *per = (steps(K) + n - 1) / n;
+        return (steps(K) + *per - 1) / *per;
+    }
+    // bytes for them of T places to M columns, and of any fewer places: WANT tiles are the most
+    static size_t bytes(int64_t T, int64_t K, int64_t M)
+    {
+        if (K < LONG) return 0;
+        const size_t all = (size_t)(steps(K) / 4) * T * M * sizeof(float), most = (size_t)WANT * SIDE * SIDE * sizeof(float);
+        return up256(all < most ? all : most);
+    }
+};
+// y, dz or dx by p, whose result's shares have room at `part`
+template <class IO, int EPI>
+hipError_t product(Product p, bool fk, bool sk, void* part, int64_t* shares, hipStream_t st)
+{
+    p.splits = Cuts<IO>::of(p.F.n, p.S.n, p.batches, p.K, &p.per);
+    if (p.splits == 1) {
+        p.per = INT64_MAX / 4;
+        p.wide = wide_tiles(p.F.n, p.S.n, p.batches, p.K);
+        return launch_product<IO, EPI>(p, fk, sk, shares, st);
+    }
+    p.wide = false;
+    p.part = (float*)part;
+    float* const sums = p.sums;
+    p.sums = nullptr;
+    int64_t none = 0;
+    hipError_t e = launch_product<IO, EPI_SUM>(p, fk, sk, &none, st);
+    p.sums = sums;
+    const uint32_t bf = (uint32_t)((p.F.n + 255) / 256), bs = (uint32_t)((p.S.n + FINISH - 1) / FINISH);
+    dim3 g;
+    if (e == hipSuccess) e = launch_grid((uint64_t)p.batches * bf * bs, 256, &g);
+    if (e != hipSuccess) return e;
+    if (shares) *shares = p.batches * (p.bias_f ? bs : bf);
+    hipLaunchKernelGGL((linear_finish_kernel<IO, EPI>), g, dim3(256), 0, st, p, bf, bs);
+    return hipGetLastError();
+}
+
 // z = x W^T + bias and what follows it
 template <class IO, int EPI>
-hipError_t forward(const LinearArgs& a, const void* x, Product p, int64_t* shares, hipStream_t st)
+hipError_t forward(const LinearArgs& a, const void* x, Product p, void* part, int64_t* shares, hipStream_t st)
 {
     const Cut c(a);
     const Side X = rows_of(x, c.x_first, c, a.K), W{a.W, a.M, a.K, 0, 0};
     p.K = a.K;
     p.segs = 1;
     p.batches = c.batches;
-    p.splits = 1;
-    p.per = INT64_MAX / 4;
     p.bias = a.bias;
     p.act = a.act;
     p.batch = c.places * a.M;
@@ -792,8 +913,7 @@ hipError_t forward(const LinearArgs& a, const void* x, Product p, int64_t* share
     p.F = c.y_first ? X : W;
     p.S = c.y_first ? W : X;
     if (EPI == EPI_OUT && !c.x_first && !c.y_first && c.places <= FEW) return launch_few<IO>(p, st);
-    p.wide = wide_tiles(p.F.n, p.S.n, p.batches, p.K);
-    return launch_product<IO, EPI>(p, c.y_first ? !c.x_first : true, c.y_first ? true : !c.x_first, shares, st);
+    return product<IO, EPI>(p, c.y_first ? !c.x_first : true, c.y_first ? true : !c.x_first, part, shares, st);
 }
 
 // Shares of the sum over places of dW, of four steps at least: as many as make 256 workgroups of 256 by 256 where there are 16 such tiles and
@@ -829,20 +949,26 @@ hipError_t linear_fwd_io(const LinearArgs& a, const void* x, const void* residua
     Product p = {};
     p.out = y;
     p.residual = residual;
-    return forward<IO, EPI_OUT>(a, x, p, nullptr, st);
+    return forward<IO, EPI_OUT>(a, x, p, ws, nullptr, st);
 }
 
 // the most shares that sums of dbias come in: two for each 64 places (a tile's halves), or as many as dW's sums; a tile of 256 makes four,
-// however few its places
-inline int64_t bias_shares(int64_t B, int64_t N) { return B * (2 * ((N + 63) / 64) + 2); }
+// however few its places; one for each FINISH places where a sum is cut, which are at most 128 tiles of 128
+inline int64_t bias_shares(int64_t B, int64_t N)
+{
+    const int64_t tiles = B * (2 * ((N + 63) / 64) + 2), cut = B * ((N + FINISH - 1) / FINISH), most = 128 * 128 / FINISH, few = cut < most ? cut : most;
+    return tiles > few ? tiles : few;
+}
+inline size_t most_of(size_t a, size_t b, size_t c) { return a > b ? (a > c ? a : c) : b > c ? b : c; }
 template <class IO>
 size_t linear_workspace_io(int64_t B, int64_t N, int64_t K, int64_t M, int backward)
 {
-    if (!backward) return 256;
+    const size_t cuts = Cuts<IO>::bytes(B * N, K, M), back = Cuts<IO>::bytes(B * N, M, K);
+    if (!backward) return cuts + 256;
     bool wide;
     const int64_t want = shares_wanted(K, M, sizeof(typename IO::T) == 4, &wide), steps = (B * ((N + 15) / 16) + 3) / 4;      // (never more shares than either)
     const int64_t shares = want < steps ? want : steps, bias = bias_shares(B, N);
-    return up256((size_t)B * N * M * sizeof(typename IO::T)) + up256((size_t)shares * K * M * sizeof(float)) +
+    return up256((size_t)B * N * M * sizeof(typename IO::T)) + most_of(up256((size_t)shares * K * M * sizeof(float)), cuts, back) +
            up256((size_t)(bias > shares ? bias : shares) * M * sizeof(float));
 }
 
@@ -856,8 +982,8 @@ hipError_t linear_bwd_io(const LinearArgs& a, const LinearGrads& d, void* ws, hi
     at += up256((size_t)a.B * a.N * a.M * sizeof(T));
     const bool by_batch = c.x_first || c.y_first;
     const Shares sh = shares_of<IO>(a.B, a.N, a.K, a.M, by_batch);
-    float* const part = (float*)at;
-    at += up256((size_t)sh.shares * a.K * a.M * sizeof(float));
+    float* const part = (float*)at;      // of dz, dW and dx in turn
+    at += most_of(up256((size_t)sh.shares * a.K * a.M * sizeof(float)), Cuts<IO>::bytes(a.B * a.N, a.K, a.M), Cuts<IO>::bytes(a.B * a.N, a.M, a.K));
     float* const sums = (float*)at;
     const void* dz = d.dy;
     hipError_t e = hipSuccess;
@@ -867,7 +993,7 @@ hipError_t linear_bwd_io(const LinearArgs& a, const LinearGrads& d, void* ws, hi
         p.out = dz_room;
         p.dy = d.dy;
         p.sums = d.dbias ? sums : nullptr;
-        e = forward<IO, EPI_DZ>(a, d.x, p, &shares, st);
+        e = forward<IO, EPI_DZ>(a, d.x, p, part, &shares, st);
         if (e != hipSuccess) return e;
         dz = dz_room;
     }
@@ -925,16 +1051,13 @@ hipError_t linear_bwd_io(const LinearArgs& a, const LinearGrads& d, void* ws, hi
     p.K = a.M;
     p.segs = 1;
     p.batches = c.batches;
-    p.splits = 1;
-    p.per = INT64_MAX / 4;
     p.act = LONGCONV_ACT_NONE;
     p.out = d.dx;
     p.batch = c.places * a.K;
     p.ld = c.x_first ? c.places : a.K;
     p.F = c.x_first ? Z : W;
     p.S = c.x_first ? W : Z;
-    p.wide = wide_tiles(p.F.n, p.S.n, p.batches, p.K);
-    return launch_product<IO, EPI_OUT>(p, c.x_first ? !c.y_first : false, c.x_first ? false : !c.y_first, nullptr, st);
+    return product<IO, EPI_OUT>(p, c.x_first ? !c.y_first : false, c.x_first ? false : !c.y_first, part, nullptr, st);
 }
 
 }  // namespace

@@ -41,7 +41,7 @@ class Selective:
         io = lc.dtype_code(self.u)
         room = lambda n: torch.empty(n, dtype=torch.uint8, device="cuda")  # noqa: E731
         self.ws_scan = lc.new_workspace_scan(B, E, N, states, groups, io, train)
-        self.ws_linear = room(max(lc.longconv_linear_workspace_bytes(B, N, k, m, io, train) for m, k in shapes.values()))
+        self.ws_linear = room(max(lc.longconv_linear_workspace_bytes(B, n, k, m, io, train) for m, k in shapes.values() for n in (N, 1)))
         self.marks = None
         if train:
             for t in self.p.values():

@@ -205,3 +205,22 @@ def test_writes_stay_within_the_workspace(io, B, N, K, M, firsts):
 @pytest.mark.parametrize("K", [1016, 1032])
 def test_the_largest_tiles(K, firsts):
     Run(1, 3400, K, 3544, "bf16", "silu", residual=True, x_first=firsts[0], y_first=firsts[1], dW="bf16", seed=13).fwd().bwd().check()
+
+
+# few tiles and a long sum, which is cut into shares: forward, behind an activation and in dx; workspaces of just the size asked for, the forward call's its own
+@pytest.mark.parametrize("B,N,K,M", [(1, 130, 4096, 40), (3, 70, 2056, 136), (2, 65, 2113, 77), (1, 200, 72, 3000), (2, 100, 2054, 2100), (1, 70, 515, 33)])
+@pytest.mark.parametrize("io", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("firsts", [(False, False), (True, True), (False, True), (True, False)])
+def test_long_sums_of_few_tiles(B, N, K, M, io, firsts):
+    for act, residual in (("silu", True), ("none", False)):
+        r = Run(B, N, K, M, io, act, residual=residual, x_first=firsts[0], y_first=firsts[1], seed=14)
+        code, back = lc.dtype_code(r.x), r.ws
+        small = lc.longconv_linear_workspace_bytes(B, N, K, M, code, False)
+        assert small <= back.numel()
+        room = torch.full((back.numel() + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+        r.ws = room[:small]
+        r.fwd()
+        assert (room[small:] == 0x5A).all()
+        r.ws = room[:back.numel()]
+        r.bwd().check()
+        assert (room[back.numel():] == 0x5A).all()
