@@ -8,13 +8,15 @@
 // forward pass's marks, one for each chunk.
 // 16 x 1024 x 1024, 16 states, gated, bf16: 362 us.  A wave spends some 560 vector instructions on a head's chunk, 15 for each of its 16 places and
 // states and the rest on the two scans, sums and a head's beginning and end; at two waves a SIMD (217 registers) they fill about 60 % of the time.
-// States a wave: with four of them and four waves, and with one and sixteen, registers spill (1395 and 815 us at 16 states).
+// States a wave: with four of them and four waves, and with one and sixteen, registers spill (1395 and 815 us at 16 states).  More than 16 states go
+// in groups of 16 for each chunk, the sums over states kept in memory between them.
 #include "scan.hpp"
 
 namespace lc {
 namespace {
 
 constexpr int K = SPAN / 64;      // places of a lane
+constexpr int GROUP = 16;         // states that a workgroup's waves hold at once
 
 // where place t of a chunk lies in LDS: a wave's reads of four places a lane are one run of memory
 __device__ __forceinline__ int place(int t) { return (t % K / 4 * 64 + t / K) * 4 + t % 4; }
@@ -29,20 +31,23 @@ struct Parts {
     float *dB, *dC;      // [blocks][B,G,S,N], or null: dB and dC are written themselves
     float *dA;           // [B segs][H,S]
     float *dDb;          // [B segs][H,2]: of D and of the bias
+    float *more;         // [B,H,segs][3][SPAN]: a chunk's sums over the states so far, where there are more than a workgroup's waves hold
 };
 
-template <class IO, int NS, int NW, bool GATED>
+// MANY: more states than NS NW, which go one group behind the other for each chunk.
+template <class IO, int NS, int NW, bool GATED, bool MANY>
 __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGrads d, Segments g, Parts parts, int blocks, int CB)
 {
     using T = typename IO::T;
     constexpr int TH = 64 * NW, SP = NS * NW, TPT = SPAN / TH;      // threads, states with those that are not there, places of a thread
     extern __shared__ __align__(16) float lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x;
+    const int S = a.S, row_of = MANY ? (S + SP - 1) / SP * SP : SP;      // states of a head in LDS
     float* const stages = lds;                       // [2][3][SPAN]: dt, dt u, dy' of a head, and of the next one
     float* const sums = stages + 2 * 3 * SPAN;       // [2][NW][3][SPAN]: sums over a wave's states of g B, A q, C h, and of the head before
-    float* const gcar = sums + 2 * NW * 3 * SPAN;    // [CB][SP]: what the chunk behind hands on
-    float* const dAsum = gcar + CB * SP;             // [CB][SP]
-    float* const small = dAsum + CB * SP;            // [NW][CB][2]: of dD and dbias
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x;
+    float* const gcar = sums + 2 * NW * 3 * SPAN;    // [CB][row_of]: what the chunk behind hands on
+    float* const dAsum = gcar + CB * row_of;         // [CB][row_of]
+    float* const small = dAsum + CB * row_of;        // [NW][CB][2]: of dD and dbias
     int64_t w = blockIdx.x;
     const int seg = (int)(w % g.segs);
     w /= g.segs;
@@ -53,27 +58,27 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
     const int64_t begin = seg * g.len, stop = begin + g.len < N ? begin + g.len : N, end = stop < len ? stop : len;
     const int64_t head0 = grp * in_group + (int64_t)blk * CB;
     const int heads = (int)(in_group - (int64_t)blk * CB < CB ? in_group - (int64_t)blk * CB : CB);
-    const int S = a.S;
     const int64_t n_marks = (N + SPAN - 1) / SPAN;
     const size_t bg = (size_t)(b * a.G + grp) * S;      // rows of B, C
-    for (int i = tid; i < heads * SP; i += TH) {
-        const int c = i / SP, s = i % SP;
+    for (int i = tid; i < heads * row_of; i += TH) {
+        const int c = i / row_of, s = i % row_of;
         const size_t row = (size_t)b * a.H + head0 + c;
         float from = 0.f;
         if (s < S) from = entering<true>(g, row, seg, S, s, LOG2E * a.A[(head0 + c) * S + s], d.dlast ? d.dlast[row * S + s] : 0.f);
-        gcar[c * SP + s] = from;
-        dAsum[c * SP + s] = 0.f;
+        gcar[c * row_of + s] = from;
+        dAsum[c * row_of + s] = 0.f;
     }
     for (int i = tid; i < NW * CB * 2; i += TH) small[i] = 0.f;
 
     const int64_t top = end > begin ? begin + (end - 1 - begin) / SPAN * SPAN : begin - SPAN;
-    for (int64_t t0 = top; t0 >= begin; t0 -= SPAN) {
+    for (int64_t t0 = top; t0 >= begin; t0 -= SPAN)
+    for (int s0 = 0; s0 < (MANY ? S : 1); s0 += SP) {
+        const bool final = !MANY || s0 + SP >= S;      // of the groups of states
         float dBv[NS][K], dCv[NS][K];
-        constexpr bool HELD = NS <= 2;      // B and C in registers for all heads, or brought in for each
-        float Bv[HELD ? NS : 2][K], Cv[HELD ? NS : 2][K];
+        float Bv[NS][K], Cv[NS][K];      // for all heads
         const int lim = (int)(end - t0 < SPAN ? end - t0 : SPAN), left = (int)(N - t0 < SPAN ? N - t0 : SPAN);
         const auto bring = [&](int n, float (&Bq)[K], float (&Cq)[K]) {
-            const int s = wave * NS + n;
+            const int s = s0 + wave * NS + n;
             Raw8<IO> rB, rC;
             ask8<IO>((const T*)a.Bm + ((bg + s) * N + t0), lane * K, left, s < S ? lim : 0, rB, lim == SPAN && s < S);
             ask8<IO>((const T*)a.Cm + ((bg + s) * N + t0), lane * K, left, s < S ? lim : 0, rC, lim == SPAN && s < S);
@@ -89,7 +94,7 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
         };
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            if constexpr (HELD) bring(n, Bv[n], Cv[n]);
+            bring(n, Bv[n], Cv[n]);
 #pragma unroll
             for (int i = 0; i < K; ++i) dBv[n][i] = dCv[n][i] = 0.f;
         }
@@ -99,7 +104,7 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
         // made zero in lay().
         T nd[TPT], nu[TPT], ny[TPT], nz[TPT];
         float nA, nm, nD, nbias;
-        const int s_mine = wave * NS + (lane < NS ? lane : 0), s_there = s_mine < S ? s_mine : 0;
+        const int s_mine = s0 + wave * NS + (lane < NS ? lane : 0), s_there = s_mine < S ? s_mine : 0;
         const float *const Dr = a.D ? a.D : a.A, *const br = a.bias ? a.bias : a.A;
         const auto ask = [&](int c) {
             const size_t row = (size_t)b * a.H + head0 + c, at0 = row * N + t0;
@@ -164,7 +169,7 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
                 x[4 * j] = r.x; x[4 * j + 1] = r.y; x[4 * j + 2] = r.z; x[4 * j + 3] = r.w;
                 f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
             }
-            cl = gcar[one_of(c) * SP + wave * NS + (lane < NS ? lane : 0)];
+            cl = gcar[one_of(c) * row_of + s_mine];
         };
         take(0);
         for (int c = 0; c < heads; ++c) {
@@ -177,18 +182,14 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
             for (int i = 0; i < K; ++i) sum += e[i];
             float dA[NS < 2 ? 2 : NS];
             dA[1] = 0.f;
-            // two states at a time (a state that is not there: A, B, C and all that comes of them zero)
+            // both states at once (a state that is not there: A, B, C and all that comes of them zero)
             constexpr int P = NS < 2 ? 1 : 2;
 #pragma unroll
             for (int n = 0; n < NS; n += P) {
-                if constexpr (!HELD) {
-#pragma unroll
-                    for (int r = 0; r < P; ++r) bring(n + r, Bv[r], Cv[r]);
-                }
                 float dec[P][K], q[P][K], v[P], p[P], all[P], A[P], in[P], back[P];
 #pragma unroll
                 for (int r = 0; r < P; ++r) {
-                    const float(&B)[K] = Bv[HELD ? n + r : r];
+                    const float(&B)[K] = Bv[n + r];
                     A[r] = lane_of(Al, n + r);
                     in[r] = lane_of(ml, n + r);
                     back[r] = lane_of(cl, n + r);
@@ -205,8 +206,8 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
                 else scan_up(p[0], v[0]);
 #pragma unroll
                 for (int r = 0; r < P; ++r) {
-                    const float(&B)[K] = Bv[HELD ? n + r : r];
-                    const float(&C)[K] = Cv[HELD ? n + r : r];
+                    const float(&B)[K] = Bv[n + r];
+                    const float(&C)[K] = Cv[n + r];
                     float w = dpp<0x138>(v[r], in[r]);      // the state in front of the lane
 #pragma unroll
                     for (int i = 0; i < K; ++i) {
@@ -224,8 +225,8 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
                 else scan_down(p[0], v[0]);
 #pragma unroll
                 for (int r = 0; r < P; ++r) {
-                    const float(&B)[K] = Bv[HELD ? n + r : r];
-                    const float(&C)[K] = Cv[HELD ? n + r : r];
+                    const float(&B)[K] = Bv[n + r];
+                    const float(&C)[K] = Cv[n + r];
                     float w = dpp<0x130>(v[r], back[r]);      // what the lane behind hands on
                     float s = 0.f;
 #pragma unroll
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
                     cl = with_lane(cl, n + r, lane_of(w, 0));
                 }
             }
-            if (lane < NS) gcar[c * SP + wave * NS + lane] = cl;
+            if (lane < NS) gcar[c * row_of + s0 + wave * NS + lane] = cl;
 #pragma unroll
             for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -272,8 +273,21 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
                     if (GATED) wC += part[r * 3 * SPAN + 2 * SPAN + at];
                 }
                 const uint32_t t = (uint32_t)(tid * TPT + i);
+                if (MANY) {      // (a thread reads here what it wrote itself)
+                    float* const m = parts.more + (((size_t)b * a.H + head0 + c) * g.segs + seg) * (3 * SPAN) + t;
+                    if (s0 > 0) {
+                        wB += m[0];
+                        wA += m[SPAN];
+                        if (GATED) wC += m[2 * SPAN];
+                    }
+                    if (!final) {
+                        m[0] = wB;
+                        m[SPAN] = wA;
+                        if (GATED) m[2 * SPAN] = wC;
+                    }
+                }
                 const float dw = __builtin_fmaf(wB, own.u[i], wA) * own.rate[i];
-                if ((int)t < here) {
+                if ((int)t < here && final) {
                     const bool is = (int)t < lim;
                     if (d.du) put1<IO>((T*)d.du + at0, t, is ? __builtin_fmaf(own.dt[i], wB, own.D * own.dyg[i]) : 0.f);
                     if (d.ddelta) put1<IO>((T*)d.ddelta + at0, t, is ? dw : 0.f);
@@ -286,20 +300,13 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
             }
             // lanes 0, 1: dA of the first two states; 2, 3: the shares of dD and dbias
             const float t = sums_of_wave(dA[0], dA[1], sD, sb);
-            if (lane < 2 && lane < NS) add(&dAsum[c * SP + wave * NS + lane], t);
+            if (lane < 2 && lane < NS) add(&dAsum[c * row_of + s0 + wave * NS + lane], t);
             if (lane == 2 || lane == 3) add(&small[(wave * CB + c) * 2 + lane - 2], t);
-            if constexpr (NS > 2) {
-#pragma unroll
-                for (int n = 2; n < NS; n += 2) {
-                    const float r = sums_of_wave(dA[n], dA[n + 1], 0.f, 0.f);
-                    if (lane < 2) add(&dAsum[c * SP + wave * NS + n + lane], r);
-                }
-            }
             own = next;
         }
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            const int s = wave * NS + n;
+            const int s = s0 + wave * NS + n;
             if (s >= S) continue;
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
@@ -336,8 +343,8 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
     for (int i = tid; i < heads * S; i += TH) {
         const int c = i / S, s = i % S;
         const size_t h = head0 + c, row = (size_t)b * a.H + h;
-        parts.dA[((size_t)(b * g.segs + seg) * a.H + h) * S + s] = dAsum[c * SP + s];
-        if (d.dstate && seg == 0) d.dstate[row * S + s] = gcar[c * SP + s];
+        parts.dA[((size_t)(b * g.segs + seg) * a.H + h) * S + s] = dAsum[c * row_of + s];
+        if (d.dstate && seg == 0) d.dstate[row * S + s] = gcar[c * row_of + s];
     }
     for (int i = tid; i < heads * 2; i += TH) {
         float s = 0.f;
@@ -415,25 +422,26 @@ int block_heads(int64_t B, int64_t H, int64_t N, int64_t G)
     return CB;
 }
 
-template <class IO, int NS, int NW, bool GATED>
+template <class IO, int NS, int NW, bool GATED, bool MANY>
 hipError_t launch_of(const ScanArgs& a, const ScanGrads& d, const Segments& g, const Parts& parts, int blocks, int CB, hipStream_t st)
 {
     dim3 grid;
     hipError_t e = launch_grid((uint64_t)(a.B * a.G * blocks * g.segs), 64 * NW, &grid);
     if (e != hipSuccess) return e;
-    const size_t bytes = (2 * (3 + 3 * NW) * SPAN + 2 * CB * NS * NW + 2 * NW * CB) * sizeof(float);
+    const size_t row_of = MANY ? (a.S + NS * NW - 1) / (NS * NW) * (NS * NW) : NS * NW;
+    const size_t bytes = (2 * (3 + 3 * NW) * SPAN + 2 * CB * row_of + 2 * NW * CB) * sizeof(float);
     if (bytes > 65536) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_bwd_kernel<IO, NS, NW, GATED>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_bwd_kernel<IO, NS, NW, GATED, MANY>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((scan_bwd_kernel<IO, NS, NW, GATED>), grid, dim3(64 * NW), bytes, st, a, d, g, parts, blocks, CB);
+    hipLaunchKernelGGL((scan_bwd_kernel<IO, NS, NW, GATED, MANY>), grid, dim3(64 * NW), bytes, st, a, d, g, parts, blocks, CB);
     return hipGetLastError();
 }
 
-template <class IO, int NS, int NW>
+template <class IO, int NS, int NW, bool MANY = false>
 hipError_t launch(const ScanArgs& a, const ScanGrads& d, const Segments& g, const Parts& parts, int blocks, int CB, hipStream_t st)
 {
-    return a.z ? launch_of<IO, NS, NW, true>(a, d, g, parts, blocks, CB, st) : launch_of<IO, NS, NW, false>(a, d, g, parts, blocks, CB, st);
+    return a.z ? launch_of<IO, NS, NW, true, MANY>(a, d, g, parts, blocks, CB, st) : launch_of<IO, NS, NW, false, MANY>(a, d, g, parts, blocks, CB, st);
 }
 
 template <class IO>
@@ -450,6 +458,8 @@ hipError_t run(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
     p += up256((size_t)a.B * g.segs * a.H * a.S * sizeof(float));
     parts.dDb = (float*)p;
     p += up256((size_t)a.B * g.segs * a.H * 2 * sizeof(float));
+    parts.more = (float*)p;
+    if (a.S > GROUP) p += up256((size_t)a.B * g.segs * a.H * 3 * SPAN * sizeof(float));
     parts.dB = parts.dC = nullptr;
     if (blocks > 1) {
         parts.dB = (float*)p;
@@ -458,8 +468,7 @@ hipError_t run(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
     if (a.S <= 4) e = launch<IO, 1, 4>(a, d, g, parts, blocks, CB, st);
     else if (a.S <= 8) e = launch<IO, 2, 4>(a, d, g, parts, blocks, CB, st);
     else if (a.S <= 16) e = launch<IO, 2, 8>(a, d, g, parts, blocks, CB, st);
-    else if (a.S <= 32) e = launch<IO, 4, 8>(a, d, g, parts, blocks, CB, st);
-    else e = launch<IO, 8, 8>(a, d, g, parts, blocks, CB, st);
+    else e = launch<IO, 2, 8, true>(a, d, g, parts, blocks, CB, st);
     if (e != hipSuccess) return e;
     const int64_t joins = blocks > 1 && (d.dB || d.dC) ? (int64_t)(2 * rows * ((a.N + 3) / 4) + 63) / 64 : 0;
     const int64_t others = d.dA || d.dD || d.dbias ? (a.H * (a.S + 2) + 255) / 256 : 0;
@@ -480,7 +489,7 @@ size_t scan_bwd_bytes(int64_t B, int64_t H, int64_t N, int S, int64_t G)
     const int64_t all = B * ((N + 1023) / 1024), some = 513 + (B < 256 ? B : 256), shares = all < some || B > some ? (all < some ? all : B) : some;
     const int64_t in_group = H / G, narrow = B * G * ((in_group + 7) / 8), wide = B * G * ((in_group + 31) / 32);
     const int64_t blocks = narrow < 512 ? narrow : wide < 512 ? 512 : wide;
-    return up256((size_t)shares * H * S * sizeof(float)) + up256((size_t)shares * H * 2 * sizeof(float)) +
+    return up256((size_t)shares * H * S * sizeof(float)) + (S > GROUP ? up256((size_t)shares * H * 3 * SPAN * sizeof(float)) : 0) + up256((size_t)shares * H * 2 * sizeof(float)) +
            (in_group > 8 ? up256((size_t)blocks * S * N * 2 * sizeof(float)) : 0);
 }
 

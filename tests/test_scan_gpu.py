@@ -313,3 +313,16 @@ def test_under_graph_capture_on_a_side_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, kept))
+
+
+# more states than the waves of a workgroup hold at once: several chunks, segments, blocks of heads, ends within chunks; writes within the workspace
+@pytest.mark.parametrize("B,H,N,S,G,lengths", [(2, 3, 1100, 17, 1, None), (3, 40, 600, 33, 2, [600, 513, 1]), (1, 9, 2600, 64, 1, [2077]), (2, 2, 512, 48, 1, [0, 511])])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("io", ["fp32", "bf16"])
+def test_many_states(B, H, N, S, G, lengths, gated, io):
+    r = Run(B, H, N, S, G, io, gated=gated, carry=True, lengths=lengths, seed=15)
+    size = r.ws.numel()
+    room = torch.full((size + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+    r.ws = room[:size]
+    r.fwd().bwd().check()
+    assert (room[size:] == 0x5A).all()
