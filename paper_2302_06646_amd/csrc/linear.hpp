@@ -847,7 +847,8 @@ inline Side rows_of(const void* p, bool first, const Cut& c, int64_t width)
 
 // Shares of a long sum of few tiles: as many as make 256 workgroups of 128 by 128 (fp32: 512 of 64 by 64), of four steps at least.  us, cut and whole:
 // bf16, 128 x 4096 -> 4096 26 and 68, 512 x 2048 -> 2048 25 and 37, 300 x 2051 -> 777 21 and 25, 1024 x 1024 -> 1024 24 and 17.5 (not taken); fp32, 128
-// x 4096 -> 4096 60 and 126, 512 x 1024 -> 1024 26 and 35, 300 x 515 -> 777 17 and 20.
+// x 4096 -> 4096 60 and 126, 512 x 1024 -> 1024 26 and 35, 300 x 515 -> 777 17 and 20; two shares: 896 x 2048 -> 896
+// 55 and 65, 2695 x 1009 -> 193 35 and 36, 1000 x 513 -> 1000 26 and 22 (not taken).
 template <class IO>
 struct Cuts {
     static constexpr bool F4 = sizeof(typename IO::T) == 4;
@@ -856,9 +857,9 @@ struct Cuts {
     static int64_t of(int64_t f, int64_t s, int64_t batches, int64_t K, int64_t* per)
     {
         const int64_t tiles = ((f + SIDE - 1) / SIDE) * ((s + SIDE - 1) / SIDE) * batches;
-        if (K < LONG || tiles > 128) return 1;
+        if (K < LONG) return 1;
         const int64_t want = WANT / tiles, most = steps(K) / 4, n = want < most ? want : most;
-        if (n < 2) return 1;
+        if (n < 2 || (n == 2 && steps(K) < 32)) return 1;
         *per = (steps(K) + n - 1) / n;
         return (steps(K) + *per - 1) / *per;
     }
@@ -953,7 +954,7 @@ hipError_t linear_fwd_io(const LinearArgs& a, const void* x, const void* residua
 }
 
 // the most shares that sums of dbias come in: two for each 64 places (a tile's halves), or as many as dW's sums; a tile of 256 makes four,
-// however few its places; one for each FINISH places where a sum is cut, which are at most 128 tiles of 128
+// however few its places; one for each FINISH places where a sum is cut, which are at most 128 tiles of 128 (256 of 64)
 inline int64_t bias_shares(int64_t B, int64_t N)
 {
     const int64_t tiles = B * (2 * ((N + 63) / 64) + 2), cut = B * ((N + FINISH - 1) / FINISH), most = 128 * 128 / FINISH, few = cut < most ? cut : most;
