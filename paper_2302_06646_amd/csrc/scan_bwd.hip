@@ -353,55 +353,60 @@ __global__ __launch_bounds__(64 * NW, 2) void scan_bwd_kernel(ScanArgs a, ScanGr
     }
 }
 
-// What the workgroups left, added up.  Workgroups 0 .. joins - 1: dB and dC from the sums of blocks of heads, 64 pieces of four places, each by four
-// threads that take every fourth block.  The others: dA, dD, dbias from the sums of sequences and segments.  (One launch: each of the two spends
-// most of its time on the way to what other dies wrote.)
+// What the workgroups left, added up.  Workgroups 0 .. joiners - 1: dB and dC from the sums of blocks of heads, 64 pieces of four places, each by four
+// threads that take every fourth block; of `joins` such sets every joiners'th, as a launch holds fewer than 2^32 threads and B and C 2^33 elements.
+// The others: dA, dD, dbias from the sums of sequences and segments.  (One launch: each of the two spends most of its time on the way to what other
+// dies wrote.)
+constexpr int64_t MOST_JOINERS = 1 << 20;
 template <class IO>
-__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, ScanGrads d, Parts parts, int blocks, int64_t joins, int64_t shares)
+__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, ScanGrads d, Parts parts, int blocks, int64_t joins, int64_t joiners, int64_t shares)
 {
     using T = typename IO::T;
-    if ((int64_t)blockIdx.x < joins) {
+    if ((int64_t)blockIdx.x < joiners) {
         __shared__ float4 lds[3][64];
         const int64_t P = (a.N + 3) / 4, rows = a.B * a.G * a.S;
         const int lane = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-        int64_t id = (int64_t)blockIdx.x * 64 + lane;
-        const bool is = id < 2 * rows * P, second = id >= rows * P;
-        if (second) id -= rows * P;
-        if (!is) id = 0;
-        const int64_t row = id / P, t = (id - row * P) * 4, len = scan_length(a, row / (a.G * a.S));
-        const float* from = (second ? parts.dC : parts.dB) + row * a.N + t;
-        const int n = a.N - t < 4 ? (int)(a.N - t) : 4;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (t < len && n == 4) {
+        for (int64_t set = blockIdx.x; set < joins; set += joiners) {
+            int64_t id = set * 64 + lane;
+            const bool is = id < 2 * rows * P, second = id >= rows * P;
+            if (second) id -= rows * P;
+            if (!is) id = 0;
+            const int64_t row = id / P, t = (id - row * P) * 4, len = scan_length(a, row / (a.G * a.S));
+            const float* from = (second ? parts.dC : parts.dB) + row * a.N + t;
+            const int n = a.N - t < 4 ? (int)(a.N - t) : 4;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (t < len && n == 4) {
 #pragma unroll 8
-            for (int q = quarter; q < blocks; q += 4) {
-                const At4 w = *reinterpret_cast<const At4*>(from + (size_t)q * rows * a.N);
+                for (int q = quarter; q < blocks; q += 4) {
+                    const At4 w = *reinterpret_cast<const At4*>(from + (size_t)q * rows * a.N);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(w[i]);
+                    for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(w[i]);
+                }
+            } else if (t < len)
+                for (int q = quarter; q < blocks; q += 4)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < n) v[i] += from[(size_t)q * rows * a.N + i];
+            if (set != blockIdx.x) __syncthreads();      // (the set before is read)
+            if (quarter) lds[quarter - 1][lane] = make_float4(v[0], v[1], v[2], v[3]);
+            __syncthreads();
+            T* const to = (T*)(second ? d.dC : d.dB);
+            if (quarter || !is || !to) continue;
+#pragma unroll
+            for (int r = 0; r < 3; ++r) {
+                const float4 w = lds[r][lane];
+                v[0] += w.x;
+                v[1] += w.y;
+                v[2] += w.z;
+                v[3] += w.w;
             }
-        } else if (t < len)
-            for (int q = quarter; q < blocks; q += 4)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < n) v[i] += from[(size_t)q * rows * a.N + i];
-        if (quarter) lds[quarter - 1][lane] = make_float4(v[0], v[1], v[2], v[3]);
-        __syncthreads();
-        T* const to = (T*)(second ? d.dC : d.dB);
-        if (quarter || !is || !to) return;
-#pragma unroll
-        for (int r = 0; r < 3; ++r) {
-            const float4 w = lds[r][lane];
-            v[0] += w.x;
-            v[1] += w.y;
-            v[2] += w.z;
-            v[3] += w.w;
+            for (int i = 0; i < 4; ++i)
+                if (i < n) put1<IO>(to + row * a.N + t, i, t + i < len ? v[i] : 0.f);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) put1<IO>(to + row * a.N + t, i, t + i < len ? v[i] : 0.f);
         return;
     }
-    const int64_t id = ((int64_t)blockIdx.x - joins) * 256 + threadIdx.x, in_A = a.H * a.S;
+    const int64_t id = ((int64_t)blockIdx.x - joiners) * 256 + threadIdx.x, in_A = a.H * a.S;
     if (id >= in_A + 2 * a.H) return;
     const int64_t i = id - in_A, each = id < in_A ? in_A : 2 * a.H;
     const float* const from = id < in_A ? parts.dA + id : parts.dDb + i;
@@ -471,12 +476,12 @@ hipError_t run(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
     else e = launch<IO, 2, 8, true>(a, d, g, parts, blocks, CB, st);
     if (e != hipSuccess) return e;
     const int64_t joins = blocks > 1 && (d.dB || d.dC) ? (int64_t)(2 * rows * ((a.N + 3) / 4) + 63) / 64 : 0;
-    const int64_t others = d.dA || d.dD || d.dbias ? (a.H * (a.S + 2) + 255) / 256 : 0;
-    if (joins + others == 0) return hipSuccess;
+    const int64_t joiners = joins < MOST_JOINERS ? joins : MOST_JOINERS, others = d.dA || d.dD || d.dbias ? (a.H * (a.S + 2) + 255) / 256 : 0;
+    if (joiners + others == 0) return hipSuccess;
     dim3 grid;
-    e = launch_grid((uint64_t)(joins + others), 256, &grid);
+    e = launch_grid((uint64_t)(joiners + others), 256, &grid);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(scan_join_kernel<IO>, grid, dim3(256), 0, st, a, d, parts, blocks, joins, (int64_t)a.B * g.segs);
+    hipLaunchKernelGGL(scan_join_kernel<IO>, grid, dim3(256), 0, st, a, d, parts, blocks, joins, joiners, (int64_t)a.B * g.segs);
     return hipGetLastError();
 }
 

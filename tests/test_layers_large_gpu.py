@@ -139,3 +139,33 @@ def test_one_workspace_of_two_captured_graphs():
         graphs[which].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want[which], pairs[which][1]))
+
+
+def test_scan_backward_where_B_and_C_have_2_31_elements():
+    # two blocks of heads, whose sums dB and dC are joined; more states than a workgroup's waves hold
+    B, H, N, S = 512, 33, 65536, 64
+    assert B * N * S == 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(4)
+    u, delta, dy = (torch.zeros(B, H, N, dtype=BF16, device="cuda") for _ in range(3))
+    Bm, Cm = (torch.zeros(B, 1, S, N, dtype=BF16, device="cuda") for _ in range(2))
+    for t in (u, delta, dy, Bm, Cm):
+        t[0].normal_(generator=g)
+        t[-1].normal_(generator=g)
+    A = -torch.rand(H, S, generator=g, device="cuda") - 0.1
+    new = lambda like: torch.full_like(like, 7.0)  # noqa: E731
+    y, marks, ws = torch.empty_like(u), lc.new_scan_marks(B, H, N, S), lc.new_workspace_scan(B, H, N, S, 1, lc.BF16, True)
+    lc.longconv_scan_fwd(u, delta, A, Bm, Cm, y, ws, marks=marks)
+    du, ddelta, dA, dB, dC = (new(t) for t in (u, u, A, Bm, Cm))
+    lc.longconv_scan_bwd(dy, u, delta, A, Bm, Cm, marks, du, ddelta, dA, dB, dC, ws)
+    sums = torch.zeros_like(dA)
+    for b in (0, B - 1):
+        one = [t[b:b + 1].clone() for t in (dy, u, delta, Bm, Cm)]
+        args = (one[1], one[2], A, one[3], one[4])
+        some, few = lc.new_scan_marks(1, H, N, S), lc.new_workspace_scan(1, H, N, S, 1, lc.BF16, True)
+        lc.longconv_scan_fwd(*args, torch.empty_like(one[1]), few, marks=some)
+        want = [new(t) for t in (one[1], one[1], A, one[3], one[4])]
+        lc.longconv_scan_bwd(one[0], *args, some, *want, few)
+        assert all(_near(got[b], w[0]) for got, w in zip((du, ddelta, dB, dC), (want[0], want[1], want[3], want[4])))
+        sums += want[2]
+    assert torch.allclose(dA, sums, rtol=1e-4, atol=1e-3 * sums.abs().max().item())
+    assert not any(t[b].any() for t in (dB, dC, du) for b in (1, B // 2, B - 2))      # all of their inputs are zero
