@@ -953,11 +953,11 @@ hipError_t linear_fwd_io(const LinearArgs& a, const void* x, const void* residua
     return forward<IO, EPI_OUT>(a, x, p, ws, nullptr, st);
 }
 
-// the most shares that sums of dbias come in: two for each 64 places (a tile's halves), or as many as dW's sums; a tile of 256 makes four,
-// however few its places; one for each FINISH places where a sum is cut, which are at most 128 tiles of 128 (256 of 64)
+// the most shares that sums of dbias come in: two for each 64 places (a tile's halves; a tile of 256 makes four, but is full to three quarters, so of
+// 192 places and more), or as many as dW's sums; one for each FINISH places where a sum is cut, which are at most 128 tiles of 128 (256 of 64)
 inline int64_t bias_shares(int64_t B, int64_t N)
 {
-    const int64_t tiles = B * (2 * ((N + 63) / 64) + 2), cut = B * ((N + FINISH - 1) / FINISH), most = 128 * 128 / FINISH, few = cut < most ? cut : most;
+    const int64_t tiles = B * 2 * ((N + 63) / 64), cut = B * ((N + FINISH - 1) / FINISH), most = 128 * 128 / FINISH, few = cut < most ? cut : most;
     return tiles > few ? tiles : few;
 }
 inline size_t most_of(size_t a, size_t b, size_t c) { return a > b ? (a > c ? a : c) : b > c ? b : c; }
@@ -966,6 +966,10 @@ size_t linear_workspace_io(int64_t B, int64_t N, int64_t K, int64_t M, int backw
 {
     const size_t cuts = Cuts<IO>::bytes(B * N, K, M), back = Cuts<IO>::bytes(B * N, M, K);
     if (!backward) return cuts + 256;
+    if (N == 1) {      // in either layout the places of one sequence (Cut); of longer ones the layouts that cut most are counted
+        N = B;
+        B = 1;
+    }
     bool wide;
     const int64_t want = shares_wanted(K, M, sizeof(typename IO::T) == 4, &wide), steps = (B * ((N + 15) / 16) + 3) / 4;      // (never more shares than either)
     const int64_t shares = want < steps ? want : steps, bias = bias_shares(B, N);

@@ -124,3 +124,13 @@ def test_the_binding_refuses_host_tensors_and_unknown_names():
         lc.longconv_linear_bwd(x, x, k, None, x, k, None, "none", k)
     with pytest.raises(KeyError):
         lc.longconv_linear_fwd(x, k, None, x, "tanh", k)
+
+
+@pytest.mark.parametrize("io", [lc.F32, lc.F16, lc.BF16])
+@pytest.mark.parametrize("K,M", [(768, 2048), (64, 4096), (100, 77), (4096, 40)])
+def test_scratch_of_many_short_sequences_is_that_of_their_places(io, K, M):
+    size = lambda B, N: lc.longconv_linear_workspace_bytes(B, N, K, M, io, True)  # noqa: E731
+    for B in (1, 3, 15, 64, 1000, 65536):
+        assert size(B, 1) == size(1, B)                    # the same product, whichever way its places are counted
+    # of two places each: beside what all places as one need, two rows of sums for each sequence, as [B,.,N] is cut
+    assert size(65536, 2) <= size(1, 131072) + 65536 * 2 * M * 4

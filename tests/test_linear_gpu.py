@@ -224,3 +224,27 @@ def test_long_sums_of_few_tiles(B, N, K, M, io, firsts):
         r.ws = room[:back.numel()]
         r.bwd().check()
         assert (room[back.numel():] == 0x5A).all()
+
+
+# sums of dbias by tiles of 256 that are filled least, by other tiles, by cut sums and by dW's shares; each within a workspace of just the size asked for
+@pytest.mark.parametrize("io,B,N,K,M,firsts", [("bf16", 13, 200, 1024, 4096, (False, True)), ("fp16", 13, 200, 1024, 4096, (True, False)), ("bf16", 200, 1, 1024, 49432, (False, False)),
+                                               ("bf16", 193, 1, 72, 136, (True, True)), ("fp32", 100, 1, 520, 72, (False, True)), ("bf16", 130, 1, 2056, 40, (False, False)),
+                                               ("fp16", 300, 2, 64, 72, (True, True)), ("fp32", 90, 3, 70, 33, (False, True)), ("bf16", 1, 1, 8, 8, (False, False))])
+def test_sums_of_dbias_stay_within_the_workspace(io, B, N, K, M, firsts):
+    for act in ("silu", "none"):
+        r = Run(B, N, K, M, io, act, x_first=firsts[0], y_first=firsts[1], seed=16)
+        room = torch.full((r.ws.numel() + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+        r.ws = room[:-65536]
+        r.bwd()
+        assert (room[-65536:] == 0x5A).all()
+        r.bwd(dx=False, dW=False)
+        assert (room[-65536:] == 0x5A).all()
+        if M < 10000:
+            r.fwd().bwd().check()
+            continue
+        z = r.x.double().view(-1, K) @ r.W.double().t() + r.bias        # (as check() bounds it, on the GPU)
+        q, dy = torch.sigmoid(z), r.dy.double().view(-1, M)
+        dz = dy * (q * (1 + z * (1 - q))) if act == "silu" else dy
+        size = r.x.double().abs().view(-1, K) @ r.W.double().abs().t() + r.bias.abs()
+        err = 0 * dz if act == "none" else dy.abs() * (1.13 * (K + 4) * U * size + U * (8 + 2 * z.abs()) * (1 + z.abs()))
+        assert ((r.dbias - dz.sum(0)).abs() <= (err + (B * N + 4) * U * (dz.abs() + err)).sum(0)).all()
