@@ -49,7 +49,8 @@ class Selective:
             self.marks = lc.new_scan_marks(B, E, N, states)
             self.ws_short = lc.new_workspace_short(B, E, N, taps, io)
             self.du0, self.du, self.dz, self.ddelta, self.dy, self.more = (new(*wide) for _ in range(6))
-            self.dr, self.dB, self.dC, self.dx = new(B, R, N), new(*of_states), new(*of_states), new(B, H, N)
+            self.dr, self.dB, self.dC, self.dx, self.x = new(B, R, N), new(*of_states), new(*of_states), new(B, H, N), new(B, H, N)
+            self.one = torch.ones(H, 1, device="cuda")
             self.dA = torch.empty_like(self.A)
         self.refresh()
 
@@ -64,6 +65,11 @@ class Selective:
 
     def _linear_back(self, name, dy, x, dx):
         lc.longconv_linear_bwd(dy, x, self.low[name], None, dx, self.p[name].grad, None, "none", self.ws_linear, FIRST, FIRST)
+
+    def _inside(self, t, to, lengths):
+        """`to` <- t up to each sequence's end and zeros behind it: the short convolution whose one tap is 1."""
+        lc.longconv_short_fwd(t, self.one, None, to, "none", lengths=lengths)
+        return to
 
     def _rows(self, t):
         return t.view(self.B, self.G * self.S, self.N)
@@ -91,6 +97,8 @@ class Selective:
         """dx and the parameters' gradients from dy, behind forward() of the same x and lengths (the residual's gradient is dy).  Where several
         gradients of a tensor meet they are added in the I/O type, as they are kept."""
         p = self.p
+        if lengths is not None:      # (products over places take all of them: zeros of the other operand do not take NaN or infinity out)
+            x, dy = self._inside(x, self.x, lengths), self._inside(dy, self.dx, lengths)
         self._linear_back("W_y", dy, self.y, self.dy)
         lc.longconv_scan_bwd(self.dy, self.u, self.delta, self.A, self.Bm, self.Cm, self.marks, self.du, self.ddelta, self.dA, self.dB, self.dC,
                              self.ws_scan, D=p["D"], z=self.z, bias=p["dt_bias"], dD=p["D"].grad, dz=self.dz, dbias=p["dt_bias"].grad,

@@ -138,3 +138,30 @@ def test_the_command_runs_and_another_mixer_is_refused():
     assert np.isfinite(classifier.main(["--mixer", "scan", "--steps", "3", "--batch", "4", "--length", "256", "--width", "16"]))
     with pytest.raises(ValueError, match="mixer"):
         classifier.Classifier(2, 256, 16, mixer="other")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_padding_that_is_not_finite_takes_no_part_in_gradients(dtype):
+    B, N, H = 4, 200, 16
+    m, x, dy = _block(B, N, H, dtype=dtype, seed=6)
+    lengths = torch.tensor([200, 77, 0, 513], device="cuda")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+
+    def run():
+        m.forward(x, y, lengths)
+        m.backward(dy, x, dx, lengths)
+        return [t.clone() for t in (y, dx, *(p.grad for p in m.p.values()))]
+
+    def pad(to_x, to_dy):
+        for b, n in enumerate(lengths.tolist()):
+            x[b, :, n:], dy[b, :, n:] = to_x, to_dy
+
+    pad(0.0, 0.0)
+    want = run()
+    assert all(t.isfinite().all() for t in want)
+    for to_x, to_dy in ((float("nan"), float("inf")), (float("-inf"), float("nan")), (100.0, -50.0)):
+        pad(to_x, to_dy)
+        before = x.clone(), dy.clone()
+        assert all(torch.equal(a, b) for a, b in zip(run(), want)), (to_x, to_dy)
+        assert torch.equal(x.view(-1).view(torch.uint8), before[0].view(-1).view(torch.uint8))      # the caller's own, as they were
+        assert torch.equal(dy.view(-1).view(torch.uint8), before[1].view(-1).view(torch.uint8))
