@@ -298,10 +298,11 @@ __device__ __forceinline__ range_t make_range(const void* p, uint32_t bytes)
                    (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00027000u};
 }
 constexpr uint32_t BEYOND = 0x80000000u;
-// 16 bytes of each lane from byte `off` on to LDS byte `to` + 16 lane; they are there when vmcnt says so
+// 16 bytes of each lane from byte `off` on to LDS byte `to` + 16 lane; they are there when vmcnt says so.  (m0 is named, so that no value that the
+// compiler puts there for an instruction of its own is taken to last across this.)
 __device__ __forceinline__ void bring16(const range_t& r, uint32_t off, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(to) : "memory", "m0");
 }
 
 // rows (k fast) or columns (k slow) i0 .. i0 + BI - 1 of an operand, 64 values of k a step, by NW waves
