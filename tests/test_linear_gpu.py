@@ -248,3 +248,17 @@ def test_sums_of_dbias_stay_within_the_workspace(io, B, N, K, M, firsts):
         size = r.x.double().abs().view(-1, K) @ r.W.double().abs().t() + r.bias.abs()
         err = 0 * dz if act == "none" else dy.abs() * (1.13 * (K + 4) * U * size + U * (8 + 2 * z.abs()) * (1 + z.abs()))
         assert ((r.dbias - dz.sum(0)).abs() <= (err + (B * N + 4) * U * (dz.abs() + err)).sum(0)).all()
+
+
+# dbias has the same bits whichever results are asked for beside it: rows of whole pieces, where it comes of dW's products, tiles of 128 and of 256, and others
+@pytest.mark.parametrize("io,B,N,K,M", [("bf16", 3, 400, 128, 264), ("fp16", 1, 72, 8, 8), ("bf16", 2, 520, 1024, 1032), ("bf16", 2, 51, 40, 136),
+                                        ("fp16", 5, 1, 64, 4096), ("fp32", 2, 90, 40, 72), ("bf16", 2, 2600, 64, 8)])
+@pytest.mark.parametrize("firsts", [(False, False), (True, True), (False, True), (True, False)])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_dbias_is_the_same_beside_any_results(io, B, N, K, M, firsts, act):
+    r = Run(B, N, K, M, io, act, x_first=firsts[0], y_first=firsts[1], seed=15).fwd().bwd().check()
+    want = r.dbias.clone()
+    for dx, dW in ((False, False), (True, False), (False, True)):
+        r.dbias.fill_(5.0)
+        r.bwd(dx=dx, dW=dW)
+        assert torch.equal(r.dbias, want), (dx, dW)
