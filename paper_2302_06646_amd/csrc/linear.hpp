@@ -913,8 +913,9 @@ inline Side rows_of(const void* p, bool first, const Cut& c, int64_t width)
 
 // Shares of a long sum of few tiles: as many as make 256 workgroups of 128 by 128 (fp32: 512 of 64 by 64), of four steps at least.  us, cut and whole:
 // bf16, 128 x 4096 -> 4096 26 and 68, 512 x 2048 -> 2048 25 and 37, 300 x 2051 -> 777 21 and 25, 1024 x 1024 -> 1024 24 and 17.5 (not taken); fp32, 128
-// x 4096 -> 4096 60 and 126, 512 x 1024 -> 1024 26 and 35, 300 x 515 -> 777 17 and 20; two shares: 896 x 2048 -> 896
-// 55 and 65, 2695 x 1009 -> 193 35 and 36, 1000 x 513 -> 1000 26 and 22 (not taken).
+// x 4096 -> 4096 60 and 126, 512 x 1024 -> 1024 26 and 35, 300 x 515 -> 777 17 and 20.  Two shares: bf16, 1408 x 2048 -> 1408 26 and 37;
+// fp32, five shapes of 172 to 256 tiles, K = 640 (20 steps) 25 to 27 and 23.5 (not taken), 768 27 to 28.5 and 27.2 (not taken), 896 (28 steps) 30 to 31 and
+// 31, 1024 33 and 34.6, 1280 38 and 42, 2048 55 and 64.
 template <class IO>
 struct Cuts {
     static constexpr bool F4 = sizeof(typename IO::T) == 4;
@@ -925,7 +926,7 @@ struct Cuts {
         const int64_t tiles = ((f + SIDE - 1) / SIDE) * ((s + SIDE - 1) / SIDE) * batches;
         if (K < LONG) return 1;
         const int64_t want = WANT / tiles, most = steps(K) / 4, n = want < most ? want : most;
-        if (n < 2 || (n == 2 && steps(K) < 32)) return 1;
+        if (n < 2 || (n == 2 && steps(K) < 28)) return 1;
         *per = (steps(K) + n - 1) / n;
         return (steps(K) + *per - 1) / *per;
     }

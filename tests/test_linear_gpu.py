@@ -262,3 +262,11 @@ def test_dbias_is_the_same_beside_any_results(io, B, N, K, M, firsts, act):
         r.dbias.fill_(5.0)
         r.bwd(dx=dx, dW=dW)
         assert torch.equal(r.dbias, want), (dx, dW)
+
+
+# fp32, a sum that makes two shares, on both sides of the length from which it is cut: forward, behind an activation, and in dx
+@pytest.mark.parametrize("K", [513, 864, 865, 900, 1009])
+@pytest.mark.parametrize("T,M", [(700, 1400), (2695, 193), (65 * 16, 11 * 64 - 3)])
+def test_sums_of_two_shares(K, T, M):
+    Run(1, T, K, M, "fp32", "silu", residual=True, y_first=True, seed=17).fwd().bwd().check()
+    Run(5, T // 5, M, K, "fp32", "none", seed=18).fwd().bwd().check()
