@@ -418,12 +418,13 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, ScanGrads d,
     to[id < in_A ? id : i >> 1] = s;
 }
 
-// Heads of a workgroup: as many as leave 256 workgroups (with the segments a sequence may be cut into), 32 at most.  us with 8, 16, 32 at 16 states:
-// 16 x 1024 x 1024 429, 345, 318 (taken); 4 x 1024 x 1024 108, 93 (taken), 158; 2 x 256 x 2048 70 (taken), 101, 170.
-int block_heads(int64_t B, int64_t H, int64_t N, int64_t G)
+// Heads of a workgroup: as many as leave 256 workgroups, counting the segments that a sequence is cut into, 32 at most.  us with 8, 16, 32 at 16 states,
+// gated, bf16: 16 x 1024 x 1024 480, 392, 357 (taken); 4 x 1024 x 1024 117, 103 (taken), 175; 4 x 1024 x 4096 470, 388 (taken), 675; 1 x 1024 x 16384 in four
+// segments 548, 474 (taken), 762; 2 x 256 x 2048 in two 75 (taken), 112, 189; 2 x 1024 x 8192 466 (taken), 725, 1323; 8 x 256 x 16384 955 (taken), 1453, 2634.
+int block_heads(int64_t B, int64_t H, int64_t G, int segs)
 {
     int CB = 32;
-    while (CB > 8 && B * G * ((H / G + CB - 1) / CB) * ((N + 1023) / 1024) < 256) CB /= 2;
+    while (CB > 8 && B * G * ((H / G + CB - 1) / CB) * segs < 256) CB /= 2;
     return CB;
 }
 
@@ -455,7 +456,7 @@ hipError_t run(const ScanArgs& a, const ScanGrads& d, void* ws, hipStream_t st)
     Segments g;
     hipError_t e = scan_back(a, d.dy, ws, &g, st);
     if (e != hipSuccess) return e;
-    const int CB = block_heads(a.B, a.H, a.N, a.G), blocks = (int)((a.H / a.G + CB - 1) / CB);
+    const int CB = block_heads(a.B, a.H, a.G, g.segs), blocks = (int)((a.H / a.G + CB - 1) / CB);
     const size_t rows = (size_t)a.B * a.G * a.S;
     Parts parts;
     char* p = (char*)ws + scan_segment_bytes(a.B, a.H, a.N, a.S, a.G);

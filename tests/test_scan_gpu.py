@@ -326,3 +326,16 @@ def test_many_states(B, H, N, S, G, lengths, gated, io):
     r.ws = room[:size]
     r.fwd().bwd().check()
     assert (room[size:] == 0x5A).all()
+
+
+# several blocks of heads, the last one not full, of 32, 16 and 8 heads; short sequences, and more than two chunks in one segment; writes within the workspace
+@pytest.mark.parametrize("B,H,N,S,io,ragged", [(90, 70, 20, 5, "fp32", False), (90, 70, 20, 20, "bf16", True), (130, 33, 1100, 1, "bf16", True), (86, 40, 1100, 2, "fp32", True),
+                                               (26, 80, 1300, 2, "fp16", False), (26, 80, 1030, 17, "fp32", True)])
+def test_blocks_of_heads(B, H, N, S, io, ragged):
+    lengths = [(N * (7 * b + 3)) // (7 * B) for b in range(B)] if ragged else None
+    r = Run(B, H, N, S, 1, io, carry=True, lengths=lengths, seed=19)
+    size = r.ws.numel()
+    room = torch.full((size + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+    r.ws = room[:size]
+    r.fwd().bwd().check()
+    assert (room[size:] == 0x5A).all()
