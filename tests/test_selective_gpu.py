@@ -165,3 +165,26 @@ def test_padding_that_is_not_finite_takes_no_part_in_gradients(dtype):
         assert all(torch.equal(a, b) for a, b in zip(run(), want)), (to_x, to_dy)
         assert torch.equal(x.view(-1).view(torch.uint8), before[0].view(-1).view(torch.uint8))      # the caller's own, as they were
         assert torch.equal(dy.view(-1).view(torch.uint8), before[1].view(-1).view(torch.uint8))
+
+
+# 16-bit: each stored tensor is off by half a step at most (2^-8, 2^-11 of a value), everything else by some 2^-24.  Forward, nine of them stand between x and
+# y (u0, u, z, r, delta, B, C, the scan's y, y), and u, with what u0 brings to it, reaches the scan's y four ways (u itself, delta, B, C), each at most in
+# proportion: 9 + 2 * 3 = 15 half steps.  A gradient takes what its forward values are off by, 15, and the gradients on its way down, at most twelve: of the scan's
+# y, delta, B, C, z, u, r, three sums into u's, u0's, its own.  Both are sums of sizes, not of squares: norms stay well within.
+@pytest.mark.parametrize("dtype,unit", [(torch.bfloat16, 2.0 ** -8), (torch.float16, 2.0 ** -11)])
+@pytest.mark.parametrize("uneven", [False, True])
+def test_sixteen_bits_against_the_oracles(dtype, unit, uneven):
+    B, N, H = 3, 330, 48
+    m, x, dy = _block(B, N, H, dtype=dtype, seed=8, states=6, groups=2)
+    lengths = torch.tensor([N, 200, 31], device="cuda") if uneven else None
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    m.forward(x, y, lengths)
+    m.backward(dy, x, dx, lengths)
+    p = {k: _np(m.low.get(k, v)) for k, v in m.p.items()}      # the products' operands as they are
+    n = None if lengths is None else lengths.cpu().numpy()
+    want, kept, _ = selective.forward(_np(x), p, m.S, m.G, n)
+    assert _rel(_np(y), want) < 15 * unit
+    want_dx, grads = selective.backward(_np(dy), p, kept, n)
+    assert _rel(_np(dx), want_dx) < 27 * unit
+    for name, w in grads.items():
+        assert _rel(_np(m.p[name].grad), w) < 27 * unit, name
