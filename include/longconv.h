@@ -390,7 +390,8 @@ int longconv_linear_fwd(const void* x, const void* W, const float* bias, const v
 /* Backward (the residual's gradient is dy): with z = x W^T + bias made again and dz = dy act'(z),
  *     dx = dz W,      dW = sum over places of dz^T x,      dbias = sum over places of dz
  * dx in the I/O dtype, dW in dtype dW_type (float32 or the I/O dtype), dbias float32; each may be NULL.  Behind an activation dz is
- * rounded to the I/O dtype on its way into dx and dW (the matrix cores' operands are that wide); dbias sums it before that.
+ * rounded to the I/O dtype on its way into dx and dW (the matrix cores' operands are that wide: beyond the type's largest value it is
+ * infinite); dbias sums it before that, and its bits do not depend on which other results are asked for.
  * longconv_linear_workspace_bytes (backward = 1; it serves the forward call too; 0 on bad arguments) does not fall as B grows. */
 int longconv_linear_bwd(const void* dy, const void* x, const void* W, const float* bias, void* dx, void* dW, int dW_type, float* dbias,
                         int64_t B, int64_t N, int64_t K, int64_t M, int act, int x_layout, int y_layout, int io, void* workspace,

@@ -1,5 +1,7 @@
 // Dense product between layers, y = act(x W^T + bias) + residual, x and y each as [B,N,.] or [B,.,N], and its backward pass
 //     dz = dy act'(z),   dx = dz W,   dW = dz^T x,   dbias = sum over places of dz,      z made again by the same product.
+// Behind an activation dz is rounded to the I/O type in front of dx and dW, as the matrix instructions' operands are that wide: a second rounding of
+// the size of dy's own (fp16, 131072 x 256 -> 1024 with gelu: errors of the gradients 2.9e-4 instead of 2.1e-4).
 //
 // All four products are one kernel: out[s][f] = sum_k F(f,k) S(s,k), f the index that is neighbouring in the result's memory.  Either operand
 // may have k neighbouring in its memory (its tile then lies in LDS as rows along k) or its own index (rows along that).
@@ -32,7 +34,7 @@ struct Product {
     int act;
     const void* residual;             // EPI_OUT
     const void* dy;                   // EPI_DZ: out = dy act'(z)
-    float* sums;                      // EPI_DZ: [batches tiles 2][n of the bias], sums of dz over a tile's places
+    float* sums;                      // EPI_DZ: [batches tiles 2][n of the bias], sums of dz over a tile's places, before dz is rounded
     // EPI_SUM: [batches][splits][n_s][n_f]
     float* part;
 };
@@ -833,7 +835,8 @@ hipError_t launch_fast(const Product& p, int64_t* shares, hipStream_t st)
 // the sum is long, and where they are full to three quarters and more, and so is the last round of 256 units.  Else tiles of 128 by 128, one of
 // each operand (four workgroups a unit, whose loads, products and epilogues lie side by side).  us, 256 and 128, bf16: 16384 x K -> 2048: K = 768
 // 61 and 60, 1024 76 and 71 (in other layouts 78 to 81 and 78 to 85), 1536 101 and 108, 2048 121 and 129, 4096 217 and 241; 8192^3 957 and 1300;
-// 131072 x 256 -> 1024 with gelu, fp16, 220 and 187.  Two operands of 128 each in LDS, two workgroups a unit: K = 768 69, the last 234.
+// 131072 x 256 -> 1024 with gelu, fp16, 220 and 187.  Two operands of 128 each in LDS, two workgroups a unit: K = 768 69, the last 234.  (Back to back on
+// one set of tensors; under the profiler and on two sets in turn K = 768 takes 69, of tiles of 128.)
 inline bool wide_tiles(int64_t f, int64_t s, int64_t batches, int64_t K)
 {
     const int64_t tiles = ((f + 255) / 256) * ((s + 255) / 256) * batches, rounds = (tiles + 255) / 256;

@@ -15,8 +15,8 @@ enum Mode { WHOLE, STATES, BACK };
 // Workgroup: eight heads of one group, one segment.  B and C of FB states at a time are laid out in fp32 for all of them; a wave has two
 // states at a time.
 // What bounds it is the vector instructions: for each state eight places of a lane take 72 of them, eight exponentials (8 cycles each) and five
-// multiplications or multiply-adds a place among them (2.7).  16 x 1024 x 1024, 16 states, gated, bf16: 133 us, of which they are about 75; 8 x 256 x
-// 16384, fp16, 270 us at two waves a SIMD.
+// multiplications or multiply-adds a place among them (2.7).  16 x 1024 x 1024, 16 states, gated, bf16: 132 us, 100 of them vector
+// instructions by the counter (54 M, at 2.4 GHz); 8 x 256 x 16384, fp16, uneven lengths, 266 and 128 (70 M), at two waves a SIMD.
 // WHOLE: y, marks and the last state.  STATES: what Segments holds of segments 0 .. segs - 2.  BACK: the same for the gradient of the state,
 // g_t = C_t dy_t + a_{t+1} g_{t+1}, as v_t = a_t (C_t dy_t + v_{t+1}) in reversed time, of segments 1 .. segs - 1.
 // A and the states between chunks are kept one in a lane, lane s for state s.

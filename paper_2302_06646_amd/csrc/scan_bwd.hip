@@ -6,8 +6,9 @@
 // Chunks of SPAN places, from the last to the first.  A wave has NS states and walks over a block of heads: the sums over heads, dB and dC,
 // stay in its registers for the chunk; the sums over states, of every head, go through LDS between the NW waves.  h runs again from the
 // forward pass's marks, one for each chunk.
-// 16 x 1024 x 1024, 16 states, gated, bf16: 362 us.  A wave spends some 560 vector instructions on a head's chunk, 15 for each of its 16 places and
-// states and the rest on the two scans, sums and a head's beginning and end; at two waves a SIMD (217 registers) they fill about 60 % of the time.
+// 16 x 1024 x 1024, 16 states, gated, bf16: 359 us under the profiler, the call with its joining launch 356 back to back.  A wave spends some 550 vector
+// instructions on a head's chunk, 15 for each of its 16 places and states and the rest on the two scans, sums and a head's beginning and end; by the
+// counter they are 245 us at 2.4 GHz, at two waves a SIMD (217 registers).
 // States a wave: with four of them and four waves, and with one and sixteen, registers spill (1395 and 815 us at 16 states).  More than 16 states go
 // in groups of 16 for each chunk, the sums over states kept in memory between them.
 #include "scan.hpp"
